@@ -15,6 +15,9 @@
  *   4. the surviving experts (plus shared experts) run as a grouped SwiGLU
  *      FFN and their outputs are combined with the gate weights (the MoE
  *      output equation of Sec. II-A).
+ * The attention block that precedes the layer in a decoder is here as well:
+ * page plans and a latent cache, latent attention, block-scaled 8-bit
+ * products.
  *
  * Conventions shared by every entry point
  *   - Every tensor pointer is caller-owned DEVICE memory (hipMalloc'd or a
@@ -378,6 +381,147 @@ caee_status_t caee_lru_step(int32_t E, int32_t n_cache, int32_t n_stage, int32_t
                             int64_t* slot_used, int64_t call, const uint8_t* need, int32_t* fetch,
                             int32_t* fetch_slot, int32_t* counts);
 
+/* ---------------------------------------------------------------------------
+ * The attention block in front of the MoE layer: 8-bit projections, a paged
+ * cache of latent vectors, and latent attention over it.
+ *
+ * Latent attention keeps one row of `latent + rope` bf16 values per token for
+ * all heads: a latent vector c_j (from which head h's key and value are
+ * W_uk[h] c_j and W_uv[h] c_j) and a rotary key r_j that every head shares.
+ * The cache is an array of pages, [n_blocks][block_size][latent + rope];
+ * token j of request b is row j % block_size of page block_table[b][j /
+ * block_size], its slot the row's index in the whole array. */
+
+/* What caee_paged_plan writes, caller-owned device memory. */
+typedef struct caee_paged_plan_out {
+    int32_t* cu_new;     /* [B + 1] first new token of each request in the step's token list; last: their number */
+    int32_t* cu_kv;      /* [B + 1] prefix sums of seq_len */
+    int32_t* seq_len;    /* [B] ctx_len + new_len */
+    int64_t* slots;      /* [T] cache slot of each new token; -1 past the last one and where no page is */
+    int32_t* position;   /* [T] position of each new token in its request, -1 past the last one (optional) */
+    int32_t* request;    /* [T] request of each new token, -1 past the last one (optional) */
+    int32_t* free_head;  /* [1] free_head + pages taken; must not be the input free_head */
+    int32_t* lacking;    /* [1] pages that were needed and not given */
+} caee_paged_plan_out_t;
+
+/* The paging step of a serving loop: B requests with ctx_len[b] tokens in the
+ * cache receive new_len[b] further ones (0: none).  Pages that the requests
+ * then lack are taken from free_list[free_head[0] ..] (n_free entries) in
+ * request order and written to block_table [B][max_blocks], whose first
+ * ceil(ctx_len[b] / block_size) entries a request holds already; every new
+ * token's slot, position and request follow.  T is the length of the token
+ * lists: tokens past it get no entry, entries past the last token are -1, so
+ * a step can be padded to a fixed size.  Where the free list ends (or a
+ * row of the table), entries are -1 (not written), their tokens' slots -1 and
+ * `lacking` counts the pages.  Nothing else is changed: a call with the same
+ * inputs writes the same outputs.  Negative lengths count as 0, and the sums
+ * of lengths must fit an int32.  Device lengths stay on the device: the call
+ * can be captured in a graph.  B in [0, 65536], T >= 0, block_size in
+ * [1, 65536]. */
+caee_status_t caee_paged_plan(int32_t B, int32_t T, int32_t block_size, int32_t max_blocks, const int32_t* ctx_len,
+                              const int32_t* new_len, int32_t* block_table, const int32_t* free_list, int32_t n_free,
+                              const int32_t* free_head, const caee_paged_plan_out_t* out, void* stream);
+
+/* Writes T tokens' rows into the cache: row slots[t] = [c_t | r_t], rounded to
+ * bf16 (nearest, ties to even).  c and r are x_dtype (CAEE_BF16 or CAEE_F32)
+ * rows c_stride and r_stride elements apart (slices of a wider projection,
+ * 16-byte aligned rows).  A slot outside [0, n_slots) writes nothing; of two
+ * tokens with one slot either is stored.  latent and rope are multiples
+ * of 8. */
+caee_status_t caee_latent_store(int32_t T, int32_t latent, int32_t rope, int32_t x_dtype, const void* c,
+                                int64_t c_stride, const void* r, int64_t r_stride, const int64_t* slots, void* cache,
+                                int64_t n_slots, void* stream);
+
+/* How latent attention is computed.  Both forms give the same function. */
+typedef enum caee_latent_form {
+    /* By the batch's size: expanded from CAEE_LATENT_EXPAND_NEW new tokens per request on average. */
+    CAEE_LATENT_AUTO = 0,
+    /* Queries are multiplied by W_uk and attend to the cache rows
+     * themselves, whose values W_uv is applied to afterwards: few new tokens
+     * over a long cache (reads each row once for all heads). */
+    CAEE_LATENT_ABSORBED = 1,
+    /* Every head's keys and values are formed from the cache rows first:
+     * prompts (a fifth to a third of the work per pair). */
+    CAEE_LATENT_EXPANDED = 2
+} caee_latent_form_t;
+#define CAEE_LATENT_EXPAND_NEW 128
+
+typedef struct caee_latent_desc {
+    int32_t T;            /* query rows, >= 0 (padded ones included) */
+    int32_t B;            /* requests, 0..65536 */
+    int32_t heads;        /* 1..1024 */
+    int32_t nope, rope;   /* parts of a query: 64 or 128, and 64 */
+    int32_t latent;       /* 128, 256 or 512 */
+    int32_t v;            /* output width of a head, 64 or 128 */
+    int32_t block_size;   /* tokens of a cache page, 1..65536 */
+    int32_t n_blocks;     /* pages of the cache */
+    int32_t max_blocks;   /* row length of block_table */
+    int32_t max_new;      /* no request has more new tokens than this */
+    int32_t causal;       /* 1: new token i of a request sees its first seq_len - new + i + 1 tokens; 0: all seq_len */
+    int32_t form;         /* caee_latent_form_t */
+    int32_t y_dtype;      /* CAEE_BF16 or CAEE_F32 */
+    int64_t max_kv;       /* sum of seq_len at most */
+    int64_t q_stride;     /* elements from one token of q to the next, a multiple of 8, >= heads * (nope + rope) */
+    float scale;          /* factor on the scores, finite and > 0 */
+} caee_latent_desc_t;
+
+typedef struct caee_latent_weights {
+    const void* w_uk;     /* [heads][nope][latent] bf16 (expanded form) */
+    const void* w_uk_t;   /* [heads][latent][nope] bf16, the same matrices transposed (absorbed form) */
+    const void* w_uv;     /* [heads][v][latent] bf16 */
+} caee_latent_weights_t;
+
+/* Bytes of workspace caee_latent_attention needs.  Host-only. */
+caee_status_t caee_latent_workspace_size(const caee_latent_desc_t* desc, size_t* bytes);
+
+/* Latent attention of the new tokens over the paged cache, which holds their
+ * own rows already (caee_latent_store):
+ *   s_tj = scale * (q_nope . W_uk[h] c_j + q_rope . r_j),
+ *   y_t = W_uv[h] sum_j softmax_j(s_t)_j c_j   per head h.
+ *   q [T][heads][nope + rope] bf16 (rope part rotated), tokens q_stride apart;
+ *   cache [n_blocks][block_size][latent + rope] bf16; block_table
+ *   [B][max_blocks], cu_new [B + 1], cu_kv [B + 1], seq_len [B] as
+ *   caee_paged_plan writes them; y [T][heads][v] (y_dtype), fully overwritten;
+ *   lse [T][heads] fp32 natural log of sum_j exp(s_tj), or NULL.
+ * A row that sees no token (padding past cu_new[B], seq_len 0) is zero, its
+ * lse -inf.  Cache rows at or past a request's seq_len are never read;
+ * rows that a query does not see do not change its result, whatever they hold.
+ * Scores, softmax statistics and sums are fp32; absorbed queries, expanded
+ * keys and values, and the softmax weights are rounded to bf16 before
+ * their products.
+ * Preconditions on device contents (violations: unspecified results,
+ * memory-safe): page numbers in [0, n_blocks) for the pages seq_len covers,
+ * at most max_new new tokens per request and max_kv tokens in all. */
+caee_status_t caee_latent_attention(const caee_latent_desc_t* desc, const void* q,
+                                    const caee_latent_weights_t* weights, const void* cache,
+                                    const int32_t* block_table, const int32_t* cu_new, const int32_t* cu_kv,
+                                    const int32_t* seq_len, void* y, float* lse, void* ws, size_t ws_bytes,
+                                    void* stream);
+
+/* y = x W^T with e4m3 weights: w [N][K] codes (`layout` order; tiled: N a
+ * multiple of 16), w_scale [ceil(N/128)][K/128] fp32, one per 128x128 block
+ * (the last row of blocks may be partial). */
+typedef struct caee_block_matmul_desc {
+    int32_t M;            /* rows of x, >= 0 */
+    int32_t N;            /* outputs, >= 1 */
+    int32_t K;            /* contraction, a positive multiple of 128, at most 65536 */
+    int32_t x_dtype;      /* CAEE_BF16, CAEE_F32 (quantised in the call, as by caee_quantize_rows) or CAEE_FP8_E4M3 */
+    int32_t y_dtype;      /* CAEE_BF16 or CAEE_F32 */
+    int32_t layout;       /* caee_layout_t of w */
+    int64_t x_stride;     /* elements from one row of x to the next, >= K, rows 16-byte aligned */
+    int64_t y_stride;     /* elements from one row of y to the next, >= N */
+} caee_block_matmul_desc_t;
+
+/* Bytes of workspace caee_block_matmul needs.  Host-only. */
+caee_status_t caee_block_matmul_workspace_size(const caee_block_matmul_desc_t* desc, size_t* bytes);
+
+/*   x_scale [M][K/128] fp32 for CAEE_FP8_E4M3 x (its row stride is K/128), else NULL.
+ * Per 128-deep block the code products are summed exactly enough (fp32) and
+ * the block's sum times x_scale times w_scale is added in fp32. */
+caee_status_t caee_block_matmul(const caee_block_matmul_desc_t* desc, const void* x, const float* x_scale,
+                                const void* w, const float* w_scale, void* y, void* ws, size_t ws_bytes,
+                                void* stream);
+
 /* Static description of a status code. */
 const char* caee_status_str(caee_status_t status);
 /* Message of the last error raised on the calling thread ("" if none). */
@@ -396,7 +540,10 @@ typedef enum caee_kernel_kind {
     CAEE_KERNEL_DOWN = 2,     /* expert down products */
     CAEE_KERNEL_COMBINE = 3,  /* weighted combine into y */
     CAEE_KERNEL_QUANT = 4,    /* fp8 activation quantisation (x and the SwiGLU rows) */
-    CAEE_KERNEL_KINDS = 5
+    CAEE_KERNEL_PLAN = 5,     /* paging plan and cache stores */
+    CAEE_KERNEL_ATTENTION = 6,/* latent attention, its products with W_uk and W_uv included */
+    CAEE_KERNEL_MATMUL = 7,   /* block-scaled 8-bit products (their quantisation counts as QUANT) */
+    CAEE_KERNEL_KINDS = 8
 } caee_kernel_kind_t;
 caee_status_t caee_timing_enable(int on);
 caee_status_t caee_timing_reset(void);

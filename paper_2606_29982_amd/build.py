@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcaee.so")
 SOURCES = ["api.hip", "route.hip", "ffn.hip", "ffn_fp8.hip", "ffn_gemm.hip", "ffn_prefill8.hip", "ffn_prefill8_down.hip",
-           "offload.hip"]
+           "offload.hip", "paged.hip", "latent.hip", "latent_absorbed.hip", "latent_expanded.hip", "block_matmul.hip"]
 
 # Packed-fp32 VALU ops are disabled on every HIP translation unit.
 HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

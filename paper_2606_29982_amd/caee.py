@@ -18,9 +18,10 @@ LIB_PATH = os.environ.get("CAEE_LIBRARY") or os.path.join(HERE, "libcaee.so")
 
 CAEE_OK, CAEE_ERR_INVALID_ARG, CAEE_ERR_UNSUPPORTED, CAEE_ERR_WORKSPACE, CAEE_ERR_HIP, CAEE_ERR_CAPACITY = range(6)
 CAEE_F32, CAEE_BF16, CAEE_FP8_E4M3 = 0, 1, 2
-KERNEL_KINDS = {"route": 0, "gate_up": 1, "down": 2, "combine": 3, "quant": 4}
+KERNEL_KINDS = {"route": 0, "gate_up": 1, "down": 2, "combine": 3, "quant": 4, "plan": 5, "attention": 6, "matmul": 7}
 DTYPE_CODE = {"f32": CAEE_F32, "bf16": CAEE_BF16, "fp8": CAEE_FP8_E4M3}
 IMPORTANCE_CODE = {"max": 0, "sum": 1, "cir": 2}
+LATENT_FORM_CODE = {"auto": 0, "absorbed": 1, "expanded": 2}
 REFILL_CODE = {"score": 0, "none": 1, "random": 2, "literal": 3}
 
 
@@ -68,6 +69,27 @@ class RouteOut(ctypes.Structure):
                 ("topk_ids", "topk_w", "orig_ids", "masks", "stats", "bin_loads")]
 
 
+class PagedPlanOut(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in
+                ("cu_new", "cu_kv", "seq_len", "slots", "position", "request", "free_head", "lacking")]
+
+
+class LatentDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("T", "B", "heads", "nope", "rope", "latent", "v", "block_size", "n_blocks", "max_blocks", "max_new",
+                 "causal", "form", "y_dtype")] + [
+        ("max_kv", ctypes.c_int64), ("q_stride", ctypes.c_int64), ("scale", ctypes.c_float)]
+
+
+class LatentWeights(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w_uk", "w_uk_t", "w_uv")]
+
+
+class BlockMatmulDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("M", "N", "K", "x_dtype", "y_dtype", "layout")] + [
+        ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64)]
+
+
 def _load(path: str = LIB_PATH):
     if not os.path.exists(path):
         raise ImportError(f"{path} is missing: build it with __graft_entry__.build() "
@@ -97,6 +119,15 @@ def _load(path: str = LIB_PATH):
         "caee_offload_residency": (st, [P, P]),
         "caee_offload_reset": (st, [P]),
         "caee_lru_step": (st, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, P, P, P, ctypes.c_int64, P, P, P, P]),
+        "caee_paged_plan": (st, [ctypes.c_int32] * 4 + [P, P, P, P, ctypes.c_int32, P,
+                                                        ctypes.POINTER(PagedPlanOut), P]),
+        "caee_latent_store": (st, [ctypes.c_int32] * 4 + [P, ctypes.c_int64, P, ctypes.c_int64, P, P, ctypes.c_int64,
+                                                          P]),
+        "caee_latent_workspace_size": (st, [ctypes.POINTER(LatentDesc), ctypes.POINTER(ctypes.c_size_t)]),
+        "caee_latent_attention": (st, [ctypes.POINTER(LatentDesc), P, ctypes.POINTER(LatentWeights), P, P, P, P, P, P,
+                                       P, P, ctypes.c_size_t, P]),
+        "caee_block_matmul_workspace_size": (st, [ctypes.POINTER(BlockMatmulDesc), ctypes.POINTER(ctypes.c_size_t)]),
+        "caee_block_matmul": (st, [ctypes.POINTER(BlockMatmulDesc), P, P, P, P, P, P, ctypes.c_size_t, P]),
         "caee_status_str": (ctypes.c_char_p, [st]),
         "caee_last_error": (ctypes.c_char_p, []),
         "caee_abi_version": (ctypes.c_int, []),
@@ -125,7 +156,8 @@ def load_library(path: str) -> None:
 EXPORTED = ("caee_workspace_size", "caee_route_prune", "caee_expert_ffn", "caee_moe_layer", "caee_moe_layer_noalloc",
             "caee_pack_matrix", "caee_quantize_rows", "caee_offload_create", "caee_offload_destroy",
             "caee_offload_layer", "caee_offload_stats", "caee_offload_residency", "caee_offload_reset",
-            "caee_lru_step", "caee_status_str", "caee_last_error", "caee_abi_version",
+            "caee_lru_step", "caee_paged_plan", "caee_latent_store", "caee_latent_workspace_size",
+            "caee_latent_attention", "caee_block_matmul_workspace_size", "caee_block_matmul", "caee_status_str", "caee_last_error", "caee_abi_version",
             "caee_timing_enable", "caee_timing_reset", "caee_timing_query")
 
 
@@ -321,6 +353,201 @@ def moe_layer_noalloc(layer: Layer, x, logits, bias, cost, bins, weights: dict, 
     _check(lib.caee_moe_layer_noalloc(ctypes.byref(d), _ptr(x), _ptr(logits), _ptr(bias), _ptr(cost), _ptr(bins),
                                       ctypes.byref(w), _ptr(y), None if ro is None else ctypes.byref(ro),
                                       _stream(x)))
+    return y
+
+
+# ---------------------------------------------------------------------------
+# The attention block in front of the layer.
+
+def _code(t) -> int:
+    import torch
+    code = {torch.bfloat16: CAEE_BF16, torch.float32: CAEE_F32, torch.uint8: CAEE_FP8_E4M3,
+            torch.float8_e4m3fn: CAEE_FP8_E4M3}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"tensor of dtype {t.dtype}: bfloat16, float32 or e4m3 codes (uint8, float8_e4m3fn) are taken")
+    return code
+
+
+def _need(t, name: str, dtype=None, shape=None, dense: bool = True):
+    """The argument checks that only the tensors' owner can make: device, dtype, shape, layout."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def alloc_paged_plan(B: int, T: int, device) -> dict:
+    """Device buffers for the plan of B requests and T token entries (caee_paged_plan_out_t)."""
+    import torch
+    i32 = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
+    return {"cu_new": i32(B + 1), "cu_kv": i32(B + 1), "seq_len": i32(B),
+            "slots": torch.empty(T, dtype=torch.int64, device=device), "position": i32(T), "request": i32(T),
+            "free_head": i32(1), "lacking": i32(1)}
+
+
+def paged_plan(block_size: int, ctx_len, new_len, block_table, free_list, free_head, out: dict) -> dict:
+    """Pages, slots and positions of a step's new tokens (caee_paged_plan).
+
+    ``ctx_len``/``new_len`` [B] int32: tokens each request has in the cache and receives; ``block_table``
+    [B][max_blocks] int32, updated in place; ``free_list`` int32 pages, used from ``free_head[0]`` on; ``out`` as
+    made by ``alloc_paged_plan`` (its ``free_head`` is the next call's input)."""
+    import torch
+    B, T = ctx_len.shape[0], out["slots"].shape[0]
+    i32 = torch.int32
+    _need(ctx_len, "ctx_len", i32)
+    _need(new_len, "new_len", i32, (B,))
+    if _need(block_table, "block_table", i32).dim() != 2 or block_table.shape[0] != B:
+        raise ValueError(f"block_table must be [{B}][max_blocks]")
+    _need(free_list, "free_list", i32)
+    _need(free_head, "free_head", i32, (1,))
+    for name, n in (("cu_new", B + 1), ("cu_kv", B + 1), ("seq_len", B), ("position", T), ("request", T),
+                    ("free_head", 1), ("lacking", 1)):
+        if out.get(name) is not None or name not in ("position", "request"):
+            _need(out[name], name, i32, (n,))
+    _need(out["slots"], "slots", torch.int64)
+    o = PagedPlanOut(*[_ptr(out.get(n)) for n, _ in PagedPlanOut._fields_])
+    _check(lib.caee_paged_plan(B, T, block_size, block_table.shape[1], _ptr(ctx_len), _ptr(new_len), _ptr(block_table),
+                               _ptr(free_list), free_list.shape[0], _ptr(free_head), ctypes.byref(o),
+                               _stream(free_head)))
+    return out
+
+
+def _rows(t, name: str):
+    """A 2-D tensor whose rows are dense; its row stride."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be 2-D with dense rows")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def latent_store(c, r, slots, cache):
+    """Rows [c_t | r_t] of T tokens into ``cache`` [n_blocks][block_size][latent + rope] bf16 at ``slots`` [T] int64
+    (caee_latent_store).  ``c`` [T][latent] and ``r`` [T][rope], bf16 or f32, may be slices of wider rows."""
+    import torch
+    T = c.shape[0]
+    cs, rs = _rows(c, "c"), _rows(r, "r")
+    _need(cache, "cache", torch.bfloat16)
+    _need(slots, "slots", torch.int64, (T,))
+    if c.dtype != r.dtype or r.shape[0] != T or cache.dim() != 3 or cache.shape[2] != c.shape[1] + r.shape[1]:
+        raise ValueError("c, r and cache do not fit together")
+    _check(lib.caee_latent_store(T, c.shape[1], r.shape[1], _code(c), _ptr(c), cs, _ptr(r), rs, _ptr(slots),
+                                 _ptr(cache), cache.shape[0] * cache.shape[1], _stream(cache)))
+    return cache
+
+
+@dataclass
+class Latent:
+    """Descriptor fields of latent attention that a layer keeps (see caee_latent_desc_t)."""
+
+    heads: int
+    nope: int
+    rope: int
+    latent: int
+    v: int
+    scale: float
+    causal: bool = True
+    form: str = "auto"          # "auto" | "absorbed" | "expanded" (caee_latent_form_t)
+
+    def desc(self, T: int, B: int, max_new: int, max_kv: int, block_size: int = 1, n_blocks: int = 1,
+             max_blocks: int = 1, q_stride: Optional[int] = None, y_dtype: int = CAEE_BF16) -> LatentDesc:
+        qs = self.heads * (self.nope + self.rope) if q_stride is None else q_stride
+        return LatentDesc(T, B, self.heads, self.nope, self.rope, self.latent, self.v, block_size, n_blocks,
+                          max_blocks, max_new, 1 if self.causal else 0, LATENT_FORM_CODE[self.form], y_dtype, max_kv,
+                          qs, self.scale)
+
+
+def latent_workspace_size(att: Latent, T: int, B: int, max_new: int, max_kv: int) -> int:
+    n = ctypes.c_size_t(0)
+    d = att.desc(T, B, max_new, max_kv)
+    _check(lib.caee_latent_workspace_size(ctypes.byref(d), ctypes.byref(n)))
+    return int(n.value)
+
+
+def alloc_latent_workspace(att: Latent, T: int, B: int, max_new: int, max_kv: int, device):
+    import torch
+    return torch.empty(max(latent_workspace_size(att, T, B, max_new, max_kv), 256), dtype=torch.uint8, device=device)
+
+
+def pack_latent_weights(w_uk, w_uv) -> dict:
+    """The weight dict of ``latent_attention`` from ``w_uk`` [heads][nope][latent] and ``w_uv`` [heads][v][latent]."""
+    return {"w_uk": w_uk.contiguous(), "w_uk_t": w_uk.transpose(1, 2).contiguous(), "w_uv": w_uv.contiguous()}
+
+
+def latent_attention(att: Latent, q, weights: dict, cache, block_table, plan: dict, y, ws, max_new: int, max_kv: int,
+                     lse=None):
+    """Latent attention of the new tokens over the paged cache (caee_latent_attention).
+
+    ``q`` [T][heads][nope + rope] bf16 (tokens may be strided); ``weights`` as made by ``pack_latent_weights``;
+    ``plan`` with ``cu_new``, ``cu_kv`` and ``seq_len`` as ``paged_plan`` writes them; ``max_new``/``max_kv``: host
+    bounds of a request's new tokens and of the sum of ``seq_len``; ``y`` [T][heads][v] bf16 or f32."""
+    import torch
+    bf, i32, H, R = torch.bfloat16, torch.int32, att.heads, att.latent
+    T, B = q.shape[0], block_table.shape[0]
+    _need(q, "q", bf, (T, H, att.nope + att.rope), dense=False)
+    if q.stride(2) != 1 or (H > 1 and q.stride(1) != att.nope + att.rope):
+        raise ValueError("q must have dense heads")
+    if _need(cache, "cache", bf).dim() != 3 or cache.shape[2] != R + att.rope:
+        raise ValueError(f"cache must be [n_blocks][block_size][{R + att.rope}]")
+    if _need(block_table, "block_table", i32).dim() != 2:
+        raise ValueError("block_table must be [B][max_blocks]")
+    for name, n in (("cu_new", B + 1), ("cu_kv", B + 1), ("seq_len", B)):
+        _need(plan[name], name, i32, (n,))
+    for name, shape in (("w_uk", (H, att.nope, R)), ("w_uk_t", (H, R, att.nope)), ("w_uv", (H, att.v, R))):
+        if weights.get(name) is not None:
+            _need(weights[name], name, bf, shape)
+    _need(y, "y", None, (T, H, att.v))
+    if lse is not None:
+        _need(lse, "lse", torch.float32, (T, H))
+    stride = q.stride(0) if T > 1 else H * (att.nope + att.rope)
+    d = att.desc(T, B, max_new, max_kv, cache.shape[1], cache.shape[0], block_table.shape[1], stride, _code(y))
+    w = LatentWeights(_ptr(weights.get("w_uk")), _ptr(weights.get("w_uk_t")), _ptr(weights.get("w_uv")))
+    _check(lib.caee_latent_attention(ctypes.byref(d), _ptr(q), ctypes.byref(w), _ptr(cache), _ptr(block_table),
+                                     _ptr(plan["cu_new"]), _ptr(plan["cu_kv"]), _ptr(plan["seq_len"]), _ptr(y),
+                                     _ptr(lse), _ptr(ws), ws.numel(), _stream(y)))
+    return y
+
+
+def _block_matmul_desc(x, N: int, y_dtype: int, layout: int, y_stride: int) -> BlockMatmulDesc:
+    return BlockMatmulDesc(x.shape[0], N, x.shape[1], _code(x), y_dtype, layout, _rows(x, "x"), y_stride)
+
+
+def block_matmul_workspace_size(x, N: int) -> int:
+    n = ctypes.c_size_t(0)
+    d = _block_matmul_desc(x, N, CAEE_F32, LAYOUT_ROWMAJOR, N)
+    _check(lib.caee_block_matmul_workspace_size(ctypes.byref(d), ctypes.byref(n)))
+    return int(n.value)
+
+
+def alloc_block_matmul_workspace(x, N: int, device):
+    import torch
+    return torch.empty(max(block_matmul_workspace_size(x, N), 256), dtype=torch.uint8, device=device)
+
+
+def block_matmul(x, w, w_scale, y, ws=None, x_scale=None, layout: int = LAYOUT_ROWMAJOR):
+    """y = x W^T with e4m3 weights and one fp32 scale per 128x128 block (caee_block_matmul).
+
+    ``x`` [M][K]: bf16 or f32 (quantised in the call) or e4m3 codes with ``x_scale`` [M][K/128]; rows may be strided,
+    those of ``y`` [M][N] (bf16 or f32) too.  ``w`` [N][K] codes in ``layout`` order, ``w_scale``
+    [ceil(N/128)][K/128].  ``ws`` as made by ``alloc_block_matmul_workspace`` (not needed for codes)."""
+    import torch
+    (M, K), N = x.shape, w.shape[0]
+    if _code(_need(w, "w", None, (N, K))) != CAEE_FP8_E4M3:
+        raise TypeError("w must be e4m3 codes")
+    _need(w_scale, "w_scale", torch.float32, ((N + 127) // 128, K // 128))
+    if x_scale is not None:
+        _need(x_scale, "x_scale", torch.float32, (M, K // 128))
+    ys = _rows(y, "y")
+    if tuple(y.shape) != (M, N):
+        raise ValueError(f"y must have shape {(M, N)}, got {tuple(y.shape)}")
+    d = _block_matmul_desc(x, N, _code(y), layout, ys)
+    _check(lib.caee_block_matmul(ctypes.byref(d), _ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(y), _ptr(ws),
+                                 0 if ws is None else ws.numel(), _stream(y)))
     return y
 
 

@@ -1,0 +1,165 @@
+// Host side of caee_latent_attention: checks, workspace, the two forms'
+// launches.
+#include <math.h>
+
+#include "latent.h"
+
+namespace caee {
+namespace {
+
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+bool latent_expanded(const caee_latent_desc_t& d) {
+    if (d.form != CAEE_LATENT_AUTO) return d.form == CAEE_LATENT_EXPANDED;
+    return (long long)d.T >= (long long)CAEE_LATENT_EXPAND_NEW * (d.B > 0 ? d.B : 1);
+}
+
+LatentWs latent_ws(const caee_latent_desc_t& d) {
+    LatentWs L{};
+    L.expanded = latent_expanded(d);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up256(bytes);
+        return here;
+    };
+    L.meta = take((size_t)(d.B + 1) * 4);
+    if (L.expanded) {
+        L.kv = take((size_t)d.max_kv * d.heads * (d.nope + d.v) * 2);
+        L.kr = take((size_t)d.max_kv * kRopeDim * 2);
+    } else {
+        const size_t th = (size_t)d.T * d.heads;
+        const size_t part_rows = (size_t)2 * kAbsGroups * kAbsTileRows;
+        L.q = take(th * (d.latent + kRopeDim) * 2);
+        L.o = take(th * d.latent * 4);
+        L.part = take(part_rows * d.latent * 4);
+        L.part_ml = take(part_rows * 2 * 4);
+    }
+    L.total = at;
+    return L;
+}
+
+caee_status_t check_latent(const caee_latent_desc_t* d) {
+    if (!d) return fail(CAEE_ERR_INVALID_ARG, "desc is NULL");
+    if (d->T < 0 || d->B < 0) return fail(CAEE_ERR_INVALID_ARG, "T=%d and B=%d must be >= 0", d->T, d->B);
+    if (d->heads < 1) return fail(CAEE_ERR_INVALID_ARG, "heads=%d must be >= 1", d->heads);
+    if (d->nope < 1 || d->rope < 1 || d->latent < 1 || d->v < 1)
+        return fail(CAEE_ERR_INVALID_ARG, "nope=%d, rope=%d, latent=%d and v=%d must be >= 1", d->nope, d->rope,
+                    d->latent, d->v);
+    if (d->block_size < 1 || d->block_size > 65536)
+        return fail(CAEE_ERR_INVALID_ARG, "block_size=%d must be in [1, 65536]", d->block_size);
+    if (d->n_blocks < 1 || d->max_blocks < 1)
+        return fail(CAEE_ERR_INVALID_ARG, "n_blocks=%d and max_blocks=%d must be >= 1", d->n_blocks, d->max_blocks);
+    if (d->max_new < 0 || d->max_kv < 0)
+        return fail(CAEE_ERR_INVALID_ARG, "max_new=%d and max_kv=%lld must be >= 0", d->max_new, (long long)d->max_kv);
+    if (d->causal != 0 && d->causal != 1) return fail(CAEE_ERR_INVALID_ARG, "causal=%d must be 0 or 1", d->causal);
+    if (d->form != CAEE_LATENT_AUTO && d->form != CAEE_LATENT_ABSORBED && d->form != CAEE_LATENT_EXPANDED)
+        return fail(CAEE_ERR_INVALID_ARG, "unknown form=%d", d->form);
+    if (d->y_dtype != CAEE_F32 && d->y_dtype != CAEE_BF16)
+        return fail(CAEE_ERR_INVALID_ARG, "y_dtype=%d must be CAEE_F32 or CAEE_BF16", d->y_dtype);
+    if (!(isfinite(d->scale) && d->scale > 0.0f)) return fail(CAEE_ERR_INVALID_ARG, "scale must be finite and > 0");
+    if (d->q_stride % 8 || d->q_stride < (int64_t)d->heads * (d->nope + d->rope))
+        return fail(CAEE_ERR_INVALID_ARG, "q_stride=%lld must be a multiple of 8 and hold heads * (nope + rope) values",
+                    (long long)d->q_stride);
+    // Limits of this build.
+    if ((d->nope != 64 && d->nope != 128) || d->rope != kRopeDim || (d->v != 64 && d->v != 128) ||
+        (d->latent != 128 && d->latent != 256 && d->latent != 512))
+        return fail(CAEE_ERR_UNSUPPORTED, "head parts nope=%d rope=%d latent=%d v=%d: nope and v must be 64 or 128, "
+                    "rope %d, latent 128, 256 or 512", d->nope, d->rope, d->latent, d->v, kRopeDim);
+    if (d->heads > 1024 || d->B > 65536 || d->T > (1 << 20))
+        return fail(CAEE_ERR_UNSUPPORTED, "heads=%d, B=%d or T=%d exceeds 1024, 65536 or %d", d->heads, d->B, d->T,
+                    1 << 20);
+    if ((long long)d->n_blocks * d->block_size > INT32_MAX || d->max_kv > INT32_MAX)
+        return fail(CAEE_ERR_UNSUPPORTED, "a cache of %lld rows, or %lld tokens in all, exceeds 2^31 - 1",
+                    (long long)d->n_blocks * d->block_size, (long long)d->max_kv);
+    // Shares of the absorbed form are counted in 32 bits.
+    const long long tiles = ((long long)d->max_new * d->heads + kAbsTileRows - 1) / kAbsTileRows;
+    if (!latent_expanded(*d) && (d->max_kv / 64 + d->B) * tiles > INT32_MAX / 2)
+        return fail(CAEE_ERR_UNSUPPORTED, "max_new=%d new tokens over max_kv=%lld: too many pairs for the absorbed form",
+                    d->max_new, (long long)d->max_kv);
+    return CAEE_OK;
+}
+
+}  // namespace
+}  // namespace caee
+
+using namespace caee;
+
+extern "C" {
+
+caee_status_t caee_latent_workspace_size(const caee_latent_desc_t* desc, size_t* bytes) {
+    clear_last_error();
+    if (!bytes) return fail(CAEE_ERR_INVALID_ARG, "bytes is NULL");
+    CAEE_TRY(check_latent(desc));
+    *bytes = latent_ws(*desc).total;
+    return CAEE_OK;
+}
+
+caee_status_t caee_latent_attention(const caee_latent_desc_t* desc, const void* q, const caee_latent_weights_t* weights,
+                                    const void* cache, const int32_t* block_table, const int32_t* cu_new,
+                                    const int32_t* cu_kv, const int32_t* seq_len, void* y, float* lse, void* ws,
+                                    size_t ws_bytes, void* stream) {
+    clear_last_error();
+    CAEE_TRY(check_latent(desc));
+    const caee_latent_desc_t& d = *desc;
+    const LatentWs L = latent_ws(d);
+    if (!weights) return fail(CAEE_ERR_INVALID_ARG, "weights is NULL");
+    const bool any = d.T > 0;
+    CAEE_TRY(check_ptr(q, "q", any));
+    CAEE_TRY(check_ptr(weights->w_uk, "weights->w_uk", any && L.expanded));
+    CAEE_TRY(check_ptr(weights->w_uk_t, "weights->w_uk_t", any && !L.expanded));
+    CAEE_TRY(check_ptr(weights->w_uv, "weights->w_uv", any));
+    CAEE_TRY(check_ptr(cache, "cache", any));
+    CAEE_TRY(check_ptr(block_table, "block_table", any && d.B > 0));
+    CAEE_TRY(check_ptr(cu_new, "cu_new", any));
+    CAEE_TRY(check_ptr(cu_kv, "cu_kv", any && L.expanded));
+    CAEE_TRY(check_ptr(seq_len, "seq_len", any && d.B > 0));
+    CAEE_TRY(check_ptr(y, "y", any));
+    CAEE_TRY(check_ptr(lse, "lse", false));
+    if (!any) return CAEE_OK;
+    if (!ws) return fail(CAEE_ERR_WORKSPACE, "workspace is NULL");
+    if (((uintptr_t)ws & 255u) != 0) return fail(CAEE_ERR_WORKSPACE, "workspace is not 256-byte aligned");
+    if (ws_bytes < L.total) return fail(CAEE_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, L.total);
+    char* w = (char*)ws;
+    LatentParams p{};
+    p.T = d.T;
+    p.B = d.B;
+    p.H = d.heads;
+    p.nope = d.nope;
+    p.latent = d.latent;
+    p.v = d.v;
+    p.block = d.block_size;
+    p.n_blocks = d.n_blocks;
+    p.max_blocks = d.max_blocks;
+    p.max_new = d.max_new;
+    p.causal = d.causal;
+    p.y_bf16 = d.y_dtype == CAEE_BF16;
+    p.max_kv = d.max_kv;
+    p.q_stride = d.q_stride;
+    p.scale = d.scale;
+    p.scale_log2 = d.scale * 1.4426950408889634f;
+    p.q = (const uint16_t*)q;
+    p.w_uk = (const uint16_t*)weights->w_uk;
+    p.w_uk_t = (const uint16_t*)weights->w_uk_t;
+    p.w_uv = (const uint16_t*)weights->w_uv;
+    p.cache = (const uint16_t*)cache;
+    p.table = block_table;
+    p.cu_new = cu_new;
+    p.cu_kv = cu_kv;
+    p.seq_len = seq_len;
+    p.y = y;
+    p.lse = lse;
+    p.meta = (int32_t*)(w + L.meta);
+    p.qw = (uint16_t*)(w + L.q);
+    p.o = (float*)(w + L.o);
+    p.part = (float*)(w + L.part);
+    p.part_ml = (float*)(w + L.part_ml);
+    p.kv = (uint16_t*)(w + L.kv);
+    p.kr = (uint16_t*)(w + L.kr);
+    hipStream_t s = (hipStream_t)stream;
+    return timed_launch(CAEE_KERNEL_ATTENTION, s, "latent attention", [&] {
+        return L.expanded ? launch_latent_expanded(p, s) : launch_latent_absorbed(p, s);
+    });
+}
+
+}  // extern "C"

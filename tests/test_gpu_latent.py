@@ -1,0 +1,184 @@
+"""GPU parity of latent attention, both forms, against the formula in
+float64."""
+import numpy as np
+import pytest
+import torch
+
+from attention_cases import LatentCase, TOL_ALL, check_attention
+from paper_2606_29982_amd import caee
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+FORMS = ["absorbed", "expanded"]
+
+
+def _check(form, causal=True, y_dtype=torch.bfloat16, **kw):
+    c = LatentCase(**kw)
+    print("case", form, causal, {k: v for k, v in kw.items()}, flush=True)
+    check_attention(c.run(DEV, form, causal, y_dtype), c.ref(causal))
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("S", [1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300, 1025])
+def test_one_new_token(S, form):
+    _check(form, seq=[S], new=[1], H=4, seed=S)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("H", [1, 3, 16, 33, 64, 65, 128])
+def test_heads(H, form):
+    _check(form, seq=[70, 5, 129], new=[1, 1, 1], H=H, seed=H)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("nope,latent,v", [(128, 512, 128), (64, 512, 128), (128, 512, 64), (128, 256, 128),
+                                           (64, 256, 64), (128, 128, 128), (64, 128, 64)])
+def test_head_layouts(nope, latent, v, form):
+    _check(form, seq=[90, 200], new=[3, 40], H=5 if nope + v == 256 else 6, nope=nope, latent=latent, v=v, seed=latent + v)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("block", [1, 3, 16, 64, 100])
+def test_page_sizes(block, form):
+    _check(form, seq=[1, 64, 150], new=[1, 2, 30], H=8, block=block, seed=block)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompts_ragged(form, causal):
+    _check(form, causal=causal, seq=[1, 17, 64, 255, 256, 257, 400], new=[1, 17, 64, 255, 256, 257, 300], H=2, seed=7)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_prompt_behind_a_prefix(form):
+    _check(form, seq=[700, 333], new=[290, 1], H=3, seed=8)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_requests_without_new_tokens_and_padding(form):
+    _check(form, seq=[40, 0, 9, 100, 5], new=[2, 0, 0, 1, 5], H=4, pad=11, seed=9)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_more_new_tokens_than_cached_leaves_rows_empty(form):
+    """seq_len below the new tokens: the first of them see nothing."""
+    _check(form, seq=[3, 20], new=[7, 2], H=4, seed=10)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_many_requests(form):
+    rng = np.random.default_rng(11)
+    seq = rng.integers(1, 90, 300)
+    _check(form, seq=seq, new=np.minimum(seq, rng.integers(1, 3, 300)), H=2, latent=128, seed=11)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_float32_output_and_strided_queries(form):
+    _check(form, y_dtype=torch.float32, seq=[50, 130], new=[2, 9], H=4, wide=40, seed=12)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_sharp_scores(form):
+    """Scores of spread 6: single tokens dominate, maxima move late.  The score's rounding weighs six times as much."""
+    c = LatentCase(seq=[500, 77], new=[1, 40], H=4, seed=13, q_std=6.0)
+    f = 1 + 6 * 3
+    check_attention(c.run(DEV, form), c.ref(), tol_all=f * TOL_ALL / 4, tol_row=f * TOL_ALL, tol_lse=6 * TOL_ALL * 2)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_growing_scores(form):
+    """Every later tile's scores exceed the ones before by far: each tile moves the running maximum."""
+    c = LatentCase(seq=[400], new=[2], H=4, seed=14)
+    for j in range(400):
+        c.set_row(0, j, c.rows[0][j] * (0.05 + j / 60.0))
+    got, ref = c.run(DEV, form), c.ref()
+    spread = 7.0
+    check_attention(got, ref, tol_all=(1 + 3 * spread) * TOL_ALL / 4, tol_row=(1 + 3 * spread) * TOL_ALL,
+                    tol_lse=4 * spread * TOL_ALL)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf"), 3.3e38])
+def test_unseen_tokens_may_hold_anything(bad, form):
+    """The last of five new tokens is garbage: the four before it do not see it (the cache's unowned rows are NaN always)."""
+    c = LatentCase(seq=[70, 130], new=[5, 2], H=4, seed=15)
+    c.set_row(0, 69, torch.full((576,), bad, dtype=torch.bfloat16))
+    (y, lse), (ry, rl) = c.run(DEV, form), c.ref()
+    keep = [0, 1, 2, 3, 5, 6]
+    check_attention((y[keep], lse[keep]), (ry[keep], rl[keep]))
+    if bad != bad:
+        assert np.all(np.isnan(y[4]))
+
+
+@pytest.mark.parametrize("heads,new", [(128, 1), (16, 1), (32, 2), (64, 1)])
+def test_long_context_is_split_and_joined(heads, new):
+    _check("absorbed", seq=[20000, 3], new=[new, 1], H=heads, block=64, seed=16)
+
+
+def test_long_prompt():
+    _check("expanded", seq=[1500], new=[1400], H=2, block=64, seed=17)
+
+
+def test_auto_takes_both_forms():
+    few, many = LatentCase(seq=[200], new=[1], H=4, seed=18), LatentCase(seq=[300], new=[200], H=4, seed=18)
+    for c, form in ((few, "absorbed"), (many, "expanded")):
+        a, f = c.run(DEV, "auto"), c.run(DEV, form)
+        assert np.array_equal(a[0], f[0]) and np.array_equal(a[1], f[1])
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_results_repeat_bit_for_bit(form):
+    c = LatentCase(seq=[3000, 40, 999], new=[2, 1, 30], H=16, seed=19)
+    a, b = c.run(DEV, form), c.run(DEV, form)
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
+def test_cache_past_4_gib():
+    """Pages whose byte offset does not fit 32 bits."""
+    c = LatentCase(seq=[100], new=[1], H=4, block=64, seed=20)
+    n = (5 << 30) // (64 * 576 * 2)
+    cache = torch.zeros((n + 2, 64, 576), dtype=torch.bfloat16, device=DEV)
+    for j, page in enumerate((n, n + 1)):
+        cache[page] = c.cache[int(c.table[0, j])].to(DEV)
+    c.table[0, :2] = (n, n + 1)
+    c.cache = cache
+    for form in FORMS:
+        check_attention(c.run(DEV, form), c.ref())
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_in_a_graph(form):
+    c = LatentCase(seq=[130, 64], new=[3, 2], H=4, seed=21)
+    att = caee.Latent(heads=4, nope=128, rope=64, latent=512, v=128, scale=c.scale, form=form)
+    to = lambda a, dt=None: torch.as_tensor(a).to(DEV, dt)  # noqa: E731
+    plan = dict(cu_new=to(c.cu_new, torch.int32), cu_kv=to(c.cu_kv, torch.int32), seq_len=to(c.seq, torch.int32))
+    q, cache, table, w = to(c.q), to(c.cache), to(c.table), caee.pack_latent_weights(to(c.w_uk), to(c.w_uv))
+    y = torch.empty((c.T, 4, 128), dtype=torch.bfloat16, device=DEV)
+    ws = caee.alloc_latent_workspace(att, c.T, 2, 8, 400, DEV)
+    call = lambda: caee.latent_attention(att, q, w, cache, table, plan, y, ws, max_new=8, max_kv=400)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for k in range(4):
+        q.copy_(torch.randn(q.shape, device=DEV).to(q.dtype))
+        plan["seq_len"].copy_(to(np.array([130 - 7 * k, 64 - k]), torch.int32))
+        plan["cu_kv"].copy_(to(np.array([0, 130 - 7 * k, 194 - 8 * k]), torch.int32))
+        y.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        y.zero_()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got, y) and float(y.float().abs().sum()) > 0
+
+
+def test_forms_agree_on_another_stream():
+    c = LatentCase(seq=[600, 31], new=[150, 31], H=4, seed=22)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        a, e = c.run(DEV, "absorbed"), c.run(DEV, "expanded")
+    d = np.linalg.norm(a[0] - e[0]) / np.linalg.norm(e[0])
+    assert d <= 2 * TOL_ALL
