@@ -15,6 +15,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace caee {
 namespace {
 
@@ -27,10 +29,12 @@ typedef __bf16 bm_bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bm_bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t bm_u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void bm_lds_void;
-typedef const __attribute__((address_space(1))) void bm_g_void;
 typedef const __attribute__((address_space(1))) bm_u32x4 bm_g_u32x4;
 
 constexpr int kBmMaxK = 65536;
+constexpr int kBmMaxStride = 1 << 22;  // elements from row to row of x: 256 rows stay within 2^32 bytes
+constexpr int kBmBufBytes = 0x7FFFFFFF, kBmBufWord3 = 0x00020000;   // buffer descriptor: size, raw 32-bit access
+constexpr int kBmBand = 8;            // row tiles of a band of k_bm_many's tile order
 constexpr int kUnitScale = 127;       // E8M0 1.0
 
 struct BmParams {
@@ -49,6 +53,17 @@ struct BmParams {
 
 __device__ inline bm_i32x8 bm_join(const bm_u32x4& a, const bm_u32x4& b) {
     return bm_i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+
+template <int N>
+using BmInt = std::integral_constant<int, N>;
+// f(BmInt<B>{}), ..., f(BmInt<E - 1>{}).
+template <int B, int E, class F>
+__device__ __attribute__((always_inline)) inline void bm_for(F&& f) {
+    if constexpr (B < E) {
+        f(BmInt<B>{});
+        bm_for<B + 1, E>(f);
+    }
 }
 
 __device__ inline uint32_t bm_pack(float a, float b) {
@@ -194,104 +209,181 @@ __global__ __launch_bounds__(WAVES * 64) void k_bm_few(BmParams p) {
     }
 }
 
-// Many rows: 256 outputs x 256 rows per workgroup, 8 waves of 128 x 64, one
-// 128-deep block per stage; both operands go global -> LDS directly, one
-// block ahead.  Blocks of 8 rows x 128 bytes, piece c of row r at
-// 8 (r % 8) + (c ^ (r % 8)).
+// Many rows: 256 outputs x 32 NT rows per workgroup, a 128-deep
+// block per stage, both operands two stages ahead.  Each of the 8 waves owns
+// 32 outputs, whose codes go straight to its registers (three sets in turn);
+// the rows' codes and scales go global -> LDS directly into a ring of three
+// and every wave reads all of them.  (Both operands through LDS leave room for
+// two stages only, and one stage of lookahead does not cover a fetch: 345 us
+// for 8000 rows, K = 4096, N = 7168, of which the loads alone take 244.)
+// Rows in LDS are blocks of 8 x 128 bytes, piece c of row r at
+// 8 (r % 8) + (c ^ bm_swz(r)): 16 rows' reads of a piece hit all 64 banks.
+__device__ inline int bm_swz(int r) { return (r >> 1) & 7; }
+template <int NT>
 struct BmStage {
-    bm_u32x4 a[32][kWave], b[32][kWave];
-    float xs[256];
+    bm_u32x4 b[4 * NT][kWave];
+    float xs[8][kWave];
+};
+struct BmCodes {
+    bm_u32x4 v[4];        // pieces hf, 2 + hf, 4 + hf, 6 + hf of a block of this lane's weight row
 };
 
-template <bool kExact>
-__global__ __launch_bounds__(512) void k_bm_many(BmParams p, int n_tiles) {
-    __shared__ BmStage st0, st1;
+template <int NT, bool kExact>
+__global__ __launch_bounds__(512) void k_bm_many(BmParams p, int n_tiles, int m_tiles) {
+#if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
+    using Stage = BmStage<NT>;
+    __shared__ Stage st0, st1, st2;
+    __shared__ float wscale[2][kBmMaxK / 128];
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave & 1, wn = wave >> 1;
-    const int n0 = (blockIdx.x % n_tiles) * 256, m0 = (blockIdx.x / n_tiles) * 256;
-    const uint8_t *asrc[4], *bsrc[4];
+    // Workgroups go to the XCDs round robin; each XCD takes a contiguous run
+    // of tiles, ordered by bands of kBmBand row tiles, so that the about 32
+    // that run there at a time share few rows and few outputs in its L2.
+    const int total = n_tiles * m_tiles, run = (total + kXcds - 1) / kXcds;
+    const int id = blockIdx.x % kXcds * run + blockIdx.x / kXcds;
+    if ((int)blockIdx.x / kXcds >= run || id >= total) return;
+    const int band = id / (kBmBand * n_tiles), high = min(kBmBand, m_tiles - band * kBmBand);
+    const int in_band = id - band * kBmBand * n_tiles;
+    const int n0 = in_band / high * 256, m0 = (band * kBmBand + in_band % high) * (32 * NT);
+    // Sources: buffers that begin at the workgroup's first row, 32-bit
+    // offsets of this lane's rows (clamped to the last; 256 rows span less
+    // than 2^31 bytes) and a uniform offset that moves with the block.
+    const uint8_t* wbase = p.w + (p.tiled ? (size_t)(n0 >> 4) * (p.K / 64) * 1024 : (size_t)n0 * p.K);
+    const uint8_t* xbase = p.xq + (size_t)m0 * p.xq_stride;
+    const __amdgpu_buffer_rsrc_t wbuf = __builtin_amdgcn_make_buffer_rsrc((void*)wbase, 0, kBmBufBytes, kBmBufWord3);
+    const __amdgpu_buffer_rsrc_t xbuf = __builtin_amdgcn_make_buffer_rsrc((void*)xbase, 0, kBmBufBytes, kBmBufWord3);
+    const __amdgpu_buffer_rsrc_t sbuf =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(p.xs + (size_t)m0 * p.kb), 0, kBmBufBytes, kBmBufWord3);
+    const int wr = min(32 * wave + n, p.N - 1 - n0);
+    uint32_t aoff = p.tiled ? (uint32_t)((wr >> 4) * (p.K / 64) * 1024 + ((wr & 15) + 16 * hf) * 16)
+                            : (uint32_t)(wr * p.K + 16 * hf);
+    const int half_step = p.tiled ? 1024 : 64, pair_step = p.tiled ? 512 : 32;    // pieces + 4, + 2
+    constexpr int kBLoads = (NT + 1) / 2;      // row blocks a wave fetches per stage (odd NT: the last ones twice)
+    uint32_t boff[kBLoads];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = 32 * wave + 8 * i + (lane >> 3), c = (lane & 7) ^ (lane >> 3);
-        asrc[i] = p.w + bm_piece(p, min(n0 + r, p.N - 1), c);
-        bsrc[i] = p.xq + (size_t)min(m0 + r, p.M - 1) * p.xq_stride + 16 * c;
+    for (int i = 0; i < kBLoads; ++i) {
+        const int blk = min(kBLoads * wave + i, 4 * NT - 1), rr = 8 * blk + (lane >> 3), c = (lane & 7) ^ bm_swz(rr);
+        boff[i] = (uint32_t)min(rr, p.M - 1 - m0) * (uint32_t)p.xq_stride + 16u * c;
+        asm volatile("" : "+v"(boff[i]));       // one register from here on
     }
-    const float* xsrc = p.xs + (size_t)min(m0 + 64 * (wave & 3) + lane, p.M - 1) * p.kb;
+    asm volatile("" : "+v"(aoff));
+    // Row scales: wave w loads rows 32 w .. + 31 (lanes 32 .. 63 repeat them).
+    const uint32_t xsoff = (uint32_t)min(32 * (wave % NT) + n, p.M - 1 - m0) * (uint32_t)p.kb * 4u;
     const int wstep = bm_block(p);
-    const float* wsc = p.ws + (size_t)min((n0 + 128 * wm) >> 7, (p.N - 1) >> 7) * p.kb;
-    auto load = [&](int k, BmStage& t) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            __builtin_amdgcn_global_load_lds((bm_g_void*)(asrc[i] + (size_t)k * wstep), (bm_lds_void*)&t.a[4 * wave + i][0], 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((bm_g_void*)(bsrc[i] + (size_t)k * 128), (bm_lds_void*)&t.b[4 * wave + i][0], 16, 0, 0);
+    constexpr int kLoads = 4 + kBLoads + 1;
+    // Load i of this wave's share of a stage.
+    auto load = [&](auto ic, int k, Stage& t, BmCodes& w) __attribute__((always_inline)) {
+        constexpr int i = decltype(ic)::value;
+        if constexpr (i < 4) {
+            w.v[i] = __builtin_bit_cast(bm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                wbuf, aoff, k * wstep + (i >> 1) * half_step + (i & 1) * pair_step, 0));
+        } else if constexpr (i < 4 + kBLoads) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xbuf, (bm_lds_void*)&t.b[min(kBLoads * wave + i - 4, 4 * NT - 1)][0], 16, boff[i - 4], k * 128, 0, 0);
+        } else {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(sbuf, (bm_lds_void*)&t.xs[wave][0], 4, xsoff, k * 4, 0, 0);
         }
-        if (wave < 4)
-            __builtin_amdgcn_global_load_lds((bm_g_void*)(xsrc + k), (bm_lds_void*)&t.xs[64 * wave], 4, 0, 0);
     };
-    bm_f32x16 acc[4][2] = {};
+    // This lane's fragments of a 32-row tile: row n, pieces 2 q + hf of a
+    // block, at base ^ 2 q.
+    const int base = (n >> 3) * kWave + (n & 7) * 8 + (hf ^ bm_swz(n));
+    bm_f32x16 acc[NT] = {};
     const bm_f32x16 zero = {};
-    auto step = [&](int k, BmStage& t, BmStage& next) __attribute__((always_inline)) {
-        __builtin_amdgcn_s_waitcnt((0) | (7 << 4) | (15 << 8));
+    const int wrow = (32 * wave) >> 7;
+    auto step = [&](int k, Stage& t, const BmCodes& w, Stage& tn, BmCodes& wn) __attribute__((always_inline)) {
+        // All but the next stage's loads have landed; after the barrier
+        // everybody's have, and nobody reads the stage `tn` any more.
+        __builtin_amdgcn_s_waitcnt((kLoads & 15) | (7 << 4) | (15 << 8) | ((kLoads >> 4) << 14));
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (k + 1 < p.kb) load(k + 1, next);
-        auto frag = [&](const bm_u32x4* row, int kk) __attribute__((always_inline)) {
-            return bm_join(row[(n & 7) * 8 + ((4 * kk + hf) ^ (n & 7))], row[(n & 7) * 8 + ((4 * kk + 2 + hf) ^ (n & 7))]);
+        const int ahead = min(k + 2, p.kb - 1);     // past the end the last block again, read by nobody
+        const float ws = wscale[wrow][k];
+        int at[4];
+        at[0] = base;
+        asm volatile("" : "+v"(at[0]));     // the other three are made in the step, not kept through the loop
+#pragma unroll
+        for (int q = 1; q < 4; ++q) at[q] = at[0] ^ (2 * q);
+        auto rows = [&](int i, int q) __attribute__((always_inline)) { return t.b[4 * i][at[q]]; };
+        auto scale = [&](int i) __attribute__((always_inline)) { return t.xs[i][n]; };
+        auto add = [&](bm_f32x16& c, const bm_f32x16& q, float f) __attribute__((always_inline)) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) c[v] += q[v] * f;
         };
-        bm_i32x8 b[2][2];
-        float f[2];
+        if constexpr (kExact) {
+            bm_bf16x8 a[8];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) b[e][kk] = frag(t.b[8 * wn + 4 * e + (n >> 3)], kk);
-            f[e] = t.xs[64 * wn + 32 * e + n] * wsc[k];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bm_u32x4* row = t.a[16 * wm + 4 * i + (n >> 3)];
-            const bm_i32x8 a0 = frag(row, 0), a1 = frag(row, 1);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                bm_f32x16 q = zero;
-                if constexpr (kExact) {
-#pragma unroll
-                    for (int kk = 0; kk < 2; ++kk) {
-                        const bm_i32x8& a = kk ? a1 : a0;
-#pragma unroll
-                        for (int v = 0; v < 4; ++v)
-                            q = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bm_wide(a[2 * v], a[2 * v + 1]),
-                                                                        bm_wide(b[e][kk][2 * v], b[e][kk][2 * v + 1]), q,
-                                                                        0, 0, 0);
-                    }
-                } else {
-                    q = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a0, b[e][0], zero, 0, 0, 0, kUnitScale, 0,
-                                                                        kUnitScale);
-                    q = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a1, b[e][1], q, 0, 0, 0, kUnitScale, 0,
-                                                                        kUnitScale);
-                }
-#pragma unroll
-                for (int v = 0; v < 16; ++v) acc[i][e][v] += q[v] * f[e];
+            for (int q = 0; q < 4; ++q) {
+                a[2 * q] = bm_wide(w.v[q][0], w.v[q][1]);
+                a[2 * q + 1] = bm_wide(w.v[q][2], w.v[q][3]);
             }
+            bm_for<0, NT>([&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value;
+                bm_f32x16 s = zero;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const bm_u32x4 v = rows(i, q);
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[2 * q], bm_wide(v[0], v[1]), s, 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[2 * q + 1], bm_wide(v[2], v[3]), s, 0, 0, 0);
+                }
+                bm_for<i * kLoads / NT, (i + 1) * kLoads / NT>(
+                    [&](auto lc) __attribute__((always_inline)) { load(lc, ahead, tn, wn); });
+                add(acc[i], s, scale(i) * ws);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        } else {
+            // Tile by tile: the next tile's rows are read and one of the loads
+            // of the stage after next issued while this one is multiplied
+            // (a CU takes only so many requests at a time, and a wave waits at
+            // a load that is not taken).
+            const bm_i32x8 a0 = bm_join(w.v[0], w.v[1]), a1 = bm_join(w.v[2], w.v[3]);
+            bm_u32x4 bq[2][4];
+            float f[2];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) bq[0][q] = rows(0, q);
+            f[0] = scale(0);
+            bm_for<0, NT>([&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value;
+                bm_f32x16 q = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a0, bm_join(bq[i & 1][0], bq[i & 1][1]), zero,
+                                                                             0, 0, 0, kUnitScale, 0, kUnitScale);
+                q = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a1, bm_join(bq[i & 1][2], bq[i & 1][3]), q, 0, 0, 0,
+                                                                    kUnitScale, 0, kUnitScale);
+                if constexpr (i + 1 < NT) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) bq[(i + 1) & 1][v] = rows(i + 1, v);
+                    f[(i + 1) & 1] = scale(i + 1);
+                }
+                bm_for<i * kLoads / NT, (i + 1) * kLoads / NT>(
+                    [&](auto lc) __attribute__((always_inline)) { load(lc, ahead, tn, wn); });
+                add(acc[i], q, f[i & 1] * ws);
+                __builtin_amdgcn_sched_barrier(0);
+            });
         }
     };
-    load(0, st0);
-    for (int k = 0; k < p.kb; k += 2) {
-        step(k, st0, st1);
-        if (k + 1 < p.kb) step(k + 1, st1, st0);
+    BmCodes w0, w1, w2;
+    bm_for<0, kLoads>([&](auto ic) __attribute__((always_inline)) { load(ic, 0, st0, w0); });
+    bm_for<0, kLoads>([&](auto ic) __attribute__((always_inline)) { load(ic, min(1, p.kb - 1), st1, w1); });
+    for (int i = threadIdx.x; i < 2 * p.kb; i += 512) {
+        const int h = i / p.kb;
+        wscale[h][i - h * p.kb] = p.ws[(size_t)min((n0 >> 7) + h, (p.N - 1) >> 7) * p.kb + i - h * p.kb];
     }
+    __syncthreads();
+    for (int k = 0; k < p.kb; k += 3) {
+        step(k, st0, w0, st2, w2);
+        if (k + 1 < p.kb) step(k + 1, st1, w1, st0, w0);
+        if (k + 2 < p.kb) step(k + 2, st2, w2, st1, w1);
+    }
+    __builtin_amdgcn_s_waitcnt((0) | (7 << 4) | (15 << 8));      // the last blocks' second readings have landed
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int m = m0 + 64 * wn + 32 * e + n;
+    for (int e = 0; e < NT; ++e) {
+        int m = m0 + 32 * e + n;
+        asm volatile("" : "+v"(m));     // keeps the address arithmetic here, out of the stage loop
         if (m >= p.M) continue;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                bm_store4(p, m, n0 + 128 * wm + 32 * i + 8 * q + 4 * hf, acc[i][e][4 * q], acc[i][e][4 * q + 1],
-                          acc[i][e][4 * q + 2], acc[i][e][4 * q + 3]);
+        for (int q = 0; q < 4; ++q)
+            bm_store4(p, m, n0 + 32 * wave + 8 * q + 4 * hf, acc[e][4 * q], acc[e][4 * q + 1], acc[e][4 * q + 2],
+                      acc[e][4 * q + 3]);
     }
+#endif
 }
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -319,6 +411,8 @@ caee_status_t check_bm(const caee_block_matmul_desc_t* d) {
                     (long long)d->x_stride, d->K);
     if (d->y_stride < d->N) return fail(CAEE_ERR_INVALID_ARG, "y_stride=%lld must be >= N=%d", (long long)d->y_stride, d->N);
     // Limits of this build.
+    if (d->x_stride > kBmMaxStride)
+        return fail(CAEE_ERR_UNSUPPORTED, "x_stride=%lld exceeds %d", (long long)d->x_stride, kBmMaxStride);
     if (d->K > kBmMaxK || d->M > (1 << 24) || d->N > (1 << 24))
         return fail(CAEE_ERR_UNSUPPORTED, "M=%d, N=%d or K=%d exceeds %d, %d, %d", d->M, d->N, d->K, 1 << 24, 1 << 24,
                     kBmMaxK);
@@ -326,6 +420,7 @@ caee_status_t check_bm(const caee_block_matmul_desc_t* d) {
 }
 
 constexpr int kBmExactK = 256;
+constexpr int kBmCus = 256;            // CUs of the chip, one workgroup of k_bm_many each at a time
 
 template <int WAVES, bool kExact>
 void launch_few(const BmParams& p, hipStream_t s) {
@@ -336,11 +431,44 @@ void launch_few(const BmParams& p, hipStream_t s) {
     else hipLaunchKernelGGL((k_bm_few<4, WAVES, kExact>), dim3(nt, (unsigned)((p.M + 63) / 64)), block, 0, s, p);
 }
 
+// Row tiles per workgroup: the height whose whole rounds of the chip's CUs
+// take the least (8000 rows x 7168 outputs: 4 rounds of 8, 4 of 7, 5 of 6).
+int bm_height(const BmParams& p) {
+    int best = 8;
+    long long least = 0;
+    for (int nt = 8; nt >= 4; --nt) {
+        const long long tiles = (long long)((p.M + 32 * nt - 1) / (32 * nt)) * ((p.N + 255) / 256);
+        const long long cost = (tiles + kBmCus - 1) / kBmCus * (nt + 1);     // a workgroup's fixed part: about a tile row
+        if (least == 0 || cost < least) {
+            least = cost;
+            best = nt;
+        }
+    }
+    return best;
+}
+
+template <int NT, bool kExact>
+void launch_many(const BmParams& p, hipStream_t s) {
+    const int n_tiles = (p.N + 255) / 256, m_tiles = (p.M + 32 * NT - 1) / (32 * NT);
+    const unsigned grid = (unsigned)((n_tiles * m_tiles + kXcds - 1) / kXcds * kXcds);
+    hipLaunchKernelGGL((k_bm_many<NT, kExact>), dim3(grid), dim3(512), 0, s, p, n_tiles, m_tiles);
+}
+
 template <bool kExact>
 hipError_t launch_bm(const BmParams& p, hipStream_t s) {
     const long long tiles = (long long)((p.M + 255) / 256) * ((p.N + 255) / 256);
     if (p.M > 64 && (tiles >= 128 || p.M > 1024)) {
-        hipLaunchKernelGGL(k_bm_many<kExact>, dim3((unsigned)tiles), dim3(512), 0, s, p, (p.N + 255) / 256);
+        if constexpr (kExact) {
+            launch_many<4, true>(p, s);
+        } else {
+            switch (bm_height(p)) {
+                case 4: launch_many<4, false>(p, s); break;
+                case 5: launch_many<5, false>(p, s); break;
+                case 6: launch_many<6, false>(p, s); break;
+                case 7: launch_many<7, false>(p, s); break;
+                default: launch_many<8, false>(p, s); break;
+            }
+        }
     } else {
         launch_few<8, kExact>(p, s);
     }

@@ -14,7 +14,6 @@ constexpr int kRopeDim = 64;          // rotary part of a query and of a cache r
 // requests; a share begins and ends inside a request, so a workgroup leaves
 // at most two partial results.
 constexpr int kAbsGroups = 256;
-constexpr int kAbsTileRows = 64;      // query rows of such a workgroup
 constexpr int kExpRows = 256;         // query rows of a workgroup of the expanded form
 
 struct LatentWs {
@@ -24,6 +23,7 @@ struct LatentWs {
     size_t part, part_ml; // absorbed: [2 groups][rows][latent] partial sums and [..][rows][2] (maximum, sum)
     size_t kv, kr;        // expanded: [max_kv][heads][nope + v] keys and values, [max_kv][rope] rotary keys
     size_t total;
+    int row_tiles;        // absorbed: 32-row tiles of a workgroup (1, 2 or 4)
     bool expanded;
 };
 
@@ -52,7 +52,7 @@ struct LatentParams {
     uint16_t* kr;
 };
 
-hipError_t launch_latent_absorbed(const LatentParams& p, hipStream_t s);
+hipError_t launch_latent_absorbed(const LatentParams& p, int row_tiles, hipStream_t s);
 hipError_t launch_latent_expanded(const LatentParams& p, hipStream_t s);
 
 typedef uint32_t lat_u32x4 __attribute__((ext_vector_type(4)));
@@ -61,17 +61,30 @@ typedef short lat_s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 lat_bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 lat_bf16x2 __attribute__((ext_vector_type(2)));
 typedef float lat_f32x2 __attribute__((ext_vector_type(2)));
+typedef float lat_f32x4 __attribute__((ext_vector_type(4)));
 typedef float lat_f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) lat_s16x4 lat_lds_s16x4;
 typedef __attribute__((address_space(3))) void lat_lds_void;
 typedef const __attribute__((address_space(1))) void lat_g_void;
 
+constexpr int kLatBufBytes = 0x7FFFFFFF, kLatBufWord3 = 0x00020000;   // buffer descriptor: size, raw 32-bit access
+template <int N>
+using LatInt = std::integral_constant<int, N>;
+// f(LatInt<B>{}), ..., f(LatInt<E - 1>{}).
+template <int B, int E, class F>
+__device__ __attribute__((always_inline)) inline void lat_for(F&& f) {
+    if constexpr (B < E) {
+        f(LatInt<B>{});
+        lat_for<B + 1, E>(f);
+    }
+}
+
 constexpr float kNoScore = -1e30f;    // running maximum of a row that has seen nothing
-// The running maximum follows the tiles' only when it would grow by more than
-// this (in powers of two): the weights are then at most 2^8, which costs
+// The running maximum moves only when a score exceeds it by more than
+// kMaxSlack (in powers of two): the weights are then at most 2^8, which costs
 // neither fp32 sums nor bf16 weights any precision, and the accumulators are
 // rescaled a few times per row instead of at every new maximum.
-constexpr float kMaxSlack = 8.0f;
+constexpr float kMaxSlack = 8.0f, kMaxWeight = 256.0f;
 
 template <int N>
 __device__ inline void lat_wait_vm() {
@@ -88,18 +101,31 @@ __device__ inline lat_f32x16 lat_mma(const lat_u32x4& a, const lat_u32x4& b, con
                                                    __builtin_bit_cast(lat_bf16x8, b), c, 0, 0, 0);
 }
 
+__device__ inline lat_f32x4 lat_mma16(const lat_u32x4& a, const lat_u32x4& b, const lat_f32x4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(lat_bf16x8, a),
+                                                   __builtin_bit_cast(lat_bf16x8, b), c, 0, 0, 0);
+}
+
 // Two floats rounded to bf16 (nearest even), a in the low half.
 __device__ inline uint32_t lat_pack(float a, float b) {
     const lat_f32x2 t = {a, b};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(t, lat_bf16x2));
 }
 
-// Position of 16-byte piece c of row r in an LDS row whose length is a
-// multiple of eight pieces: c ^ lat_swz(r).  Rows r .. r + 7 get eight
-// different values, so the one-piece-per-row reads of the score product hit
-// eight different bank groups; rows r .. r + 3 differ by multiples of two
-// (4 | r), so the two pieces per row of a transposed read do as well.
-__device__ inline int lat_swz(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+// sum + both bf16 values of v.
+__device__ inline float lat_sum2(uint32_t v, float sum) {
+    const lat_bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(lat_bf16x2, v), one, sum, false);
+}
+
+// KV tiles in LDS are blocks of 8 rows x 128 bytes; piece c (16 bytes) of row
+// r is at 8 (r % 8) + (c ^ lat_swz(r)).  A 16-byte read takes 16 lanes at a
+// time over 64 banks: 16 rows' piece c, of which the even and the odd rows
+// fall into different halves of the banks and the eight of each half into
+// different places by the three bits that lat_swz permutes.  A transposed
+// read takes four pieces of each of four rows: rows r and r + 2 (4 | r) differ
+// in the swizzle's top bit, so in different quarters.
+__device__ inline int lat_swz(int r) { return ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3); }
 
 // Maximum, or sum, over a lane and its partner 32 lanes away (the two halves
 // of a 32 x 32 tile's column).
@@ -128,6 +154,20 @@ __device__ inline int lat_find(const int32_t* a, int n, int x) {
         else hi = mid;
     }
     return lo;
+}
+
+// The same for an x that the wave's lanes share, 64 entries at a time.
+__device__ inline int lat_find_wave(const int32_t* a, int n, int x) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int lo = 0, len = n;
+    while (len > 1) {
+        const int step = (len + kWave - 1) / kWave, at = lane * step;
+        const unsigned long long le = __ballot(at < len && a[lo + min(at, len - 1)] <= x);
+        const int k = (63 - __clzll(le | 1ull)) * step;
+        lo += k;
+        len = min(step, len - k);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
 }
 
 // Cache row of token `pos` of request b.

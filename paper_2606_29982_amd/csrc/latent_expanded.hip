@@ -67,14 +67,14 @@ __global__ __launch_bounds__(kExpandThreads) void k_expand(LatentParams p) {
         const int b = lat_find(p.cu_kv, p.B, s);
         return p.cache + (size_t)lat_slot(p, b, s - p.cu_kv[b]) * row_bytes;
     };
-    const int swz = 8 * ((lane & 7) ^ lat_swz(lane >> 3));
     const uint16_t *wsrc[4], *xsrc[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int j = ft * 128 + 32 * wave + 8 * i + (lane >> 3), h = j / hw, jj = j - h * hw;
+        const int r = 8 * i + (lane >> 3), swz = 8 * ((lane & 7) ^ lat_swz(r));
+        const int j = ft * 128 + 32 * wave + r, h = j / hw, jj = j - h * hw;
         wsrc[i] = (jj < p.nope ? p.w_uk + ((size_t)h * p.nope + jj) * p.latent
                                : p.w_uv + ((size_t)h * p.v + jj - p.nope) * p.latent) + swz;
-        xsrc[i] = cache_row(s0 + 32 * wave + 8 * i + (lane >> 3)) + swz;
+        xsrc[i] = cache_row(s0 + 32 * wave + r) + swz;
     }
     if (ft == 0) {
         for (int i = threadIdx.x; i < 128 * 8; i += kExpandThreads) {
@@ -133,22 +133,26 @@ __global__ __launch_bounds__(kExpandThreads) void k_expand(LatentParams p) {
     }
 }
 
-// One KV tile of a head: keys (nope groups, then the rotary one) and values,
-// blocks of 8 tokens x 128 bytes as above.
-template <int NOPE, int V>
+// One tile of a head's keys (nope groups, then the rotary one) or values: G
+// groups of 128 bytes of 64 tokens, blocks of 8 tokens x 128 bytes as above.
+template <int G>
 struct PromptTile {
-    static constexpr int kGk = NOPE / 64 + 1, kGv = V / 64;
-    lat_u32x4 k[kKvTile / 8][kGk][kWave];
-    lat_u32x4 v[kKvTile / 8][kGv][kWave];
+    lat_u32x4 v[kKvTile / 8][G][kWave];
 };
 
 template <int NOPE, int V>
 __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int tiles) {
-    using Tile = PromptTile<NOPE, V>;
-    constexpr int kGk = Tile::kGk, kGv = Tile::kGv;
+#if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
+    constexpr int kGk = NOPE / 64 + 1, kGv = V / 64;
+    using Keys = PromptTile<kGk>;
+    using Values = PromptTile<kGv>;
     constexpr int kJ = 4 * kGk, NC = V / 32;
+    constexpr int kAhead = 5;                  // fragments read from LDS ahead of their MFMAs
     constexpr int kLoads = kGk + kGv;          // loads of a wave per tile: one block of 8 tokens
-    __shared__ Tile st0, st1, st2;
+    // An object per stage: the compiler can tell the reads of one from the
+    // loads that fill another.
+    __shared__ Keys kt0, kt1, kt2;
+    __shared__ Values vt0, vt1, vt2;
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Workgroups go to the XCDs round robin: all tiles of a head run on one
@@ -165,7 +169,7 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
     }
     const int tile = p.meta[p.B] - 1 - q;
     if (tile < 0) return;
-    const int b = lat_find(p.meta, p.B, tile);
+    const int b = lat_find_wave(p.meta, p.B, tile);
     const LatentReq rq = lat_req(p, b);
     const int row0 = (tile - p.meta[b]) * kExpRows;
     const int kv0 = p.cu_kv[b];
@@ -173,8 +177,7 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
     const int my0 = row0 + 32 * wave;
     const int row = min(my0 + n, rq.add - 1);
     const int limit = sees(row);
-    const int lim_min = sees(min(my0, rq.add - 1)), lim_max = sees(min(my0 + 31, rq.add - 1));
-    const int lim_wg = sees(row0);
+    const int lim_min = sees(min(my0, rq.add - 1)), lim_wg = sees(row0);
     const int end = sees(min(row0 + kExpRows, rq.add) - 1);
     const int steps = (end + kKvTile - 1) / kKvTile;
     const int t = rq.t0 + row;
@@ -188,107 +191,213 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
     for (int c = 0; c < NC; ++c) o[c] = lat_f32x16{};
     float m = kNoScore, l = 0.0f;
 
-    int kpos[4], vpos[2];
+    int kpos[4], vpos[2][2];       // [piece], [column tile parity][eight of a 16-token step]
 #pragma unroll
     for (int j = 0; j < 4; ++j) kpos[j] = (n >> 3) * (kGk * kWave) + (n & 7) * 8 + ((2 * j + hf) ^ lat_swz(n));
     const int vrow = 4 * hf + ((lane & 15) >> 2);
 #pragma unroll
     for (int j = 0; j < 2; ++j)
-        vpos[j] = 2 * (vrow * 8 + ((4 * j + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ lat_swz(vrow))) + (lane & 1);
-
-    const int swz = 8 * ((lane & 7) ^ lat_swz(lane >> 3));
-    const size_t kv_row = (size_t)p.H * (NOPE + V);
-    auto load = [&](int s, Tile& d) __attribute__((always_inline)) {
-        const int tok = min(s * kKvTile + 8 * wave + (lane >> 3), rq.seq - 1);
-        const long long at = min((long long)kv0 + tok, p.max_kv - 1);
-        const uint16_t* src = p.kv + (size_t)at * kv_row + (size_t)h * (NOPE + V) + swz;
-#pragma unroll
-        for (int g = 0; g < NOPE / 64; ++g)
-            __builtin_amdgcn_global_load_lds((lat_g_void*)(src + 64 * g), (lat_lds_void*)&d.k[wave][g][0], 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((lat_g_void*)(p.kr + (size_t)at * kRopeDim + swz),
-                                         (lat_lds_void*)&d.k[wave][kGk - 1][0], 16, 0, 0);
-#pragma unroll
-        for (int g = 0; g < kGv; ++g)
-            __builtin_amdgcn_global_load_lds((lat_g_void*)(src + NOPE + 64 * g), (lat_lds_void*)&d.v[wave][g][0], 16, 0, 0);
-    };
-    auto step = [&](int s, Tile& d, Tile& next) __attribute__((always_inline)) {
-        const int tb = s * kKvTile;
-        // The loads of one later tile may stay in flight; the barrier says that
-        // the tile is whole and that nobody reads the stage `next` fills.
-        if (s + 1 < steps) lat_wait_vm<kLoads>();
-        else lat_wait_vm<0>();
-        lat_barrier();
-        if (s + 2 < steps) load(s + 2, next);
-        if (tb + kKvTile > lim_wg) {
-            // Tokens that some rows do not see may hold anything: infinities
-            // and NaNs must not meet their zero weights (rows that see such
-            // a token have it in their scores).
-            const int r0 = max(lim_wg - tb, 0);
-            for (int i = threadIdx.x; i < (kKvTile - r0) * (V / 8); i += kPromptThreads) {
-                const int r = r0 + i / (V / 8), c = i % (V / 8);
-                lat_u32x4& v = d.v[r >> 3][c >> 3][(r & 7) * 8 + (c & 7)];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = lat_finite(v[e]);
-            }
-            __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
-            lat_barrier();
-        }
-        if (tb >= lim_max || my0 >= rq.add) return;    // this wave's rows see none of it
-        lat_f32x16 sc[2] = {};
-#pragma unroll
-        for (int j = 0; j < kJ; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                sc[e] = lat_mma((&d.k[0][0][0])[kpos[j % 4] + (4 * e * kGk + j / 4) * kWave], qf[j], sc[e]);
-        const bool masked = tb + kKvTile > lim_min;
-        float mt = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 2; ++e)
+            vpos[j][e] = 2 * (vrow * 8 + ((4 * j + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ lat_swz(8 * e + vrow))) + (lane & 1);
+
+    // A wave fetches 8 tokens of a tile: descriptors begin at the tile's first
+    // row (uniform), lanes at piece lane % 8 (swizzled) of row lane / 8.
+    // (Buffer loads: the compiler counts the LDS reads apart from them.)
+    const uint32_t kv_row = (uint32_t)p.H * (NOPE + V) * 2u;
+    const int swz = 16 * ((lane & 7) ^ lat_swz(8 * wave + (lane >> 3)));
+    struct Source {
+        const char *kv, *kr;      // uniform: the tile's first row (this head's part), its rotary row
+        uint32_t row;             // this lane's row
+    };
+    const char* kv_head = (const char*)p.kv + (size_t)h * (NOPE + V) * 2;
+    auto source = [&](int s) __attribute__((always_inline)) {
+        const int first = (int)min((long long)kv0 + s * kKvTile, p.max_kv - 1);
+        const int most = min(rq.seq - 1 - s * kKvTile, (int)p.max_kv - 1 - first);
+        return Source{kv_head + (size_t)first * kv_row, (const char*)p.kr + (size_t)first * (kRopeDim * 2),
+                      (uint32_t)max(min(8 * wave + (lane >> 3), most), 0)};
+    };
+    // Load i of the wave's part of a tile: the groups of the keys (the rotary
+    // one last), then of the values.
+    auto load = [&](auto ic, const Source& from, Keys& k, Values& v) __attribute__((always_inline)) {
+        constexpr int i = decltype(ic)::value;
+        const char* base = i == kGk - 1 ? from.kr : from.kv;
+        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, kLatBufBytes, kLatBufWord3);
+        if constexpr (i == kGk - 1) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&k.v[wave][i][0], 16,
+                                                     from.row * (kRopeDim * 2) + swz, 0, 0, 0);
+        } else if constexpr (i < kGk - 1) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&k.v[wave][i][0], 16, from.row * kv_row + swz,
+                                                     128 * i, 0, 0);
+        } else {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&v.v[wave][i - kGk][0], 16,
+                                                     from.row * kv_row + swz, 128 * (i - 1), 0, 0);
+        }
+    };
+    // Step s has two phases: X multiplies the keys of tile s and sums the
+    // values of tile s - 1 (40 MFMAs at 128 + 64, 128), Y makes the weights of
+    // tile s (exponentials) and starts loads.  The two waves of a SIMD take
+    // turns: waves 4 .. 7 run one barrier behind waves 0 .. 3, so that one is in
+    // X while the other is in Y.  Keys of tile s are read in phases 2 s (waves
+    // 0 .. 3) and 2 s + 1 (4 .. 7), values in 2 s + 2 and 2 s + 3; so in Y(s) the
+    // first waves, in phase 2 s + 1, may load the keys of tile s + 2 and the
+    // values of tile s + 1 into rings of three, the others, in phase 2 s + 2,
+    // those of one tile more.  At the end of the odd phases (Y of the first
+    // waves, X of the others) a wave waits for all but its latest step's loads:
+    // what the next phase reads is then there.  Past the last tile the loads
+    // read it again, for nobody.  (The loads among the MFMAs of X instead: 1645
+    // us where this takes 1448, a prompt of 7161 tokens behind 1030, 64 heads.)
+    const bool second = wave >= 4;
+    // Tokens that some rows do not see may hold anything: infinities and NaNs
+    // must not meet their zero weights, so a wave clears them from the values
+    // that it loaded, before the barrier that publishes them (rows that see
+    // such a token have it in their scores).
+    auto clear = [&](int s, Values& d) __attribute__((always_inline)) {
+        if (s >= steps || (s + 1) * kKvTile <= lim_wg) return;
+        if (s * kKvTile + 8 * wave + (lane >> 3) >= lim_wg) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                sc[e][i] *= p.scale_log2;
-                if (masked && tb + 32 * e + 8 * (i >> 2) + 4 * hf + (i & 3) >= limit) sc[e][i] = -INFINITY;
-                mt = fmaxf(mt, sc[e][i]);
+            for (int g = 0; g < kGv; ++g) {
+                lat_u32x4 v = d.v[wave][g][lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = lat_finite(v[e]);
+                d.v[wave][g][lane] = v;
             }
-        mt = lat_max_pair(mt);
-        if (__any(mt > m + kMaxSlack)) {
+        }
+        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+    };
+    auto odd_end = [&](int s, Values& values) __attribute__((always_inline)) {
+        lat_wait_vm<kLoads>();
+        asm volatile("" ::: "memory");
+        clear(s, values);
+    };
+    lat_u32x4 pf[4] = {};          // weights of the tile before
+    lat_f32x16 sc[2];
+    // X's MFMAs, 2 kJ of the scores and 4 NC of the sums, evenly mixed (two
+    // chains of sums alone would wait for each other), their fragments read
+    // kAhead before they are used.
+    constexpr int kOps = 2 * kJ + 4 * NC;
+    auto sums_before = [](int i) constexpr { return i * (4 * NC) / kOps; };
+    auto value = [&](const Values& d, int i) __attribute__((always_inline)) {
+        const lat_u32x2* base = (const lat_u32x2*)&d.v[0][0][0];
+        const int ks = i / NC, c = i % NC;
+        lat_u32x2 w[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const lat_u32x2* at = base + ((2 * ks + e) * kGv + (c >> 1)) * (2 * kWave) + vpos[c & 1][e];
+            w[e] = __builtin_bit_cast(lat_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lat_lds_s16x4*)at));
+        }
+        return lat_u32x4{w[0][0], w[0][1], w[1][0], w[1][1]};
+    };
+    auto load_tiles = [&](const Source& from_k, const Source& from_v, Keys& k, Values& v) __attribute__((always_inline)) {
+        lat_for<0, kLoads>([&](auto ic) __attribute__((always_inline)) {
+            load(ic, decltype(ic)::value < kGk ? from_k : from_v, k, v);
+        });
+    };
+    // k, k2: the keys of tile s (their stage then takes those of tile s + 3)
+    // and the stage for those of tile s + 2; v0, v1, v2: the values of tiles
+    // s - 1 (their stage then takes those of tile s + 2) and s and the stage
+    // for those of tile s + 1.
+    auto step = [&](int s, Keys& k, Keys& k2, Values& v0, Values& v1, Values& v2) __attribute__((always_inline)) {
+        const int tb = s * kKvTile;
+        const lat_u32x4* keys = &k.v[0][0][0];
+        auto fetch = [&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value, v = sums_before(i);
+            if constexpr (sums_before(i + 1) > v) {
+                return value(v0, v);
+            } else {
+                constexpr int j = (i - v) >> 1, e = (i - v) & 1;
+                return keys[kpos[j % 4] + (4 * e * kGk + j / 4) * kWave];
+            }
+        };
+        __builtin_amdgcn_sched_barrier(0);
+        lat_u32x4 fr[kAhead];
+        sc[0] = sc[1] = lat_f32x16{};
+        lat_for<0, kAhead>([&](auto ic) __attribute__((always_inline)) { fr[decltype(ic)::value] = fetch(ic); });
+        lat_for<0, kOps>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value, v = sums_before(i), j = i - v;
+            if constexpr (sums_before(i + 1) > v) o[v % NC] = lat_mma(fr[i % kAhead], pf[v / NC], o[v % NC]);
+            else sc[j & 1] = lat_mma(fr[i % kAhead], qf[j >> 1], sc[j & 1]);
+            if constexpr (i + kAhead < kOps) fr[i % kAhead] = fetch(LatInt<i + kAhead>{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if (second) odd_end(s, v1);
+        lat_barrier();
+        const int more_k = second ? 3 : 2;
+        const Source from_k = source(min(s + more_k, steps - 1)), from_v = source(min(s + more_k - 1, steps - 1));
+        if (second) load_tiles(from_k, from_v, k, v0);
+        else load_tiles(from_k, from_v, k2, v2);
+        if (tb + kKvTile > lim_min) {
+            asm volatile("");       // a branch, not 32 selects in every step
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (tb + 32 * e + 8 * (i >> 2) + 4 * hf + (i & 3) >= limit) sc[e][i] = -INFINITY;
+        }
+        // The weights by the running maximum; where one exceeds the slack the
+        // maximum moves and they are made again.
+        float big = 0.0f, more = 0.0f;
+        auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float a = __builtin_amdgcn_exp2f(fmaf(sc[k >> 1][8 * (k & 1) + 2 * i], p.scale_log2, -m));
+                    const float e = __builtin_amdgcn_exp2f(fmaf(sc[k >> 1][8 * (k & 1) + 2 * i + 1], p.scale_log2, -m));
+                    big = fmaxf(fmaxf(big, a), e);
+                    pf[k][i] = lat_pack(a, e);
+                    more = lat_sum2(pf[k][i], more);
+                }
+        };
+        weights();
+        if (__any(big > kMaxWeight)) {
+            float mt = fmaxf(sc[0][0], sc[1][0]);
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mt = fmaxf(mt, fmaxf(sc[0][i], sc[1][i]));
+            mt = lat_max_pair(mt) * p.scale_log2;
             const float mn = fmaxf(m, mt), f = __builtin_amdgcn_exp2f(m - mn);
             l *= f;
             m = mn;
 #pragma unroll
             for (int c = 0; c < NC; ++c) o[c] *= f;
+            more = 0.0f;
+            weights();
         }
-        lat_u32x4 pf[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = __builtin_amdgcn_exp2f(sc[k >> 1][8 * (k & 1) + 2 * i] - m);
-                const float e = __builtin_amdgcn_exp2f(sc[k >> 1][8 * (k & 1) + 2 * i + 1] - m);
-                l += a + e;
-                pf[k][i] = lat_pack(a, e);
-            }
-        const lat_u32x2* base = (const lat_u32x2*)&d.v[0][0][0];
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                lat_u32x2 w[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const lat_u32x2* at = base + ((2 * ks + e) * kGv + (c >> 1)) * (2 * kWave) + vpos[c & 1];
-                    w[e] = __builtin_bit_cast(lat_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lat_lds_s16x4*)at));
-                }
-                const lat_u32x4 a = {w[0][0], w[0][1], w[1][0], w[1][1]};
-                o[c] = lat_mma(a, pf[ks], o[c]);
-            }
+        l += more;
+        if (!second) odd_end(s, v1);
+        lat_barrier();
     };
-    if (steps > 0) load(0, st0);
-    if (steps > 1) load(1, st1);
-    for (int s = 0; s < steps; s += 3) {
-        step(s, st0, st2);
-        if (s + 1 < steps) step(s + 1, st1, st0);
-        if (s + 2 < steps) step(s + 2, st2, st1);
+    if (steps > 0) {
+        // Tile 0, the keys of tile 1 (and what the second waves' Y(-1) would
+        // have loaded); the values of "tile -1" are zeros.
+        const Source from0 = source(0), from1 = source(min(1, steps - 1)), from2 = source(min(2, steps - 1));
+        load_tiles(from0, from0, kt0, vt0);
+        lat_for<0, kGk>([&](auto ic) __attribute__((always_inline)) { load(ic, from1, kt1, vt1); });
+        if (second) load_tiles(from2, from1, kt2, vt1);
+#pragma unroll
+        for (int g = 0; g < kGv; ++g) vt2.v[wave][g][lane] = lat_u32x4{0, 0, 0, 0};
+        if (second) lat_wait_vm<kLoads>();
+        else lat_wait_vm<0>();
+        asm volatile("" ::: "memory");
+        clear(0, vt0);
+        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+        lat_barrier();
+        if (second) lat_barrier();
+        for (int s = 0; s < steps; s += 3) {
+            step(s, kt0, kt2, vt2, vt0, vt1);
+            if (s + 1 < steps) step(s + 1, kt1, kt0, vt0, vt1, vt2);
+            if (s + 2 < steps) step(s + 2, kt2, kt1, vt1, vt2, vt0);
+        }
+        if (!second) lat_barrier();
+        lat_wait_vm<0>();          // the last tile's second readings have landed
+        auto finish = [&](const Values& d) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 4 * NC; ++i) o[i % NC] = lat_mma(value(d, i), pf[i / NC], o[i % NC]);
+        };
+        const int at = (steps - 1) % 3;
+        if (at == 0) finish(vt0);
+        else if (at == 1) finish(vt1);
+        else finish(vt2);
     }
 
     l = lat_sum_pair(l);
@@ -309,6 +418,7 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
                 *(float4*)((float*)p.y + y) = make_float4(v0, v1, v2, v3);
             }
         }
+#endif
 }
 
 // Rows of no request (padding) are zero, their lse -inf.
