@@ -14,6 +14,7 @@ constexpr int kRopeDim = 64;          // rotary part of a query and of a cache r
 // requests; a share begins and ends inside a request, so a workgroup leaves
 // at most two partial results.
 constexpr int kAbsGroups = 256;
+constexpr int kAbsTileRows = 64;      // query rows of such a workgroup
 constexpr int kExpRows = 256;         // query rows of a workgroup of the expanded form
 
 struct LatentWs {
@@ -23,7 +24,6 @@ struct LatentWs {
     size_t part, part_ml; // absorbed: [2 groups][rows][latent] partial sums and [..][rows][2] (maximum, sum)
     size_t kv, kr;        // expanded: [max_kv][heads][nope + v] keys and values, [max_kv][rope] rotary keys
     size_t total;
-    int row_tiles;        // absorbed: 32-row tiles of a workgroup (1, 2 or 4)
     bool expanded;
 };
 
@@ -52,7 +52,7 @@ struct LatentParams {
     uint16_t* kr;
 };
 
-hipError_t launch_latent_absorbed(const LatentParams& p, int row_tiles, hipStream_t s);
+hipError_t launch_latent_absorbed(const LatentParams& p, hipStream_t s);
 hipError_t launch_latent_expanded(const LatentParams& p, hipStream_t s);
 
 typedef uint32_t lat_u32x4 __attribute__((ext_vector_type(4)));

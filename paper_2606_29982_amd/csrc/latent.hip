@@ -17,8 +17,6 @@ bool latent_expanded(const caee_latent_desc_t& d) {
 LatentWs latent_ws(const caee_latent_desc_t& d) {
     LatentWs L{};
     L.expanded = latent_expanded(d);
-    const long long rows = (long long)d.max_new * d.heads;
-    L.row_tiles = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -31,7 +29,7 @@ LatentWs latent_ws(const caee_latent_desc_t& d) {
         L.kr = take((size_t)d.max_kv * kRopeDim * 2);
     } else {
         const size_t th = (size_t)d.T * d.heads;
-        const size_t part_rows = (size_t)2 * kAbsGroups * 32 * L.row_tiles;
+        const size_t part_rows = (size_t)2 * kAbsGroups * kAbsTileRows;
         L.q = take(th * (d.latent + kRopeDim) * 2);
         L.o = take(th * d.latent * 4);
         L.part = take(part_rows * d.latent * 4);
@@ -75,8 +73,8 @@ caee_status_t check_latent(const caee_latent_desc_t* d) {
         return fail(CAEE_ERR_UNSUPPORTED, "a cache of %lld rows, or %lld tokens in all, exceeds 2^31 - 1",
                     (long long)d->n_blocks * d->block_size, (long long)d->max_kv);
     // Shares of the absorbed form are counted in 32 bits.
-    const long long tiles = ((long long)d->max_new * d->heads + 127) / 128 + 1;
-    if (!latent_expanded(*d) && (d->max_kv / 32 + d->B) * tiles > INT32_MAX / 2)
+    const long long tiles = ((long long)d->max_new * d->heads + kAbsTileRows - 1) / kAbsTileRows;
+    if (!latent_expanded(*d) && (d->max_kv / 64 + d->B) * tiles > INT32_MAX / 2)
         return fail(CAEE_ERR_UNSUPPORTED, "max_new=%d new tokens over max_kv=%lld: too many pairs for the absorbed form",
                     d->max_new, (long long)d->max_kv);
     return CAEE_OK;
@@ -160,7 +158,7 @@ caee_status_t caee_latent_attention(const caee_latent_desc_t* desc, const void* 
     p.kr = (uint16_t*)(w + L.kr);
     hipStream_t s = (hipStream_t)stream;
     return timed_launch(CAEE_KERNEL_ATTENTION, s, "latent attention", [&] {
-        return L.expanded ? launch_latent_expanded(p, s) : launch_latent_absorbed(p, L.row_tiles, s);
+        return L.expanded ? launch_latent_expanded(p, s) : launch_latent_absorbed(p, s);
     });
 }
 
