@@ -72,6 +72,9 @@ caee_status_t check_latent(const caee_latent_desc_t* d) {
     if ((long long)d->n_blocks * d->block_size > INT32_MAX || d->max_kv > INT32_MAX)
         return fail(CAEE_ERR_UNSUPPORTED, "a cache of %lld rows, or %lld tokens in all, exceeds 2^31 - 1",
                     (long long)d->n_blocks * d->block_size, (long long)d->max_kv);
+    if (latent_expanded(*d) && d->max_kv > 65534 * 256)
+        return fail(CAEE_ERR_UNSUPPORTED, "the expanded form takes at most %d tokens in all, not max_kv=%lld", 65534 * 256,
+                    (long long)d->max_kv);
     // Shares of the absorbed form are counted in 32 bits.
     const long long tiles = ((long long)d->max_new * d->heads + kAbsTileRows - 1) / kAbsTileRows;
     if (!latent_expanded(*d) && (d->max_kv / 64 + d->B) * tiles > INT32_MAX / 2)

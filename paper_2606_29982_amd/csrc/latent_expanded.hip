@@ -2,7 +2,8 @@
 // from the cache rows first, then attended to as in ordinary attention.
 //
 //   k_expand   [k_nope | v] of every cached token and head = W c, rotary keys
-//              copied next to them in token order (and the query tiles below)
+//              copied next to them in token order (and the query tiles below;
+//              rows of no request are zeroed)
 //   k_prompt   per head and 256 query rows of one request: softmax attention
 //              over its tokens, tile by tile
 #include "latent.h"
@@ -10,7 +11,7 @@
 namespace caee {
 namespace {
 
-constexpr int kExpandThreads = 256;
+constexpr int kExpandThreads = 512;
 constexpr int kPromptThreads = 512;
 constexpr int kKvTile = 64;            // tokens of a KV tile
 
@@ -38,99 +39,184 @@ __device__ void prompt_tiles(const LatentParams& p) {
     if (tid == kExpandThreads - 1) p.meta[p.B] = part[kExpandThreads - 1];
 }
 
-// 64 contraction elements of 128 weight rows and 128 tokens: blocks of 8
+// Rows of no request (padding) are zero, their lse -inf; `groups` workgroups.
+__device__ void blank_rows(const LatentParams& p, int group, int groups) {
+    const int end = p.B > 0 ? min(max(p.cu_new[p.B], 0), p.T) : 0;
+    const long long words = (long long)p.H * p.v * (p.y_bf16 ? 2 : 4) / 16, n = (p.T - end) * words;
+    const long long first = (long long)group * kExpandThreads + threadIdx.x, by = (long long)groups * kExpandThreads;
+    const lat_u32x4 zero = {0, 0, 0, 0};
+    for (long long i = first; i < n; i += by) ((lat_u32x4*)p.y)[end * words + i] = zero;
+    if (p.lse)
+        for (long long i = first; i < (long long)(p.T - end) * p.H; i += by) p.lse[(long long)end * p.H + i] = -INFINITY;
+}
+
+// 64 contraction elements of 256 weight rows and 256 tokens: blocks of 8
 // rows x 128 bytes, piece c of row r at 8 (r % 8) + (c ^ lat_swz(r)).
+constexpr int kExpandTile = 256;
 struct ExpandStage {
-    lat_u32x4 a[16][kWave], b[16][kWave];
+    lat_u32x4 a[kExpandTile / 8][kWave], b[kExpandTile / 8][kWave];
 };
 
-// A product of 128 outputs (of the heads' nope + v rows, in that order) and
-// 128 cached tokens per workgroup: weight rows as the M side, tokens, looked
-// up in the block tables, as the N side; 2 x 2 waves of 64 x 64.
+// A product of 256 outputs (of the heads' nope + v rows, in that order) and
+// 256 cached tokens per workgroup: weight rows as the M side, tokens, looked
+// up in the block tables, as the N side; 2 x 4 waves of 128 x 64.  Two stages,
+// the next one's loads between the first half of a stage's MFMAs; workgroups
+// that run together share weight tiles by XCD (they are numbered weights
+// first) and the outputs leave through LDS, 512 bytes of a token at a time.
+// 8191 tokens of 64 heads take 185 us, 0.74 PFLOP/s: 100 us of products at the
+// rate of a large one and 55 us of writes, which a CU's one workgroup does not
+// overlap (128 x 128 tiles, two workgroups a CU, 16-byte pieces written from
+// the registers: 264 us).
 __global__ __launch_bounds__(kExpandThreads) void k_expand(LatentParams p) {
+#if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
     const int ft = blockIdx.x;
-    if (ft == (int)gridDim.x - 1) {
-        if (blockIdx.y == 0) prompt_tiles(p);
+    if (blockIdx.y == gridDim.y - 1) {
+        if (ft == 0) prompt_tiles(p);
+        blank_rows(p, ft, gridDim.x);
         return;
     }
+    constexpr int kWaves = kExpandThreads / kWave, kBlocks = kExpandTile / 8 / kWaves;     // blocks of 8 rows a wave fetches
     __shared__ ExpandStage st0, st1;
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave & 1, wn = wave >> 1;
     const int total = p.B > 0 ? (int)min((long long)p.cu_kv[p.B], p.max_kv) : 0;
-    const int s0 = blockIdx.y * 128;
+    const int s0 = blockIdx.y * kExpandTile;
     if (s0 >= total) return;
-    const int hw = p.nope + p.v, row_bytes = p.latent + kRopeDim;
+    const int hw = p.nope + p.v, outs = p.H * hw, row_bytes = (p.latent + kRopeDim) * 2;
     // Cache row of token s of all requests' tokens.
     auto cache_row = [&](int s) {
         s = min(s, total - 1);
         const int b = lat_find(p.cu_kv, p.B, s);
-        return p.cache + (size_t)lat_slot(p, b, s - p.cu_kv[b]) * row_bytes;
+        return lat_slot(p, b, s - p.cu_kv[b]);
     };
-    const uint16_t *wsrc[4], *xsrc[4];
+    // Buffer loads (the compiler counts the LDS reads apart from them).  Eight
+    // weight rows lie in one head's keys or values.  A token's row is a 32-bit
+    // offset where the cache has at most 4 GiB, else rows go one by one, each
+    // with a descriptor of its own.
+    const bool near = (unsigned long long)p.n_blocks * p.block * row_bytes < 0xFFFFFFFFull;
+    const char* wbase[kBlocks];
+    uint32_t xrow[kBlocks];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = 8 * i + (lane >> 3), swz = 8 * ((lane & 7) ^ lat_swz(r));
-        const int j = ft * 128 + 32 * wave + r, h = j / hw, jj = j - h * hw;
-        wsrc[i] = (jj < p.nope ? p.w_uk + ((size_t)h * p.nope + jj) * p.latent
-                               : p.w_uv + ((size_t)h * p.v + jj - p.nope) * p.latent) + swz;
-        xsrc[i] = cache_row(s0 + 32 * wave + r) + swz;
+    for (int i = 0; i < kBlocks; ++i) {
+        const int r = 8 * (kBlocks * wave + i);
+        const int j = min(ft * kExpandTile + r, outs - 8), h = j / hw, jj = j - h * hw;
+        wbase[i] = (const char*)(jj < p.nope ? p.w_uk + ((size_t)h * p.nope + jj) * p.latent
+                                             : p.w_uv + ((size_t)h * p.v + jj - p.nope) * p.latent);
+        xrow[i] = cache_row(s0 + r + (lane >> 3));
     }
+    auto piece = [&](int i) { return 16u * ((lane & 7) ^ lat_swz(8 * i + (lane >> 3))); };     // kBlocks is even
     if (ft == 0) {
-        for (int i = threadIdx.x; i < 128 * 8; i += kExpandThreads) {
+        for (int i = threadIdx.x; i < kExpandTile * 8; i += kExpandThreads) {
             const int s = s0 + (i >> 3);
             if (s < total)
-                *(lat_u32x4*)(p.kr + (size_t)s * kRopeDim + 8 * (i & 7)) =
-                    *(const lat_u32x4*)(cache_row(s) + p.latent + 8 * (i & 7));
+                *(lat_u32x4*)(p.kr + (size_t)s * kRopeDim + 8 * (i & 7)) = *(const lat_u32x4*)(
+                    p.cache + (size_t)cache_row(s) * (p.latent + kRopeDim) + p.latent + 8 * (i & 7));
         }
     }
-    auto load = [&](int k, ExpandStage& t) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            __builtin_amdgcn_global_load_lds((lat_g_void*)(wsrc[i] + 64 * k), (lat_lds_void*)&t.a[4 * wave + i][0], 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((lat_g_void*)(xsrc[i] + 64 * k), (lat_lds_void*)&t.b[4 * wave + i][0], 16, 0, 0);
+    // Load i of a wave's part of stage k: weight blocks, then token blocks.
+    auto load = [&](int k, int i, ExpandStage& t) __attribute__((always_inline)) {
+        if (i < kBlocks) {
+            const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc((void*)wbase[i], 0, kLatBufBytes, kLatBufWord3);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&t.a[kBlocks * wave + i][0], 16,
+                                                     (uint32_t)(lane >> 3) * (uint32_t)(p.latent * 2) + piece(i), 128 * k, 0, 0);
+        } else {
+            const int e = i - kBlocks;
+            const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc((void*)p.cache, 0, -1, kLatBufWord3);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&t.b[kBlocks * wave + e][0], 16,
+                                                     xrow[e] * (uint32_t)row_bytes + piece(e), 128 * k, 0, 0);
         }
     };
-    lat_f32x16 acc[2][2] = {};
+    auto load_far = [&](int k, ExpandStage& t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < kBlocks; ++e) {
+#pragma unroll 1
+            for (int r = 0; r < 8; ++r) {
+                const uint32_t row = __builtin_amdgcn_readlane(xrow[e], 8 * r);
+                const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
+                    (void*)((const char*)p.cache + (size_t)row * (uint32_t)row_bytes), 0, kLatBufBytes, kLatBufWord3);
+                if (lane >> 3 == r)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&t.b[kBlocks * wave + e][0], 16, piece(e),
+                                                             128 * k, 0, 0);
+            }
+        }
+    };
+    lat_f32x16 acc[4][2] = {};
     const int steps = p.latent / 64;
     auto step = [&](int k, ExpandStage& t, ExpandStage& next) __attribute__((always_inline)) {
-        lat_wait_vm<0>();
-        lat_barrier();
-        if (k + 1 < steps) load(k + 1, next);
+        lat_wait_vm<0>();                  // this wave's part of the stage is there; after the barrier all of it is,
+        lat_barrier();                     // and nobody reads the other
+        const bool more = k + 1 < steps;
+        if (more && !near) load_far(k + 1, next);
+        const int loads = !more ? 0 : near ? 2 * kBlocks : kBlocks;
+        auto a_at = [&](int j, int i) __attribute__((always_inline)) {
+            return t.a[16 * wm + 4 * i + (n >> 3)][(n & 7) * 8 + ((2 * j + hf) ^ lat_swz(n))];
+        };
+        auto b_at = [&](int j, int i) __attribute__((always_inline)) {
+            return t.b[8 * wn + 4 * i + (n >> 3)][(n & 7) * 8 + ((2 * j + hf) ^ lat_swz(n))];
+        };
+        lat_u32x4 a[2][4], b[2][2];
+        auto fetch = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int at = (n & 7) * 8 + ((2 * j + hf) ^ lat_swz(n));
-            lat_u32x4 a[2], b[2];
+            for (int i = 0; i < 2; ++i) b[j & 1][i] = b_at(j, i);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                a[i] = t.a[8 * wm + 4 * i + (n >> 3)][at];
-                b[i] = t.b[8 * wn + 4 * i + (n >> 3)][at];
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) acc[i][e] = lat_mma(a[i], b[e], acc[i][e]);
-        }
+            for (int i = 0; i < 4; ++i) a[j & 1][i] = a_at(j, i);
+        };
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(0);
+        lat_for<0, 4>([&](auto jc) __attribute__((always_inline)) {
+            constexpr int j = decltype(jc)::value;
+            if constexpr (j < 3) fetch(j + 1);
+            lat_for<0, 8>([&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value, op = 8 * j + i;
+                acc[i >> 1][i & 1] = lat_mma(a[j & 1][i >> 1], b[j & 1][i & 1], acc[i >> 1][i & 1]);
+                if constexpr (op % 2 == 1 && op / 2 < 2 * kBlocks) {
+                    if (op / 2 < loads) load(k + 1, op / 2, next);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
     };
-    load(0, st0);
+    for (int i = 0; i < (near ? 2 * kBlocks : kBlocks); ++i) load(0, i, st0);
+    if (!near) load_far(0, st0);
     for (int k = 0; k < steps; k += 2) {
         step(k, st0, st1);
         step(k + 1, st1, st0);      // latent is a multiple of 128
     }
+    // The tile's tokens, 512 bytes each, half in either stage; piece c of token
+    // r at c ^ (r % 32).
+    __syncthreads();
+    lat_u32x4* const half = wn < 2 ? &st0.a[0][0] : &st1.a[0][0];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int s = s0 + 64 * wn + 32 * e + n;
-        if (s >= total) continue;
-        uint16_t* dst = p.kv + (size_t)s * p.H * hw + ft * 128 + 64 * wm + 4 * hf;
+    for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const lat_u32x2 v = {lat_pack(acc[i][e][4 * q], acc[i][e][4 * q + 1]),
-                                     lat_pack(acc[i][e][4 * q + 2], acc[i][e][4 * q + 3])};
-                *(lat_u32x2*)(dst + 32 * i + 8 * q) = v;
+                lat_u32x2* at = (lat_u32x2*)&half[(64 * (wn & 1) + 32 * e + n) * 32 + ((16 * wm + 4 * i + q) ^ n)];
+                at[hf] = lat_u32x2{lat_pack(acc[i][e][4 * q], acc[i][e][4 * q + 1]),
+                                   lat_pack(acc[i][e][4 * q + 2], acc[i][e][4 * q + 3])};
             }
+    __syncthreads();
+    const int c8 = threadIdx.x & 31, out = ft * kExpandTile + 8 * c8;
+    if (out >= outs) return;
+    uint16_t* dst = p.kv + (size_t)s0 * outs + out;
+    constexpr int kRows = kExpandThreads / 32;
+#pragma unroll
+    for (int i = 0; i < kExpandTile / kRows; i += 4) {
+        lat_u32x4 v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = kRows * (i + e) + (threadIdx.x >> 5);
+            v[e] = (r < 128 ? &st0.a[0][0] : &st1.a[0][0])[(r & 127) * 32 + (c8 ^ (r & 31))];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = kRows * (i + e) + (threadIdx.x >> 5);
+            if (s0 + r < total) *(lat_u32x4*)(dst + (size_t)r * outs) = v[e];
+        }
     }
+#endif
 }
 
 // One tile of a head's keys (nope groups, then the rotary one) or values: G
@@ -421,20 +507,6 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
 #endif
 }
 
-// Rows of no request (padding) are zero, their lse -inf.
-__global__ __launch_bounds__(256) void k_blank_rows(LatentParams p) {
-    const int end = p.B > 0 ? min(max(p.cu_new[p.B], 0), p.T) : 0;
-    const long long words = (long long)p.H * p.v * (p.y_bf16 ? 2 : 4) / 16;
-    const long long n = (p.T - end) * words;
-    const lat_u32x4 zero = {0, 0, 0, 0};
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256)
-        ((lat_u32x4*)p.y)[end * words + i] = zero;
-    if (p.lse)
-        for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)(p.T - end) * p.H;
-             i += (long long)gridDim.x * 256)
-            p.lse[(long long)end * p.H + i] = -INFINITY;
-}
-
 template <int NOPE>
 void prompt(const LatentParams& p, unsigned grid, int tiles, hipStream_t s) {
     if (p.v == 128) hipLaunchKernelGGL((k_prompt<NOPE, 128>), dim3(grid), dim3(kPromptThreads), 0, s, p, tiles);
@@ -444,10 +516,9 @@ void prompt(const LatentParams& p, unsigned grid, int tiles, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_latent_expanded(const LatentParams& p, hipStream_t s) {
-    const unsigned ft = (unsigned)((long long)p.H * (p.nope + p.v) / 128);
-    const unsigned st = (unsigned)((p.max_kv + 127) / 128);
-    hipLaunchKernelGGL(k_expand, dim3(ft + 1, st > 0 ? st : 1), dim3(kExpandThreads), 0, s, p);
-    hipLaunchKernelGGL(k_blank_rows, dim3(64), dim3(256), 0, s, p);
+    const unsigned ft = (unsigned)(((long long)p.H * (p.nope + p.v) + kExpandTile - 1) / kExpandTile);
+    const unsigned st = (unsigned)((p.max_kv + kExpandTile - 1) / kExpandTile);
+    hipLaunchKernelGGL(k_expand, dim3(ft, st + 1), dim3(kExpandThreads), 0, s, p);
     long long tiles = (long long)p.B * ((p.max_new + kExpRows - 1) / kExpRows);
     if (tiles > p.T / kExpRows + p.B) tiles = p.T / kExpRows + p.B;
     if (tiles > 0) {
