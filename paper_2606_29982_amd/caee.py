@@ -374,7 +374,7 @@ def _need(t, name: str, dtype=None, shape=None, dense: bool = True):
         raise ValueError(f"{name} must be a device tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if dense and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -405,12 +405,15 @@ def paged_plan(block_size: int, ctx_len, new_len, block_table, free_list, free_h
         raise ValueError(f"block_table must be [{B}][max_blocks]")
     _need(free_list, "free_list", i32)
     _need(free_head, "free_head", i32, (1,))
-    for name, n in (("cu_new", B + 1), ("cu_kv", B + 1), ("seq_len", B), ("position", T), ("request", T),
-                    ("free_head", 1), ("lacking", 1)):
-        if out.get(name) is not None or name not in ("position", "request"):
-            _need(out[name], name, i32, (n,))
-    _need(out["slots"], "slots", torch.int64)
-    o = PagedPlanOut(*[_ptr(out.get(n)) for n, _ in PagedPlanOut._fields_])
+    at = []
+    for name, shape, optional in (("cu_new", (B + 1,), False), ("cu_kv", (B + 1,), False), ("seq_len", (B,), False),
+                                  ("slots", (T,), False), ("position", (T,), True), ("request", (T,), True),
+                                  ("free_head", (1,), False), ("lacking", (1,), False)):
+        t = out.get(name) if optional else out[name]
+        if t is not None:
+            _need(t, name, torch.int64 if name == "slots" else i32, shape)
+        at.append(_ptr(t))
+    o = PagedPlanOut(*at)
     _check(lib.caee_paged_plan(B, T, block_size, block_table.shape[1], _ptr(ctx_len), _ptr(new_len), _ptr(block_table),
                                _ptr(free_list), free_list.shape[0], _ptr(free_head), ctypes.byref(o),
                                _stream(free_head)))

@@ -35,29 +35,31 @@ __device__ inline PlanLen plan_len(const PlanParams& p, int b) {
     return r;
 }
 
-// Inclusive scan of one value per thread over the workgroup.
-__device__ inline int scan_inclusive(int v, int* part, int tid) {
+// Inclusive scans of N values per thread over the workgroup.
+template <int N>
+__device__ inline void scan_inclusive(int (&v)[N], int (*part)[kPlanThreads / kWave], int tid) {
+    constexpr int kWaves = kPlanThreads / kWave;
     const int lane = tid & (kWave - 1), wave = tid / kWave;
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int u = __shfl_up(v, d);
-        if (lane >= d) v += u;
-    }
-    if (lane == kWave - 1) part[wave] = v;
-    __syncthreads();
-    if (wave == 0) {
-        int s = lane < kPlanThreads / kWave ? part[lane] : 0;
+    for (int d = 1; d < kWave; d <<= 1)
 #pragma unroll
-        for (int d = 1; d < kPlanThreads / kWave; d <<= 1) {
-            const int u = __shfl_up(s, d);
-            if (lane >= d) s += u;
+        for (int i = 0; i < N; ++i) {
+            const int u = __shfl_up(v[i], d);
+            if (lane >= d) v[i] += u;
         }
-        if (lane < kPlanThreads / kWave) part[lane] = s;
+    if (lane == kWave - 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) part[i][wave] = v[i];
     }
     __syncthreads();
-    if (wave > 0) v += part[wave - 1];
-    __syncthreads();
-    return v;
+    // Every wave adds up the waves before it.
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        int u = lane < wave ? part[i][lane & (kWaves - 1)] : 0;
+#pragma unroll
+        for (int d = kWaves / 2; d >= 1; d >>= 1) u += __shfl_xor(u, d);
+        v[i] += __builtin_amdgcn_readfirstlane(u);
+    }
 }
 
 // Three prefix sums over the requests (new tokens, pages to take, cached
@@ -72,9 +74,11 @@ __device__ inline int scan_inclusive(int v, int* part, int tid) {
 // nothing.
 __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanParams p) {
     __shared__ int s_new[kPlanThreads + 1], s_take[kPlanThreads + 1];
-    __shared__ int part[kPlanThreads / kWave];
+    __shared__ int part[3][kPlanThreads / kWave], part_over[1][kPlanThreads / kWave];
     const int tid = threadIdx.x;
     const int b0 = min(tid * p.chunk, p.B), b1 = min(b0 + p.chunk, p.B);
+    const int head = max(p.free_head[0], 0);
+    const int left = max(p.n_free - head, 0);
     int n_new = 0, n_take = 0, n_kv = 0;
     for (int b = b0; b < b1; ++b) {
         const PlanLen l = plan_len(p, b);
@@ -82,15 +86,13 @@ __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanParams p) {
         n_take += l.want;
         n_kv += l.ctx + l.add;
     }
-    const int i_new = scan_inclusive(n_new, part, tid);
-    const int i_take = scan_inclusive(n_take, part, tid);
+    int scan[3] = {n_new, n_take, n_kv};
+    scan_inclusive(scan, part, tid);
+    const int i_new = scan[0], i_take = scan[1], i_kv = scan[2];
     s_new[tid + 1] = i_new;
     s_take[tid + 1] = i_take;
     if (tid == 0) s_new[0] = s_take[0] = 0;
-    const int head = max(p.free_head[0], 0);
-    const int left = max(p.n_free - head, 0);
     if (blockIdx.x == 0) {
-        const int i_kv = scan_inclusive(n_kv, part, tid);
         int a = i_new - n_new, kv = i_kv - n_kv, over = 0, take = i_take - n_take;
         for (int b = b0; b < b1; ++b) {
             const PlanLen l = plan_len(p, b);
@@ -104,7 +106,9 @@ __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanParams p) {
             over += max(to - from, 0);
             take += l.want;
         }
-        const int i_over = scan_inclusive(over, part, tid);
+        int sum[1] = {over};
+        scan_inclusive(sum, part_over, tid);
+        const int i_over = sum[0];
         if (tid == kPlanThreads - 1) {
             p.o.cu_new[p.B] = i_new;
             p.o.cu_kv[p.B] = i_kv;
@@ -116,8 +120,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanParams p) {
 
     // Table rows: one wave per range of requests, lanes over the new pages.
     const int lane = tid & (kWave - 1), wave = tid / kWave;
-    const int n_waves = gridDim.x * (kPlanThreads / kWave);
-    for (int i = blockIdx.x * (kPlanThreads / kWave) + wave; i < kPlanThreads; i += n_waves) {
+    const int n_waves = gridDim.x * (kPlanThreads / kWave), ranges = (p.B + p.chunk - 1) / p.chunk;
+    for (int i = blockIdx.x * (kPlanThreads / kWave) + wave; i < ranges; i += n_waves) {
         int at = s_take[i];
         if (s_take[i + 1] == at) continue;
         const int e1 = min((i + 1) * p.chunk, p.B);
@@ -135,7 +139,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanParams p) {
         long long slot = -1;
         int pos = -1, b = -1;
         if (t < total) {
-            int lo = 0, hi = kPlanThreads;          // s_new[lo] <= t < s_new[hi]
+            int lo = 0, hi = ranges;                // s_new[lo] <= t < s_new[hi]
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (s_new[mid] <= t) lo = mid;
