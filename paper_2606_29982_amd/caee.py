@@ -225,7 +225,8 @@ def _stream(*tensors) -> Optional[int]:
     import torch
     for t in tensors:
         if t is not None:
-            return int(torch.cuda.current_stream(t.device).cuda_stream)
+            # what torch.cuda.current_stream(t.device).cuda_stream returns, without the Stream object (2 us a call)
+            return torch._C._cuda_getCurrentRawStream(t.get_device())
     return None
 
 
