@@ -29,7 +29,6 @@ typedef __bf16 bm_bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bm_bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t bm_u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void bm_lds_void;
-typedef const __attribute__((address_space(1))) bm_u32x4 bm_g_u32x4;
 
 constexpr int kBmMaxK = 65536;
 constexpr int kBmMaxStride = 1 << 22;  // elements from row to row of x: 256 rows stay within 2^32 bytes
@@ -113,100 +112,162 @@ __global__ __launch_bounds__(256) void k_bm_quant(BmParams p) {
     }
 }
 
-// Byte offset of 16-byte piece c of block 0 of weight row n; the next block
-// is bm_block bytes further.
-__device__ inline size_t bm_piece(const BmParams& p, int n, int c) {
-    if (p.tiled) return (((size_t)(n >> 4) * (p.K / 64) + (c >> 2)) * 64 + (n & 15) + 16 * (c & 3)) * 16;
-    return (size_t)n * p.K + 16 * c;
-}
+// Bytes from a 128-deep block of a weight row to the next.
 __device__ inline int bm_block(const BmParams& p) { return p.tiled ? 2048 : 128; }
 
-// Few rows: the weight stream bounds it.  A workgroup takes 16 outputs and
-// up to 16 NT rows, its waves a range of blocks each; a wave's weights go
-// straight to registers, U blocks of loads in flight, and the waves' sums
-// are added through LDS in wave order.
-template <int NT, int WAVES, bool kExact>
-__global__ __launch_bounds__(WAVES * 64) void k_bm_few(BmParams p) {
-    constexpr int U = 4;
-    __shared__ float red[WAVES][NT][16 * 17];
-    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+// Blocks of 8 rows x 128 bytes in LDS have piece c of row r at
+// 8 (r % 8) + (c ^ bm_swz(r)): 16 rows' reads of a piece hit all 64 banks.
+__device__ inline int bm_swz(int r) { return (r >> 1) & 7; }
+
+// Few outputs: 32 T x 32 T outputs and rows per workgroup, its waves a range
+// of the contraction's blocks each, so that small products fill the chip too.
+// A wave keeps its own two stages in LDS (no barriers), one filled by direct
+// loads while the other is multiplied; the waves' sums are added through LDS
+// in wave order.  Bound by the weights of few rows (5 rows, 4096 outputs, K =
+// 7168: 7.3 us, 4.0 TB/s), else by the lines a CU's requests take: eight lanes
+// read one, 16 cycles a load.  (Straight to registers a lane's 16-byte piece is
+// a line of its own, 64 cycles a load: 8 and 20 us for 5 and 131 rows x 576
+// outputs, K = 7168, 57 for 512 x 2048, K = 4096, where this takes 6, 10, 14.)
+template <int T, int WAVES>
+struct BmSplitStage {
+    bm_u32x4 w[WAVES][4 * T][kWave], x[WAVES][4 * T][kWave];
+};
+template <int T, int WAVES, bool kExact>
+__global__ __launch_bounds__(WAVES * 64, 2) void k_bm_split(BmParams p) {
+#if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
+    using Stage = BmSplitStage<T, WAVES>;
+    __shared__ Stage st0, st1;
+    constexpr int kTile = 32 * T;
+    const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * NT;
+    const int n0 = blockIdx.x * kTile, m0 = blockIdx.y * kTile;
     const int b0 = (int)((long long)p.kb * wave / WAVES), b1 = (int)((long long)p.kb * (wave + 1) / WAVES);
-    const int n = min(n0 + r, p.N - 1);
-    const uint8_t* w0 = p.w + bm_piece(p, n, g);
-    const uint8_t* w1 = p.w + bm_piece(p, n, 4 + g);
-    const int wstep = bm_block(p);
-    const uint8_t* xr[NT];
-    const float* xs[NT];
+    // Tiled weights have 8 rows' pieces c next to each other: block slots
+    // 8 (c ^ (r / 8) % 2) + r % 8 keep lanes and lines together.
+    const size_t first = p.tiled ? (size_t)(n0 >> 4) * (p.K / 64) * 1024 : (size_t)n0 * p.K;
+    const __amdgpu_buffer_rsrc_t wbuf =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(p.w + first), 0, kBmBufBytes, kBmBufWord3);
+    const __amdgpu_buffer_rsrc_t xbuf =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(p.xq + (size_t)m0 * p.xq_stride), 0, kBmBufBytes, kBmBufWord3);
+    uint32_t woff[4 * T], xoff[4 * T];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int m = min(m0 + 16 * t + r, p.M - 1);
-        xr[t] = p.xq + (size_t)m * p.xq_stride + 16 * g;
-        xs[t] = p.xs + (size_t)m * p.kb;
+    for (int i = 0; i < 4 * T; ++i) {
+        const int r = 8 * i + (lane >> 3), c = (lane & 7) ^ bm_swz(r);
+        xoff[i] = (uint32_t)min(r, p.M - 1 - m0) * (uint32_t)p.xq_stride + 16u * c;
+        const int wr = min(p.tiled ? 8 * i + (lane & 7) : r, p.N - 1 - n0), wc = p.tiled ? (lane >> 3) ^ (i & 1) : c;
+        woff[i] = p.tiled ? (uint32_t)((wr >> 4) * (p.K / 64) * 1024 + (wc >> 2) * 1024 + ((wr & 15) + 16 * (wc & 3)) * 16)
+                          : (uint32_t)(wr * p.K + 16 * wc);
     }
+    const float* xs[T];
+#pragma unroll
+    for (int e = 0; e < T; ++e) xs[e] = p.xs + (size_t)min(m0 + 32 * e + n, p.M - 1) * p.kb;
     const float* wsc = p.ws + (size_t)(n0 >> 7) * p.kb;
-    bm_f32x4 acc[NT];
+    const int wstep = bm_block(p);
+    // A fragment's pieces 2 q + hf of row n: at xat ^ 2 q and wat ^ wq q.
+    const int xat = (n >> 3) * kWave + 8 * (n & 7) + (hf ^ bm_swz(n));
+    const int wat = p.tiled ? (n >> 3) * kWave + 8 * (hf ^ ((n >> 3) & 1)) + (n & 7) : xat, wq = p.tiled ? 16 : 2;
+    struct Scales {
+        float x[T], w;
+    } c0, c1;
+    auto fetch = [&](Stage& t, Scales& c, int b) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = bm_f32x4{0.f, 0.f, 0.f, 0.f};
-    const bm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    bm_u32x4 cw[U][2], nw[U][2];
-    auto fetch = [&](bm_u32x4 (&d)[U][2], int b) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const size_t o = (size_t)min(b + u, p.kb - 1) * wstep;
-            d[u][0] = __builtin_nontemporal_load((bm_g_u32x4*)(w0 + o));
-            d[u][1] = __builtin_nontemporal_load((bm_g_u32x4*)(w1 + o));
+        for (int i = 0; i < 4 * T; ++i) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wbuf, (bm_lds_void*)&t.w[wave][i][0], 16, woff[i], b * wstep, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xbuf, (bm_lds_void*)&t.x[wave][i][0], 16, xoff[i], b * 128, 0, 0);
         }
+#pragma unroll
+        for (int e = 0; e < T; ++e) c.x[e] = xs[e][b];
+        c.w = wsc[b];
+        __builtin_amdgcn_sched_barrier(0);
     };
-    auto mul = [&](const bm_u32x4 (&d)[U][2], int b) __attribute__((always_inline)) {
+    bm_f32x16 acc[T][T] = {};
+    const bm_f32x16 zero = {};
+    // `later`: another stage's loads were issued after this one's.
+    auto mul = [&](Stage& t, const Scales& c, auto later) __attribute__((always_inline)) {
+        constexpr int kLater = decltype(later)::value ? 9 * T + 1 : 0;
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt((kLater & 15) | (7 << 4) | (15 << 8) | ((kLater >> 4) << 14));
+        asm volatile("" ::: "memory");
+        bm_u32x4 w[T][4], x[T][4];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (b + u >= b1) continue;
-            const bm_i32x8 a = bm_join(d[u][0], d[u][1]);
-            const float sc = wsc[b + u];
+        for (int i = 0; i < T; ++i)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const uint8_t* x = xr[t] + (size_t)(b + u) * 128;
-                const bm_i32x8 c = bm_join(*(const bm_u32x4*)x, *(const bm_u32x4*)(x + 64));
-                bm_f32x4 q = zero;
+            for (int q = 0; q < 4; ++q) {
+                w[i][q] = (&t.w[wave][4 * i][0])[wat ^ (wq * q)];
+                x[i][q] = (&t.x[wave][4 * i][0])[xat ^ (2 * q)];
+            }
+#pragma unroll
+        for (int i = 0; i < T; ++i)
+#pragma unroll
+            for (int e = 0; e < T; ++e) {
+                bm_f32x16 s = zero;
                 if constexpr (kExact) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        q = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bm_wide(a[2 * i], a[2 * i + 1]),
-                                                                    bm_wide(c[2 * i], c[2 * i + 1]), q, 0, 0, 0);
+                    for (int q = 0; q < 4; ++q) {
+                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bm_wide(w[i][q][0], w[i][q][1]),
+                                                                    bm_wide(x[e][q][0], x[e][q][1]), s, 0, 0, 0);
+                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bm_wide(w[i][q][2], w[i][q][3]),
+                                                                    bm_wide(x[e][q][2], x[e][q][3]), s, 0, 0, 0);
+                    }
                 } else {
-                    q = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, c, zero, 0, 0, 0, kUnitScale, 0, kUnitScale);
+#pragma unroll
+                    for (int q = 0; q < 4; q += 2)
+                        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(bm_join(w[i][q], w[i][q + 1]),
+                                                                            bm_join(x[e][q], x[e][q + 1]), s, 0, 0, 0,
+                                                                            kUnitScale, 0, kUnitScale);
                 }
-                const float f = sc * xs[t][b + u];
+                const float f = c.w * c.x[e];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[t][i] += q[i] * f;
+                for (int v = 0; v < 16; ++v) acc[i][e][v] += s[v] * f;
             }
-        }
+        // The stage's reads are over before it is filled again.
+        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+        asm volatile("" ::: "memory");
     };
-    fetch(cw, b0);
-    for (int b = b0; b < b1; b += 2 * U) {
-        fetch(nw, b + U);
-        mul(cw, b);
-        if (b + U >= b1) break;
-        fetch(cw, b + 2 * U);
-        mul(nw, b + U);
+    if (b0 < b1) {
+        fetch(st0, c0, b0);
+        int b = b0;
+        for (; b + 2 < b1; b += 2) {
+            fetch(st1, c1, b + 1);
+            mul(st0, c0, BmInt<1>{});
+            fetch(st0, c0, b + 2);
+            mul(st1, c1, BmInt<1>{});
+        }
+        if (b + 1 < b1) {
+            fetch(st1, c1, b + 1);
+            mul(st0, c0, BmInt<1>{});
+            mul(st1, c1, BmInt<0>{});
+        } else {
+            mul(st0, c0, BmInt<0>{});
+        }
     }
-    // Lane (r, g) holds outputs n0 + 4 g .. + 3 of row m0 + 16 t + r.
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) red[wave][t][r * 17 + 4 * g + i] = acc[t][i];
     __syncthreads();
-    for (int i = threadIdx.x; i < NT * 64; i += WAVES * 64) {
-        const int t = i >> 6, rr = (i >> 2) & 15, q = i & 3;
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int v = 0; v < WAVES; ++v)
+    float4* const red = (float4*)&st0;          // [wave][tile][eight outputs][lane]
+    auto place = [](int wv, int tile, int q, int ln) { return ((wv * T * T + tile) * 4 + q) * kWave + ln; };
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[e] += red[v][t][rr * 17 + 4 * q + e];
-        const int m = m0 + 16 * t + rr;
-        if (m < p.M) bm_store4(p, m, n0 + 4 * q, s[0], s[1], s[2], s[3]);
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int e = 0; e < T; ++e)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                red[place(wave, T * i + e, q, lane)] = make_float4(acc[i][e][4 * q], acc[i][e][4 * q + 1],
+                                                                   acc[i][e][4 * q + 2], acc[i][e][4 * q + 3]);
+    __syncthreads();
+    // Four outputs of a row a thread, 8 T threads a row.
+    for (int j = threadIdx.x; j < 256 * T * T; j += WAVES * 64) {
+        const int row = j / (8 * T), c = j % (8 * T), e = row >> 5, i = c >> 3, q = (c & 7) >> 1, from = (row & 31) + 32 * (c & 1);
+        float4 s = red[place(0, T * i + e, q, from)];
+#pragma unroll
+        for (int v = 1; v < WAVES; ++v) {
+            const float4 x = red[place(v, T * i + e, q, from)];
+            s.x += x.x;
+            s.y += x.y;
+            s.z += x.z;
+            s.w += x.w;
+        }
+        if (m0 + row < p.M) bm_store4(p, m0 + row, n0 + 4 * c, s.x, s.y, s.z, s.w);
     }
+#endif
 }
 
 // Many rows: 256 outputs x 32 NT rows per workgroup, a 128-deep
@@ -216,9 +277,6 @@ __global__ __launch_bounds__(WAVES * 64) void k_bm_few(BmParams p) {
 // and every wave reads all of them.  (Both operands through LDS leave room for
 // two stages only, and one stage of lookahead does not cover a fetch: 345 us
 // for 8000 rows, K = 4096, N = 7168, of which the loads alone take 244.)
-// Rows in LDS are blocks of 8 x 128 bytes, piece c of row r at
-// 8 (r % 8) + (c ^ bm_swz(r)): 16 rows' reads of a piece hit all 64 banks.
-__device__ inline int bm_swz(int r) { return (r >> 1) & 7; }
 template <int NT>
 struct BmStage {
     bm_u32x4 b[4 * NT][kWave];
@@ -422,15 +480,6 @@ caee_status_t check_bm(const caee_block_matmul_desc_t* d) {
 constexpr int kBmExactK = 256;
 constexpr int kBmCus = 256;            // CUs of the chip, one workgroup of k_bm_many each at a time
 
-template <int WAVES, bool kExact>
-void launch_few(const BmParams& p, hipStream_t s) {
-    const unsigned nt = (unsigned)((p.N + 15) / 16);
-    const dim3 block(WAVES * 64);
-    if (p.M <= 16) hipLaunchKernelGGL((k_bm_few<1, WAVES, kExact>), dim3(nt, 1), block, 0, s, p);
-    else if (p.M <= 32) hipLaunchKernelGGL((k_bm_few<2, WAVES, kExact>), dim3(nt, 1), block, 0, s, p);
-    else hipLaunchKernelGGL((k_bm_few<4, WAVES, kExact>), dim3(nt, (unsigned)((p.M + 63) / 64)), block, 0, s, p);
-}
-
 // Row tiles per workgroup: the height whose whole rounds of the chip's CUs
 // take the least (8000 rows x 7168 outputs: 4 rounds of 8, 4 of 7, 5 of 6).
 int bm_height(const BmParams& p) {
@@ -454,23 +503,31 @@ void launch_many(const BmParams& p, hipStream_t s) {
     hipLaunchKernelGGL((k_bm_many<NT, kExact>), dim3(grid), dim3(512), 0, s, p, n_tiles, m_tiles);
 }
 
+// By the number of 64 x 64 tiles.  Up to half a round of the CUs 32 x 32
+// tiles, which make two of them, are faster (M x N, K = 4096: 64 x 7168 12.6
+// and 12.9 us, 256 x 2048 11.4 and 12.7, 1024 x 576 16.5 and 13.8, 128 x 7168
+// 22 and 13); k_bm_many needs K / 128 + 2 steps of 1.5 us for any product of
+// one round and then gains (512 x 7168: 46 and 53 us, 2048 x 2048 45 and 53,
+// 1024 x 7168 79 and 58; K = 512: 512 x 4096 9.4 and 12.6, 768 x 4096 13.5 and
+// 13.1, 1024 x 4096 17.6 and 13.5; K = 2048: 1024 x 4096 28 and 30).
 template <bool kExact>
 hipError_t launch_bm(const BmParams& p, hipStream_t s) {
-    const long long tiles = (long long)((p.M + 255) / 256) * ((p.N + 255) / 256);
-    if (p.M > 64 && (tiles >= 128 || p.M > 1024)) {
-        if constexpr (kExact) {
-            launch_many<4, true>(p, s);
-        } else {
-            switch (bm_height(p)) {
-                case 4: launch_many<4, false>(p, s); break;
-                case 5: launch_many<5, false>(p, s); break;
-                case 6: launch_many<6, false>(p, s); break;
-                case 7: launch_many<7, false>(p, s); break;
-                default: launch_many<8, false>(p, s); break;
-            }
-        }
+    const long long nt = (p.N + 63) / 64, mt = (p.M + 63) / 64, tiles = nt * mt;
+    if (tiles <= kBmCus / 2) {
+        const dim3 grid((p.N + 31) / 32, (p.M + 31) / 32);
+        hipLaunchKernelGGL((k_bm_split<1, 8, kExact>), grid, dim3(512), 0, s, p);
+    } else if (tiles <= (p.K < 2048 ? 3 : 4) * kBmCus) {
+        hipLaunchKernelGGL((k_bm_split<2, 4, kExact>), dim3((unsigned)nt, (unsigned)mt), dim3(256), 0, s, p);
+    } else if constexpr (kExact) {
+        launch_many<4, true>(p, s);
     } else {
-        launch_few<8, kExact>(p, s);
+        switch (bm_height(p)) {
+            case 4: launch_many<4, false>(p, s); break;
+            case 5: launch_many<5, false>(p, s); break;
+            case 6: launch_many<6, false>(p, s); break;
+            case 7: launch_many<7, false>(p, s); break;
+            default: launch_many<8, false>(p, s); break;
+        }
     }
     return hipGetLastError();
 }
