@@ -434,7 +434,9 @@ caee_status_t caee_latent_store(int32_t T, int32_t latent, int32_t rope, int32_t
 
 /* How latent attention is computed.  Both forms give the same function. */
 typedef enum caee_latent_form {
-    /* By the batch's size: expanded from CAEE_LATENT_EXPAND_NEW new tokens per request on average. */
+    /* By the batch's size: expanded from CAEE_LATENT_EXPAND_NEW new tokens
+     * per request on average, or from CAEE_LATENT_EXPAND_FRESH where the
+     * cache holds little else (max_kv <= 2 T). */
     CAEE_LATENT_AUTO = 0,
     /* Queries are multiplied by W_uk and attend to the cache rows
      * themselves, whose values W_uv is applied to afterwards: few new tokens
@@ -445,6 +447,7 @@ typedef enum caee_latent_form {
     CAEE_LATENT_EXPANDED = 2
 } caee_latent_form_t;
 #define CAEE_LATENT_EXPAND_NEW 128
+#define CAEE_LATENT_EXPAND_FRESH 16
 
 typedef struct caee_latent_desc {
     int32_t T;            /* query rows, >= 0 (padded ones included) */

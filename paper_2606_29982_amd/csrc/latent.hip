@@ -9,9 +9,18 @@ namespace {
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// The expanded form pays for every cached token once, the absorbed one 3.4
+// times as much per pair of tokens, so the new tokens per request decide.
+// Absorbed and expanded, us, 128 heads: 8 requests behind 8000 tokens with 64
+// new ones each 1359 and 3899, with 256 5788 and 4237; behind 1000 with 64 414
+// and 566, with 128 813 and 619; one request behind 8000 with 128 356 and 576,
+// with 256 685 and 595.  Without a cached prefix the expanded form is ahead
+// from about 8 (8 requests: 52 and 53, with 32 137 and 61; 16 heads: with 8 41
+// and 27).
 bool latent_expanded(const caee_latent_desc_t& d) {
     if (d.form != CAEE_LATENT_AUTO) return d.form == CAEE_LATENT_EXPANDED;
-    return (long long)d.T >= (long long)CAEE_LATENT_EXPAND_NEW * (d.B > 0 ? d.B : 1);
+    const long long B = d.B > 0 ? d.B : 1;
+    return d.T >= CAEE_LATENT_EXPAND_NEW * B || (d.T >= CAEE_LATENT_EXPAND_FRESH * B && d.max_kv <= 2ll * d.T);
 }
 
 LatentWs latent_ws(const caee_latent_desc_t& d) {

@@ -167,3 +167,10 @@ def test_pack_latent_weights_transposes():
     w = caee.pack_latent_weights(torch.arange(24.0).view(2, 3, 4), torch.zeros(2, 5, 4))
     assert w["w_uk_t"].shape == (2, 4, 3) and w["w_uk_t"].is_contiguous()
     assert torch.equal(w["w_uk_t"][1].t(), w["w_uk"][1])
+
+
+def test_auto_form_by_new_tokens_and_prefix():
+    size = lambda form, **kw: _latent_ws(_latent_desc(form=form, **kw))[1]  # noqa: E731
+    for T, kv, form in ((256, 9000, 2), (255, 9000, 1), (32, 64, 2), (32, 65, 1), (31, 62, 1)):
+        kw = dict(T=T, B=2, max_new=T, max_kv=kv)
+        assert size(0, **kw) == size(form, **kw) != size(3 - form, **kw), (T, kv)
