@@ -202,6 +202,12 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rg = wave & 1, th = wave >> 1;
+    int mine_at = 0;
+    LatentReq mine = {};
+    if (lane < p.B && p.B <= kWave) {
+        mine_at = p.meta[lane];
+        mine = lat_req(p, lane);
+    }
     const AbsShare sh = abs_share_of<kPairs>(p.meta[p.B], blockIdx.x);
     const uint32_t pw_at = (uint32_t)(uintptr_t)(lat_lds_void*)&pw[0][0][0], over_at = (uint32_t)(uintptr_t)(lat_lds_void*)&over[0];
     // Fragment places in a tile.  Keys: row 32 th + n, piece 2 j + hf.
@@ -212,11 +218,22 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
     const int vp0 = 2 * (vr * 8 + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ lat_swz(vr))) + (lane & 1);
 
     for (int u = sh.u0; u < sh.u1;) {
-        const int b = lat_find_wave(p.meta, p.B, u);
-        const LatentReq rq = lat_req(p, b);
+        // Up to 64 requests: each lane has read one, all at once.
+        int b, at_u;
+        LatentReq rq;
+        if (p.B <= kWave) {
+            b = 63 - __clzll(__ballot(lane < p.B && mine_at <= u) | 1ull);
+            at_u = __builtin_amdgcn_readlane(mine_at, b);
+            rq = {__builtin_amdgcn_readlane(mine.t0, b), __builtin_amdgcn_readlane(mine.add, b),
+                  __builtin_amdgcn_readlane(mine.seq, b)};
+        } else {
+            b = lat_find_wave(p.meta, p.B, u);
+            rq = lat_req(p, b);
+            at_u = p.meta[b];
+        }
         const int rows = rq.add * p.H;
         const int n_u = (rq.seq + kUnit - 1) / kUnit;
-        const int rel = u - p.meta[b], rp = rel / n_u, first = rel - rp * n_u;
+        const int rel = u - at_u, rp = rel / n_u, first = rel - rp * n_u;
         const int rt = kPairs ? 2 * rp + sh.member : rp;
         const int last = min(n_u, first + (sh.u1 - u));
         const bool whole = first == 0 && last == n_u;
@@ -285,15 +302,33 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
         };
 
         __syncthreads();       // the segment before is done with the tiles
+        // The queries come through the other stage, laid out as a tile's rows
+        // (a lane's piece of a row straight to its registers is a line of its
+        // own, 64 cycles a load: 1.5 us more).
+        {
+            const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
+                (void*)(p.qw + ((size_t)rq.t0 * p.H + row0) * (R + kRopeDim)), 0, kLatBufBytes, kLatBufWord3);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = 16 * wave + 8 * i + (lane >> 3);
+                const uint32_t at = (uint32_t)min(r, rows - 1 - row0) * kRowBytes + 16 * ((lane & 7) ^ lat_swz(8 * i + (lane >> 3)));
+#pragma unroll
+                for (int g = 0; g < kG; ++g)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st1.v[2 * wave + i][g][0], 16, at, 128 * g, 0, 0);
+            }
+        }
         Pages ahead = {};
         if (steps > 0) {
             load(pages_of(0), st0);
             ahead = pages_of(1);
         }
+        lat_wait_vm<0>();
+        lat_barrier();
         lat_u32x4 qf[kJ];
-        const uint16_t* qrow = p.qw + ((size_t)rq.t0 * p.H + row) * (R + kRopeDim) + 8 * hf;
+        const int qp = kp0 + 4 * (rg - th) * (kG * kWave);
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) qf[j] = *(const lat_u32x4*)(qrow + 16 * j);
+        for (int j = 0; j < kJ; ++j) qf[j] = (&st1.v[0][0][0])[(qp ^ (2 * (j & 3))) + (j >> 2) * kWave];
+        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));      // before the stage is filled again
         lat_f32x16 o[NC][2];
 #pragma unroll
         for (int c = 0; c < NC; ++c) o[c][0] = o[c][1] = lat_f32x16{};
@@ -375,14 +410,18 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
                     lds_put16(pw_at + ((rg * 4 + 2 * th + k) * kWave + lane) * 16, w);
                 }
             };
-            weights();
-            const bool mine = __any(big > kMaxWeight);
-            if (lane == 0) lds_put4(over_at + 4 * wave, mine);
-            lds_barrier();
             lat_u32x4 bw[4][2], ov;
-            lds_get(pw_at + 16 * lane, over_at, bw, ov);
-            if (__builtin_amdgcn_readfirstlane(ov[0] | ov[1] | ov[2] | ov[3])) {
-                // Some maxima move: rows' maxima and factors go round.
+            bool moves = s == 0;
+            if (!moves) {
+                weights();
+                const bool over_it = __any(big > kMaxWeight);
+                if (lane == 0) lds_put4(over_at + 4 * wave, over_it);
+                lds_barrier();
+                lds_get(pw_at + 16 * lane, over_at, bw, ov);
+                moves = __builtin_amdgcn_readfirstlane(ov[0] | ov[1] | ov[2] | ov[3]);
+            }
+            if (moves) {
+                // Some maxima move (all do in the first step): they and the factors go round.
                 float mt = sc[0];
 #pragma unroll
                 for (int i = 1; i < 16; ++i) mt = fmaxf(mt, sc[i]);
@@ -453,19 +492,28 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
             if (!whole) *(float2*)(p.part_ml + 2 * (slot0 + lane)) = make_float2(sf[lane], lr);
             else if (p.lse) p.lse[(size_t)rq.t0 * p.H + row0 + lane] = lat_lse(sf[lane], lr);
         }
+        // The sums leave through the stages, 32 rows each, unit c (16 bytes) of
+        // a row at c ^ (row % 32): a store then writes 1 KiB of a row.
+        float4* const out[2] = {(float4*)&st0, (float4*)&st1};
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const int i32 = 32 * r + n;
-            if (row0 + i32 >= rows) continue;
-            const float f = whole ? lat_inverse(sm[0][i32] + sm[1][i32]) : 1.0f;
-            float* dst = (whole ? p.o + ((size_t)rq.t0 * p.H + row0 + i32) * R : p.part + (slot0 + i32) * R) + 4 * hf;
+            const float f = whole ? lat_inverse(sm[0][32 * r + n] + sm[1][32 * r + n]) : 1.0f;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    *(float4*)(dst + 32 * (NC * wave + c) + 8 * i) =
-                        make_float4(o[c][r][4 * i] * f, o[c][r][4 * i + 1] * f, o[c][r][4 * i + 2] * f,
-                                    o[c][r][4 * i + 3] * f);
+                    out[r][n * (R / 4) + ((8 * (NC * wave + c) + 2 * i + hf) ^ n)] =
+                        make_float4(o[c][r][4 * i] * f, o[c][r][4 * i + 1] * f, o[c][r][4 * i + 2] * f, o[c][r][4 * i + 3] * f);
+        }
+        __syncthreads();
+        float* const dst = whole ? p.o + ((size_t)rq.t0 * p.H + row0) * R : p.part + slot0 * R;
+        const int n_rows = min(kAbsRows, rows - row0);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int n_here = min(max(n_rows - 32 * r, 0), 32) * (R / 4);
+#pragma unroll 8
+            for (int i = threadIdx.x; i < n_here; i += kAbsThreads)
+                ((float4*)dst)[32 * r * (R / 4) + i] = out[r][i ^ (i / (R / 4))];
         }
     }
 #endif
