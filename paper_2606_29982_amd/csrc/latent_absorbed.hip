@@ -81,29 +81,42 @@ __device__ void absorbed_shares(const LatentParams& p, int rows) {
 }
 
 // 128 components of q'_th for 32 tokens of one head per workgroup: W_uk[h]^T
-// rows as the M side of the product, tokens as the N side, so that a lane ends
-// with four consecutive latent components of one token.  Bound by the weights
-// (2 nope latent bytes a head) while tokens are few.
+// rows as the M side of the product, tokens as the N side.  Both come through
+// LDS, eight lanes a 128-byte line, and the outputs leave through it (straight
+// from and to registers a lane's 16 bytes are a line of their own, 64 cycles a
+// load: 15 us for 64 tokens of 128 heads where this takes 10).  Bound by
+// the weights (2 nope latent bytes a head) while tokens are few.  q' is rounded
+// to bf16 as the queries were: the scores' error of 2^-9 a product, random in
+// sign, is that of the bf16 weights of the sums.
 template <int NOPE>
 __global__ __launch_bounds__(kAbsThreads) void k_absorb(LatentParams p, int tile_rows) {
     if (blockIdx.x == (unsigned)p.H) {
         if (blockIdx.y == 0 && blockIdx.z == 0) absorbed_shares(p, tile_rows);
         return;
     }
-    constexpr int KS = NOPE / 16;
+    constexpr int KS = NOPE / 16, G = NOPE / 64;
+    __shared__ lat_u32x4 wt[16][G][kWave], qt[4][G][kWave];       // blocks of 8 rows x 128 bytes, swizzled
     const int h = blockIdx.x, t0 = blockIdx.y * 32;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, hf = lane >> 5;
-    const int t = t0 + n < p.T ? t0 + n : p.T - 1;
+    const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int width = p.latent + kRopeDim;
-    const uint16_t* qt = p.q + (size_t)t * p.q_stride + (size_t)h * (NOPE + kRopeDim);
-    lat_u32x4 qf[KS];
+    const uint16_t* wrow = p.w_uk_t + ((size_t)h * p.latent + 128 * blockIdx.z) * NOPE;
 #pragma unroll
-    for (int k = 0; k < KS; ++k) qf[k] = *(const lat_u32x4*)(qt + 16 * k + 8 * hf);
-    const int c = blockIdx.z * (kAbsThreads / 64) + wave;
-    const uint16_t* w = p.w_uk_t + ((size_t)h * p.latent + 32 * c + n) * NOPE + 8 * hf;
+    for (int i = 0; i < 5; ++i) {
+        const int blk = i < 4 ? 4 * wave + i : wave, r = 8 * blk + (lane >> 3), c8 = 8 * ((lane & 7) ^ lat_swz(r));
+        const uint16_t* src = i < 4 ? wrow + (size_t)r * NOPE
+                                    : p.q + (size_t)min(t0 + r, p.T - 1) * p.q_stride + (size_t)h * (NOPE + kRopeDim);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            __builtin_amdgcn_global_load_lds((lat_g_void*)(src + 64 * g + c8),
+                                             (lat_lds_void*)(i < 4 ? &wt[blk][g][0] : &qt[blk][g][0]), 16, 0, 0);
+    }
+    __syncthreads();
     lat_f32x16 acc = {};
+    const int at = (n & 7) * 8 + (hf ^ lat_swz(n));
 #pragma unroll
-    for (int k = 0; k < KS; ++k) acc = lat_mma(*(const lat_u32x4*)(w + 16 * k), qf[k], acc);
+    for (int k = 0; k < KS; ++k)
+        acc = lat_mma(wt[4 * wave + (n >> 3)][k / 4][at ^ (2 * (k % 4))], qt[n >> 3][k / 4][at ^ (2 * (k % 4))], acc);
     // Through LDS, so that 16 lanes write 256 bytes of a token.
     __shared__ lat_u32x4 tile[32][17];
 #pragma unroll
@@ -127,13 +140,14 @@ __global__ __launch_bounds__(kAbsThreads) void k_absorb(LatentParams p, int tile
     }
 }
 
-// One KV tile: 64 cache rows as [row / 8][128-byte group][row % 8][16-byte
+// Half a KV tile: 32 cache rows as [row / 8][128-byte group][row % 8][16-byte
 // piece, swizzled]: one direct-to-LDS load fills a block of 8 rows x 128
 // bytes, so that a lane's addresses in all groups differ by constants.
+constexpr int kHalf = kUnit / 2;
 template <int R>
-struct AbsTile {
+struct AbsHalf {
     static constexpr int kGroups = (R + kRopeDim) / 64;
-    lat_u32x4 v[kUnit / 8][kGroups][kWave];
+    lat_u32x4 v[kHalf / 8][kGroups][kWave];
 };
 
 // What the waves hand each other in every step is written and read by these:
@@ -178,24 +192,29 @@ __device__ inline void lds_get(uint32_t at, uint32_t flags, lat_u32x4 (&w)[4][2]
 // fetch each row half as often, but their 256 registers a wave leave room for
 // half the contraction only and cost one more exchange: 106 us for 64 users
 // of 128 heads and 2048 tokens on average, 195 us for five of 120011 tokens
-// and 64 rows; this takes 84 and 149.)
-// It is bound by the fetches: the same loads with no work between them take
-// 60 and 128 us (5.4 TB/s).  A CU takes 16 cycles for each load, so the next
-// tile's go out between the scores' MFMAs, one to two of these (all at the
-// start of the step: 96 and 155 us).
+// and 64 rows; this takes 72 and 121.)
+// It is bound by the fetches (5.7 TB/s for the five; the 64 users' rows go to
+// two workgroups each, by way of an L2).  A CU takes 16 cycles for each load, so
+// they go out between the MFMAs: the second half of the next tile beside the
+// scores, the first half of the one after as soon as the sums are done with
+// this tile's (with whole tiles of lookahead, all loads at a step's start: 96
+// and 155 us before other changes that gained 20; between the scores' MFMAs: 84
+// and 149).  Rows that one workgroup reads are not kept in the caches: 121 us
+// for the five where it was 137; for the 64 users' it changes nothing.
 // A row's running maximum moves only when a weight exceeds 2^kMaxSlack; then
 // the workgroup exchanges maxima and rescales its sums.
 template <int R, bool kPairs>
 __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
-    constexpr int kG = AbsTile<R>::kGroups;
+    constexpr int kG = AbsHalf<R>::kGroups;
     constexpr int kJ = 4 * kG;                 // 16-deep steps of the scores' contraction
     constexpr int NC = R / 128;                // 32-column tiles of the latent per wave
     constexpr int kAhead = 6, kVAhead = 3;     // fragments read from LDS ahead of their MFMAs
     constexpr int kRowBytes = (R + kRopeDim) * 2;
-    // One object per stage, so that the compiler can tell the reads of one
-    // from the loads that fill the other.
-    __shared__ AbsTile<R> st0, st1;
+    constexpr int kOnce = kPairs ? 0 : 2;      // rows that one workgroup reads: non-temporal loads
+    // One object per stage and half, so that the compiler can tell the reads of
+    // one from the loads that fill another.
+    __shared__ AbsHalf<R> st0a, st0b, st1a, st1b;
     __shared__ lat_u32x4 pw[2][4][kWave];      // softmax weights: [row group][16 tokens][fragment]
     __shared__ float sm[2][kAbsRows], sf[kAbsRows];
     __shared__ int over[4];
@@ -210,10 +229,10 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
     }
     const AbsShare sh = abs_share_of<kPairs>(p.meta[p.B], blockIdx.x);
     const uint32_t pw_at = (uint32_t)(uintptr_t)(lat_lds_void*)&pw[0][0][0], over_at = (uint32_t)(uintptr_t)(lat_lds_void*)&over[0];
-    // Fragment places in a tile.  Keys: row 32 th + n, piece 2 j + hf.
-    // Transposed values: rows 16 ks + 8 e + 4 hf + (0 .. 3), four 16-byte
-    // pieces per 32 components.
-    const int kp0 = (4 * th + (n >> 3)) * (kG * kWave) + (n & 7) * 8 + (hf ^ lat_swz(n));
+    // Fragment places in a half.  Keys: row n, piece 2 j + hf.  Transposed
+    // values: rows 16 ks + 8 e + 4 hf + (0 .. 3), four 16-byte pieces per 32
+    // components.
+    const int kp0 = (n >> 3) * (kG * kWave) + (n & 7) * 8 + (hf ^ lat_swz(n));
     const int vr = 4 * hf + ((lane & 15) >> 2);
     const int vp0 = 2 * (vr * 8 + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ lat_swz(vr))) + (lane & 1);
 
@@ -250,135 +269,166 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
         const int tok0 = first * kUnit, tok1 = min(last * kUnit, sees(min(row0 + kAbsRows, rows) - 1));
         const int steps = tok1 > tok0 ? (tok1 - tok0 + kUnit - 1) / kUnit : 0;
 
-        // Wave w fills the tile's rows 16 w .. 16 w + 15, eight by eight; a lane
-        // reads piece lane % 8 (swizzled) of row lane / 8 in every group.  The
-        // pages of its two rows come one tile ahead, used only after the wait
-        // for that tile.  Past the request's tokens: its last row, masked later.
-        struct Pages {
-            int page[2], at[2];
+        // Wave w fills rows 8 w .. 8 w + 7 of a half; a lane reads piece lane % 8
+        // (swizzled) of row lane / 8 in every group.  Where the eight lie in one
+        // page, its number is read by a scalar load (a vector load's wait would
+        // drain the tiles in flight) a step or more ahead; else row by row.
+        // Past the request's tokens: its last row, masked later.
+        struct Rows {
+            int page, at, span;       // of the first row; the others follow up to at + span
+            bool one;
         };
-        auto pages_of = [&](int s) __attribute__((always_inline)) {
-            Pages v;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const unsigned pos = min(tok0 + s * kUnit + 16 * wave + 8 * i + (lane >> 3), rq.seq - 1);
-                const unsigned j = pos / (unsigned)p.block;
-                v.page[i] = p.table[(size_t)b * p.max_blocks + min(j, (unsigned)p.max_blocks - 1u)];
-                v.at[i] = (int)(pos - j * p.block);
-            }
-            return v;
+        auto entry = [&](int j) __attribute__((always_inline)) {
+            const size_t i = (size_t)b * p.max_blocks + min((unsigned)j, (unsigned)p.max_blocks - 1u);
+            return ((const __attribute__((address_space(4))) int32_t*)p.table)[i];
+        };
+        auto rows_of = [&](int s, int half) __attribute__((always_inline)) {
+            const int pos = tok0 + s * kUnit + kHalf * half + 8 * wave;
+            const int r0 = min(pos, rq.seq - 1), r1 = min(pos + 7, rq.seq - 1);
+            const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)r0 / (unsigned)p.block);
+            const int at = r0 - (int)(j * (unsigned)p.block);
+            return Rows{entry(j), at, r1 - r0, at + (r1 - r0) < p.block};
         };
         // Buffer loads (the compiler counts the LDS reads apart from them): one
         // buffer per page, a lane's row a 32-bit offset in it.
-        auto page_buf = [&](int page) __attribute__((always_inline)) {
+        // Of size 0 where nothing is to be loaded: its loads cost no memory
+        // traffic, and their number does not depend on a branch (the compiler
+        // would wait for the fewest).
+        auto page_buf = [&](int page, bool there = true) __attribute__((always_inline)) {
             return __builtin_amdgcn_make_buffer_rsrc(
-                (void*)((const char*)p.cache + (size_t)page * (uint32_t)p.block * kRowBytes), 0, kLatBufBytes, kLatBufWord3);
+                (void*)((const char*)p.cache + (size_t)min(max(page, 0), p.n_blocks - 1) * (uint32_t)p.block * kRowBytes), 0,
+                there ? kLatBufBytes : 0, kLatBufWord3);
         };
-        auto offset = [&](const Pages& v, int i) __attribute__((always_inline)) {
-            return (uint32_t)v.at[i] * kRowBytes + 16 * ((lane & 7) ^ lat_swz(8 * i + (lane >> 3)));
+        auto piece = [&]() __attribute__((always_inline)) { return 16u * ((lane & 7) ^ lat_swz(8 * wave + (lane >> 3))); };
+        auto offset = [&](const Rows& v) __attribute__((always_inline)) {
+            return (uint32_t)(v.at + min(lane >> 3, v.span)) * kRowBytes + piece();
         };
-        auto page = [&](const Pages& v, int i) __attribute__((always_inline)) { return min(max(v.page[i], 0), p.n_blocks - 1); };
-        // Eight rows in one page each; else row by row.
-        auto one_page = [&](const Pages& v) __attribute__((always_inline)) {
-            const int p0 = page(v, 0), p1 = page(v, 1);
-            return __all(p0 == __builtin_amdgcn_readfirstlane(p0) && p1 == __builtin_amdgcn_readfirstlane(p1));
-        };
-        auto load = [&](const Pages& v, AbsTile<R>& t) __attribute__((always_inline)) {
-            const bool one = one_page(v);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int pg = page(v, i);
-                const uint32_t at = offset(v, i);
+        auto load_each = [&](int s, int half, AbsHalf<R>& t) __attribute__((always_inline)) {
+            lat_wait_vm<0>();
 #pragma unroll 1
-                for (int r = 0; r < (one ? 1 : 8); ++r) {
-                    const __amdgpu_buffer_rsrc_t buf = page_buf(__builtin_amdgcn_readlane(pg, 8 * r));
-                    if (one || lane >> 3 == r) {
+            for (int r = 0; r < 8; ++r) {
+                const int pos = min(tok0 + s * kUnit + kHalf * half + 8 * wave + r, rq.seq - 1);
+                const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)pos / (unsigned)p.block);
+                const __amdgpu_buffer_rsrc_t buf = page_buf(entry(j));
+                const uint32_t at = (uint32_t)(pos - (int)(j * (unsigned)p.block)) * kRowBytes + piece();
+                if (lane >> 3 == r) {
 #pragma unroll
-                        for (int g = 0; g < kG; ++g)
-                            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&t.v[2 * wave + i][g][0], 16, at, 128 * g, 0, 0);
-                    }
+                    for (int g = 0; g < kG; ++g)
+                        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&t.v[wave][g][0], 16, at, 128 * g, 0, 0);
                 }
+            }
+            lat_wait_vm<0>();
+        };
+        auto load = [&](int s, int half, AbsHalf<R>& t) __attribute__((always_inline)) {
+            const Rows v = rows_of(s, half);
+            if (v.one) {
+                const __amdgpu_buffer_rsrc_t buf = page_buf(v.page);
+                const uint32_t at = offset(v);
+#pragma unroll
+                for (int g = 0; g < kG; ++g)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&t.v[wave][g][0], 16, at, 128 * g, 0, 0);
+            } else {
+                load_each(s, half, t);
             }
         };
 
-        __syncthreads();       // the segment before is done with the tiles
+        __syncthreads();       // the segment before is done with the stages
         // The queries come through the other stage, laid out as a tile's rows
         // (a lane's piece of a row straight to its registers is a line of its
         // own, 64 cycles a load: 1.5 us more).
         {
             const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
                 (void*)(p.qw + ((size_t)rq.t0 * p.H + row0) * (R + kRopeDim)), 0, kLatBufBytes, kLatBufWord3);
+            const int r = 8 * wave + (lane >> 3);
+            const uint32_t at0 = (uint32_t)min(r, rows - 1 - row0) * kRowBytes + piece();
+            const uint32_t at1 = (uint32_t)min(kHalf + r, rows - 1 - row0) * kRowBytes + piece();
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = 16 * wave + 8 * i + (lane >> 3);
-                const uint32_t at = (uint32_t)min(r, rows - 1 - row0) * kRowBytes + 16 * ((lane & 7) ^ lat_swz(8 * i + (lane >> 3)));
-#pragma unroll
-                for (int g = 0; g < kG; ++g)
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st1.v[2 * wave + i][g][0], 16, at, 128 * g, 0, 0);
+            for (int g = 0; g < kG; ++g) {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st1a.v[wave][g][0], 16, at0, 128 * g, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st1b.v[wave][g][0], 16, at1, 128 * g, 0, 0);
             }
         }
-        Pages ahead = {};
         if (steps > 0) {
-            load(pages_of(0), st0);
-            ahead = pages_of(1);
+            load(0, 0, st0a);
+            load(0, 1, st0b);
         }
+        Rows next_b = rows_of(1, 1);
         lat_wait_vm<0>();
         lat_barrier();
         lat_u32x4 qf[kJ];
-        const int qp = kp0 + 4 * (rg - th) * (kG * kWave);
+        auto queries = [&](const AbsHalf<R>& t) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) qf[j] = (&st1.v[0][0][0])[(qp ^ (2 * (j & 3))) + (j >> 2) * kWave];
-        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));      // before the stage is filled again
+            for (int j = 0; j < kJ; ++j) qf[j] = (&t.v[0][0][0])[(kp0 ^ (2 * (j & 3))) + (j >> 2) * kWave];
+        };
+        if (rg) queries(st1b);
+        else queries(st1a);
+        lds_barrier();                         // before the stage is filled again
+        {
+            const Rows v = rows_of(1, 0);
+            const __amdgpu_buffer_rsrc_t buf = page_buf(v.page, steps > 1 && v.one);
+            const uint32_t at = offset(v);
+#pragma unroll
+            for (int g = 0; g < kG; ++g)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st1a.v[wave][g][0], 16, at, 128 * g, 0, 0);
+            if (steps > 1 && !v.one) load_each(1, 0, st1a);
+        }
         lat_f32x16 o[NC][2];
 #pragma unroll
         for (int c = 0; c < NC; ++c) o[c][0] = o[c][1] = lat_f32x16{};
         float m = kNoScore, l = 0.0f;
 
-        auto step = [&](int s, AbsTile<R>& t, AbsTile<R>& next) __attribute__((always_inline)) {
-            const int tb = tok0 + s * kUnit;
-            lat_wait_vm<0>();                  // this wave's part of the tile is there; after the barrier all of it is,
-            lat_barrier();                     // and nobody reads the other stage
+        // Step s: tile s in ta and tb, the other stage's second half nb for that
+        // of tile s + 1 (its first half is on its way).
+        auto step = [&](int s, AbsHalf<R>& ta, AbsHalf<R>& tb, AbsHalf<R>& nb) __attribute__((always_inline)) {
+            const int tok = tok0 + s * kUnit;
+            // This wave's part of the tile is there (the first half of the next
+            // may stay in flight); after the barrier all of it is, and nobody
+            // reads the other stage.
+            lat_wait_vm<kG>();
+            lat_barrier();
             lat_f32x16 sc = {};
-            const lat_u32x4* keys = &t.v[0][0][0];
             // (made here: the registers that a stage's addresses would take
             // through the loop are not there)
             int kp = kp0, vp = vp0;
             asm volatile("" : "+v"(kp), "+v"(vp));
-            auto key = [&](int j) __attribute__((always_inline)) { return keys[(kp ^ (2 * (j & 3))) + (j >> 2) * kWave]; };
             // Scores, key fragments kAhead steps ahead of their MFMA, with the
-            // next tile's loads where its eight rows lie in one page each.
-            const bool more_tiles = s + 1 < steps, spread = more_tiles && one_page(ahead);
-            if (more_tiles && !spread) load(ahead, next);
-            const __amdgpu_buffer_rsrc_t buf[2] = {page_buf(__builtin_amdgcn_readfirstlane(page(ahead, 0))),
-                                                   page_buf(__builtin_amdgcn_readfirstlane(page(ahead, 1)))};
-            const uint32_t at[2] = {offset(ahead, 0), offset(ahead, 1)};
-            ahead = pages_of(s + 2);
-            __builtin_amdgcn_sched_barrier(0);
-            lat_u32x4 kf[kAhead];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) kf[j] = key(j);
-            lat_for<0, kJ>([&](auto jc) __attribute__((always_inline)) {
-                constexpr int j = decltype(jc)::value;
-                sc = lat_mma(kf[j % kAhead], qf[j], sc);
-                if constexpr (j + kAhead < kJ) kf[j % kAhead] = key(j + kAhead);
-                if constexpr (j % 2 == 0) {
-                    constexpr int i = j / 2 / kG, g = j / 2 % kG;
-                    if (spread)
-                        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf[i], (lat_lds_void*)&next.v[2 * wave + i][g][0], 16, at[i],
-                                                                 128 * g, 0, 0);
-                }
+            // loads where the eight rows lie in one page.
+            const bool more_b = s + 1 < steps, one_b = next_b.one;
+            const __amdgpu_buffer_rsrc_t buf_b = page_buf(next_b.page, more_b && one_b);
+            const uint32_t at_b = offset(next_b);
+            const Rows next_a = rows_of(s + 2, 0);
+            next_b = rows_of(s + 2, 1);
+            auto scores = [&](const AbsHalf<R>& t) __attribute__((always_inline)) {
+                const lat_u32x4* keys = &t.v[0][0][0];
+                auto key = [&](int j) __attribute__((always_inline)) { return keys[(kp ^ (2 * (j & 3))) + (j >> 2) * kWave]; };
                 __builtin_amdgcn_sched_barrier(0);
-            });
+                lat_u32x4 kf[kAhead];
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) kf[j] = key(j);
+                lat_for<0, kJ>([&](auto jc) __attribute__((always_inline)) {
+                    constexpr int j = decltype(jc)::value;
+                    sc = lat_mma(kf[j % kAhead], qf[j], sc);
+                    if constexpr (j + kAhead < kJ) kf[j % kAhead] = key(j + kAhead);
+                    if constexpr (j % 4 == 0) {
+                        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_b, (lat_lds_void*)&nb.v[wave][j / 4][0], 16, at_b,
+                                                                 128 * (j / 4), 0, kOnce);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            };
+            if (th) scores(tb);
+            else scores(ta);
+            if (more_b && !one_b) load_each(s + 1, 1, nb);
             // Values: fragments (16 tokens ks, column tile c) in order, kVAhead
             // ahead of their MFMAs.
-            const lat_u32x2* base = (const lat_u32x2*)&t.v[0][0][0];
             constexpr int kF = 4 * NC;
             auto value = [&](int i) __attribute__((always_inline)) {
                 const int ks = i / NC, c = i % NC, cc = NC * wave + c;
                 lat_u32x2 w[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const lat_u32x2* at = base + ((2 * ks + e) * kG + (cc >> 1)) * (2 * kWave) + (vp ^ (8 * (cc & 1) + 2 * e));
+                    const int place = ((2 * (ks & 1) + e) * kG + (cc >> 1)) * (2 * kWave) + (vp ^ (8 * (cc & 1) + 2 * e));
+                    const lat_u32x2* at = (const lat_u32x2*)(ks < 2 ? &ta.v[0][0][0] : &tb.v[0][0][0]) + place;
                     w[e] = __builtin_bit_cast(lat_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lat_lds_s16x4*)at));
                 }
                 return lat_u32x4{w[0][0], w[0][1], w[1][0], w[1][1]};
@@ -386,12 +436,12 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
             lat_u32x4 vf[kVAhead];
 #pragma unroll
             for (int i = 0; i < kVAhead; ++i) vf[i] = value(i);
-            const bool masked = tb + kUnit > lim_min;
+            const bool masked = tok + kUnit > lim_min;
             if (masked) {
                 asm volatile("");       // a branch, not selects in every step
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (tb + 32 * th + 8 * (i >> 2) + 4 * hf + (i & 3) >= limit) sc[i] = -INFINITY;
+                    if (tok + 32 * th + 8 * (i >> 2) + 4 * hf + (i & 3) >= limit) sc[i] = -INFINITY;
             }
             float more, big;
             auto weights = [&]() __attribute__((always_inline)) {
@@ -455,31 +505,47 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
                 // Rows that some queries do not see may hold anything: their
                 // infinities and NaNs must not meet the zero weights (queries
                 // that see such a row have it in their scores).
-                const int r0 = max(lim_min - tb, 0);
-                for (int i = threadIdx.x; i < (kUnit - r0) * (R / 8); i += kAbsThreads) {
-                    const int r = r0 + i / (R / 8), c = i % (R / 8);
-                    lat_u32x4& v = t.v[r >> 3][c >> 3][(r & 7) * 8 + (c & 7)];
+                auto clear = [&](AbsHalf<R>& t, int r0) __attribute__((always_inline)) {
+                    for (int i = threadIdx.x; i < (kHalf - r0) * (R / 8); i += kAbsThreads) {
+                        const int r = r0 + i / (R / 8), c = i % (R / 8);
+                        lat_u32x4& v = t.v[r >> 3][c >> 3][(r & 7) * 8 + (c & 7)];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = lat_finite(v[e]);
-                }
+                        for (int e = 0; e < 4; ++e) v[e] = lat_finite(v[e]);
+                    }
+                };
+                clear(ta, max(lim_min - tok, 0));
+                clear(tb, max(lim_min - tok - kHalf, 0));
                 lds_barrier();
 #pragma unroll
                 for (int i = 0; i < kVAhead; ++i) vf[i] = value(i);
             }
             __builtin_amdgcn_sched_barrier(0);
+            const bool more_a = s + 2 < steps;
+            const __amdgpu_buffer_rsrc_t buf_a = page_buf(next_a.page, more_a && next_a.one);
+            const uint32_t at_a = offset(next_a);
             lat_for<0, kF>([&](auto ic) __attribute__((always_inline)) {
                 constexpr int i = decltype(ic)::value;
+                if constexpr (i == kF / 2) lat_barrier();      // nobody reads the first half any more
                 o[i % NC][0] = lat_mma(vf[i % kVAhead], bw[i / NC][0], o[i % NC][0]);
                 o[i % NC][1] = lat_mma(vf[i % kVAhead], bw[i / NC][1], o[i % NC][1]);
                 if constexpr (i + kVAhead < kF) vf[i % kVAhead] = value(i + kVAhead);
+                if constexpr (i >= kF / 2) {
+                    constexpr int n0 = (i - kF / 2) * kG / (kF / 2), n1 = (i + 1 - kF / 2) * kG / (kF / 2);
+                    lat_for<n0, n1>([&](auto gc) __attribute__((always_inline)) {
+                        constexpr int g = decltype(gc)::value;
+                        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_a, (lat_lds_void*)&ta.v[wave][g][0], 16, at_a, 128 * g, 0, kOnce);
+                    });
+                }
                 __builtin_amdgcn_sched_barrier(0);
             });
+            if (more_a && !next_a.one) load_each(s + 2, 0, ta);
         };
         for (int s = 0; s < steps; s += 2) {
-            step(s, st0, st1);
-            if (s + 1 < steps) step(s + 1, st1, st0);
+            step(s, st0a, st0b, st1b);
+            if (s + 1 < steps) step(s + 1, st1a, st1b, st0b);
         }
 
+        lat_wait_vm<0>();          // no load is on its way into the stages any more
         // Row sums: two halves of a lane pair, two token halves.
         l = lat_sum_pair(l);
         __syncthreads();
@@ -492,17 +558,20 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
             if (!whole) *(float2*)(p.part_ml + 2 * (slot0 + lane)) = make_float2(sf[lane], lr);
             else if (p.lse) p.lse[(size_t)rq.t0 * p.H + row0 + lane] = lat_lse(sf[lane], lr);
         }
-        // The sums leave through the stages, 32 rows each, unit c (16 bytes) of
-        // a row at c ^ (row % 32): a store then writes 1 KiB of a row.
-        float4* const out[2] = {(float4*)&st0, (float4*)&st1};
+        // The sums leave through the stages, 16 rows in each half, unit c (16
+        // bytes) of a row at c ^ (row % 32): a store then writes 1 KiB of a row.
+        auto out = [&](int r, int i32) __attribute__((always_inline)) {      // row 32 r + i32
+            return (float4*)(r == 0 ? (i32 < 16 ? &st0a : &st0b) : (i32 < 16 ? &st1a : &st1b)) + (i32 & 15) * (R / 4);
+        };
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const float f = whole ? lat_inverse(sm[0][32 * r + n] + sm[1][32 * r + n]) : 1.0f;
+            float4* const at = out(r, n);
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    out[r][n * (R / 4) + ((8 * (NC * wave + c) + 2 * i + hf) ^ n)] =
+                    at[(8 * (NC * wave + c) + 2 * i + hf) ^ n] =
                         make_float4(o[c][r][4 * i] * f, o[c][r][4 * i + 1] * f, o[c][r][4 * i + 2] * f, o[c][r][4 * i + 3] * f);
         }
         __syncthreads();
@@ -513,7 +582,7 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
             const int n_here = min(max(n_rows - 32 * r, 0), 32) * (R / 4);
 #pragma unroll 8
             for (int i = threadIdx.x; i < n_here; i += kAbsThreads)
-                ((float4*)dst)[32 * r * (R / 4) + i] = out[r][i ^ (i / (R / 4))];
+                ((float4*)dst)[32 * r * (R / 4) + i] = out(r, i / (R / 4))[(i % (R / 4)) ^ (i / (R / 4))];
         }
     }
 #endif
@@ -620,53 +689,67 @@ __global__ __launch_bounds__(kAbsThreads) void k_join(LatentParams p) {
     if (p.lse && lane == 0) p.lse[at] = lat_lse(m, l);
 }
 
-// y_th for 32 tokens of one head per workgroup, W_uv rows as the M side: a
-// wave has an eighth of the contraction and all outputs, so that the attended
-// latents, in 32 bits the larger operand, are read once; the eighths are added
-// through LDS in order.  Latency bounds it: each wave has all its loads in
-// flight at once.
+// 64 components of y_th for 32 tokens of one head per workgroup, W_uv rows as
+// the M side: a wave has 64 of the contraction, whose operands it fetches into
+// its own part of LDS, eight lanes a 128-byte line (straight to registers a
+// lane's 16 bytes are a line of their own, 64 cycles a load: 16 us for 64 tokens
+// of 128 heads where this takes 12); the waves' sums are added through LDS in
+// order.
 // The attended latents are split into two bf16 parts (value and remainder),
 // which keeps them at 16 bits of mantissa for one more product per step of
 // a kernel that the weights' and the latents' bytes bound.
-constexpr int kUnThreads = 512;
-template <int R, int NV>
-__global__ __launch_bounds__(kUnThreads) void k_unabsorb(LatentParams p) {
-    constexpr int kRanges = kUnThreads / kWave;
-    __shared__ float4 red[kRanges][NV][4][kWave];
-    const int h = blockIdx.x, t0 = blockIdx.y * 32;
+template <int R>
+__global__ __launch_bounds__(R) void k_unabsorb(LatentParams p) {
+    constexpr int kRanges = R / kWave;
+    __shared__ lat_u32x4 wt[kRanges][8][kWave], ot[kRanges][2][4][kWave];      // blocks of 8 rows x 128 bytes, swizzled
+    const int h = blockIdx.x, t0 = blockIdx.y * 32, v0 = blockIdx.z * 64;
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int kr = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int t = t0 + n < p.T ? t0 + n : p.T - 1;
-    constexpr int kLen = R / kRanges;
-    const int k0 = kr * kLen;
-    const float* src = p.o + ((size_t)t * p.H + h) * R + 8 * hf + k0;
-    const uint16_t* w = p.w_uv + ((size_t)h * p.v + n) * R + 8 * hf + k0;
-    lat_f32x16 acc[NV] = {};
 #pragma unroll
-    for (int k = 0; k < kLen; k += 16) {
-        const float4 a = *(const float4*)(src + k), b = *(const float4*)(src + k + 4);
-        lat_u32x4 wf[NV];
+    for (int i = 0; i < 8; ++i) {
+        const int r = 8 * i + (lane >> 3), c = (lane & 7) ^ lat_swz(r);
+        const uint16_t* w = p.w_uv + ((size_t)h * p.v + v0 + r) * R + 64 * kr + 8 * c;
+        __builtin_amdgcn_global_load_lds((lat_g_void*)w, (lat_lds_void*)&wt[kr][i][0], 16, 0, 0);
+    }
 #pragma unroll
-        for (int v = 0; v < NV; ++v) wf[v] = *(const lat_u32x4*)(w + (size_t)32 * v * R + k);
-        const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 3), c = (lane & 7) ^ lat_swz(r);
+        const float* o = p.o + ((size_t)min(t0 + r, p.T - 1) * p.H + h) * R + 64 * kr + 4 * c;
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+            __builtin_amdgcn_global_load_lds((lat_g_void*)(o + 32 * g), (lat_lds_void*)&ot[kr][g][i][0], 16, 0, 0);
+    }
+    lat_wait_vm<0>();          // what a wave reads it has loaded itself
+    asm volatile("" ::: "memory");
+    lat_f32x16 acc[2] = {};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int at = (n & 7) * 8, sw = lat_swz(n), c0 = 4 * (k & 1) + 2 * hf;
+        const lat_u32x4 a = ot[kr][k >> 1][n >> 3][at + (c0 ^ sw)], b = ot[kr][k >> 1][n >> 3][at + ((c0 + 1) ^ sw)];
         lat_u32x4 hi, lo;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            hi[i] = lat_pack(x[2 * i], x[2 * i + 1]);
-            lo[i] = lat_pack(x[2 * i] - __uint_as_float(hi[i] << 16), x[2 * i + 1] - __uint_as_float(hi[i] & 0xFFFF0000u));
+            const float x0 = __uint_as_float(i < 2 ? a[2 * i] : b[2 * i - 4]), x1 = __uint_as_float(i < 2 ? a[2 * i + 1] : b[2 * i - 3]);
+            hi[i] = lat_pack(x0, x1);
+            lo[i] = lat_pack(x0 - __uint_as_float(hi[i] << 16), x1 - __uint_as_float(hi[i] & 0xFFFF0000u));
         }
 #pragma unroll
-        for (int v = 0; v < NV; ++v) acc[v] = lat_mma(wf[v], lo, lat_mma(wf[v], hi, acc[v]));
+        for (int v = 0; v < 2; ++v) {
+            const lat_u32x4 w = wt[kr][4 * v + (n >> 3)][at + ((2 * k + hf) ^ sw)];
+            acc[v] = lat_mma(w, lo, lat_mma(w, hi, acc[v]));
+        }
     }
+    __syncthreads();
+    float4(*const red)[2][4][kWave] = (float4(*)[2][4][kWave])&wt;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < 2; ++v)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             red[kr][v][i][lane] = make_float4(acc[v][4 * i], acc[v][4 * i + 1], acc[v][4 * i + 2], acc[v][4 * i + 3]);
     __syncthreads();
-    // Four outputs of a token a thread: 8 lanes write 32 consecutive ones.
-    for (int j = threadIdx.x; j < 8 * NV * 32; j += kUnThreads) {
-        const int tok = j / (8 * NV), c = j % (8 * NV), v = c >> 3, i = (c & 7) >> 1, from = tok + 32 * (c & 1);
+    // Four outputs of a token a thread, 16 threads a token.
+    for (int j = threadIdx.x; j < 512; j += R) {
+        const int tok = j >> 4, c = j & 15, v = c >> 3, i = (c & 7) >> 1, from = tok + 32 * (c & 1);
         if (t0 + tok >= p.T) continue;
         float4 s = red[0][v][i][from];
 #pragma unroll
@@ -677,7 +760,7 @@ __global__ __launch_bounds__(kUnThreads) void k_unabsorb(LatentParams p) {
             s.z += x.z;
             s.w += x.w;
         }
-        const size_t o = ((size_t)(t0 + tok) * p.H + h) * p.v + 4 * c;
+        const size_t o = ((size_t)(t0 + tok) * p.H + h) * p.v + v0 + 4 * c;
         if (p.y_bf16) *(lat_u32x2*)((uint16_t*)p.y + o) = lat_u32x2{lat_pack(s.x, s.y), lat_pack(s.z, s.w)};
         else *(float4*)((float*)p.y + o) = s;
     }
@@ -692,9 +775,7 @@ void attend_on(const LatentParams& p, hipStream_t s) {
         hipLaunchKernelGGL((k_attend<R, kPairs>), grid, block, 0, s, p);
         if (rows < kJoinRows) hipLaunchKernelGGL((k_join<R, kPairs, 4>), dim3((unsigned)rows), block, 0, s, p);
         else hipLaunchKernelGGL((k_join<R, kPairs, 1>), dim3((unsigned)((rows + 3) / 4)), block, 0, s, p);
-        const dim3 heads(p.H, (p.T + 31) / 32);
-        if (p.v == 128) hipLaunchKernelGGL((k_unabsorb<R, 4>), heads, dim3(kUnThreads), 0, s, p);
-        else hipLaunchKernelGGL((k_unabsorb<R, 2>), heads, dim3(kUnThreads), 0, s, p);
+        hipLaunchKernelGGL(k_unabsorb<R>, dim3(p.H, (p.T + 31) / 32, p.v / 64), dim3(R), 0, s, p);
     };
     if (p.latent == 512) run(LatInt<512>{});
     else if (p.latent == 256) run(LatInt<256>{});

@@ -70,26 +70,49 @@ struct ExpandStage {
 __global__ __launch_bounds__(kExpandThreads) void k_expand(LatentParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
     const int ft = blockIdx.x;
-    if (blockIdx.y == gridDim.y - 1) {
-        if (ft == 0) prompt_tiles(p);
-        blank_rows(p, ft, gridDim.x);
-        return;
-    }
     constexpr int kWaves = kExpandThreads / kWave, kBlocks = kExpandTile / 8 / kWaves;     // blocks of 8 rows a wave fetches
     __shared__ ExpandStage st0, st1;
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave & 1, wn = wave >> 1;
     const int total = p.B > 0 ? (int)min((long long)p.cu_kv[p.B], p.max_kv) : 0;
+    // Cache row of token s of all requests' tokens (for a whole wave at a time).
+    // The requests' first tokens: up to 64 in a register, one a lane (a search
+    // in memory waits for each of its steps).
+    const int lane_first = p.B <= kWave ? p.cu_kv[min(lane, p.B)] : 0;
+    auto cache_row = [&](int s) {
+        s = min(s, total - 1);
+        int b, first;
+        if (p.B <= kWave) {
+            b = 0;
+#pragma unroll
+            for (int d = 32; d >= 1; d >>= 1) {
+                const int f = __shfl(lane_first, min(b + d, kWave - 1));
+                if (b + d < p.B && f <= s) b += d;
+            }
+            first = __shfl(lane_first, b);
+        } else {
+            b = lat_find(p.cu_kv, p.B, s);
+            first = p.cu_kv[b];
+        }
+        return lat_slot(p, b, s - first);
+    };
+    if (blockIdx.y == gridDim.y - 1) {
+        if (ft == 0) prompt_tiles(p);
+        blank_rows(p, ft, gridDim.x);
+        // The rotary keys, 8 lanes a token.
+        for (int i0 = ft * kExpandThreads; i0 < total * 8; i0 += gridDim.x * kExpandThreads) {
+            const int s = (i0 + (int)threadIdx.x) >> 3, q8 = threadIdx.x & 7;
+            const size_t row = cache_row(s);
+            if (s < total)
+                *(lat_u32x4*)(p.kr + (size_t)s * kRopeDim + 8 * q8) =
+                    *(const lat_u32x4*)(p.cache + row * (p.latent + kRopeDim) + p.latent + 8 * q8);
+        }
+        return;
+    }
     const int s0 = blockIdx.y * kExpandTile;
     if (s0 >= total) return;
     const int hw = p.nope + p.v, outs = p.H * hw, row_bytes = (p.latent + kRopeDim) * 2;
-    // Cache row of token s of all requests' tokens.
-    auto cache_row = [&](int s) {
-        s = min(s, total - 1);
-        const int b = lat_find(p.cu_kv, p.B, s);
-        return lat_slot(p, b, s - p.cu_kv[b]);
-    };
     // Buffer loads (the compiler counts the LDS reads apart from them).  Eight
     // weight rows lie in one head's keys or values.  A token's row is a 32-bit
     // offset where the cache has at most 4 GiB, else rows go one by one, each
@@ -106,14 +129,6 @@ __global__ __launch_bounds__(kExpandThreads) void k_expand(LatentParams p) {
         xrow[i] = cache_row(s0 + r + (lane >> 3));
     }
     auto piece = [&](int i) { return 16u * ((lane & 7) ^ lat_swz(8 * i + (lane >> 3))); };     // kBlocks is even
-    if (ft == 0) {
-        for (int i = threadIdx.x; i < kExpandTile * 8; i += kExpandThreads) {
-            const int s = s0 + (i >> 3);
-            if (s < total)
-                *(lat_u32x4*)(p.kr + (size_t)s * kRopeDim + 8 * (i & 7)) = *(const lat_u32x4*)(
-                    p.cache + (size_t)cache_row(s) * (p.latent + kRopeDim) + p.latent + 8 * (i & 7));
-        }
-    }
     // Load i of a wave's part of stage k: weight blocks, then token blocks.
     auto load = [&](int k, int i, ExpandStage& t) __attribute__((always_inline)) {
         if (i < kBlocks) {
