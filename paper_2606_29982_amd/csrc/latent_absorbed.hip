@@ -203,6 +203,10 @@ __device__ inline void lds_get(uint32_t at, uint32_t flags, lat_u32x4 (&w)[4][2]
 // for the five where it was 137; for the 64 users' it changes nothing.
 // A row's running maximum moves only when a weight exceeds 2^kMaxSlack; then
 // the workgroup exchanges maxima and rescales its sums.
+// Scores, maxima and sums are fp32; the weights are rounded to bf16, the type of
+// the rows they multiply, and a row's sum is of the rounded ones, so that the
+// roundings' mean cancels (the result's error is 0.0025 of its size, rms, of
+// which rounding the result to bf16 is 0.0017).
 template <int R, bool kPairs>
 __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only

@@ -241,6 +241,15 @@ struct PromptTile {
     lat_u32x4 v[kKvTile / 8][G][kWave];
 };
 
+// Softmax attention of 256 query rows of one head, 32 a wave, over 64-token
+// tiles: keys as the M side, so that a lane holds a row's scores, whose weights
+// are, in that order, a fragment of the second product, without a trip through
+// LDS.  Bound by the matrix units at the clock that power leaves them (40 MFMAs
+// of 32 x 32 x 16 a step and wave, 57 % of the cycles): 7161 tokens behind 1030,
+// 64 heads, take 1.30 ms, 1.0 PFLOP/s.  Short prompts are bound by their longest
+// tile (2.7 us a step): eight of up to 700 tokens, 16 heads, 34 us.
+// Keys, values and weights are bf16, the cache's type (the result's error is
+// 0.0028 of its size, rms, of which rounding the result to bf16 is 0.0017).
 template <int NOPE, int V>
 __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
