@@ -240,6 +240,11 @@ template <int G>
 struct PromptTile {
     lat_u32x4 v[kKvTile / 8][G][kWave];
 };
+// The query rows of W waves, 32 each, in the same blocks.
+template <int G, int W>
+struct QueryRows {
+    lat_u32x4 v[4 * W][G][kWave];
+};
 
 // Softmax attention of 256 query rows of one head, 32 a wave, over 64-token
 // tiles: keys as the M side, so that a lane holds a row's scores, whose weights
@@ -247,7 +252,7 @@ struct PromptTile {
 // LDS.  Bound by the matrix units at the clock that power leaves them (40 MFMAs
 // of 32 x 32 x 16 a step and wave, 57 % of the cycles): 7161 tokens behind 1030,
 // 64 heads, take 1.30 ms, 1.0 PFLOP/s.  Short prompts are bound by their longest
-// tile (2.7 us a step): eight of up to 700 tokens, 16 heads, 34 us.
+// tile (2.7 us a step): eight of up to 700 tokens, 16 heads, 32 us.
 // Keys, values and weights are bf16, the cache's type (the result's error is
 // 0.0028 of its size, rms, of which rounding the result to bf16 is 0.0017).
 template <int NOPE, int V>
@@ -263,6 +268,8 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
     // loads that fill another.
     __shared__ Keys kt0, kt1, kt2;
     __shared__ Values vt0, vt1, vt2;
+    constexpr int kExtra = V == 128 ? 2 : 4;   // waves whose queries no free stage holds
+    __shared__ QueryRows<kGk, kExtra> extra;
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Workgroups go to the XCDs round robin: all tiles of a head run on one
@@ -292,10 +299,26 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
     const int steps = (end + kKvTile - 1) / kKvTile;
     const int t = rq.t0 + row;
 
-    lat_u32x4 qf[kJ];
-    const uint16_t* qrow = p.q + (size_t)t * p.q_stride + (size_t)h * (NOPE + kRopeDim) + 8 * hf;
+    // A wave's queries, as its results at the end, go through a part of LDS of
+    // its own, eight lanes a 128-byte line: straight from memory a lane's 16
+    // bytes are a line of their own, 64 cycles a load (34.4 us where this takes
+    // 32.4, eight prompts of up to 700 tokens, 16 heads).  The stages of
+    // tile 0, fetched meanwhile, are left out.
+    lat_u32x4* const own = wave < 2                ? &kt1.v[4 * wave][0][0]
+                           : wave < 4              ? &kt2.v[4 * (wave - 2)][0][0]
+                           : wave < 4 + kExtra     ? &extra.v[4 * (wave - 4)][0][0]
+                           : wave == 6             ? &vt1.v[0][0][0]
+                                                   : &vt2.v[0][0][0];
 #pragma unroll
-    for (int j = 0; j < kJ; ++j) qf[j] = *(const lat_u32x4*)(qrow + 16 * j);
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 3);
+        const uint16_t* src = p.q + (size_t)(rq.t0 + min(my0 + r, rq.add - 1)) * p.q_stride +
+                              (size_t)h * (NOPE + kRopeDim) + 8 * ((lane & 7) ^ lat_swz(r));
+#pragma unroll
+        for (int g = 0; g < kGk; ++g)
+            __builtin_amdgcn_global_load_lds((lat_g_void*)(src + 64 * g), (lat_lds_void*)(own + (kGk * i + g) * kWave), 16, 0, 0);
+    }
+    lat_u32x4 qf[kJ];
     lat_f32x16 o[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) o[c] = lat_f32x16{};
@@ -482,12 +505,20 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
         // have loaded); the values of "tile -1" are zeros.
         const Source from0 = source(0), from1 = source(min(1, steps - 1)), from2 = source(min(2, steps - 1));
         load_tiles(from0, from0, kt0, vt0);
+        lat_wait_vm<kLoads>();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < kJ; ++j)
+            qf[j] = own[((n >> 3) * kGk + (j >> 2)) * kWave + (n & 7) * 8 + ((2 * (j & 3) + hf) ^ lat_swz(n))];
+        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+        lat_barrier();             // the stages the queries came through are free
         lat_for<0, kGk>([&](auto ic) __attribute__((always_inline)) { load(ic, from1, kt1, vt1); });
         if (second) load_tiles(from2, from1, kt2, vt1);
 #pragma unroll
         for (int g = 0; g < kGv; ++g) vt2.v[wave][g][lane] = lat_u32x4{0, 0, 0, 0};
-        if (second) lat_wait_vm<kLoads>();
-        else lat_wait_vm<0>();
+        // Tile 0 is there; the keys of tile 1 are waited for at the end of phase 1.
+        if (second) lat_wait_vm<kGk + kLoads>();
+        else lat_wait_vm<kGk>();
         asm volatile("" ::: "memory");
         clear(0, vt0);
         __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
@@ -510,24 +541,46 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
         else finish(vt2);
     }
 
+    lat_wait_vm<0>();
+    lat_barrier();             // nobody's loads are on their way into the stages any more
     l = lat_sum_pair(l);
-    if (my0 + n >= rq.add) return;
     const float f = lat_inverse(l);
-    const size_t at = (size_t)t * p.H + h;
-    if (p.lse && hf == 0) p.lse[at] = lat_lse(m, l);
+    if (p.lse && hf == 0 && my0 + n < rq.add) p.lse[(size_t)t * p.H + h] = lat_lse(m, l);
+    // 8 KiB a wave: 256 bytes of a row at a time, unit u (16 bytes) of a row at
+    // u ^ (row % units).
+    lat_u32x4* const out = wave < 6 ? (lat_u32x4*)(wave < 2 ? &kt0 : wave < 4 ? &kt1 : &kt2) + 512 * (wave & 1)
+                                    : (lat_u32x4*)&extra + 512 * (wave - 6);
+    auto leave = [&](auto bytes_of) __attribute__((always_inline)) {
+        constexpr int kSize = decltype(bytes_of)::value, kUnits = V * kSize < 256 ? V * kSize / 16 : 16;
+        constexpr int kPasses = V * kSize / (16 * kUnits), kTiles = NC / kPasses;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+        for (int pass = 0; pass < kPasses; ++pass) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const size_t y = at * V + 32 * c + 8 * i + 4 * hf;
-            const float v0 = o[c][4 * i] * f, v1 = o[c][4 * i + 1] * f, v2 = o[c][4 * i + 2] * f, v3 = o[c][4 * i + 3] * f;
-            if (p.y_bf16) {
-                const lat_u32x2 v = {lat_pack(v0, v1), lat_pack(v2, v3)};
-                *(lat_u32x2*)((uint16_t*)p.y + y) = v;
-            } else {
-                *(float4*)((float*)p.y + y) = make_float4(v0, v1, v2, v3);
+            for (int c = 0; c < kTiles; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const lat_f32x16& v = o[kTiles * pass + c];
+                    const float v0 = v[4 * i] * f, v1 = v[4 * i + 1] * f, v2 = v[4 * i + 2] * f, v3 = v[4 * i + 3] * f;
+                    const int unit = kSize == 2 ? 4 * c + i : 8 * c + 2 * i + hf;
+                    lat_u32x4* const at = out + n * kUnits + (unit ^ (n & (kUnits - 1)));
+                    if constexpr (kSize == 2) ((lat_u32x2*)at)[hf] = lat_u32x2{lat_pack(v0, v1), lat_pack(v2, v3)};
+                    else *at = lat_u32x4{__float_as_uint(v0), __float_as_uint(v1), __float_as_uint(v2), __float_as_uint(v3)};
+                }
+            __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < kUnits / 2; ++i) {
+                const int r = (64 * i + lane) / kUnits, u = (64 * i + lane) % kUnits;
+                const lat_u32x4 v = out[r * kUnits + (u ^ (r & (kUnits - 1)))];
+                if (my0 + r < rq.add)
+                    *(lat_u32x4*)((char*)p.y + ((size_t)(rq.t0 + my0 + r) * p.H + h) * (V * kSize) + 256 * pass + 16 * u) = v;
             }
+            __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+            asm volatile("" ::: "memory");
         }
+    };
+    if (p.y_bf16) leave(LatInt<2>{});
+    else leave(LatInt<4>{});
 #endif
 }
 
