@@ -63,10 +63,12 @@ struct ExpandStage {
 // the next one's loads between the first half of a stage's MFMAs; workgroups
 // that run together share weight tiles by XCD (they are numbered weights
 // first) and the outputs leave through LDS, 512 bytes of a token at a time.
-// 8191 tokens of 64 heads take 185 us, 0.74 PFLOP/s: 100 us of products at the
-// rate of a large one and 55 us of writes, which a CU's one workgroup does not
-// overlap (128 x 128 tiles, two workgroups a CU, 16-byte pieces written from
-// the registers: 264 us).
+// 8191 tokens of 64 heads take 189 us, 0.73 PFLOP/s (100 us of products at the
+// rate of a large one): bound by the fetches into LDS, 173 us without the
+// products, 159 without the outputs, which pass the caches by (kept there: 201).
+// Neither 128 x 128 tiles with outputs straight from the registers (264 us) nor
+// 128 x 256 ones of half the depth, two workgroups a CU and a third stage (212)
+// are faster.
 __global__ __launch_bounds__(kExpandThreads) void k_expand(LatentParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
     const int ft = blockIdx.x;
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(kExpandThreads) void k_expand(LatentParams p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int r = kRows * (i + e) + (threadIdx.x >> 5);
-            if (s0 + r < total) *(lat_u32x4*)(dst + (size_t)r * outs) = v[e];
+            if (s0 + r < total) __builtin_nontemporal_store(v[e], (lat_u32x4*)(dst + (size_t)r * outs));
         }
     }
 #endif
