@@ -78,26 +78,11 @@ __global__ __launch_bounds__(kExpandThreads) void k_expand(LatentParams p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave & 1, wn = wave >> 1;
     const int total = p.B > 0 ? (int)min((long long)p.cu_kv[p.B], p.max_kv) : 0;
-    // Cache row of token s of all requests' tokens (for a whole wave at a time).
-    // The requests' first tokens: up to 64 in a register, one a lane (a search
-    // in memory waits for each of its steps).
-    const int lane_first = p.B <= kWave ? p.cu_kv[min(lane, p.B)] : 0;
+    // Cache row of token s of all requests' tokens.
     auto cache_row = [&](int s) {
         s = min(s, total - 1);
-        int b, first;
-        if (p.B <= kWave) {
-            b = 0;
-#pragma unroll
-            for (int d = 32; d >= 1; d >>= 1) {
-                const int f = __shfl(lane_first, min(b + d, kWave - 1));
-                if (b + d < p.B && f <= s) b += d;
-            }
-            first = __shfl(lane_first, b);
-        } else {
-            b = lat_find(p.cu_kv, p.B, s);
-            first = p.cu_kv[b];
-        }
-        return lat_slot(p, b, s - first);
+        const int b = lat_find(p.cu_kv, p.B, s);
+        return lat_slot(p, b, s - p.cu_kv[b]);
     };
     if (blockIdx.y == gridDim.y - 1) {
         if (ft == 0) prompt_tiles(p);
@@ -105,10 +90,9 @@ __global__ __launch_bounds__(kExpandThreads) void k_expand(LatentParams p) {
         // The rotary keys, 8 lanes a token.
         for (int i0 = ft * kExpandThreads; i0 < total * 8; i0 += gridDim.x * kExpandThreads) {
             const int s = (i0 + (int)threadIdx.x) >> 3, q8 = threadIdx.x & 7;
-            const size_t row = cache_row(s);
             if (s < total)
                 *(lat_u32x4*)(p.kr + (size_t)s * kRopeDim + 8 * q8) =
-                    *(const lat_u32x4*)(p.cache + row * (p.latent + kRopeDim) + p.latent + 8 * q8);
+                    *(const lat_u32x4*)(p.cache + (size_t)cache_row(s) * (p.latent + kRopeDim) + p.latent + 8 * q8);
         }
         return;
     }
@@ -275,8 +259,10 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Workgroups go to the XCDs round robin: all tiles of a head run on one
-    // XCD, whose L2 holds the head's keys and values; the last tiles, which
-    // see the most tokens, first.
+    // XCD, whose L2 holds the head's keys and values, where the heads divide
+    // evenly (64 heads, 7161 tokens behind 1030: 1312 us; in plain order, as with
+    // other numbers of heads, 1486; 16 heads, short prompts: 32 and 49); the last
+    // tiles, which see the most tokens, first.
     int h, q;
     if (p.H % kXcds == 0) {
         const int k = blockIdx.x / kXcds;
