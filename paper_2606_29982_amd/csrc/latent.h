@@ -61,7 +61,6 @@ typedef short lat_s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 lat_bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 lat_bf16x2 __attribute__((ext_vector_type(2)));
 typedef float lat_f32x2 __attribute__((ext_vector_type(2)));
-typedef float lat_f32x4 __attribute__((ext_vector_type(4)));
 typedef float lat_f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) lat_s16x4 lat_lds_s16x4;
 typedef __attribute__((address_space(3))) void lat_lds_void;
@@ -98,11 +97,6 @@ __device__ inline void lat_barrier() {
 
 __device__ inline lat_f32x16 lat_mma(const lat_u32x4& a, const lat_u32x4& b, const lat_f32x16& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(lat_bf16x8, a),
-                                                   __builtin_bit_cast(lat_bf16x8, b), c, 0, 0, 0);
-}
-
-__device__ inline lat_f32x4 lat_mma16(const lat_u32x4& a, const lat_u32x4& b, const lat_f32x4& c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(lat_bf16x8, a),
                                                    __builtin_bit_cast(lat_bf16x8, b), c, 0, 0, 0);
 }
 

@@ -159,22 +159,41 @@ __device__ inline void lds_put16(uint32_t at, const lat_u32x4& v) {
     asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(v) : "memory");
 }
 __device__ inline void lds_put4(uint32_t at, uint32_t v) { asm volatile("ds_write_b32 %0, %1" ::"v"(at), "v"(v) : "memory"); }
-__device__ inline void lds_get(uint32_t at, uint32_t flags, lat_u32x4 (&w)[4][2], lat_u32x4& f) {
+__device__ inline void lds_get(uint32_t at, lat_u32x4 (&w)[4][2]) {
+    asm volatile(
+        "ds_read_b128 %0, %8\n"
+        "ds_read_b128 %1, %8 offset:4 * 1024\n"
+        "ds_read_b128 %2, %8 offset:1 * 1024\n"
+        "ds_read_b128 %3, %8 offset:5 * 1024\n"
+        "ds_read_b128 %4, %8 offset:2 * 1024\n"
+        "ds_read_b128 %5, %8 offset:6 * 1024\n"
+        "ds_read_b128 %6, %8 offset:3 * 1024\n"
+        "ds_read_b128 %7, %8 offset:7 * 1024\n"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(w[0][0]), "=&v"(w[0][1]), "=&v"(w[1][0]), "=&v"(w[1][1]), "=&v"(w[2][0]), "=&v"(w[2][1]), "=&v"(w[3][0]),
+          "=&v"(w[3][1])
+        : "v"(at)
+        : "memory");
+}
+// The same and four flags.
+__device__ inline uint32_t lds_get(uint32_t at, uint32_t flags, lat_u32x4 (&w)[4][2]) {
+    lat_u32x4 f;
     asm volatile(
         "ds_read_b128 %0, %9\n"
-        "ds_read_b128 %1, %9 offset:4096\n"
-        "ds_read_b128 %2, %9 offset:1024\n"
-        "ds_read_b128 %3, %9 offset:5120\n"
-        "ds_read_b128 %4, %9 offset:2048\n"
-        "ds_read_b128 %5, %9 offset:6144\n"
-        "ds_read_b128 %6, %9 offset:3072\n"
-        "ds_read_b128 %7, %9 offset:7168\n"
+        "ds_read_b128 %1, %9 offset:4 * 1024\n"
+        "ds_read_b128 %2, %9 offset:1 * 1024\n"
+        "ds_read_b128 %3, %9 offset:5 * 1024\n"
+        "ds_read_b128 %4, %9 offset:2 * 1024\n"
+        "ds_read_b128 %5, %9 offset:6 * 1024\n"
+        "ds_read_b128 %6, %9 offset:3 * 1024\n"
+        "ds_read_b128 %7, %9 offset:7 * 1024\n"
         "ds_read_b128 %8, %10\n"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(w[0][0]), "=&v"(w[0][1]), "=&v"(w[1][0]), "=&v"(w[1][1]), "=&v"(w[2][0]), "=&v"(w[2][1]), "=&v"(w[3][0]),
           "=&v"(w[3][1]), "=&v"(f)
         : "v"(at), "v"(flags)
         : "memory");
+    return f[0] | f[1] | f[2] | f[3];
 }
 
 // A workgroup holds 64 query rows and walks over the tiles of its share.
@@ -466,15 +485,14 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
                     lds_put16(pw_at + ((rg * 4 + 2 * th + k) * kWave + lane) * 16, w);
                 }
             };
-            lat_u32x4 bw[4][2], ov;
+            lat_u32x4 bw[4][2];
             bool moves = s == 0;
             if (!moves) {
                 weights();
                 const bool over_it = __any(big > kMaxWeight);
                 if (lane == 0) lds_put4(over_at + 4 * wave, over_it);
                 lds_barrier();
-                lds_get(pw_at + 16 * lane, over_at, bw, ov);
-                moves = __builtin_amdgcn_readfirstlane(ov[0] | ov[1] | ov[2] | ov[3]);
+                moves = __builtin_amdgcn_readfirstlane(lds_get(pw_at + 16 * lane, over_at, bw));
             }
             if (moves) {
                 // Some maxima move (all do in the first step): they and the factors go round.
@@ -491,7 +509,7 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
                 if (th == 0 && hf == 0) sf[32 * rg + n] = f;
                 weights();
                 lds_barrier();
-                lds_get(pw_at + 16 * lane, over_at, bw, ov);
+                lds_get(pw_at + 16 * lane, bw);
                 if (s > 0) {
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {

@@ -154,3 +154,14 @@ def test_in_a_graph_on_another_stream():
         caee.block_matmul(x, w, ws, y, wsp)
         torch.cuda.synchronize()
         assert torch.equal(got, y) and float(y.float().abs().sum()) > 0
+
+
+@pytest.mark.parametrize("M,N,K,tiled", [(300, 3000, 384, False), (700, 1040, 1152, True), (1200, 701, 512, False),
+                                         (130, 4096, 896, True), (65, 8200, 384, False)])
+@pytest.mark.parametrize("x_dtype,y_dtype", [("bf16", "bf16"), ("e4m3", "f32")])
+def test_middle(M, N, K, tiled, x_dtype, y_dtype):
+    _run(M, N, K, x_dtype, y_dtype, tiled=tiled)
+
+
+def test_past_four_rounds_of_tiles():
+    _run(2100, 2064, 2048, tiled=True)

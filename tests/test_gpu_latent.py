@@ -182,3 +182,24 @@ def test_forms_agree_on_another_stream():
         a, e = c.run(DEV, "absorbed"), c.run(DEV, "expanded")
     d = np.linalg.norm(a[0] - e[0]) / np.linalg.norm(e[0])
     assert d <= 2 * TOL_ALL
+
+
+@pytest.mark.parametrize("heads,seq,block", [(128, 20000, 100), (8, 60000, 3), (64, 40000, 12)])
+def test_long_context_in_pages_that_end_inside_eight_rows(heads, seq, block):
+    """Several tiles a workgroup, whose rows come page by page."""
+    _check("absorbed", seq=[seq, 70], new=[1, 1], H=heads, block=block, seed=block)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("B", [63, 64, 65, 200])
+def test_numbers_of_requests(B, form):
+    rng = np.random.default_rng(B)
+    seq = rng.integers(0, 90, B)
+    new = np.minimum(rng.integers(0, 4, B), seq)
+    _check(form, seq=list(seq), new=list(new), H=5, block=16, seed=B)
+
+
+def test_few_and_many_rows_of_split_requests():
+    """Partial results of a request joined by one wave a row and by four."""
+    for heads, new, seq in ((128, 20, 3000), (16, 4, 9000)):
+        _check("absorbed", seq=[seq, 500], new=[new, 1], H=heads, block=32, seed=new)
