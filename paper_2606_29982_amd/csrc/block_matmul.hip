@@ -163,7 +163,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_bm_split(BmParams p) {
     const float* xs[T];
 #pragma unroll
     for (int e = 0; e < T; ++e) xs[e] = p.xs + (size_t)min(m0 + 32 * e + n, p.M - 1) * p.kb;
-    const float* wsc = p.ws + (size_t)(n0 >> 7) * p.kb;
+    // (an address of the lane's own, so that this is a vector load and counts as one)
+    int zero_lane = 0;
+    asm volatile("" : "+v"(zero_lane));
+    const float* wsc = p.ws + (size_t)(n0 >> 7) * p.kb + zero_lane;
     const int wstep = bm_block(p);
     // A fragment's pieces 2 q + hf of row n: at xat ^ 2 q and wat ^ wq q.
     const int xat = (n >> 3) * kWave + 8 * (n & 7) + (hf ^ bm_swz(n));
