@@ -463,7 +463,7 @@ typedef struct caee_latent_desc {
     int32_t causal;       /* 1: new token i of a request sees its first seq_len - new + i + 1 tokens; 0: all seq_len */
     int32_t form;         /* caee_latent_form_t */
     int32_t y_dtype;      /* CAEE_BF16 or CAEE_F32 */
-    int64_t max_kv;       /* sum of seq_len at most */
+    int64_t max_kv;       /* sum of seq_len at most, <= 2^30 */
     int64_t q_stride;     /* elements from one token of q to the next, a multiple of 8, >= heads * (nope + rope) */
     float scale;          /* factor on the scores, finite and > 0 */
 } caee_latent_desc_t;
@@ -494,7 +494,8 @@ caee_status_t caee_latent_workspace_size(const caee_latent_desc_t* desc, size_t*
  * their products.
  * Preconditions on device contents (violations: unspecified results,
  * memory-safe): page numbers in [0, n_blocks) for the pages seq_len covers,
- * at most max_new new tokens per request and max_kv tokens in all. */
+ * at most max_new new tokens per request and max_kv tokens in all (what a
+ * request has past either is left out). */
 caee_status_t caee_latent_attention(const caee_latent_desc_t* desc, const void* q,
                                     const caee_latent_weights_t* weights, const void* cache,
                                     const int32_t* block_table, const int32_t* cu_new, const int32_t* cu_kv,

@@ -174,7 +174,8 @@ __device__ inline uint32_t lat_slot(const LatentParams& p, int b, int pos) {
 }
 
 // New tokens and length of request b as the kernels use them: 0 <= new <=
-// max_new, rows within [0, T).
+// max_new, rows within [0, T), 0 <= seq <= max_kv (the host's bounds size the
+// workspace and the counters, so lengths past them are cut).
 struct LatentReq {
     int t0, add, seq;
 };
@@ -183,7 +184,7 @@ __device__ inline LatentReq lat_req(const LatentParams& p, int b) {
     const int a = p.cu_new[b], e = p.cu_new[b + 1];
     r.t0 = min(max(a, 0), p.T);
     r.add = min(max(min(e, p.T) - r.t0, 0), p.max_new);
-    r.seq = max(p.seq_len[b], 0);
+    r.seq = min(max(p.seq_len[b], 0), (int)p.max_kv);
     return r;
 }
 

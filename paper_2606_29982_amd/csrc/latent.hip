@@ -78,8 +78,8 @@ caee_status_t check_latent(const caee_latent_desc_t* d) {
     if (d->heads > 1024 || d->B > 65536 || d->T > (1 << 20))
         return fail(CAEE_ERR_UNSUPPORTED, "heads=%d, B=%d or T=%d exceeds 1024, 65536 or %d", d->heads, d->B, d->T,
                     1 << 20);
-    if ((long long)d->n_blocks * d->block_size > INT32_MAX || d->max_kv > INT32_MAX)
-        return fail(CAEE_ERR_UNSUPPORTED, "a cache of %lld rows, or %lld tokens in all, exceeds 2^31 - 1",
+    if ((long long)d->n_blocks * d->block_size > INT32_MAX || d->max_kv > (1 << 30))
+        return fail(CAEE_ERR_UNSUPPORTED, "a cache of %lld rows exceeds 2^31 - 1, or %lld tokens in all 2^30",
                     (long long)d->n_blocks * d->block_size, (long long)d->max_kv);
     if (latent_expanded(*d) && d->max_kv > 65534 * 256)
         return fail(CAEE_ERR_UNSUPPORTED, "the expanded form takes at most %d tokens in all, not max_kv=%lld", 65534 * 256,

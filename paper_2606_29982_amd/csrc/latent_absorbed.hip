@@ -53,6 +53,11 @@ __device__ inline void lds_barrier() {
     lat_barrier();
 }
 
+// Units are counted up to this; no request has more (a limit of the host's,
+// as is that of all requests while their lengths add up to max_kv at most).
+constexpr int kMaxUnits = INT32_MAX / 2;
+__device__ inline int add_units(int a, int b) { return min(a + b, kMaxUnits); }
+
 // First unit of each request's row tiles (meta[b]; meta[B] the total).
 __device__ void absorbed_shares(const LatentParams& p, int rows) {
     __shared__ int part[kAbsThreads];
@@ -64,19 +69,19 @@ __device__ void absorbed_shares(const LatentParams& p, int rows) {
         return ((r.add * p.H + rows - 1) / rows) * ((r.seq + kUnit - 1) / kUnit);
     };
     int n = 0;
-    for (int b = b0; b < b1; ++b) n += units(b);
+    for (int b = b0; b < b1; ++b) n = add_units(n, units(b));
     part[tid] = n;
     __syncthreads();
     for (int d = 1; d < kAbsThreads; d <<= 1) {
         const int u = tid >= d ? part[tid - d] : 0;
         __syncthreads();
-        part[tid] += u;
+        part[tid] = add_units(part[tid], u);
         __syncthreads();
     }
-    int at = part[tid] - n;
+    int at = tid > 0 ? part[tid - 1] : 0;
     for (int b = b0; b < b1; ++b) {
         p.meta[b] = at;
-        at += units(b);
+        at = add_units(at, units(b));
     }
     if (tid == kAbsThreads - 1) p.meta[p.B] = part[kAbsThreads - 1];
 }
@@ -645,8 +650,9 @@ __global__ __launch_bounds__(kAbsThreads) void k_join(LatentParams p) {
         if (!none) {
             per = abs_share<kPairs>(p.meta[p.B]);
             a = p.meta[b] + (kPairs ? rt >> 1 : rt) * n_u;
-            g0 = a / per;
-            g1 = (a + n_u - 1) / per;
+            constexpr int kLast = (kPairs ? kAbsGroups / 2 : kAbsGroups) - 1;
+            g0 = min((int)((unsigned)a / (unsigned)per), kLast);
+            g1 = min((int)((unsigned)(a + n_u - 1) / (unsigned)per), kLast);
         }
     }
     if (none) {

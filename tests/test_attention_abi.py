@@ -76,6 +76,13 @@ def test_latent_descriptor(kw, status):
         assert caee.lib.caee_last_error().decode()
 
 
+def test_latent_tokens_in_all_are_bounded():
+    for form in (1, 2):
+        for kv in ((1 << 30) + 1, (1 << 31) - 1):
+            assert _latent_ws(_latent_desc(max_kv=kv, form=form))[0] == LIMIT
+    assert _latent_ws(_latent_desc(max_kv=1 << 30, form=1))[0] == OK
+
+
 def test_latent_workspace_grows_with_the_call():
     for form in (1, 2):
         a, b = (_latent_ws(_latent_desc(form=form, T=t, max_kv=kv, max_new=t))[1] for t, kv in ((4, 1000), (8, 4000)))

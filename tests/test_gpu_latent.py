@@ -203,3 +203,26 @@ def test_few_and_many_rows_of_split_requests():
     """Partial results of a request joined by one wave a row and by four."""
     for heads, new, seq in ((128, 20, 3000), (16, 4, 9000)):
         _check("absorbed", seq=[seq, 500], new=[new, 1], H=heads, block=32, seed=new)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_lengths_past_the_hosts_bound_are_cut(form):
+    """Device lengths above max_kv: with max_kv = 0 no row sees a token, with one request's length it alone counts."""
+    c = LatentCase(seq=[90, 40], new=[2, 3], H=4, seed=23)
+    att = caee.Latent(heads=4, nope=128, rope=64, latent=512, v=128, scale=c.scale, form=form)
+    to = lambda a, dt=None: torch.as_tensor(a).to(DEV, dt)  # noqa: E731
+    plan = dict(cu_new=to(c.cu_new, torch.int32), cu_kv=to(c.cu_kv, torch.int32), seq_len=to(c.seq, torch.int32))
+    w = caee.pack_latent_weights(to(c.w_uk), to(c.w_uv))
+    for kv in (0, 90):
+        y = torch.full((c.T + 2, 4, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+        lse = torch.full((c.T + 2, 4), 7.0, device=DEV)
+        ws = caee.alloc_latent_workspace(att, c.T, 2, 3, kv, DEV)
+        caee.latent_attention(att, to(c.q), w, to(c.cache), to(c.table), plan, y[1:-1], ws, max_new=3, max_kv=kv,
+                              lse=lse[1:-1])
+        torch.cuda.synchronize()
+        assert torch.all(y[0] == 7.0) and torch.all(y[-1] == 7.0) and torch.all(lse[0] == 7.0) and torch.all(lse[-1] == 7.0)
+        if kv == 0:
+            assert torch.all(y[1:-1] == 0.0) and torch.all(torch.isneginf(lse[1:-1]))
+        else:
+            ry, rl = c.ref()
+            check_attention((y[1:3].double().cpu().numpy(), lse[1:3].cpu().numpy()), (ry[:2], rl[:2]))
