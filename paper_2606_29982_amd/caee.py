@@ -360,10 +360,15 @@ def moe_layer_noalloc(layer: Layer, x, logits, bias, cost, bins, weights: dict, 
 # ---------------------------------------------------------------------------
 # The attention block in front of the layer.
 
+_CODES: dict = {}          # torch dtype -> caee_dtype_t, made by the first call
+
+
 def _code(t) -> int:
-    import torch
-    code = {torch.bfloat16: CAEE_BF16, torch.float32: CAEE_F32, torch.uint8: CAEE_FP8_E4M3,
-            torch.float8_e4m3fn: CAEE_FP8_E4M3}.get(t.dtype)
+    if not _CODES:
+        import torch
+        _CODES.update({torch.bfloat16: CAEE_BF16, torch.float32: CAEE_F32, torch.uint8: CAEE_FP8_E4M3,
+                       torch.float8_e4m3fn: CAEE_FP8_E4M3})
+    code = _CODES.get(t.dtype)
     if code is None:
         raise TypeError(f"tensor of dtype {t.dtype}: bfloat16, float32 or e4m3 codes (uint8, float8_e4m3fn) are taken")
     return code
@@ -380,6 +385,14 @@ def _need(t, name: str, dtype=None, shape=None, dense: bool = True):
     if dense and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t
+
+
+def _at(t, name: str, dtype, shape) -> int:
+    """Address of a dense device tensor, checked as by ``_need`` (one expression where all is well: a call of a dozen
+    tensors is bound by these checks)."""
+    if t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    return _need(t, name, dtype, shape).data_ptr()
 
 
 def alloc_paged_plan(B: int, T: int, device) -> dict:
@@ -399,25 +412,22 @@ def paged_plan(block_size: int, ctx_len, new_len, block_table, free_list, free_h
     made by ``alloc_paged_plan`` (its ``free_head`` is the next call's input)."""
     import torch
     B, T = ctx_len.shape[0], out["slots"].shape[0]
-    i32 = torch.int32
-    _need(ctx_len, "ctx_len", i32)
-    _need(new_len, "new_len", i32, (B,))
-    if _need(block_table, "block_table", i32).dim() != 2 or block_table.shape[0] != B:
+    i32, per_request, per_token, one = torch.int32, (B,), (T,), (1,)
+    if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError(f"block_table must be [{B}][max_blocks]")
-    _need(free_list, "free_list", i32)
-    _need(free_head, "free_head", i32, (1,))
-    at = []
-    for name, shape, optional in (("cu_new", (B + 1,), False), ("cu_kv", (B + 1,), False), ("seq_len", (B,), False),
-                                  ("slots", (T,), False), ("position", (T,), True), ("request", (T,), True),
-                                  ("free_head", (1,), False), ("lacking", (1,), False)):
-        t = out.get(name) if optional else out[name]
-        if t is not None:
-            _need(t, name, torch.int64 if name == "slots" else i32, shape)
-        at.append(_ptr(t))
-    o = PagedPlanOut(*at)
-    _check(lib.caee_paged_plan(B, T, block_size, block_table.shape[1], _ptr(ctx_len), _ptr(new_len), _ptr(block_table),
-                               _ptr(free_list), free_list.shape[0], _ptr(free_head), ctypes.byref(o),
-                               _stream(free_head)))
+    width, n_free = block_table.shape[1], free_list.shape[0]
+    position, request = out.get("position"), out.get("request")
+    o = PagedPlanOut(_at(out["cu_new"], "cu_new", i32, (B + 1,)), _at(out["cu_kv"], "cu_kv", i32, (B + 1,)),
+                     _at(out["seq_len"], "seq_len", i32, per_request),
+                     _at(out["slots"], "slots", torch.int64, per_token),
+                     None if position is None else _at(position, "position", i32, per_token),
+                     None if request is None else _at(request, "request", i32, per_token),
+                     _at(out["free_head"], "free_head", i32, one), _at(out["lacking"], "lacking", i32, one))
+    _check(lib.caee_paged_plan(B, T, block_size, width, _at(ctx_len, "ctx_len", i32, per_request),
+                               _at(new_len, "new_len", i32, per_request),
+                               _at(block_table, "block_table", i32, (B, width)),
+                               _at(free_list, "free_list", i32, (n_free,)), n_free,
+                               _at(free_head, "free_head", i32, one), ctypes.byref(o), _stream(free_head)))
     return out
 
 
@@ -425,23 +435,23 @@ def _rows(t, name: str):
     """A 2-D tensor whose rows are dense; its row stride."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (shape[1] > 1 and stride[1] != 1):
         raise ValueError(f"{name} must be 2-D with dense rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return stride[0] if shape[0] > 1 else max(stride[0], shape[1])
 
 
 def latent_store(c, r, slots, cache):
     """Rows [c_t | r_t] of T tokens into ``cache`` [n_blocks][block_size][latent + rope] bf16 at ``slots`` [T] int64
     (caee_latent_store).  ``c`` [T][latent] and ``r`` [T][rope], bf16 or f32, may be slices of wider rows."""
     import torch
-    T = c.shape[0]
     cs, rs = _rows(c, "c"), _rows(r, "r")
-    _need(cache, "cache", torch.bfloat16)
-    _need(slots, "slots", torch.int64, (T,))
-    if c.dtype != r.dtype or r.shape[0] != T or cache.dim() != 3 or cache.shape[2] != c.shape[1] + r.shape[1]:
+    (T, latent), (Tr, rope), pages = c.shape, r.shape, cache.shape
+    if c.dtype != r.dtype or Tr != T or len(pages) != 3 or pages[2] != latent + rope:
         raise ValueError("c, r and cache do not fit together")
-    _check(lib.caee_latent_store(T, c.shape[1], r.shape[1], _code(c), _ptr(c), cs, _ptr(r), rs, _ptr(slots),
-                                 _ptr(cache), cache.shape[0] * cache.shape[1], _stream(cache)))
+    _check(lib.caee_latent_store(T, latent, rope, _code(c), c.data_ptr(), cs, r.data_ptr(), rs,
+                                 _at(slots, "slots", torch.int64, (T,)), _at(cache, "cache", torch.bfloat16, pages),
+                                 pages[0] * pages[1], _stream(cache)))
     return cache
 
 
