@@ -106,6 +106,11 @@ __device__ inline uint32_t lat_pack(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(t, lat_bf16x2));
 }
 
+// What rounding a and b to the bf16 pair v left.
+__device__ inline lat_f32x2 lat_rest(uint32_t v, float a, float b) {
+    return lat_f32x2{a - __uint_as_float(v << 16), b - __uint_as_float(v & 0xFFFF0000u)};
+}
+
 // sum + both bf16 values of v.
 __device__ inline float lat_sum2(uint32_t v, float sum) {
     const lat_bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};

@@ -180,6 +180,36 @@ __device__ inline void lds_get(uint32_t at, lat_u32x4 (&w)[4][2]) {
         : "v"(at)
         : "memory");
 }
+__device__ inline void lds_put8(uint32_t at, const lat_u32x2& v) {
+    asm volatile("ds_write_b64 %0, %1" ::"v"(at), "v"(v) : "memory");
+}
+__device__ inline void lds_get(uint32_t at, lat_u32x2 (&w)[4][2]) {
+    asm volatile(
+        "ds_read_b64 %0, %8\n"
+        "ds_read_b64 %1, %8 offset:4 * 512\n"
+        "ds_read_b64 %2, %8 offset:1 * 512\n"
+        "ds_read_b64 %3, %8 offset:5 * 512\n"
+        "ds_read_b64 %4, %8 offset:2 * 512\n"
+        "ds_read_b64 %5, %8 offset:6 * 512\n"
+        "ds_read_b64 %6, %8 offset:3 * 512\n"
+        "ds_read_b64 %7, %8 offset:7 * 512\n"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(w[0][0]), "=&v"(w[0][1]), "=&v"(w[1][0]), "=&v"(w[1][1]), "=&v"(w[2][0]), "=&v"(w[2][1]), "=&v"(w[3][0]),
+          "=&v"(w[3][1])
+        : "v"(at)
+        : "memory");
+}
+// Weights' remainders in 8 bits (e5m2, times 2^10: at most 2^10 for weights of
+// up to kMaxWeight) and back as bf16.
+constexpr float kRestScale = 1024.0f;
+__device__ inline lat_u32x4 abs_rest(const lat_u32x2& v) {
+    lat_u32x4 w;
+    w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(v[0], 1.0f / kRestScale, false));
+    w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(v[0], 1.0f / kRestScale, true));
+    w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(v[1], 1.0f / kRestScale, false));
+    w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(v[1], 1.0f / kRestScale, true));
+    return w;
+}
 // The same and four flags.
 __device__ inline uint32_t lds_get(uint32_t at, uint32_t flags, lat_u32x4 (&w)[4][2]) {
     lat_u32x4 f;
@@ -228,11 +258,13 @@ __device__ inline uint32_t lds_get(uint32_t at, uint32_t flags, lat_u32x4 (&w)[4
 // for the five where it was 137; for the 64 users' it changes nothing.
 // A row's running maximum moves only when a weight exceeds 2^kMaxSlack; then
 // the workgroup exchanges maxima and rescales its sums.
-// Scores, maxima and sums are fp32; the weights are rounded to bf16, the type of
-// the rows they multiply, and a row's sum is of the rounded ones, so that the
-// roundings' mean cancels (the result's error is 0.0025 of its size, rms, of
-// which rounding the result to bf16 is 0.0017).
-template <int R, bool kPairs>
+// Scores, maxima and sums are fp32.  The weights are rounded to bf16, the type of
+// the rows they multiply.  With kRest what the rounding left, in 8 bits, is
+// multiplied too; without, a row's sum is of the rounded weights, so that the
+// roundings' mean cancels.  (The result's error, rms, with and without: 0.0022
+// and 0.0026 of its size for 64 users, of which rounding it to bf16 is 0.0017;
+// both 0.0024 for the five.)
+template <int R, bool kPairs, bool kRest>
 __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
     constexpr int kG = AbsHalf<R>::kGroups;
@@ -245,6 +277,7 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
     // one from the loads that fill another.
     __shared__ AbsHalf<R> st0a, st0b, st1a, st1b;
     __shared__ lat_u32x4 pw[2][4][kWave];      // softmax weights: [row group][16 tokens][fragment]
+    __shared__ lat_u32x2 pr[kRest ? 2 : 1][4][kRest ? kWave : 1];      // their remainders
     __shared__ float sm[2][kAbsRows], sf[kAbsRows];
     __shared__ int over[4];
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
@@ -258,6 +291,7 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
     }
     const AbsShare sh = abs_share_of<kPairs>(p.meta[p.B], blockIdx.x);
     const uint32_t pw_at = (uint32_t)(uintptr_t)(lat_lds_void*)&pw[0][0][0], over_at = (uint32_t)(uintptr_t)(lat_lds_void*)&over[0];
+    [[maybe_unused]] const uint32_t pr_at = (uint32_t)(uintptr_t)(lat_lds_void*)&pr[0][0][0];
     // Fragment places in a half.  Keys: row n, piece 2 j + hf.  Transposed
     // values: rows 16 ks + 8 e + 4 hf + (0 .. 3), four 16-byte pieces per 32
     // components.
@@ -479,15 +513,24 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     lat_u32x4 w;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    [[maybe_unused]] int rest[2] = {0, 0};
+                    lat_for<0, 4>([&](auto ic) __attribute__((always_inline)) {
+                        constexpr int i = decltype(ic)::value;
                         const float a = __builtin_amdgcn_exp2f(fmaf(sc[8 * k + 2 * i], p.scale_log2, -m));
                         const float e = __builtin_amdgcn_exp2f(fmaf(sc[8 * k + 2 * i + 1], p.scale_log2, -m));
                         big = fmaxf(fmaxf(big, a), e);
                         w[i] = lat_pack(a, e);
-                        more = lat_sum2(w[i], more);
-                    }
-                    lds_put16(pw_at + ((rg * 4 + 2 * th + k) * kWave + lane) * 16, w);
+                        if constexpr (kRest) {
+                            const lat_f32x2 r = lat_rest(w[i], a, e);
+                            rest[i / 2] = __builtin_amdgcn_cvt_pk_bf8_f32(r[0] * kRestScale, r[1] * kRestScale, rest[i / 2], i & 1);
+                            more += a + e;
+                        } else {
+                            more = lat_sum2(w[i], more);
+                        }
+                    });
+                    const int at = (rg * 4 + 2 * th + k) * kWave + lane;
+                    lds_put16(pw_at + at * 16, w);
+                    if constexpr (kRest) lds_put8(pr_at + at * 8, lat_u32x2{(uint32_t)rest[0], (uint32_t)rest[1]});
                 }
             };
             lat_u32x4 bw[4][2];
@@ -529,6 +572,8 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
                     }
                 }
             }
+            [[maybe_unused]] lat_u32x2 br[4][2];
+            if constexpr (kRest) lds_get(pr_at + 8 * lane, br);
             l += more;
             if (masked) {
                 // Rows that some queries do not see may hold anything: their
@@ -552,11 +597,20 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
             const bool more_a = s + 2 < steps;
             const __amdgpu_buffer_rsrc_t buf_a = page_buf(next_a.page, more_a && next_a.one);
             const uint32_t at_a = offset(next_a);
+            [[maybe_unused]] lat_u32x4 rest[2];
             lat_for<0, kF>([&](auto ic) __attribute__((always_inline)) {
                 constexpr int i = decltype(ic)::value;
+                if constexpr (kRest && i % NC == 0) {
+                    rest[0] = abs_rest(br[i / NC][0]);
+                    rest[1] = abs_rest(br[i / NC][1]);
+                }
                 if constexpr (i == kF / 2) lat_barrier();      // nobody reads the first half any more
                 o[i % NC][0] = lat_mma(vf[i % kVAhead], bw[i / NC][0], o[i % NC][0]);
                 o[i % NC][1] = lat_mma(vf[i % kVAhead], bw[i / NC][1], o[i % NC][1]);
+                if constexpr (kRest) {
+                    o[i % NC][0] = lat_mma(vf[i % kVAhead], rest[0], o[i % NC][0]);
+                    o[i % NC][1] = lat_mma(vf[i % kVAhead], rest[1], o[i % NC][1]);
+                }
                 if constexpr (i + kVAhead < kF) vf[i % kVAhead] = value(i + kVAhead);
                 if constexpr (i >= kF / 2) {
                     constexpr int n0 = (i - kF / 2) * kG / (kF / 2), n1 = (i + 1 - kF / 2) * kG / (kF / 2);
@@ -797,13 +851,21 @@ __global__ __launch_bounds__(R) void k_unabsorb(LatentParams p) {
     }
 }
 
+// Tokens per request up to which the weights' remainders are multiplied too:
+// rounding errors weigh most where few rows share a sum, over long contexts
+// they average out (error of the result with and without, and time: 901 tokens
+// 0.0022 and 0.0026, 24.3 and 23.5 us; 64 requests of 2048 on average 0.0022 and
+// 0.0026, 114 and 104 us; five of 120011 0.0024 both, 161 and 139 us).
+constexpr long long kRestTokens = 16384;
+
 template <bool kPairs>
 void attend_on(const LatentParams& p, hipStream_t s) {
     const long long rows = (long long)p.T * p.H;
     const dim3 grid(kAbsGroups), block(kAbsThreads);
     auto run = [&](auto latent) {
         constexpr int R = decltype(latent)::value;
-        hipLaunchKernelGGL((k_attend<R, kPairs>), grid, block, 0, s, p);
+        if (p.max_kv <= kRestTokens * p.B) hipLaunchKernelGGL((k_attend<R, kPairs, true>), grid, block, 0, s, p);
+        else hipLaunchKernelGGL((k_attend<R, kPairs, false>), grid, block, 0, s, p);
         if (rows < kJoinRows) hipLaunchKernelGGL((k_join<R, kPairs, 4>), dim3((unsigned)rows), block, 0, s, p);
         else hipLaunchKernelGGL((k_join<R, kPairs, 1>), dim3((unsigned)((rows + 3) / 4)), block, 0, s, p);
         hipLaunchKernelGGL(k_unabsorb<R>, dim3(p.H, (p.T + 31) / 32, p.v / 64), dim3(R), 0, s, p);

@@ -226,3 +226,18 @@ def test_lengths_past_the_hosts_bound_are_cut(form):
         else:
             ry, rl = c.ref()
             check_attention((y[1:3].double().cpu().numpy(), lse[1:3].cpu().numpy()), (ry[:2], rl[:2]))
+
+
+@pytest.mark.parametrize("heads,new", [(16, 1), (128, 1), (64, 2)])
+def test_one_request_of_forty_thousand_tokens(heads, new):
+    """Weights rounded to bf16 only, whole pages, one row tile and pairs of them."""
+    _check("absorbed", seq=[40000], new=[new], H=heads, block=64, seed=heads)
+
+
+def test_weights_of_short_contexts_keep_their_remainders():
+    """Without a cached query's rounding (no nope part) and in float32 the result's error is the weights' alone: the
+    remainder's 8 bits leave at most 2^-3 of a rounding to bf16, whose 2^-9 the plain weights would show."""
+    c = LatentCase(seq=[700, 90], new=[1, 2], H=8, seed=24)
+    c.q[..., :128] = 0
+    (y, _), (ry, _) = c.run(DEV, "absorbed", y_dtype=torch.float32), c.ref()
+    assert np.linalg.norm(y - ry) <= 2.0 ** -12 * np.linalg.norm(ry)
