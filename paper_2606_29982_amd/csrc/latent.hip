@@ -11,7 +11,8 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // The expanded form pays for every cached token once, the absorbed one 3.4
 // times as much per pair of tokens, so the new tokens per request decide.
-// Absorbed and expanded, us, 128 heads: 8 requests behind 8000 tokens with 64
+// Absorbed (its weights plain bf16, a tenth less than with their remainders)
+// and expanded, us, 128 heads: 8 requests behind 8000 tokens with 64
 // new ones each 1359 and 3899, with 256 5788 and 4237; behind 1000 with 64 414
 // and 566, with 128 813 and 619; one request behind 8000 with 128 356 and 576,
 // with 256 685 and 595.  Without a cached prefix the expanded form is ahead

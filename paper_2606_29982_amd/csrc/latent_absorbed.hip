@@ -24,7 +24,7 @@ constexpr int kUnit = 64;                // tokens of a tile, the unit shares ar
 // A workgroup's share of the units.  With pairs, two workgroups of one XCD
 // (neighbours in its launch order) take the two row tiles of the same
 // tokens, so that the second reads them from the L2 the first filled (64 users
-// of 128 heads: 72 us for k_attend, 79 without).
+// of 128 heads: 72 us for k_attend, 79 without; both of plain bf16 weights).
 struct AbsShare {
     int u0, u1, member;
 };
@@ -247,7 +247,8 @@ __device__ inline uint32_t lds_get(uint32_t at, uint32_t flags, lat_u32x4 (&w)[4
 // fetch each row half as often, but their 256 registers a wave leave room for
 // half the contraction only and cost one more exchange: 106 us for 64 users
 // of 128 heads and 2048 tokens on average, 195 us for five of 120011 tokens
-// and 64 rows; this takes 72 and 121.)
+// and 64 rows; this takes 72 and 121.  These and the figures below are of
+// plain bf16 weights; with kRest the 64 users take 81.)
 // It is bound by the fetches (5.7 TB/s for the five; the 64 users' rows go to
 // two workgroups each, by way of an L2).  A CU takes 16 cycles for each load, so
 // they go out between the MFMAs: the second half of the next tile beside the
