@@ -400,7 +400,7 @@ typedef struct caee_paged_plan_out {
     int64_t* slots;      /* [T] cache slot of each new token; -1 past the last one and where no page is */
     int32_t* position;   /* [T] position of each new token in its request, -1 past the last one (optional) */
     int32_t* request;    /* [T] request of each new token, -1 past the last one (optional) */
-    int32_t* free_head;  /* [1] free_head + pages taken; must not be the input free_head */
+    int32_t* free_head;  /* [1] free_head + pages taken */
     int32_t* lacking;    /* [1] pages that were needed and not given */
 } caee_paged_plan_out_t;
 
@@ -414,7 +414,9 @@ typedef struct caee_paged_plan_out {
  * a step can be padded to a fixed size.  Where the free list ends (or a
  * row of the table), entries are -1 (not written), their tokens' slots -1 and
  * `lacking` counts the pages.  Nothing else is changed: a call with the same
- * inputs writes the same outputs.  Negative lengths count as 0, and the sums
+ * inputs writes the same outputs.  An array that the call writes may not
+ * overlap any other one (refused): lengths kept from step to step alternate
+ * between two buffers, as the free head does.  Negative lengths count as 0, and the sums
  * of lengths must fit an int32.  Device lengths stay on the device: the call
  * can be captured in a graph.  B in [0, 65536], T >= 0, block_size in
  * [1, 65536]. */

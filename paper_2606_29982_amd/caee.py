@@ -409,7 +409,8 @@ def paged_plan(block_size: int, ctx_len, new_len, block_table, free_list, free_h
 
     ``ctx_len``/``new_len`` [B] int32: tokens each request has in the cache and receives; ``block_table``
     [B][max_blocks] int32, updated in place; ``free_list`` int32 pages, used from ``free_head[0]`` on; ``out`` as
-    made by ``alloc_paged_plan`` (its ``free_head`` is the next call's input)."""
+    made by ``alloc_paged_plan`` (its ``seq_len`` and ``free_head`` are the next call's inputs, whose ``out`` is then
+    another one: no output may overlap an input)."""
     import torch
     B, T = ctx_len.shape[0], out["slots"].shape[0]
     i32, per_request, per_token, one = torch.int32, (B,), (T,), (1,)

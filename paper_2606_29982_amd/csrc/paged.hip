@@ -205,6 +205,34 @@ __global__ __launch_bounds__(256) void k_latent_store(StoreParams p) {
     }
 }
 
+// Workgroups read lengths, pages and the head while others write, in any
+// order: an array that the plan writes may share no byte with another one.
+caee_status_t check_plan_apart(const PlanParams& p) {
+    struct Span {
+        const char* name;
+        const void* at;
+        size_t bytes;
+    };
+    const size_t b = (size_t)p.B * 4, t = (size_t)p.T;
+    const Span written[] = {{"block_table", p.table, b * (size_t)p.max_blocks}, {"out->cu_new", p.o.cu_new, b + 4},
+                            {"out->cu_kv", p.o.cu_kv, b + 4},   {"out->seq_len", p.o.seq_len, b},
+                            {"out->slots", p.o.slots, 8 * t},   {"out->position", p.o.position, 4 * t},
+                            {"out->request", p.o.request, 4 * t}, {"out->free_head", p.o.free_head, 4},
+                            {"out->lacking", p.o.lacking, 4}};
+    const Span read[] = {{"ctx_len", p.ctx_len, b}, {"new_len", p.new_len, b},
+                         {"free_list", p.free_list, (size_t)p.n_free * 4}, {"free_head", p.free_head, 4}};
+    auto check = [](const Span& u, const Span& v) {
+        const uintptr_t a = (uintptr_t)u.at, c = (uintptr_t)v.at;
+        if (!u.at || !v.at || !u.bytes || !v.bytes || (a < c ? c - a >= u.bytes : a - c >= v.bytes)) return CAEE_OK;
+        return fail(CAEE_ERR_INVALID_ARG, "%s overlaps %s", u.name, v.name);
+    };
+    for (const Span& w : written) {
+        for (const Span& r : read) CAEE_TRY(check(w, r));
+        for (const Span* other = written; other != &w; ++other) CAEE_TRY(check(w, *other));
+    }
+    return CAEE_OK;
+}
+
 }  // namespace
 }  // namespace caee
 
@@ -235,12 +263,11 @@ caee_status_t caee_paged_plan(int32_t B, int32_t T, int32_t block_size, int32_t 
     CAEE_TRY(check_ptr(out->request, "out->request", false));
     CAEE_TRY(check_ptr(out->free_head, "out->free_head", true));
     CAEE_TRY(check_ptr(out->lacking, "out->lacking", true));
-    if (out->free_head == free_head)
-        return fail(CAEE_ERR_INVALID_ARG, "out->free_head must not be free_head (other workgroups may still read it)");
     if (B > kMaxRequests) return fail(CAEE_ERR_UNSUPPORTED, "B=%d exceeds %d", B, kMaxRequests);
     PlanParams p{B, T, block_size, max_blocks, n_free, (B + kPlanThreads - 1) / kPlanThreads, ctx_len, new_len,
                  block_table, free_list, free_head, *out};
     if (p.chunk < 1) p.chunk = 1;
+    CAEE_TRY(check_plan_apart(p));
     int groups = (T + kPlanTokens - 1) / kPlanTokens;
     groups = groups < 1 ? 1 : groups > kPlanMaxGroups ? kPlanMaxGroups : groups;
     hipStream_t s = (hipStream_t)stream;

@@ -181,3 +181,20 @@ def test_auto_form_by_new_tokens_and_prefix():
     for T, kv, form in ((256, 9000, 2), (255, 9000, 1), (32, 64, 2), (32, 65, 1), (31, 62, 1)):
         kw = dict(T=T, B=2, max_new=T, max_kv=kv)
         assert size(0, **kw) == size(form, **kw) != size(3 - form, **kw), (T, kv)
+
+
+PLAN_READS = dict(ctx=4 * 4, new=4 * 4, free=4 * 4, head=4)
+PLAN_WRITES = dict(table=4 * 4 * 4, cu_new=5 * 4, cu_kv=5 * 4, seq_len=4 * 4, slots=8 * 8, position=8 * 4, request=8 * 4,
+                   free_head=4, lacking=4)
+
+
+@pytest.mark.parametrize("written,other", [(w, o) for w in PLAN_WRITES for o in [*PLAN_READS, *PLAN_WRITES] if o != w])
+def test_plan_refuses_what_it_writes_over_another_array(written, other):
+    """The next step's ctx_len is this step's seq_len: handed in as both, the lengths change while they are read.
+    The same address, and an array that begins in the last 16 bytes of the other one."""
+    sizes = dict(PLAN_READS, **PLAN_WRITES)
+    apart = {name: FAKE + 4096 * i for i, name in enumerate(sizes)}
+    for a, b in ((written, other), (other, written)):
+        for into in (0, (sizes[b] - 1) // 16 * 16):
+            assert _plan(**dict(apart, **{a: apart[b] + into})) == BAD, (a, b, into)
+            assert "overlaps" in caee.lib.caee_last_error().decode()
