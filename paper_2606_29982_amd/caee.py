@@ -225,6 +225,8 @@ def _stream(*tensors) -> Optional[int]:
     import torch
     for t in tensors:
         if t is not None:
+            if not t.is_cuda:
+                raise ValueError(f"expected a tensor on a GPU, got one on {t.device}")
             # what torch.cuda.current_stream(t.device).cuda_stream returns, without the Stream object (2 us a call)
             return torch._C._cuda_getCurrentRawStream(t.get_device())
     return None

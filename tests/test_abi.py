@@ -216,3 +216,36 @@ def test_noalloc_refuses_oversize_and_empty_calls_on_the_host():
     d = _layer(k=17).desc()
     assert caee.lib.caee_moe_layer_noalloc(ctypes.byref(d), FAKE, FAKE, None, FAKE, FAKE, ctypes.byref(w), FAKE,
                                            None, None) == caee.CAEE_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("call", ["pack_matrix", "quantize_rows", "route_prune", "expert_ffn", "moe_layer",
+                                  "moe_layer_noalloc", "offload"])
+def test_binding_refuses_host_tensors(call, monkeypatch):
+    """A tensor in host memory is refused before the library sees its address."""
+    import types
+
+    import torch
+    reached = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: reached.append(name) or caee.CAEE_OK
+
+    monkeypatch.setattr(caee, "lib", Library())
+    layer = _layer(T=4, d=256, f=128, E=16, n_group=4, topk_group=2, k=2)
+    f, b = torch.zeros(4, 256), torch.zeros(4096, dtype=torch.uint8)
+    ids = torch.zeros((4, 2), dtype=torch.int32)
+    out, w = dict(topk_ids=ids, topk_w=f), dict(w13=f, w2=f)
+    handle = caee.Offload.__new__(caee.Offload)
+    handle.handle = None
+    calls = dict(
+        pack_matrix=lambda: caee.pack_matrix("bf16", f, f, 4, 256, 1),
+        quantize_rows=lambda: caee.quantize_rows(f, b, f),
+        route_prune=lambda: caee.route_prune(layer, f, None, f, ids, out, b),
+        expert_ffn=lambda: caee.expert_ffn(layer, f, ids, f, w, f, b),
+        moe_layer=lambda: caee.moe_layer(layer, f, f, None, f, ids, w, f, b),
+        moe_layer_noalloc=lambda: caee.moe_layer_noalloc(layer, f, f, None, f, ids, w, f),
+        offload=lambda: handle(layer, f, f, None, f, b, copy_stream=types.SimpleNamespace(cuda_stream=0)))
+    with pytest.raises(ValueError):
+        calls[call]()
+    assert not reached
