@@ -397,6 +397,14 @@ def _at(t, name: str, dtype, shape) -> int:
     return _need(t, name, dtype, shape).data_ptr()
 
 
+def _workspace(ws) -> tuple:
+    """Address and bytes of a workspace."""
+    if ws is None:
+        return None, 0
+    _need(ws, "ws")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def alloc_paged_plan(B: int, T: int, device) -> dict:
     """Device buffers for the plan of B requests and T token entries (caee_paged_plan_out_t)."""
     import torch
@@ -505,6 +513,7 @@ def latent_attention(att: Latent, q, weights: dict, cache, block_table, plan: di
     bounds of a request's new tokens and of the sum of ``seq_len``; ``y`` [T][heads][v] bf16 or f32."""
     import torch
     bf, i32, H, R = torch.bfloat16, torch.int32, att.heads, att.latent
+    ws_at, ws_bytes = _workspace(ws)
     T, B = q.shape[0], block_table.shape[0]
     _need(q, "q", bf, (T, H, att.nope + att.rope), dense=False)
     if q.stride(2) != 1 or (H > 1 and q.stride(1) != att.nope + att.rope):
@@ -526,7 +535,7 @@ def latent_attention(att: Latent, q, weights: dict, cache, block_table, plan: di
     w = LatentWeights(_ptr(weights.get("w_uk")), _ptr(weights.get("w_uk_t")), _ptr(weights.get("w_uv")))
     _check(lib.caee_latent_attention(ctypes.byref(d), _ptr(q), ctypes.byref(w), _ptr(cache), _ptr(block_table),
                                      _ptr(plan["cu_new"]), _ptr(plan["cu_kv"]), _ptr(plan["seq_len"]), _ptr(y),
-                                     _ptr(lse), _ptr(ws), ws.numel(), _stream(y)))
+                                     _ptr(lse), ws_at, ws_bytes, _stream(y)))
     return y
 
 
@@ -553,6 +562,7 @@ def block_matmul(x, w, w_scale, y, ws=None, x_scale=None, layout: int = LAYOUT_R
     those of ``y`` [M][N] (bf16 or f32) too.  ``w`` [N][K] codes in ``layout`` order, ``w_scale``
     [ceil(N/128)][K/128].  ``ws`` as made by ``alloc_block_matmul_workspace`` (not needed for codes)."""
     import torch
+    ws_at, ws_bytes = _workspace(ws)
     (M, K), N = x.shape, w.shape[0]
     if _code(_need(w, "w", None, (N, K))) != CAEE_FP8_E4M3:
         raise TypeError("w must be e4m3 codes")
@@ -563,8 +573,8 @@ def block_matmul(x, w, w_scale, y, ws=None, x_scale=None, layout: int = LAYOUT_R
     if tuple(y.shape) != (M, N):
         raise ValueError(f"y must have shape {(M, N)}, got {tuple(y.shape)}")
     d = _block_matmul_desc(x, N, _code(y), layout, ys)
-    _check(lib.caee_block_matmul(ctypes.byref(d), _ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(y), _ptr(ws),
-                                 0 if ws is None else ws.numel(), _stream(y)))
+    _check(lib.caee_block_matmul(ctypes.byref(d), _ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(y), ws_at,
+                                 ws_bytes, _stream(y)))
     return y
 
 

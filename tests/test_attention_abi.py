@@ -198,3 +198,21 @@ def test_plan_refuses_what_it_writes_over_another_array(written, other):
         for into in (0, (sizes[b] - 1) // 16 * 16):
             assert _plan(**dict(apart, **{a: apart[b] + into})) == BAD, (a, b, into)
             assert "overlaps" in caee.lib.caee_last_error().decode()
+
+
+def test_binding_refuses_a_workspace_in_host_memory():
+    att = caee.Latent(heads=1, nope=64, rope=64, latent=128, v=64, scale=1.0)
+    ws, f = torch.zeros(1 << 10, dtype=torch.uint8), torch.zeros(1, 1, 128)
+    with pytest.raises(ValueError, match="ws must be a device tensor"):
+        caee.latent_attention(att, f, {}, f, f[0].int(), {}, f, ws, max_new=1, max_kv=1)
+    with pytest.raises(ValueError, match="ws must be a device tensor"):
+        caee.block_matmul(f[0], f[0].byte(), f[0], f[0], ws)
+
+
+def test_workspaces_are_counted_in_bytes():
+    class Buffer:
+        is_cuda, dtype = True, torch.int64
+        is_contiguous, data_ptr = (lambda self: True), (lambda self: FAKE)
+        numel, element_size = (lambda self: 40), (lambda self: 8)
+
+    assert caee._workspace(Buffer()) == (FAKE, 320) and caee._workspace(None) == (None, 0)
