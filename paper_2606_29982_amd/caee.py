@@ -443,13 +443,13 @@ def paged_plan(block_size: int, ctx_len, new_len, block_table, free_list, free_h
 
 
 def _rows(t, name: str):
-    """A 2-D tensor whose rows are dense; its row stride."""
+    """A 2-D tensor whose rows are dense; its row stride (of a single row, which may be any, the row's length)."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     shape, stride = t.shape, t.stride()
     if len(shape) != 2 or (shape[1] > 1 and stride[1] != 1):
         raise ValueError(f"{name} must be 2-D with dense rows")
-    return stride[0] if shape[0] > 1 else max(stride[0], shape[1])
+    return stride[0] if shape[0] > 1 else shape[1]
 
 
 def latent_store(c, r, slots, cache):

@@ -216,3 +216,14 @@ def test_workspaces_are_counted_in_bytes():
         numel, element_size = (lambda self: 40), (lambda self: 8)
 
     assert caee._workspace(Buffer()) == (FAKE, 320) and caee._workspace(None) == (None, 0)
+
+
+@pytest.mark.parametrize("rows,stride,want", [(1, 577, 576), (1, 0, 576), (1, 600, 576), (2, 600, 600), (2, 577, 577),
+                                              (0, 576, 576)])
+def test_a_single_row_has_no_stride(rows, stride, want):
+    """A row cut out of an array of any width: nothing lies a stride away from it, so no stride is refused."""
+    class Rows:
+        is_cuda, shape = True, (rows, 576)
+        stride = lambda self: (stride, 1)  # noqa: E731
+
+    assert caee._rows(Rows(), "x") == want

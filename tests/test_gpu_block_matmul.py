@@ -165,3 +165,18 @@ def test_middle(M, N, K, tiled, x_dtype, y_dtype):
 
 def test_past_four_rounds_of_tiles():
     _run(2100, 2064, 2048, tiled=True)
+
+
+def test_one_row_of_an_array_of_any_width():
+    """x and y of a single row, cut out of arrays whose widths no two rows could have."""
+    rng = np.random.default_rng(7)
+    codes, ws = _weights(144, 512, rng)
+    wide = torch.randn(3, 517, device=DEV).to(torch.bfloat16)
+    x, y = wide[:1, :512], torch.full((2, 147), 7.0, device=DEV)
+    want = torch.empty((1, 144), device=DEV)
+    call = lambda a, b: caee.block_matmul(a, codes.to(DEV), ws.to(DEV), b,  # noqa: E731
+                                          caee.alloc_block_matmul_workspace(a, 144, DEV))
+    call(x, y[:1, :144])
+    call(x.contiguous(), want)
+    torch.cuda.synchronize()
+    assert torch.equal(y[:1, :144], want) and torch.all(y[0, 144:] == 7.0) and torch.all(y[1] == 7.0)

@@ -174,3 +174,11 @@ def test_plan_and_store_in_a_graph():
         want = torch.zeros(320, 192, dtype=torch.bfloat16)
         want[ref["slots"][live]] = rows.cpu()[torch.from_numpy(live)].to(torch.bfloat16)
         assert torch.equal(cache.cpu().view(320, 192), want)
+
+
+def test_store_one_row_of_an_array_of_any_width():
+    wide = torch.randn(2, 133 + 72, device=DEV).to(torch.bfloat16)
+    cache = torch.zeros((2, 4, 192), dtype=torch.bfloat16, device=DEV)
+    caee.latent_store(wide[:1, :128], wide[:1, 128:192], torch.tensor([5], dtype=torch.int64, device=DEV), cache)
+    torch.cuda.synchronize()
+    assert torch.equal(cache[1, 1], wide[0, :192]) and float(cache.float().abs().sum(2).count_nonzero()) == 1
