@@ -489,7 +489,8 @@ caee_status_t caee_latent_workspace_size(const caee_latent_desc_t* desc, size_t*
  *   caee_paged_plan writes them; y [T][heads][v] (y_dtype), fully overwritten;
  *   lse [T][heads] fp32 natural log of sum_j exp(s_tj), or NULL.
  * A row that sees no token (padding past cu_new[B], seq_len 0) is zero, its
- * lse -inf.  Cache rows at or past a request's seq_len are never read;
+ * lse -inf.  Where T is less than cu_new[B] the first T new tokens have rows,
+ * whose results are as if all had.  Cache rows at or past a request's seq_len are never read;
  * rows that a query does not see do not change its result, whatever they hold.
  * Scores, softmax statistics and sums are fp32; absorbed queries, expanded
  * keys and values, and the softmax weights are rounded to bf16 before

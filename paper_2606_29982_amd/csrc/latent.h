@@ -180,16 +180,24 @@ __device__ inline uint32_t lat_slot(const LatentParams& p, int b, int pos) {
 
 // New tokens and length of request b as the kernels use them: 0 <= new <=
 // max_new, rows within [0, T), 0 <= seq <= max_kv (the host's bounds size the
-// workspace and the counters, so lengths past them are cut).
+// workspace and the counters, so lengths past them are cut), and the tokens
+// before its new ones, by the lengths as they are: what a causal row sees does
+// not change where the rows end inside a request.
 struct LatentReq {
-    int t0, add, seq;
+    int t0, add, seq, before;
 };
+// Tokens that new token i of the request sees.
+__device__ inline int lat_sees(const LatentParams& p, const LatentReq& r, int i) {
+    return p.causal ? min(max(r.before + i + 1, 0), r.seq) : r.seq;
+}
 __device__ inline LatentReq lat_req(const LatentParams& p, int b) {
     LatentReq r;
     const int a = p.cu_new[b], e = p.cu_new[b + 1];
     r.t0 = min(max(a, 0), p.T);
     r.add = min(max(min(e, p.T) - r.t0, 0), p.max_new);
-    r.seq = min(max(p.seq_len[b], 0), (int)p.max_kv);
+    const int len = max(p.seq_len[b], 0);
+    r.seq = min(len, (int)p.max_kv);
+    r.before = len - (e - a);
     return r;
 }
 

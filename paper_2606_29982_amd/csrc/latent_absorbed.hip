@@ -309,7 +309,7 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
             b = 63 - __clzll(__ballot(lane < p.B && mine_at <= u) | 1ull);
             at_u = __builtin_amdgcn_readlane(mine_at, b);
             rq = {__builtin_amdgcn_readlane(mine.t0, b), __builtin_amdgcn_readlane(mine.add, b),
-                  __builtin_amdgcn_readlane(mine.seq, b)};
+                  __builtin_amdgcn_readlane(mine.seq, b), __builtin_amdgcn_readlane(mine.before, b)};
         } else {
             b = lat_find_wave(p.meta, p.B, u);
             rq = lat_req(p, b);
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
         // This lane's query row and how many tokens it sees.
         const int row0 = rt * kAbsRows;
         const int row = min(row0 + 32 * rg + n, rows - 1);
-        auto sees = [&](int r) { return p.causal ? min(max(rq.seq - rq.add + r / p.H + 1, 0), rq.seq) : rq.seq; };
+        auto sees = [&](int r) { return lat_sees(p, rq, r / p.H); };
         const int limit = sees(row);
         const int lim_min = __builtin_amdgcn_readfirstlane(sees(row0));
         const int tok0 = first * kUnit, tok1 = min(last * kUnit, sees(min(row0 + kAbsRows, rows) - 1));

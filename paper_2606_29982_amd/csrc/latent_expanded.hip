@@ -278,7 +278,7 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
     const LatentReq rq = lat_req(p, b);
     const int row0 = (tile - p.meta[b]) * kExpRows;
     const int kv0 = p.cu_kv[b];
-    auto sees = [&](int r) { return p.causal ? min(max(rq.seq - rq.add + r + 1, 0), rq.seq) : rq.seq; };
+    auto sees = [&](int r) { return lat_sees(p, rq, r); };
     const int my0 = row0 + 32 * wave;
     const int row = min(my0 + n, rq.add - 1);
     const int limit = sees(row);

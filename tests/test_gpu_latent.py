@@ -241,3 +241,14 @@ def test_weights_of_short_contexts_keep_their_remainders():
     c.q[..., :128] = 0
     (y, _), (ry, _) = c.run(DEV, "absorbed", y_dtype=torch.float32), c.ref()
     assert np.linalg.norm(y - ry) <= 2.0 ** -12 * np.linalg.norm(ry)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("T", [1, 10, 23, 300])
+def test_rows_that_end_inside_a_request(T, causal, form):
+    """Fewer query rows than the plan has new tokens: the rows there are see what they would see among all of them."""
+    c = LatentCase(seq=[40, 90, 400, 7], new=[3, 20, 290, 5], H=4, seed=25)
+    y, lse = c.ref(causal)
+    c.T, c.q = T, c.q[:T]
+    check_attention(c.run(DEV, form, causal), (y[:T], lse[:T]))
