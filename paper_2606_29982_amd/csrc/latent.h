@@ -78,7 +78,16 @@ __device__ __attribute__((always_inline)) inline void lat_for(F&& f) {
     }
 }
 
-constexpr float kNoScore = -1e30f;    // running maximum of a row that has seen nothing
+constexpr float kNoScore = -3.40282347e38f;    // running maximum of a row that has seen nothing: the lowest finite score
+// Softmax weight of score s where the running maximum is m (a product s
+// scale_log2 of fp32).  The product is rounded before m is taken off, as m's
+// was: in one multiply-add a score past 2^30 would leave its product's rounding,
+// up to any power of two, as the weight of the maximum itself.
+__device__ inline float lat_weight(float s, float scale_log2, float m) {
+#pragma clang fp contract(off)
+    const float t = s * scale_log2;
+    return __builtin_amdgcn_exp2f(t - m);
+}
 // The running maximum moves only when a score exceeds it by more than
 // kMaxSlack (in powers of two): the weights are then at most 2^8, which costs
 // neither fp32 sums nor bf16 weights any precision, and the accumulators are

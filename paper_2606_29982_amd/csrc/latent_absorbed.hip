@@ -517,8 +517,8 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
                     [[maybe_unused]] int rest[2] = {0, 0};
                     lat_for<0, 4>([&](auto ic) __attribute__((always_inline)) {
                         constexpr int i = decltype(ic)::value;
-                        const float a = __builtin_amdgcn_exp2f(fmaf(sc[8 * k + 2 * i], p.scale_log2, -m));
-                        const float e = __builtin_amdgcn_exp2f(fmaf(sc[8 * k + 2 * i + 1], p.scale_log2, -m));
+                        const float a = lat_weight(sc[8 * k + 2 * i], p.scale_log2, m);
+                        const float e = lat_weight(sc[8 * k + 2 * i + 1], p.scale_log2, m);
                         big = fmaxf(fmaxf(big, a), e);
                         w[i] = lat_pack(a, e);
                         if constexpr (kRest) {

@@ -463,8 +463,8 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
             for (int k = 0; k < 4; ++k)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float a = __builtin_amdgcn_exp2f(fmaf(sc[k >> 1][8 * (k & 1) + 2 * i], p.scale_log2, -m));
-                    const float e = __builtin_amdgcn_exp2f(fmaf(sc[k >> 1][8 * (k & 1) + 2 * i + 1], p.scale_log2, -m));
+                    const float a = lat_weight(sc[k >> 1][8 * (k & 1) + 2 * i], p.scale_log2, m);
+                    const float e = lat_weight(sc[k >> 1][8 * (k & 1) + 2 * i + 1], p.scale_log2, m);
                     big = fmaxf(fmaxf(big, a), e);
                     pf[k][i] = lat_pack(a, e);
                     more = lat_sum2(pf[k][i], more);

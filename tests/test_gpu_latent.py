@@ -252,3 +252,32 @@ def test_rows_that_end_inside_a_request(T, causal, form):
     y, lse = c.ref(causal)
     c.T, c.q = T, c.q[:T]
     check_attention(c.run(DEV, form, causal), (y[:T], lse[:T]))
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("size", [2.0 ** 24, 2.0 ** 32, 2.0 ** 40, 2.0 ** 66, 2.0 ** 106, 2.0 ** 120])
+@pytest.mark.parametrize("sign", ["below", "above", "both"])
+def test_scores_of_any_size(size, sign, form):
+    """Finite scores however large, all below zero among them: the largest takes the whole weight, a row's own value.
+
+    The rotary parts alone make the scores, by one product each, so a row's largest score is at least a 256th of its
+    size (the spacing of the rows' bf16 factors) above the next; the result is a value with the roundings of a weight
+    of one, exact, and of the value and the result (two of 2^-9 for a row, allowed: TOL_ROW's eight)."""
+    c = LatentCase(seq=[3, 100, 300], new=[1, 2, 4], H=4, seed=26)
+    c.q[..., :129] = 0
+    c.q[..., 129:] = 0
+    c.q[..., 128] = size ** 0.5
+    rng = np.random.default_rng(27)
+    for b, n in enumerate(c.seq):
+        factor = 1.0 + rng.permutation(int(n)) / 128.0              # n different bf16 factors, the largest anywhere
+        factor = np.exp2(np.floor(factor - 1.0)) * (1.0 + (factor - 1.0) % 1.0)
+        factor *= {"below": -1.0, "above": 1.0, "both": np.where(rng.random(int(n)) < 0.5, -1.0, 1.0)}[sign]
+        for j in range(int(n)):
+            row = c.rows[b][j].clone()
+            row[c.latent:] = 0
+            row[c.latent] = float(factor[j]) * size ** 0.5
+            c.set_row(b, j, row)
+    (y, lse), (ry, rl) = c.run(DEV, form), c.ref()
+    assert np.all(np.isfinite(y)) and np.all(np.isfinite(lse))
+    assert np.all(np.linalg.norm(y - ry, axis=2) <= 8 * 2.0 ** -9 * np.linalg.norm(ry, axis=2))
+    assert np.all(np.abs(lse - rl) <= 1e-6 * np.abs(rl))
