@@ -52,6 +52,12 @@ struct LatentParams {
     uint16_t* kr;
 };
 
+// A launch has fewer than 2^32 threads in x: past kLatGridX workgroups (a
+// multiple of the XCDs) a grid goes on in y, as one line of workgroups.
+constexpr unsigned kLatGridX = 1u << 22;
+inline dim3 lat_grid(unsigned n) { return n <= kLatGridX ? dim3(n) : dim3(kLatGridX, (n + kLatGridX - 1) / kLatGridX); }
+__device__ inline unsigned lat_workgroup() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 hipError_t launch_latent_absorbed(const LatentParams& p, hipStream_t s);
 hipError_t launch_latent_expanded(const LatentParams& p, hipStream_t s);
 

@@ -688,7 +688,7 @@ __global__ __launch_bounds__(kAbsThreads) void k_join(LatentParams p) {
     __shared__ float red[kWaves == 1 ? 1 : kWaves - 1][V][kWave];
     const int lane = threadIdx.x & 63, wave_of_wg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave = kWaves == 1 ? 0 : wave_of_wg;
-    const size_t at = kWaves == 1 ? (size_t)blockIdx.x * (kAbsThreads / kWave) + wave_of_wg : blockIdx.x;
+    const size_t at = kWaves == 1 ? (size_t)lat_workgroup() * (kAbsThreads / kWave) + wave_of_wg : lat_workgroup();
     const int t = (int)(at / p.H);
     if (t >= p.T) return;
     float* dst = p.o + at * R + V * lane;
@@ -867,8 +867,8 @@ void attend_on(const LatentParams& p, hipStream_t s) {
         constexpr int R = decltype(latent)::value;
         if (p.max_kv <= kRestTokens * p.B) hipLaunchKernelGGL((k_attend<R, kPairs, true>), grid, block, 0, s, p);
         else hipLaunchKernelGGL((k_attend<R, kPairs, false>), grid, block, 0, s, p);
-        if (rows < kJoinRows) hipLaunchKernelGGL((k_join<R, kPairs, 4>), dim3((unsigned)rows), block, 0, s, p);
-        else hipLaunchKernelGGL((k_join<R, kPairs, 1>), dim3((unsigned)((rows + 3) / 4)), block, 0, s, p);
+        if (rows < kJoinRows) hipLaunchKernelGGL((k_join<R, kPairs, 4>), lat_grid((unsigned)rows), block, 0, s, p);
+        else hipLaunchKernelGGL((k_join<R, kPairs, 1>), lat_grid((unsigned)((rows + 3) / 4)), block, 0, s, p);
         hipLaunchKernelGGL(k_unabsorb<R>, dim3(p.H, (p.T + 31) / 32, p.v / 64), dim3(R), 0, s, p);
     };
     if (p.latent == 512) run(LatInt<512>{});

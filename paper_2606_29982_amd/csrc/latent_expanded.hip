@@ -263,15 +263,17 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
     // evenly (64 heads, 7161 tokens behind 1030: 1312 us; in plain order, as with
     // other numbers of heads, 1486; 16 heads, short prompts: 32 and 49); the last
     // tiles, which see the most tokens, first.
+    const int wg = (int)lat_workgroup();
     int h, q;
     if (p.H % kXcds == 0) {
-        const int k = blockIdx.x / kXcds;
-        h = blockIdx.x % kXcds + kXcds * (k / tiles);
+        const int k = wg / kXcds;
+        h = wg % kXcds + kXcds * (k / tiles);
         q = k % tiles;
     } else {
-        h = blockIdx.x / tiles;
-        q = blockIdx.x % tiles;
+        h = wg / tiles;
+        q = wg % tiles;
     }
+    if (h >= p.H) return;      // the last line of a long grid
     const int tile = p.meta[p.B] - 1 - q;
     if (tile < 0) return;
     const int b = lat_find_wave(p.meta, p.B, tile);
@@ -574,8 +576,8 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt(LatentParams p, int t
 
 template <int NOPE>
 void prompt(const LatentParams& p, unsigned grid, int tiles, hipStream_t s) {
-    if (p.v == 128) hipLaunchKernelGGL((k_prompt<NOPE, 128>), dim3(grid), dim3(kPromptThreads), 0, s, p, tiles);
-    else hipLaunchKernelGGL((k_prompt<NOPE, 64>), dim3(grid), dim3(kPromptThreads), 0, s, p, tiles);
+    if (p.v == 128) hipLaunchKernelGGL((k_prompt<NOPE, 128>), lat_grid(grid), dim3(kPromptThreads), 0, s, p, tiles);
+    else hipLaunchKernelGGL((k_prompt<NOPE, 64>), lat_grid(grid), dim3(kPromptThreads), 0, s, p, tiles);
 }
 
 }  // namespace

@@ -281,3 +281,57 @@ def test_scores_of_any_size(size, sign, form):
     assert np.all(np.isfinite(y)) and np.all(np.isfinite(lse))
     assert np.all(np.linalg.norm(y - ry, axis=2) <= 8 * 2.0 ** -9 * np.linalg.norm(ry, axis=2))
     assert np.all(np.abs(lse - rl) <= 1e-6 * np.abs(rl))
+
+
+def _needs_memory(gib):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info(DEV)[0] < gib << 30:
+        pytest.skip(f"{gib} GiB of device memory")
+
+
+def test_requests_times_heads_past_a_launchs_threads():
+    """65536 requests of one token, 128 heads: 2^23 query tiles of 512 threads.  A row's result is its own value."""
+    _needs_memory(24)
+    B, H, R, V = 65536, 128, 128, 64
+    g = torch.Generator(device=DEV).manual_seed(28)
+    rand = lambda *s: torch.randn(s, generator=g, device=DEV).to(torch.bfloat16)  # noqa: E731
+    w = caee.pack_latent_weights(rand(H, 64, R) * R ** -0.5, rand(H, V, R) * R ** -0.5)
+    cache, q = rand(B, 1, R + 64), rand(B, H, 128)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    table = torch.randperm(B, generator=g, device=DEV).to(torch.int32)[:, None]
+    plan = dict(cu_new=torch.arange(B + 1, **i32), cu_kv=torch.arange(B + 1, **i32), seq_len=torch.ones(B, **i32))
+    att = caee.Latent(heads=H, nope=64, rope=64, latent=R, v=V, scale=0.1, form="expanded")
+    y = torch.full((B, H, V), 7.0, dtype=torch.bfloat16, device=DEV)
+    ws = caee.alloc_latent_workspace(att, B, B, 1, B, DEV)
+    caee.latent_attention(att, q, w, cache, table, plan, y, ws, max_new=1, max_kv=B)
+    torch.cuda.synchronize()
+    for h in (0, 1, 63, 127):
+        want = cache[table[:, 0].long(), 0, :R].double() @ w["w_uv"][h].double().t()
+        d = (y[:, h].double() - want).norm(dim=1) / want.norm(dim=1)
+        assert float(d.max()) <= 8 * 2.0 ** -9       # a value's and a result's rounding, of a row
+
+
+def test_rows_past_a_launchs_threads():
+    """2^26 query rows, a wave each where partial results are joined.  A sample of them against the formula."""
+    _needs_memory(130)
+    T, H, R, V, S = 1 << 20, 64, 128, 64, 64
+    g = torch.Generator(device=DEV).manual_seed(29)
+    rand = lambda *s: torch.randn(s, generator=g, device=DEV, dtype=torch.bfloat16)  # noqa: E731
+    w = caee.pack_latent_weights(rand(H, 64, R) * R ** -0.5, rand(H, V, R) * R ** -0.5)
+    cache, q = rand(1, S, R + 64), rand(T, H, 128)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    plan = dict(cu_new=torch.tensor([0, T - 3], **i32), cu_kv=torch.tensor([0, S], **i32), seq_len=torch.tensor([S], **i32))
+    att = caee.Latent(heads=H, nope=64, rope=64, latent=R, v=V, scale=128 ** -0.5, causal=False, form="absorbed")
+    y = torch.full((T, H, V), 7.0, dtype=torch.bfloat16, device=DEV)
+    ws = caee.alloc_latent_workspace(att, T, 1, T, S, DEV)
+    caee.latent_attention(att, q, w, cache, torch.zeros((1, 1), **i32), plan, y, ws, max_new=T, max_kv=S)
+    torch.cuda.synchronize()
+    assert torch.all(y[T - 3:] == 0)
+    c, r = cache[0, :, :R].double(), cache[0, :, R:].double()
+    for t in (0, 1, 12345, T // 2, T - 5, T - 4):
+        ql = torch.matmul(q[t, :, None, :64].double(), w["w_uk"].double())[:, 0]
+        p = torch.softmax(128 ** -0.5 * (ql @ c.t() + q[t, :, 64:].double() @ r.t()), 1)
+        want = torch.matmul(w["w_uv"].double(), (p @ c)[:, :, None])[:, :, 0]
+        assert float(((y[t].double() - want).norm(dim=1) / want.norm(dim=1)).max()) <= 8 * 2.0 ** -9
+    del q, y, ws
+    torch.cuda.empty_cache()
