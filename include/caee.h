@@ -438,18 +438,25 @@ caee_status_t caee_latent_store(int32_t T, int32_t latent, int32_t rope, int32_t
 typedef enum caee_latent_form {
     /* By the batch's size: expanded from CAEE_LATENT_EXPAND_NEW new tokens
      * per request on average, or from CAEE_LATENT_EXPAND_FRESH where the
-     * cache holds little else (max_kv <= 2 T). */
+     * cache holds little else (max_kv <= 2 T); absorbed all the same, up to
+     * twice CAEE_LATENT_EXPAND_NEW, where the expanded form needs more than
+     * CAEE_LATENT_EXPAND_BYTES of workspace and the absorbed one less.  Where
+     * only one of the forms takes a call of that size, that one. */
     CAEE_LATENT_AUTO = 0,
     /* Queries are multiplied by W_uk and attend to the cache rows
      * themselves, whose values W_uv is applied to afterwards: few new tokens
-     * over a long cache (reads each row once for all heads). */
+     * over a long cache (reads each row once for all heads).  Workspace: T
+     * heads (6 latent + 2 rope) bytes and 131072 (latent + 2).  (max_kv / 64 +
+     * B) ceil(max_new heads / 64) is at most 2^30 - 1. */
     CAEE_LATENT_ABSORBED = 1,
     /* Every head's keys and values are formed from the cache rows first:
-     * prompts (a fifth to a third of the work per pair). */
+     * prompts (a fifth to a third of the work per pair).  Workspace: 2 max_kv
+     * (heads (nope + v) + rope) bytes.  max_kv is at most 65534 * 256. */
     CAEE_LATENT_EXPANDED = 2
 } caee_latent_form_t;
 #define CAEE_LATENT_EXPAND_NEW 128
 #define CAEE_LATENT_EXPAND_FRESH 16
+#define CAEE_LATENT_EXPAND_BYTES (16ll << 30)
 
 typedef struct caee_latent_desc {
     int32_t T;            /* query rows, >= 0 (padded ones included) */
@@ -476,7 +483,8 @@ typedef struct caee_latent_weights {
     const void* w_uv;     /* [heads][v][latent] bf16 */
 } caee_latent_weights_t;
 
-/* Bytes of workspace caee_latent_attention needs.  Host-only. */
+/* Bytes of workspace caee_latent_attention needs (with CAEE_LATENT_AUTO those
+ * of the form that it takes, so a smaller call may need more).  Host-only. */
 caee_status_t caee_latent_workspace_size(const caee_latent_desc_t* desc, size_t* bytes);
 
 /* Latent attention of the new tokens over the paged cache, which holds their

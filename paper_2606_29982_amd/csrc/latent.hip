@@ -9,24 +9,19 @@ namespace {
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// The expanded form pays for every cached token once, the absorbed one 3.4
-// times as much per pair of tokens, so the new tokens per request decide.
-// Absorbed (its weights plain bf16, a tenth less than with their remainders)
-// and expanded, us, 128 heads: 8 requests behind 8000 tokens with 64
-// new ones each 1359 and 3899, with 256 5788 and 4237; behind 1000 with 64 414
-// and 566, with 128 813 and 619; one request behind 8000 with 128 356 and 576,
-// with 256 685 and 595.  Without a cached prefix the expanded form is ahead
-// from about 8 (8 requests: 52 and 53, with 32 137 and 61; 16 heads: with 8 41
-// and 27).
-bool latent_expanded(const caee_latent_desc_t& d) {
-    if (d.form != CAEE_LATENT_AUTO) return d.form == CAEE_LATENT_EXPANDED;
-    const long long B = d.B > 0 ? d.B : 1;
-    return d.T >= CAEE_LATENT_EXPAND_NEW * B || (d.T >= CAEE_LATENT_EXPAND_FRESH * B && d.max_kv <= 2ll * d.T);
+constexpr long long kExpandMaxKv = 65534ll * 256;      // tokens in all of the expanded form: one launch's rows of tiles
+
+bool expanded_fits(const caee_latent_desc_t& d) { return d.max_kv <= kExpandMaxKv; }
+
+// Shares of the absorbed form are counted in 32 bits.
+bool absorbed_fits(const caee_latent_desc_t& d) {
+    const long long tiles = ((long long)d.max_new * d.heads + kAbsTileRows - 1) / kAbsTileRows;
+    return (d.max_kv / 64 + d.B) * tiles <= INT32_MAX / 2;
 }
 
-LatentWs latent_ws(const caee_latent_desc_t& d) {
+LatentWs latent_ws(const caee_latent_desc_t& d, bool expanded) {
     LatentWs L{};
-    L.expanded = latent_expanded(d);
+    L.expanded = expanded;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -48,6 +43,34 @@ LatentWs latent_ws(const caee_latent_desc_t& d) {
     L.total = at;
     return L;
 }
+
+// The expanded form pays for every cached token once, the absorbed one 3.4
+// times as much per pair of tokens, so the new tokens per request decide.
+// Absorbed and expanded, us, 128 heads: 8 requests behind 8000 tokens with 64
+// new ones each 1598 and 3744, with 128 3304 and 3804, with 256 6988 and 3949;
+// behind 1000 with 64 391 and 524, with 128 780 and 568; one request behind 8000
+// with 128 409 and 522, with 256 816 and 549.  16 heads, behind 1000: with 64 76
+// and 89, with 128 98 and 92.  Without a cached prefix they meet at about 12 new
+// ones: 8 requests with 8 41 and 53, 12 53 and 53, 16 65 and 54, 32 119 and 57;
+// 16 heads with 8 25.3 and 25.6, 16 26.5 and 25.9, 64 requests of 15 54.4 and
+// 54.3.
+// The expanded form's keys and values may be far more than anything else the
+// call needs (8 requests of 128 new tokens behind a million, 128 heads: 61 GiB,
+// the absorbed form 0.45): where they pass CAEE_LATENT_EXPAND_BYTES the
+// absorbed form, if it needs less, goes on to twice the limit (2 requests
+// behind 130000 tokens, 128 heads, with 200 new ones each 13.6 and 15.1 ms, with
+// 400 27.4 and 18.8).
+bool latent_expanded(const caee_latent_desc_t& d) {
+    if (d.form != CAEE_LATENT_AUTO) return d.form == CAEE_LATENT_EXPANDED;
+    if (!expanded_fits(d) || !absorbed_fits(d)) return expanded_fits(d);       // the one that takes the call
+    const long long B = d.B > 0 ? d.B : 1;
+    if (d.T < CAEE_LATENT_EXPAND_NEW * B && (d.T < CAEE_LATENT_EXPAND_FRESH * B || d.max_kv > 2ll * d.T)) return false;
+    if (d.T >= 2 * CAEE_LATENT_EXPAND_NEW * B) return true;
+    const size_t keys = latent_ws(d, true).total;
+    return keys <= (size_t)CAEE_LATENT_EXPAND_BYTES || latent_ws(d, false).total >= keys;
+}
+
+LatentWs latent_ws(const caee_latent_desc_t& d) { return latent_ws(d, latent_expanded(d)); }
 
 caee_status_t check_latent(const caee_latent_desc_t* d) {
     if (!d) return fail(CAEE_ERR_INVALID_ARG, "desc is NULL");
@@ -82,12 +105,11 @@ caee_status_t check_latent(const caee_latent_desc_t* d) {
     if ((long long)d->n_blocks * d->block_size > INT32_MAX || d->max_kv > (1 << 30))
         return fail(CAEE_ERR_UNSUPPORTED, "a cache of %lld rows exceeds 2^31 - 1, or %lld tokens in all 2^30",
                     (long long)d->n_blocks * d->block_size, (long long)d->max_kv);
-    if (latent_expanded(*d) && d->max_kv > 65534 * 256)
-        return fail(CAEE_ERR_UNSUPPORTED, "the expanded form takes at most %d tokens in all, not max_kv=%lld", 65534 * 256,
-                    (long long)d->max_kv);
-    // Shares of the absorbed form are counted in 32 bits.
-    const long long tiles = ((long long)d->max_new * d->heads + kAbsTileRows - 1) / kAbsTileRows;
-    if (!latent_expanded(*d) && (d->max_kv / 64 + d->B) * tiles > INT32_MAX / 2)
+    const bool expanded = latent_expanded(*d);
+    if (expanded && !expanded_fits(*d))
+        return fail(CAEE_ERR_UNSUPPORTED, "the expanded form takes at most %lld tokens in all, not max_kv=%lld",
+                    kExpandMaxKv, (long long)d->max_kv);
+    if (!expanded && !absorbed_fits(*d))
         return fail(CAEE_ERR_UNSUPPORTED, "max_new=%d new tokens over max_kv=%lld: too many pairs for the absorbed form",
                     d->max_new, (long long)d->max_kv);
     return CAEE_OK;

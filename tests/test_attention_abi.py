@@ -227,3 +227,34 @@ def test_a_single_row_has_no_stride(rows, stride, want):
         stride = lambda self: (stride, 1)  # noqa: E731
 
     assert caee._rows(Rows(), "x") == want
+
+
+GIB = 1 << 30
+
+
+@pytest.mark.parametrize("kw,form", [
+    # tokens in all past what the expanded form takes
+    (dict(T=25600, B=200, max_new=200, max_kv=65534 * 256 + 1), 1), (dict(T=25600, B=200, max_new=200, max_kv=1 << 30), 1),
+    (dict(T=25600, B=200, max_new=200, max_kv=65534 * 256, heads=1, q_stride=192), 2),
+    # more pairs than the absorbed form counts
+    (dict(T=16000, B=200, max_new=15801, max_kv=15000000, heads=32, q_stride=32 * 192), 2),
+    # keys and values of more than 16 GiB: absorbed up to 256 new tokens per request where it needs less
+    (dict(T=1024, B=8, max_new=128, max_kv=1000000, heads=128, q_stride=128 * 192), 1),
+    (dict(T=2047, B=8, max_new=256, max_kv=1000000, heads=128, q_stride=128 * 192), 1),
+    (dict(T=2048, B=8, max_new=256, max_kv=1000000, heads=128, q_stride=128 * 192), 2),
+    (dict(T=1024, B=8, max_new=128, max_kv=261600, heads=128, q_stride=128 * 192), 2),
+    (dict(T=1024, B=8, max_new=128, max_kv=261700, heads=128, q_stride=128 * 192), 1),
+    (dict(T=100000, B=500, max_new=200, max_kv=262400, heads=128, q_stride=128 * 192), 2),
+])
+def test_auto_form_takes_what_either_form_takes(kw, form):
+    (st, size), got = _latent_ws(_latent_desc(form=form, **kw)), _latent_ws(_latent_desc(**kw))
+    assert (st, got) == (OK, (OK, size)) and _latent_ws(_latent_desc(form=3 - form, **kw)) != (OK, size)
+    if form == 2 and kw["T"] < 256 * kw["B"] and size > 16 * GIB:
+        assert _latent_ws(_latent_desc(form=1, **kw)) >= (LIMIT, 0) or _latent_ws(_latent_desc(form=1, **kw))[1] >= size
+
+
+def test_workspace_of_either_form_is_as_the_header_says():
+    d = dict(T=100, B=8, heads=128, q_stride=128 * 192, max_kv=50000, max_new=64)
+    for form, most in ((1, 100 * 128 * (6 * 512 + 2 * 64) + 131072 * (512 + 2)), (2, 2 * 50000 * (128 * 256 + 64))):
+        size = _latent_ws(_latent_desc(form=form, **d))[1]
+        assert most <= size <= most + 8 * 256
