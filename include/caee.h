@@ -502,8 +502,8 @@ caee_status_t caee_latent_workspace_size(const caee_latent_desc_t* desc, size_t*
  * rows that a query does not see do not change its result, whatever they hold.
  * Scores, softmax statistics and sums are fp32; absorbed queries, expanded
  * keys and values, and the softmax weights are rounded to bf16 before
- * their products (absorbed, up to 16384 tokens per request by max_kv / B: the
- * weights with a remainder of 8 bits).
+ * their products (absorbed, for requests of up to 16384 tokens: the weights
+ * with a remainder of 8 bits).
  * Preconditions on device contents (violations: unspecified results,
  * memory-safe): page numbers in [0, n_blocks) for the pages seq_len covers,
  * at most max_new new tokens per request and max_kv tokens in all (what a

@@ -231,6 +231,17 @@ __device__ inline uint32_t lds_get(uint32_t at, uint32_t flags, lat_u32x4 (&w)[4
     return f[0] | f[1] | f[2] | f[3];
 }
 
+// Tokens of a request up to which its weights' remainders are multiplied too:
+// rounding errors weigh most where few rows share a sum, over long contexts they
+// average out.  Errors of the result (of its size, rms; rounding it to bf16 is
+// 0.0017 of them) without and with, and us: 901 tokens 0.0025 and 0.0022, 23.6 and
+// 24.0; 64 requests of 128 heads, 2048 tokens 0.0025 and 0.0023, 81 and 92; 32 of
+// 8192 0.0024 and 0.0023, 115 and 137; 16 of 16384 0.0024 and 0.0023, 111 and 132;
+// 8 of 32768 0.0024 and 0.0023, 112 and 133; 5 of 120013, 32 heads 0.0024 and
+// 0.0023, 139 and 161.  (16384 and 32768 with 32 heads: 0.00237 and 0.00230,
+// 0.00236 and 0.00232.)
+constexpr int kRestTokens = 16384;
+
 // A workgroup holds 64 query rows and walks over the tiles of its share.
 // Four waves, one per SIMD (a wave may use 512 registers), take two parts in
 // turn:
@@ -248,7 +259,7 @@ __device__ inline uint32_t lds_get(uint32_t at, uint32_t flags, lat_u32x4 (&w)[4
 // half the contraction only and cost one more exchange: 106 us for 64 users
 // of 128 heads and 2048 tokens on average, 195 us for five of 120011 tokens
 // and 64 rows; this takes 72 and 121.  These and the figures below are of
-// plain bf16 weights; with kRest the 64 users take 81.)
+// plain bf16 weights; with remainders the 64 users take 81.)
 // It is bound by the fetches (5.7 TB/s for the five; the 64 users' rows go to
 // two workgroups each, by way of an L2).  A CU takes 16 cycles for each load, so
 // they go out between the MFMAs: the second half of the next tile beside the
@@ -260,12 +271,10 @@ __device__ inline uint32_t lds_get(uint32_t at, uint32_t flags, lat_u32x4 (&w)[4
 // A row's running maximum moves only when a weight exceeds 2^kMaxSlack; then
 // the workgroup exchanges maxima and rescales its sums.
 // Scores, maxima and sums are fp32.  The weights are rounded to bf16, the type of
-// the rows they multiply.  With kRest what the rounding left, in 8 bits, is
-// multiplied too; without, a row's sum is of the rounded weights, so that the
-// roundings' mean cancels.  (The result's error, rms, with and without: 0.0022
-// and 0.0026 of its size for 64 users, of which rounding it to bf16 is 0.0017;
-// both 0.0024 for the five.)
-template <int R, bool kPairs, bool kRest>
+// the rows they multiply.  Up to kRestTokens (by the request's own length) what
+// the rounding left, in 8 bits, is multiplied too; past them a row's sum is of
+// the rounded weights, so that the roundings' mean cancels.
+template <int R, bool kPairs>
 __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
     constexpr int kG = AbsHalf<R>::kGroups;
@@ -278,7 +287,7 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
     // one from the loads that fill another.
     __shared__ AbsHalf<R> st0a, st0b, st1a, st1b;
     __shared__ lat_u32x4 pw[2][4][kWave];      // softmax weights: [row group][16 tokens][fragment]
-    __shared__ lat_u32x2 pr[kRest ? 2 : 1][4][kRest ? kWave : 1];      // their remainders
+    __shared__ lat_u32x2 pr[2][4][kWave];      // their remainders
     __shared__ float sm[2][kAbsRows], sf[kAbsRows];
     __shared__ int over[4];
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
@@ -292,7 +301,7 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
     }
     const AbsShare sh = abs_share_of<kPairs>(p.meta[p.B], blockIdx.x);
     const uint32_t pw_at = (uint32_t)(uintptr_t)(lat_lds_void*)&pw[0][0][0], over_at = (uint32_t)(uintptr_t)(lat_lds_void*)&over[0];
-    [[maybe_unused]] const uint32_t pr_at = (uint32_t)(uintptr_t)(lat_lds_void*)&pr[0][0][0];
+    const uint32_t pr_at = (uint32_t)(uintptr_t)(lat_lds_void*)&pr[0][0][0];
     // Fragment places in a half.  Keys: row n, piece 2 j + hf.  Transposed
     // values: rows 16 ks + 8 e + 4 hf + (0 .. 3), four 16-byte pieces per 32
     // components.
@@ -444,7 +453,8 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
 
         // Step s: tile s in ta and tb, the other stage's second half nb for that
         // of tile s + 1 (its first half is on its way).
-        auto step = [&](int s, AbsHalf<R>& ta, AbsHalf<R>& tb, AbsHalf<R>& nb) __attribute__((always_inline)) {
+        auto step = [&](auto rest_too, int s, AbsHalf<R>& ta, AbsHalf<R>& tb, AbsHalf<R>& nb) __attribute__((always_inline)) {
+            constexpr bool kRest = decltype(rest_too)::value;
             const int tok = tok0 + s * kUnit;
             // This wave's part of the tile is there (the first half of the next
             // may stay in flight); after the barrier all of it is, and nobody
@@ -624,10 +634,14 @@ __global__ __launch_bounds__(kAbsThreads, 1) void k_attend(LatentParams p) {
             });
             if (more_a && !next_a.one) load_each(s + 2, 0, ta);
         };
-        for (int s = 0; s < steps; s += 2) {
-            step(s, st0a, st0b, st1b);
-            if (s + 1 < steps) step(s + 1, st1a, st1b, st0b);
-        }
+        auto walk = [&](auto rest_too) __attribute__((always_inline)) {
+            for (int s = 0; s < steps; s += 2) {
+                step(rest_too, s, st0a, st0b, st1b);
+                if (s + 1 < steps) step(rest_too, s + 1, st1a, st1b, st0b);
+            }
+        };
+        if (rq.seq <= kRestTokens) walk(LatInt<1>{});
+        else walk(LatInt<0>{});
 
         lat_wait_vm<0>();          // no load is on its way into the stages any more
         // Row sums: two halves of a lane pair, two token halves.
@@ -852,21 +866,13 @@ __global__ __launch_bounds__(R) void k_unabsorb(LatentParams p) {
     }
 }
 
-// Tokens per request up to which the weights' remainders are multiplied too:
-// rounding errors weigh most where few rows share a sum, over long contexts
-// they average out (error of the result with and without, and time: 901 tokens
-// 0.0022 and 0.0026, 24.3 and 23.5 us; 64 requests of 2048 on average 0.0022 and
-// 0.0026, 114 and 104 us; five of 120011 0.0024 both, 161 and 139 us).
-constexpr long long kRestTokens = 16384;
-
 template <bool kPairs>
 void attend_on(const LatentParams& p, hipStream_t s) {
     const long long rows = (long long)p.T * p.H;
     const dim3 grid(kAbsGroups), block(kAbsThreads);
     auto run = [&](auto latent) {
         constexpr int R = decltype(latent)::value;
-        if (p.max_kv <= kRestTokens * p.B) hipLaunchKernelGGL((k_attend<R, kPairs, true>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((k_attend<R, kPairs, false>), grid, block, 0, s, p);
+        hipLaunchKernelGGL((k_attend<R, kPairs>), grid, block, 0, s, p);
         if (rows < kJoinRows) hipLaunchKernelGGL((k_join<R, kPairs, 4>), lat_grid((unsigned)rows), block, 0, s, p);
         else hipLaunchKernelGGL((k_join<R, kPairs, 1>), lat_grid((unsigned)((rows + 3) / 4)), block, 0, s, p);
         hipLaunchKernelGGL(k_unabsorb<R>, dim3(p.H, (p.T + 31) / 32, p.v / 64), dim3(R), 0, s, p);

@@ -335,3 +335,28 @@ def test_rows_past_a_launchs_threads():
         assert float(((y[t].double() - want).norm(dim=1) / want.norm(dim=1)).max()) <= 8 * 2.0 ** -9
     del q, y, ws
     torch.cuda.empty_cache()
+
+
+def test_remainders_are_kept_by_each_requests_own_length():
+    """A short request beside one of 40000 tokens, as test_weights_of_short_contexts_keep_their_remainders: by its own
+    length, not the batch's."""
+    c = LatentCase(seq=[700, 40000], new=[2, 1], H=8, seed=30, block=64)
+    c.q[..., :128] = 0
+    (y, _), (ry, _) = c.run(DEV, "absorbed", y_dtype=torch.float32), c.ref()
+    assert np.linalg.norm(y[:2] - ry[:2]) <= 2.0 ** -12 * np.linalg.norm(ry[:2])
+
+
+def test_results_do_not_depend_on_the_hosts_bounds():
+    """Bounds that a captured graph sets generously: max_kv at any size, max_new while it asks for one row tile."""
+    c = LatentCase(seq=[700, 90], new=[1, 2], H=8, seed=31)
+    att = caee.Latent(heads=8, nope=128, rope=64, latent=512, v=128, scale=c.scale, form="absorbed")
+    to = lambda a, dt=None: torch.as_tensor(a).to(DEV, dt)  # noqa: E731
+    plan = dict(cu_new=to(c.cu_new, torch.int32), cu_kv=to(c.cu_kv, torch.int32), seq_len=to(c.seq, torch.int32))
+    w, got = caee.pack_latent_weights(to(c.w_uk), to(c.w_uv)), []
+    for max_new, max_kv in ((2, 790), (8, 790), (2, 1 << 20), (5, 1 << 30)):
+        y = torch.empty((c.T, 8, 128), device=DEV)
+        ws = caee.alloc_latent_workspace(att, c.T, 2, max_new, max_kv, DEV)
+        caee.latent_attention(att, to(c.q), w, to(c.cache), to(c.table), plan, y, ws, max_new=max_new, max_kv=max_kv)
+        torch.cuda.synchronize()
+        got.append(y)
+    assert all(torch.equal(y, got[0]) for y in got)
