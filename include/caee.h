@@ -427,9 +427,10 @@ caee_status_t caee_paged_plan(int32_t B, int32_t T, int32_t block_size, int32_t 
 /* Writes T tokens' rows into the cache: row slots[t] = [c_t | r_t], rounded to
  * bf16 (nearest, ties to even).  c and r are x_dtype (CAEE_BF16 or CAEE_F32)
  * rows c_stride and r_stride elements apart (slices of a wider projection,
- * 16-byte aligned rows).  A slot outside [0, n_slots) writes nothing; of two
- * tokens with one slot either is stored.  latent and rope are multiples
- * of 8. */
+ * 16-byte aligned rows).  A slot outside [0, n_slots) writes nothing.  Slots
+ * are distinct, as a plan over distinct pages makes them: where two tokens have
+ * one, each value of its row is of either, not all of the same.  latent and
+ * rope are multiples of 8. */
 caee_status_t caee_latent_store(int32_t T, int32_t latent, int32_t rope, int32_t x_dtype, const void* c,
                                 int64_t c_stride, const void* r, int64_t r_stride, const int64_t* slots, void* cache,
                                 int64_t n_slots, void* stream);

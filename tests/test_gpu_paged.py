@@ -182,3 +182,16 @@ def test_store_one_row_of_an_array_of_any_width():
     caee.latent_store(wide[:1, :128], wide[:1, 128:192], torch.tensor([5], dtype=torch.int64, device=DEV), cache)
     torch.cuda.synchronize()
     assert torch.equal(cache[1, 1], wide[0, :192]) and float(cache.float().abs().sum(2).count_nonzero()) == 1
+
+
+def test_store_of_two_tokens_with_one_slot():
+    """Each value of the row is of either token (the row's pieces are written apart); other rows are as ever."""
+    T, rows = 4096, 64
+    x = torch.arange(T, device=DEV, dtype=torch.float32)[:, None].expand(T, 192).contiguous() % 256     # a token's values: its number
+    slots = torch.arange(T, device=DEV) % rows + 2
+    cache = torch.full((2, 64, 192), -5.0, dtype=torch.bfloat16, device=DEV)
+    caee.latent_store(x[:, :128], x[:, 128:], slots, cache)
+    torch.cuda.synchronize()
+    flat = cache.view(128, 192).float()
+    assert torch.all(flat[:2] == -5.0) and torch.all(flat[2 + rows:] == -5.0)
+    assert torch.all(flat[2:2 + rows] % rows == torch.arange(rows, device=DEV)[:, None]) and torch.all(flat[2:2 + rows] >= 0)
