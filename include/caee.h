@@ -413,7 +413,9 @@ typedef struct caee_paged_plan_out {
  * lists: tokens past it get no entry, entries past the last token are -1, so
  * a step can be padded to a fixed size.  Where the free list ends (or a
  * row of the table), entries are -1 (not written), their tokens' slots -1 and
- * `lacking` counts the pages.  Nothing else is changed: a call with the same
+ * `lacking` counts the pages.  A page that the list gives and the table row has
+ * no entry for is passed over: the head moves past it, and it is in no row, so
+ * a program that takes up such a step again goes back to its own head.  Nothing else is changed: a call with the same
  * inputs writes the same outputs.  An array that the call writes may not
  * overlap any other one (refused): lengths kept from step to step alternate
  * between two buffers, as the free head does.  Negative lengths count as 0, and the sums
@@ -533,8 +535,11 @@ typedef struct caee_block_matmul_desc {
 caee_status_t caee_block_matmul_workspace_size(const caee_block_matmul_desc_t* desc, size_t* bytes);
 
 /*   x_scale [M][K/128] fp32 for CAEE_FP8_E4M3 x (its row stride is K/128), else NULL.
- * Per 128-deep block the code products are summed exactly enough (fp32) and
- * the block's sum times x_scale times w_scale is added in fp32. */
+ * Per 128-deep block the code products are summed, and the block's sum times
+ * x_scale times w_scale is added in fp32.  For an fp32 y, and for K up to 256,
+ * a block's sum is of fp32 too; for a bf16 y of larger K the 8-bit matrix
+ * instructions keep about 16 bits of it (relative error 1.4e-5 of a block, a
+ * three-hundredth of y's own rounding). */
 caee_status_t caee_block_matmul(const caee_block_matmul_desc_t* desc, const void* x, const float* x_scale,
                                 const void* w, const float* w_scale, void* y, void* ws, size_t ws_bytes,
                                 void* stream);
