@@ -538,8 +538,8 @@ caee_status_t caee_block_matmul_workspace_size(const caee_block_matmul_desc_t* d
  * Per 128-deep block the code products are summed, and the block's sum times
  * x_scale times w_scale is added in fp32.  For an fp32 y, and for K up to 256,
  * a block's sum is of fp32 too; for a bf16 y of larger K the 8-bit matrix
- * instructions keep about 16 bits of it (relative error 1.4e-5 of a block, a
- * three-hundredth of y's own rounding). */
+ * instructions keep about 16 bits of it (1.4e-5 of its size, a hundredth of
+ * y's own rounding). */
 caee_status_t caee_block_matmul(const caee_block_matmul_desc_t* desc, const void* x, const float* x_scale,
                                 const void* w, const float* w_scale, void* y, void* ws, size_t ws_bytes,
                                 void* stream);

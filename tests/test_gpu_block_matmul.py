@@ -180,3 +180,34 @@ def test_one_row_of_an_array_of_any_width():
     call(x.contiguous(), want)
     torch.cuda.synchronize()
     assert torch.equal(y[:1, :144], want) and torch.all(y[0, 144:] == 7.0) and torch.all(y[1] == 7.0)
+
+
+def _height(M, N, K):
+    """The library's rule for many rows and a bf16 result: row tiles of 32 per workgroup, None below its sizes."""
+    if -(-M // 64) * -(-N // 64) <= (3 if K < 2048 else 4) * 256:
+        return None
+    rounds = lambda nt: -(-(-(-M // (32 * nt)) * -(-N // 256)) // 256)  # noqa: E731
+    return min(range(8, 3, -1), key=lambda nt: rounds(nt) * (nt + 1))
+
+
+@pytest.mark.parametrize("height,M,N", [(4, 705, 4112), (5, 6529, 1040), (6, 8167, 1040), (7, 1538, 7184),
+                                        (8, 1797, 7184)])
+@pytest.mark.parametrize("K,x_dtype,tiled", [(384, "bf16", True), (512, "e4m3", False), (640, "f32", True)])
+def test_every_height_of_the_many_row_kernel(height, M, N, K, x_dtype, tiled):
+    """Heights differ in loads a wave, their place among the tiles and the wait for them; contractions of 0, 1 and 2
+    blocks modulo the ring of three; rows and columns end inside a tile (N inside 16 columns where rows are as stored)."""
+    N = N if tiled else N - 5
+    assert _height(M, N, K) == height and M % (32 * height) and N % 256
+    _run(M, N, K, x_dtype, tiled=tiled)
+
+
+@pytest.mark.parametrize("K,tiled", [(128, False), (256, True), (384, True), (512, False), (640, True)])
+def test_many_rows_into_float32(K, tiled):
+    _run(1153, 2832, K, "bf16", "f32", tiled=tiled)
+
+
+def test_many_rows_of_a_long_contraction():
+    """More blocks than the ring in each of its places, and row scales of every block."""
+    for K in (2176, 2304, 4224):
+        assert _height(1410, 4112, K) is not None
+        _run(1410, 4112, K, tiled=True)
