@@ -508,20 +508,27 @@ void launch_many(const BmParams& p, hipStream_t s) {
     hipLaunchKernelGGL((k_bm_many<NT, kExact>), dim3(grid), dim3(512), 0, s, p, n_tiles, m_tiles);
 }
 
-// By the number of 64 x 64 tiles.  Up to half a round of the CUs 32 x 32
-// tiles, which make two of them, are faster (M x N, K = 4096: 64 x 7168 12.6
-// and 12.9 us, 256 x 2048 11.4 and 12.7, 1024 x 576 16.5 and 13.8, 128 x 7168
-// 22 and 13); k_bm_many needs K / 128 + 2 steps of 1.5 us for any product of
-// one round and then gains (512 x 7168: 46 and 53 us, 2048 x 2048 45 and 53,
-// 1024 x 7168 79 and 58; K = 512: 512 x 4096 9.4 and 12.6, 768 x 4096 13.5 and
-// 13.1, 1024 x 4096 17.6 and 13.5; K = 2048: 1024 x 4096 28 and 30).
+// By the number of 64 x 64 tiles, in rounds of the CUs.  Up to half a round 32 x
+// 32 tiles, which make two of them, are about as fast or faster (K = 4096, 32 and
+// 64, us: 5 x 4096 7 and 10 of K = 7168, 256 x 2048 10.5 and 10.8, 64 x 7168 12.5
+// and 10.8; fp32 results 11.8 and 13.3, 13.2 and 13.6; past it 1024 x 576 16.2 and
+// 13.9, 128 x 7168 20.9 and 11.9).  k_bm_many takes K / 128 + 2 steps for any
+// product of one round of its own and then gains; its steps are 0.85 us, with the
+// bf16 MFMAs of kExact 1.5.  64 x 64 tiles and k_bm_many, m x 4096:
+//                    2 rounds (m = 512)   3 (m = 768)   4 (m = 1024)
+//   bf16,  K =  512     9.7 and  9.7      13.3    9.9   17.4   10.3
+//          K = 2048    15.0     17.8      21.3   18.1   28.1   18.7
+//          K = 7168    35.3     51.4      51.1   51.6   66.7   52.1
+//   exact, K =  512    10.7     13.1      15.1   13.7   19.3   14.5
+//          K = 2048    18.2     31.2      25.9   32.0   33.1   32.7
+//          K = 7168    44.5     93.0      63.6   93.7   82.1   94.1
 template <bool kExact>
 hipError_t launch_bm(const BmParams& p, hipStream_t s) {
     const long long nt = (p.N + 63) / 64, mt = (p.M + 63) / 64, tiles = nt * mt;
     if (tiles <= kBmCus / 2) {
         const dim3 grid((p.N + 31) / 32, (p.M + 31) / 32);
         hipLaunchKernelGGL((k_bm_split<1, 8, kExact>), grid, dim3(512), 0, s, p);
-    } else if (tiles <= (p.K < 2048 ? 3 : 4) * kBmCus) {
+    } else if (tiles <= (!kExact ? 2 : p.K < 2048 ? 3 : 4) * kBmCus) {
         hipLaunchKernelGGL((k_bm_split<2, 4, kExact>), dim3((unsigned)nt, (unsigned)mt), dim3(256), 0, s, p);
     } else if constexpr (kExact) {
         launch_many<4, true>(p, s);

@@ -184,7 +184,7 @@ def test_one_row_of_an_array_of_any_width():
 
 def _height(M, N, K):
     """The library's rule for many rows and a bf16 result: row tiles of 32 per workgroup, None below its sizes."""
-    if -(-M // 64) * -(-N // 64) <= (3 if K < 2048 else 4) * 256:
+    if -(-M // 64) * -(-N // 64) <= 2 * 256:
         return None
     rounds = lambda nt: -(-(-(-M // (32 * nt)) * -(-N // 256)) // 256)  # noqa: E731
     return min(range(8, 3, -1), key=lambda nt: rounds(nt) * (nt + 1))
@@ -211,3 +211,11 @@ def test_many_rows_of_a_long_contraction():
     for K in (2176, 2304, 4224):
         assert _height(1410, 4112, K) is not None
         _run(1410, 4112, K, tiled=True)
+
+
+@pytest.mark.parametrize("M", [512, 513, 700])
+@pytest.mark.parametrize("K,tiled", [(384, True), (1024, False)])
+def test_about_two_rounds_of_tiles(M, K, tiled):
+    """Both sides of the size where the many-row kernel takes over, for bf16 results."""
+    assert (_height(M, 4096, K) is None) == (M == 512)
+    _run(M, 4096, K, tiled=tiled)
