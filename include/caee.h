@@ -462,14 +462,14 @@ typedef enum caee_latent_form {
 #define CAEE_LATENT_EXPAND_BYTES (16ll << 30)
 
 typedef struct caee_latent_desc {
-    int32_t T;            /* query rows, >= 0 (padded ones included) */
+    int32_t T;            /* query rows, 0..2^20 (padded ones included) */
     int32_t B;            /* requests, 0..65536 */
     int32_t heads;        /* 1..1024 */
     int32_t nope, rope;   /* parts of a query: 64 or 128, and 64 */
     int32_t latent;       /* 128, 256 or 512 */
     int32_t v;            /* output width of a head, 64 or 128 */
     int32_t block_size;   /* tokens of a cache page, 1..65536 */
-    int32_t n_blocks;     /* pages of the cache */
+    int32_t n_blocks;     /* pages of the cache, of fewer than 2^31 tokens in all */
     int32_t max_blocks;   /* row length of block_table */
     int32_t max_new;      /* no request has more new tokens than this */
     int32_t causal;       /* 1: new token i of a request sees its first seq_len - new + i + 1 tokens; 0: all seq_len */
@@ -521,13 +521,13 @@ caee_status_t caee_latent_attention(const caee_latent_desc_t* desc, const void* 
  * multiple of 16), w_scale [ceil(N/128)][K/128] fp32, one per 128x128 block
  * (the last row of blocks may be partial). */
 typedef struct caee_block_matmul_desc {
-    int32_t M;            /* rows of x, >= 0 */
-    int32_t N;            /* outputs, >= 1 */
+    int32_t M;            /* rows of x, 0..2^24 */
+    int32_t N;            /* outputs, 1..2^24 */
     int32_t K;            /* contraction, a positive multiple of 128, at most 65536 */
     int32_t x_dtype;      /* CAEE_BF16, CAEE_F32 (quantised in the call, as by caee_quantize_rows) or CAEE_FP8_E4M3 */
     int32_t y_dtype;      /* CAEE_BF16 or CAEE_F32 */
     int32_t layout;       /* caee_layout_t of w */
-    int64_t x_stride;     /* elements from one row of x to the next, >= K, rows 16-byte aligned */
+    int64_t x_stride;     /* elements from one row of x to the next, >= K, at most 2^22, rows 16-byte aligned */
     int64_t y_stride;     /* elements from one row of y to the next, >= N */
 } caee_block_matmul_desc_t;
 

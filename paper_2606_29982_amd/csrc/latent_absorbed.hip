@@ -259,9 +259,11 @@ constexpr int kRestTokens = 16384;
 // half the contraction only and cost one more exchange: 106 us for 64 users
 // of 128 heads and 2048 tokens on average, 195 us for five of 120011 tokens
 // and 64 rows; this takes 72 and 121.  These and the figures below are of
-// plain bf16 weights; with remainders the 64 users take 81.)
-// It is bound by the fetches (5.7 TB/s for the five; the 64 users' rows go to
-// two workgroups each, by way of an L2).  A CU takes 16 cycles for each load, so
+// plain bf16 weights; with remainders the 64 users take 83.)
+// The five are bound by the fetches (5.8 TB/s).  The 64 users, whose rows go to
+// two workgroups each by way of an L2, are not: 2.1 TB/s, L2 hits of 48 %,
+// matrix units busy 26 % of the cycles, so a step's chain and the segments'
+// starts and ends with one wave a SIMD.  A CU takes 16 cycles for each load, so
 // they go out between the MFMAs: the second half of the next tile beside the
 // scores, the first half of the one after as soon as the sums are done with
 // this tile's (with whole tiles of lookahead, all loads at a step's start: 96

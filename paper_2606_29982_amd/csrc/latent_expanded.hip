@@ -63,7 +63,7 @@ struct ExpandStage {
 // the next one's loads between the first half of a stage's MFMAs; workgroups
 // that run together share weight tiles by XCD (they are numbered weights
 // first) and the outputs leave through LDS, 512 bytes of a token at a time.
-// 8191 tokens of 64 heads take 189 us, 0.73 PFLOP/s (100 us of products at the
+// 8191 tokens of 64 heads take 183 us, 0.75 PFLOP/s (100 us of products at the
 // rate of a large one): bound by the fetches into LDS, 173 us without the
 // products, 159 without the outputs, which pass the caches by (kept there: 201).
 // Neither 128 x 128 tiles with outputs straight from the registers (264 us) nor
@@ -236,9 +236,9 @@ struct QueryRows {
 // tiles: keys as the M side, so that a lane holds a row's scores, whose weights
 // are, in that order, a fragment of the second product, without a trip through
 // LDS.  Bound by the matrix units at the clock that power leaves them (40 MFMAs
-// of 32 x 32 x 16 a step and wave, 57 % of the cycles): 7161 tokens behind 1030,
-// 64 heads, take 1.30 ms, 1.0 PFLOP/s.  Short prompts are bound by their longest
-// tile (2.7 us a step): eight of up to 700 tokens, 16 heads, 32 us.
+// of 32 x 32 x 16 a step and wave, 59 % of the cycles): 7161 tokens behind 1030,
+// 64 heads, take 1.2 ms among other calls, 1.1 PFLOP/s (1.36 in a trace).  Short prompts are bound by their longest
+// tile (2.7 us a step): eight of up to 700 tokens, 16 heads, 33 us.
 // Keys, values and weights are bf16, the cache's type (the result's error is
 // 0.0028 of its size, rms, of which rounding the result to bf16 is 0.0017).
 template <int NOPE, int V>
