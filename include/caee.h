@@ -444,7 +444,9 @@ typedef enum caee_latent_form {
      * cache holds little else (max_kv <= 2 T); absorbed all the same, up to
      * twice CAEE_LATENT_EXPAND_NEW, where the expanded form needs more than
      * CAEE_LATENT_EXPAND_BYTES of workspace and the absorbed one less.  Where
-     * only one of the forms takes a call of that size, that one. */
+     * only one of the forms takes a call of that size, that one.  It is one
+     * form for all requests: a step of prompts and decode rows takes less as
+     * a plan and a call for each. */
     CAEE_LATENT_AUTO = 0,
     /* Queries are multiplied by W_uk and attend to the cache rows
      * themselves, whose values W_uv is applied to afterwards: few new tokens
@@ -501,8 +503,9 @@ caee_status_t caee_latent_workspace_size(const caee_latent_desc_t* desc, size_t*
  *   lse [T][heads] fp32 natural log of sum_j exp(s_tj), or NULL.
  * A row that sees no token (padding past cu_new[B], seq_len 0) is zero, its
  * lse -inf.  Where T is less than cu_new[B] the first T new tokens have rows,
- * whose results are as if all had.  Cache rows at or past a request's seq_len are never read;
- * rows that a query does not see do not change its result, whatever they hold.
+ * whose results are as if all had.  Cache rows at or past a request's seq_len
+ * are never read; rows that a query does not see do not change its result,
+ * whatever they hold.
  * Scores, softmax statistics and sums are fp32; absorbed queries, expanded
  * keys and values, and the softmax weights are rounded to bf16 before
  * their products (absorbed, for requests of up to 16384 tokens: the weights
