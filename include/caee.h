@@ -16,8 +16,8 @@
  *      FFN and their outputs are combined with the gate weights (the MoE
  *      output equation of Sec. II-A).
  * The attention block that precedes the layer in a decoder is here as well:
- * page plans and a latent cache, latent attention, block-scaled 8-bit
- * products.
+ * page plans, a latent cache and one of grouped heads, attention over either,
+ * block-scaled 8-bit products.
  *
  * Conventions shared by every entry point
  *   - Every tensor pointer is caller-owned DEVICE memory (hipMalloc'd or a
@@ -519,6 +519,111 @@ caee_status_t caee_latent_attention(const caee_latent_desc_t* desc, const void* 
                                     const int32_t* block_table, const int32_t* cu_new, const int32_t* cu_kv,
                                     const int32_t* seq_len, void* y, float* lse, void* ws, size_t ws_bytes,
                                     void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention with grouped heads: `kv_heads` heads of keys and values, each
+ * shared by heads / kv_heads consecutive query heads, in a paged cache that
+ * caee_paged_plan plans.  Keys and values are two arrays of bf16 with the same
+ * strides (elements): value d of head g of the token in slot s is at
+ *   (s / block_size) page_stride + (s % block_size) row_stride + g head_stride + d,
+ * so pages may hold a token's heads next to each other or a head's tokens, and
+ * keys and values may be parts of one array.  Strides are multiples of 8;
+ * rows, heads and pages may not overlap.  A page takes less than 2^30 elements. */
+typedef struct caee_head_store_desc {
+    int32_t T;            /* tokens, 0..2^20 */
+    int32_t heads;        /* query heads, 1..1024 */
+    int32_t kv_heads;     /* 1..1024 */
+    int32_t dim;          /* values of a head, 64 or 128 */
+    int32_t rope;         /* of them rotated (the first ones): 0 or a multiple of 16 */
+    int32_t adjacent;     /* the pairs that are rotated: 0 (i, i + rope/2), 1 (2i, 2i + 1) */
+    int32_t x_dtype;      /* of q, k and v: CAEE_BF16 or CAEE_F32 */
+    int32_t block_size;   /* tokens of a cache page, 1..65536 */
+    int32_t n_blocks;     /* pages of the cache, of fewer than 2^31 tokens in all */
+    float eps;            /* of the norms, finite and >= 0 */
+    int64_t q_stride, k_stride, v_stride;   /* elements from one token to the next (slices of a wider projection), rows 16-byte aligned */
+    int64_t q_out_stride;                   /* of q_out, a multiple of 8 */
+    int64_t page_stride, row_stride, head_stride;
+} caee_head_store_desc_t;
+
+/* The new tokens' heads as attention reads them:
+ *   q_out[t][h] = rotate(norm(q[t][h], q_norm)),
+ *   key   g of slots[t] = rotate(norm(k[t][g], k_norm)),
+ *   value g of slots[t] = v[t][g],
+ * rounded to bf16 (nearest, ties to even).  norm(x, w) = x / sqrt(mean(x^2) +
+ * eps) * w over a head's dim values (w [dim] fp32; NULL: x itself); rotate turns
+ * pair i by the angle position[t] * freq[i] (freq [rope/2] in double, radians;
+ * the angle is reduced in double, so far positions keep their precision).
+ * A slot outside [0, n_blocks * block_size) stores nothing; every row of q_out
+ * is written.  Slots are distinct (see caee_latent_store).  freq and position
+ * may be NULL where rope is 0.  q_out may be q itself (bf16, same stride) or
+ * lie beside q, k and v in rows of the same stride; else it may not overlap them
+ * (refused).  The caches overlap nothing else, nor each other. */
+caee_status_t caee_head_store(const caee_head_store_desc_t* desc, const void* q, const void* k, const void* v,
+                              const float* q_norm, const float* k_norm, const double* freq, const int32_t* position,
+                              const int64_t* slots, void* q_out, void* k_cache, void* v_cache, void* stream);
+
+/* How the work is dealt to the GPU.  Both give the same function. */
+typedef enum caee_head_form {
+    CAEE_HEAD_AUTO = 0,
+    /* Every request's tokens are cut into equal shares for all CUs, partial
+     * results joined: few new tokens (decode steps, trees, the next part of a
+     * long prompt). */
+    CAEE_HEAD_SPLIT = 1,
+    /* A workgroup takes all tokens that its query rows see: prompts. */
+    CAEE_HEAD_WHOLE = 2
+} caee_head_form_t;
+
+typedef struct caee_head_desc {
+    int32_t T;            /* query rows, 0..2^20 (padded ones included) */
+    int32_t B;            /* requests, 0..65536 */
+    int32_t heads;        /* query heads, 1..1024, a multiple of kv_heads */
+    int32_t kv_heads;
+    int32_t dim;          /* 64 or 128 */
+    int32_t block_size;   /* tokens of a cache page, 1..65536 */
+    int32_t n_blocks;     /* pages of the cache, of fewer than 2^31 tokens in all */
+    int32_t max_blocks;   /* row length of block_table */
+    int32_t max_new;      /* no request has more new tokens than this */
+    int32_t causal;       /* 1: new token i of a request sees its first seq_len - new + i + 1 tokens; 0: all seq_len */
+    int32_t tree_words;   /* 0, or 32-bit words of a token's tree mask, 1..32 (causal is 1, form not CAEE_HEAD_WHOLE) */
+    int32_t form;         /* caee_head_form_t */
+    int32_t y_dtype;      /* CAEE_BF16 or CAEE_F32 */
+    int64_t max_kv;       /* sum of seq_len at most, <= 2^30 */
+    int64_t q_stride;     /* elements from one token of q to the next, a multiple of 8, >= heads * dim */
+    int64_t page_stride, row_stride, head_stride;
+    float scale;          /* factor on the scores, finite and > 0 */
+} caee_head_desc_t;
+
+/* Bytes of workspace caee_head_attention needs.  Host-only. */
+caee_status_t caee_head_workspace_size(const caee_head_desc_t* desc, size_t* bytes);
+
+/* Softmax attention of the new tokens over the paged cache, which holds their
+ * own keys and values already (caee_head_store):
+ *   s_tj = scale * q[t][h] . k_j[g],  y[t][h] = sum_j softmax_j(s_t)_j v_j[g],
+ * g = h / (heads / kv_heads).
+ *   q [T][heads][dim] bf16, tokens q_stride apart; block_table [B][max_blocks],
+ *   cu_new [B + 1], seq_len [B] as caee_paged_plan writes them; y
+ *   [T][heads][dim] (y_dtype), fully overwritten; lse [T][heads] fp32 natural
+ *   log of sum_j exp(s_tj), or NULL;
+ *   tree [T][tree_words], or NULL where tree_words is 0: new token t sees the
+ *   tokens before its request's new ones, and of those the ones whose bit is
+ *   set: bit j % 32 of word j / 32 for new token j of the request (its own bit,
+ *   too, has to be set for it to see itself).  A tree's tokens lie in the
+ *   cache in the order of the list whatever their depth (their positions, for
+ *   caee_head_store, are the caller's).
+ * A row that sees no token (padding past cu_new[B], seq_len 0, an empty mask) is
+ * zero, its lse -inf.  Where T is less than cu_new[B] the first T new tokens
+ * have rows, whose results are as if all had.  Cache rows at or past a request's
+ * seq_len are never read; rows that a query does not see do not change its
+ * result, whatever they hold.
+ * Scores, softmax statistics and sums are fp32; the softmax weights are rounded
+ * to bf16 before their products, for an fp32 y with a second bf16 part that
+ * holds what the first leaves.
+ * Preconditions on device contents (violations: unspecified results,
+ * memory-safe): page numbers in [0, n_blocks) for the pages seq_len covers, at
+ * most max_new new tokens per request and max_kv tokens in all. */
+caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, const void* k_cache, const void* v_cache,
+                                  const int32_t* block_table, const int32_t* cu_new, const int32_t* seq_len,
+                                  const uint32_t* tree, void* y, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /* y = x W^T with e4m3 weights: w [N][K] codes (`layout` order; tiled: N a
  * multiple of 16), w_scale [ceil(N/128)][K/128] fp32, one per 128x128 block

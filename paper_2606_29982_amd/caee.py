@@ -22,6 +22,7 @@ KERNEL_KINDS = {"route": 0, "gate_up": 1, "down": 2, "combine": 3, "quant": 4, "
 DTYPE_CODE = {"f32": CAEE_F32, "bf16": CAEE_BF16, "fp8": CAEE_FP8_E4M3}
 IMPORTANCE_CODE = {"max": 0, "sum": 1, "cir": 2}
 LATENT_FORM_CODE = {"auto": 0, "absorbed": 1, "expanded": 2}
+HEAD_FORM_CODE = {"auto": 0, "split": 1, "whole": 2}
 REFILL_CODE = {"score": 0, "none": 1, "random": 2, "literal": 3}
 
 
@@ -85,6 +86,22 @@ class LatentWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("w_uk", "w_uk_t", "w_uv")]
 
 
+class HeadStoreDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("T", "heads", "kv_heads", "dim", "rope", "adjacent", "x_dtype", "block_size", "n_blocks")] + [
+        ("eps", ctypes.c_float)] + [(n, ctypes.c_int64) for n in
+                                    ("q_stride", "k_stride", "v_stride", "q_out_stride", "page_stride", "row_stride",
+                                     "head_stride")]
+
+
+class HeadDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("T", "B", "heads", "kv_heads", "dim", "block_size", "n_blocks", "max_blocks", "max_new", "causal",
+                 "tree_words", "form", "y_dtype")] + [
+        (n, ctypes.c_int64) for n in ("max_kv", "q_stride", "page_stride", "row_stride", "head_stride")] + [
+        ("scale", ctypes.c_float)]
+
+
 class BlockMatmulDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("M", "N", "K", "x_dtype", "y_dtype", "layout")] + [
         ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64)]
@@ -126,6 +143,9 @@ def _load(path: str = LIB_PATH):
         "caee_latent_workspace_size": (st, [ctypes.POINTER(LatentDesc), ctypes.POINTER(ctypes.c_size_t)]),
         "caee_latent_attention": (st, [ctypes.POINTER(LatentDesc), P, ctypes.POINTER(LatentWeights), P, P, P, P, P, P,
                                        P, P, ctypes.c_size_t, P]),
+        "caee_head_store": (st, [ctypes.POINTER(HeadStoreDesc)] + [P] * 12),
+        "caee_head_workspace_size": (st, [ctypes.POINTER(HeadDesc), ctypes.POINTER(ctypes.c_size_t)]),
+        "caee_head_attention": (st, [ctypes.POINTER(HeadDesc)] + [P] * 10 + [ctypes.c_size_t, P]),
         "caee_block_matmul_workspace_size": (st, [ctypes.POINTER(BlockMatmulDesc), ctypes.POINTER(ctypes.c_size_t)]),
         "caee_block_matmul": (st, [ctypes.POINTER(BlockMatmulDesc), P, P, P, P, P, P, ctypes.c_size_t, P]),
         "caee_status_str": (ctypes.c_char_p, [st]),
@@ -157,7 +177,8 @@ EXPORTED = ("caee_workspace_size", "caee_route_prune", "caee_expert_ffn", "caee_
             "caee_pack_matrix", "caee_quantize_rows", "caee_offload_create", "caee_offload_destroy",
             "caee_offload_layer", "caee_offload_stats", "caee_offload_residency", "caee_offload_reset",
             "caee_lru_step", "caee_paged_plan", "caee_latent_store", "caee_latent_workspace_size",
-            "caee_latent_attention", "caee_block_matmul_workspace_size", "caee_block_matmul", "caee_status_str", "caee_last_error", "caee_abi_version",
+            "caee_latent_attention", "caee_head_store", "caee_head_workspace_size", "caee_head_attention",
+            "caee_block_matmul_workspace_size", "caee_block_matmul", "caee_status_str", "caee_last_error", "caee_abi_version",
             "caee_timing_enable", "caee_timing_reset", "caee_timing_query")
 
 
@@ -536,6 +557,137 @@ def latent_attention(att: Latent, q, weights: dict, cache, block_table, plan: di
     _check(lib.caee_latent_attention(ctypes.byref(d), _ptr(q), ctypes.byref(w), _ptr(cache), _ptr(block_table),
                                      _ptr(plan["cu_new"]), _ptr(plan["cu_kv"]), _ptr(plan["seq_len"]), _ptr(y),
                                      _ptr(lse), ws_at, ws_bytes, _stream(y)))
+    return y
+
+
+def _head_caches(k_cache, v_cache, kv_heads: int, dim: int) -> tuple:
+    """Shape and strides of the two caches, [n_blocks][block_size][kv_heads][dim] bf16 views of the same strides whose
+    last dimension is dense (pages that hold a head's tokens next to each other: their transposed view)."""
+    import torch
+    shape, strides = k_cache.shape, k_cache.stride()
+    if not (k_cache.is_cuda and v_cache.is_cuda):
+        raise ValueError("k_cache and v_cache must be device tensors")
+    if k_cache.dtype is not torch.bfloat16 or v_cache.dtype is not torch.bfloat16:
+        raise TypeError("k_cache and v_cache must be torch.bfloat16")
+    if len(shape) != 4 or shape[2] != kv_heads or shape[3] != dim or v_cache.shape != shape:
+        raise ValueError(f"k_cache and v_cache must be [n_blocks][block_size][{kv_heads}][{dim}]")
+    if strides[3] != 1:
+        raise ValueError("k_cache and v_cache must have dense heads")
+    if v_cache.stride() != strides and any(n > 1 and a != b for n, a, b in zip(shape, strides, v_cache.stride())):
+        raise ValueError("k_cache and v_cache must have the same strides")
+    return shape, strides
+
+
+def _heads(t, name: str, dim: int):
+    """Tokens, heads and token stride of [T][heads][dim] whose heads are dense (tokens may be strided)."""
+    shape, stride = t.shape, t.stride()
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if len(shape) != 3 or shape[2] != dim:
+        raise ValueError(f"{name} must be [T][heads][{dim}]")
+    if stride[2] != 1 or (shape[1] > 1 and stride[1] != dim):
+        raise ValueError(f"{name} must have dense heads")
+    return shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1] * dim
+
+
+def head_store(q, k, v, slots, q_out, k_cache, v_cache, q_norm=None, k_norm=None, eps: float = 1e-6, position=None,
+               freq=None, adjacent: bool = False):
+    """Norms and rotation of the new tokens' heads, keys and values into the paged cache (caee_head_store).
+
+    ``q`` [T][heads][dim], ``k`` and ``v`` [T][kv_heads][dim], bf16 or f32 (tokens may be strided, as slices of one
+    projection are); ``slots`` [T] int64; ``q_out`` [T][heads][dim] bf16 (may be ``q``); ``k_cache`` and ``v_cache``
+    [n_blocks][block_size][kv_heads][dim] bf16 of any page, row and head strides.  ``q_norm`` and ``k_norm`` [dim] f32
+    or None (no norm).  ``freq`` [rope/2] float64: the angles, per position, of the pairs that are rotated, the first
+    ``rope`` values by halves or (``adjacent``) neighbours; ``position`` [T] int32; without ``freq`` no rotation."""
+    import torch
+    dim = q.shape[-1]
+    (T, H, qs), (Tk, G, ks), (Tv, Gv, vs) = _heads(q, "q", dim), _heads(k, "k", dim), _heads(v, "v", dim)
+    To, Ho, os = _heads(q_out, "q_out", dim)
+    if k.dtype != q.dtype or v.dtype != q.dtype or Tk != T or Tv != T or Gv != G or To != T or Ho != H:
+        raise ValueError("q, k, v and q_out do not fit together")
+    if q_out.dtype is not torch.bfloat16:
+        raise TypeError("q_out must be torch.bfloat16")
+    (pages, block, _, _), (ps, rs, hs, _) = _head_caches(k_cache, v_cache, G, dim)
+    f32, one = torch.float32, (dim,)
+    rope = 0 if freq is None else 2 * freq.shape[0]
+    if rope and position is None:
+        raise ValueError("a rotation needs position")
+    d = HeadStoreDesc(T, H, G, dim, rope, 1 if adjacent else 0, _code(q), block, pages, eps, qs, ks, vs, os, ps, rs, hs)
+    _check(lib.caee_head_store(ctypes.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                               None if q_norm is None else _at(q_norm, "q_norm", f32, one),
+                               None if k_norm is None else _at(k_norm, "k_norm", f32, one),
+                               None if freq is None else _at(freq, "freq", torch.float64, (rope // 2,)),
+                               None if position is None else _at(position, "position", torch.int32, (T,)),
+                               _at(slots, "slots", torch.int64, (T,)), q_out.data_ptr(), k_cache.data_ptr(),
+                               v_cache.data_ptr(), _stream(k_cache)))
+    return q_out
+
+
+@dataclass
+class Heads:
+    """Descriptor fields of attention with grouped heads that a layer keeps (see caee_head_desc_t)."""
+
+    heads: int
+    kv_heads: int
+    dim: int
+    scale: float
+    causal: bool = True
+    form: str = "auto"          # "auto" | "split" | "whole" (caee_head_form_t)
+
+    def desc(self, T: int, B: int, max_new: int, max_kv: int, block_size: int = 1, n_blocks: int = 1,
+             max_blocks: int = 1, tree_words: int = 0, q_stride: Optional[int] = None, strides=(0, 0, 0),
+             y_dtype: int = CAEE_BF16) -> HeadDesc:
+        if strides == (0, 0, 0):        # of one page of one row
+            strides = (self.kv_heads * self.dim, self.kv_heads * self.dim, self.dim)
+        return HeadDesc(T, B, self.heads, self.kv_heads, self.dim, block_size, n_blocks, max_blocks, max_new,
+                        1 if self.causal else 0, tree_words, HEAD_FORM_CODE[self.form], y_dtype, max_kv,
+                        self.heads * self.dim if q_stride is None else q_stride, *strides, self.scale)
+
+
+def head_workspace_size(att: Heads, T: int, B: int, max_new: int, max_kv: int, tree: bool = False) -> int:
+    n = ctypes.c_size_t(0)
+    d = att.desc(T, B, max_new, max_kv, tree_words=1 if tree else 0)
+    _check(lib.caee_head_workspace_size(ctypes.byref(d), ctypes.byref(n)))
+    return int(n.value)
+
+
+def alloc_head_workspace(att: Heads, T: int, B: int, max_new: int, max_kv: int, device, tree: bool = False):
+    """Workspace of ``head_attention`` calls of this size; ``tree``: of calls with a tree."""
+    import torch
+    return torch.empty(max(head_workspace_size(att, T, B, max_new, max_kv, tree), 256), dtype=torch.uint8, device=device)
+
+
+def head_attention(att: Heads, q, k_cache, v_cache, block_table, plan: dict, y, ws, max_new: int, max_kv: int, tree=None,
+                   lse=None):
+    """Attention of the new tokens over the paged keys and values (caee_head_attention).
+
+    ``q`` [T][heads][dim] bf16 (tokens may be strided); caches as in ``head_store``; ``plan`` with ``cu_new`` and
+    ``seq_len`` as ``paged_plan`` writes them; ``max_new``/``max_kv``: host bounds of a request's new tokens and of the
+    sum of ``seq_len``; ``y`` [T][heads][dim] bf16 or f32; ``tree`` [T][words] int32: bit j of a token's words is set
+    where it sees new token j of its request (None: causal, or all by ``att``); ``lse`` [T][heads] f32."""
+    import torch
+    i32, H, D = torch.int32, att.heads, att.dim
+    ws_at, ws_bytes = _workspace(ws)
+    T, heads, qs = _heads(q, "q", D)
+    if heads != H or q.dtype is not torch.bfloat16:
+        raise ValueError(f"q must be [T][{H}][{D}] torch.bfloat16")
+    (pages, block, _, _), (ps, rs, hs, _) = _head_caches(k_cache, v_cache, att.kv_heads, D)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B][max_blocks]")
+    B, width = block_table.shape
+    table_at = _at(block_table, "block_table", i32, (B, width))
+    cu_at, seq_at = _at(plan["cu_new"], "cu_new", i32, (B + 1,)), _at(plan["seq_len"], "seq_len", i32, (B,))
+    tree_at, words = None, 0
+    if tree is not None:
+        if tree.dim() != 2 or tree.shape[1] < 1:
+            raise ValueError(f"tree must be [{T}][words]")
+        words = tree.shape[1]
+        tree_at = _at(tree, "tree", i32, (T, words))
+    y_at = _at(y, "y", y.dtype, (T, H, D))
+    lse_at = None if lse is None else _at(lse, "lse", torch.float32, (T, H))
+    d = att.desc(T, B, max_new, max_kv, block, pages, width, words, qs, (ps, rs, hs), _code(y))
+    _check(lib.caee_head_attention(ctypes.byref(d), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table_at, cu_at,
+                                   seq_at, tree_at, y_at, lse_at, ws_at, ws_bytes, _stream(y)))
     return y
 
 
