@@ -15,6 +15,22 @@ struct HeadCache {
 caee_status_t head_cache(int kv_heads, int dim, int block_size, int n_blocks, long long page_stride,
                          long long row_stride, long long head_stride, HeadCache* c);
 
+// Split form: the work of all requests is one line of units, kTokens tokens of
+// one row tile (kRows rows of a request, its new tokens' heads of one group) each,
+// by request, group, row tile and token.  It is cut into equal shares, one a
+// workgroup; a share begins and ends inside a row tile's line, so a workgroup
+// leaves at most two partial results.
+struct HeadSplit {
+    int groups, rows, tokens;
+};
+constexpr HeadSplit kHeadFew = {512, 32, 128};     // up to 32 rows a request and group: two workgroups a CU
+
+struct HeadWs {
+    size_t meta;           // [B + 1] unit or query tile prefix sums, of more than 64 requests
+    size_t part, part_ml;  // split: [2 groups][rows][dim] partial sums and [..][rows][2] (maximum, sum)
+    size_t total;
+};
+
 struct HeadParams {
     int T, B, H, G, ratio, dim, max_blocks, max_new, causal, y_bf16, words;
     HeadCache c;
@@ -29,6 +45,9 @@ struct HeadParams {
     const uint32_t* tree;
     void* y;
     float* lse;
+    int32_t* meta;
+    float* part;
+    float* part_ml;
 };
 
 // New tokens and length of request b as the kernels use them: 0 <= new <=
@@ -49,6 +68,133 @@ __device__ inline int head_sees(const HeadParams& p, const LatentReq& r, int i) 
     return p.causal && !p.tree ? min(max(r.before + i + 1, 0), r.seq) : r.seq;
 }
 
+
+// Units of the split form are counted up to this; no request has more (a limit
+// of the host's, as is that of all requests while their lengths add up to
+// max_kv at most).
+constexpr int kHeadMaxUnits = INT32_MAX / 2;
+__device__ inline int head_add_units(int a, int b) { return min(a + b, kHeadMaxUnits); }
+__device__ inline int head_units(const HeadParams& p, const LatentReq& r, int rows, int tokens) {
+    return p.G * ((r.add * p.ratio + rows - 1) / rows) * ((r.seq + tokens - 1) / tokens);
+}
+
+// Request of a unit.  Up to 64 requests every wave sums their units up by
+// itself, a lane each; of more, p.meta has the sums.
+struct HeadLine {
+    LatentReq mine;      // lane b: request b
+    int at, total;       // its first unit; all units
+};
+template <class Units>
+__device__ inline HeadLine head_line(const HeadParams& p, Units&& units) {
+    HeadLine h = {};
+    if (p.B > kWave) {
+        h.total = p.meta[p.B];
+        return h;
+    }
+    const int lane = threadIdx.x & (kWave - 1);
+    int n = 0;
+    if (lane < p.B) {
+        h.mine = head_req(p, lane);
+        n = units(h.mine);
+    }
+    int sum = n;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int u = __shfl_up(sum, d);
+        if (lane >= d) sum = head_add_units(sum, u);
+    }
+    h.at = sum - n;
+    h.total = __builtin_amdgcn_readlane(sum, kWave - 1);
+    return h;
+}
+// Request b of the line: its lengths and first unit.
+__device__ inline LatentReq head_line_req(const HeadParams& p, const HeadLine& h, int b, int* at) {
+    if (p.B > kWave) {
+        *at = p.meta[b];
+        return head_req(p, b);
+    }
+    *at = __builtin_amdgcn_readlane(h.at, b);
+    return {__builtin_amdgcn_readlane(h.mine.t0, b), __builtin_amdgcn_readlane(h.mine.add, b),
+            __builtin_amdgcn_readlane(h.mine.seq, b), __builtin_amdgcn_readlane(h.mine.before, b)};
+}
+// Request that unit u is of (u below the total).
+__device__ inline int head_line_find(const HeadParams& p, const HeadLine& h, int u) {
+    if (p.B > kWave) return lat_find_wave(p.meta, p.B, u);
+    return 63 - __clzll(__ballot((int)(threadIdx.x & (kWave - 1)) < p.B && h.at <= u) | 1ull);
+}
+
+// Bits of a token's tree mask for new tokens bit .. bit + 31 of its request;
+// tokens before the new ones are seen.
+__device__ inline uint32_t head_tree_bits(const uint32_t* mask, int words, int bit) {
+    const int w = bit >> 5, sh = bit & 31;
+    const uint32_t a = w < 0 ? ~0u : w < words ? mask[w] : 0u;
+    const uint32_t b = w + 1 < 0 ? ~0u : w + 1 < words ? mask[w + 1] : 0u;
+    return sh ? (a >> sh) | (b << (32 - sh)) : a;
+}
+
+// Eight tokens from `pos` on (the last of a request again for those past it),
+// whose rows are fetched by one load where they lie in one page.
+struct HeadEight {
+    int page, at, span;       // of the first row; the others follow up to at + span
+    bool one;
+};
+__device__ inline int head_entry(const HeadParams& p, int b, unsigned j) {
+    const size_t i = (size_t)b * p.max_blocks + min(j, (unsigned)p.max_blocks - 1u);
+    return ((const __attribute__((address_space(4))) int32_t*)p.table)[i];
+}
+__device__ inline HeadEight head_eight(const HeadParams& p, int b, int seq, int pos) {
+    const int r0 = min(pos, seq - 1), r1 = min(pos + 7, seq - 1);
+    const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)r0 / (unsigned)p.c.block);
+    const int at = r0 - (int)(j * (unsigned)p.c.block);
+    return {head_entry(p, b, j), at, r1 - r0, at + (r1 - r0) < p.c.block};
+}
+// Byte offset of row `at` of a page's head g.
+__device__ inline long long head_offset(const HeadParams& p, int page, int at, int g) {
+    return 2 * (min(max(page, 0), p.c.n_blocks - 1) * p.c.page_stride + at * p.c.row_stride + g * p.c.head_stride);
+}
+
+// Whether values that are no numbers may have met weights of zero, or weights'
+// remainders, in a lane's sums o of a row whose weights add up to l.
+template <int NC>
+__device__ inline bool head_odd(const lat_f32x16 (&o)[NC], float l) {
+    float t = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t += fabsf(o[c][i]);
+    return !(t < INFINITY) && l < INFINITY;
+}
+// Puts that right, for what it may cost: where values of tokens that the row
+// sees (spans of `width` tokens, `step` apart, from tok0 to end) are infinities or
+// NaNs, the sum is theirs.
+template <int NC, class Sees>
+__device__ inline void head_put_odd(const HeadParams& p, int b, int g, int tok0, int width, int step, int end,
+                                    lat_f32x16 (&o)[NC], Sees&& sees) {
+    const int hf = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        float odd[16] = {};
+#pragma unroll 1
+        for (int t0 = tok0; t0 < end; t0 += step)
+#pragma unroll 1
+            for (int pos = t0; pos < min(t0 + width, end); ++pos) {
+                const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)pos / (unsigned)p.c.block);
+                const lat_u32x2* v = (const lat_u32x2*)((const char*)p.v + head_offset(p, head_entry(p, b, j), pos - (int)(j * (unsigned)p.c.block), g)) + 8 * c + hf;
+                const bool seen = sees(pos);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t w = v[2 * (i >> 2)][(i >> 1) & 1];
+                    const float x = __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
+                    if (seen && !(fabsf(x) < INFINITY)) odd[i] += x;
+                }
+            }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (odd[i] != 0.0f) o[c][i] = odd[i];
+    }
+}
+
+hipError_t launch_head_few(const HeadParams& p, hipStream_t s);
 hipError_t launch_head_attention(const HeadParams& p, hipStream_t s);
 
 }  // namespace caee

@@ -7,6 +7,30 @@
 namespace caee {
 namespace {
 
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Units of the split form are counted in 32 bits.
+bool split_fits(const caee_head_desc_t& d, const HeadSplit& sp) {
+    const double tiles = (double)d.kv_heads * (((long long)d.max_new * (d.heads / d.kv_heads) + sp.rows - 1) / sp.rows);
+    return (double)(d.max_kv / sp.tokens + d.B) * tiles <= kHeadMaxUnits;
+}
+
+HeadWs head_ws(const caee_head_desc_t& d) {
+    HeadWs L{};
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up256(bytes);
+        return here;
+    };
+    L.meta = take((size_t)(d.B + 1) * 4);
+    const size_t part_rows = (size_t)2 * kHeadFew.groups * kHeadFew.rows;
+    L.part = take(part_rows * d.dim * 4);
+    L.part_ml = take(part_rows * 2 * 4);
+    L.total = at;
+    return L;
+}
+
 caee_status_t check_heads(const caee_head_desc_t* d, HeadCache* c) {
     if (!d) return fail(CAEE_ERR_INVALID_ARG, "desc is NULL");
     if (d->T < 0 || d->B < 0) return fail(CAEE_ERR_INVALID_ARG, "T=%d and B=%d must be >= 0", d->T, d->B);
@@ -38,6 +62,9 @@ caee_status_t check_heads(const caee_head_desc_t* d, HeadCache* c) {
         return fail(CAEE_ERR_UNSUPPORTED, "%lld tokens in all exceed 2^30", (long long)d->max_kv);
     if (d->tree_words > 0 && d->form == CAEE_HEAD_WHOLE)
         return fail(CAEE_ERR_UNSUPPORTED, "trees are taken by the split form only");
+    if (d->form == CAEE_HEAD_SPLIT && !split_fits(*d, kHeadFew))
+        return fail(CAEE_ERR_UNSUPPORTED, "max_new=%d new tokens over max_kv=%lld: too many pairs for the split form",
+                    d->max_new, (long long)d->max_kv);
     return CAEE_OK;
 }
 
@@ -53,7 +80,7 @@ caee_status_t caee_head_workspace_size(const caee_head_desc_t* desc, size_t* byt
     if (!bytes) return fail(CAEE_ERR_INVALID_ARG, "bytes is NULL");
     HeadCache c;
     CAEE_TRY(check_heads(desc, &c));
-    *bytes = 0;
+    *bytes = head_ws(*desc).total;
     return CAEE_OK;
 }
 
@@ -75,6 +102,11 @@ caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, c
     CAEE_TRY(check_ptr(y, "y", any));
     CAEE_TRY(check_ptr(lse, "lse", false));
     if (!any) return CAEE_OK;
+    const HeadWs L = head_ws(d);
+    if (!ws) return fail(CAEE_ERR_WORKSPACE, "workspace is NULL");
+    if (((uintptr_t)ws & 255u) != 0) return fail(CAEE_ERR_WORKSPACE, "workspace is not 256-byte aligned");
+    if (ws_bytes < L.total) return fail(CAEE_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, L.total);
+    char* w = (char*)ws;
     HeadParams p{};
     p.T = d.T;
     p.B = d.B;
@@ -100,8 +132,13 @@ caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, c
     p.tree = d.tree_words > 0 ? tree : nullptr;
     p.y = y;
     p.lse = lse;
+    p.meta = (int32_t*)(w + L.meta);
+    p.part = (float*)(w + L.part);
+    p.part_ml = (float*)(w + L.part_ml);
     hipStream_t s = (hipStream_t)stream;
-    return timed_launch(CAEE_KERNEL_ATTENTION, s, "head attention", [&] { return launch_head_attention(p, s); });
+    return timed_launch(CAEE_KERNEL_ATTENTION, s, "head attention", [&] {
+        return d.form == CAEE_HEAD_WHOLE ? launch_head_attention(p, s) : launch_head_few(p, s);
+    });
 }
 
 }  // extern "C"

@@ -1,0 +1,436 @@
+// Attention with grouped heads, split form of few rows: decode steps and small
+// trees, up to 32 query rows a tile.
+//
+//   k_head_meta   unit prefix sums, where there are more than 64 requests
+//   k_head_few    a share of all requests' tokens a workgroup
+//   k_head_join   partial results of rows whose tokens several shares have
+#include "heads.h"
+
+namespace caee {
+namespace {
+
+constexpr int kFewThreads = 256;
+constexpr int kFewRows = kHeadFew.rows, kFewTokens = kHeadFew.tokens, kWaveTokens = 32;
+
+// First unit of each request (meta[b]; meta[B] the total).
+__global__ __launch_bounds__(kFewThreads) void k_head_meta(HeadParams p, HeadSplit sp) {
+    __shared__ int part[kFewThreads];
+    const int tid = threadIdx.x;
+    const int chunk = (p.B + kFewThreads - 1) / kFewThreads;
+    const int b0 = min(tid * chunk, p.B), b1 = min(b0 + chunk, p.B);
+    int n = 0;
+    for (int b = b0; b < b1; ++b) n = head_add_units(n, head_units(p, head_req(p, b), sp.rows, sp.tokens));
+    part[tid] = n;
+    __syncthreads();
+    for (int d = 1; d < kFewThreads; d <<= 1) {
+        const int u = tid >= d ? part[tid - d] : 0;
+        __syncthreads();
+        part[tid] = head_add_units(part[tid], u);
+        __syncthreads();
+    }
+    int at = tid > 0 ? part[tid - 1] : 0;
+    for (int b = b0; b < b1; ++b) {
+        p.meta[b] = at;
+        at = head_add_units(at, head_units(p, head_req(p, b), sp.rows, sp.tokens));
+    }
+    if (tid == kFewThreads - 1) p.meta[p.B] = part[kFewThreads - 1];
+}
+
+__device__ inline int head_share(const HeadSplit& sp, int total) { return max((total + sp.groups - 1) / sp.groups, 1); }
+// Neighbouring shares, which have row tiles of the same tokens, run on one XCD.
+__device__ inline int head_group(const HeadSplit& sp, int wg) { return wg % kXcds * (sp.groups / kXcds) + wg / kXcds; }
+__device__ inline int head_workgroup(const HeadSplit& sp, int g) {
+    const int per = sp.groups / kXcds;
+    return g % per * kXcds + g / per;
+}
+
+// Keys or values of 32 tokens for each wave: blocks of 8 rows x 128 bytes,
+// swizzled, so that one direct-to-LDS load fills a block.
+template <int D>
+struct FewStage {
+    lat_u32x4 v[4][kWaveTokens / 8][D / 64][kWave];
+};
+
+// A workgroup walks over its share, 32 tokens a wave and step.  A wave keeps its
+// tokens' keys and values in a part of LDS of its own and its row statistics and
+// sums in registers, so the waves meet only at a row tile's end.  Keys are the
+// M side of the scores, so that a lane holds 16 scores of one row, whose
+// weights are, in that order, a fragment of the second product; values are read
+// transposed.  The next keys are fetched as soon as the scores are made, the
+// next values after the sums; another workgroup of the CU fills the gaps.
+template <int D, bool kTree, bool kOnce>
+__global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
+#if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
+    constexpr int kG = D / 64, kJ = D / 16, NC = D / 32, kLoads = kWaveTokens / 8 * kG;
+    __shared__ FewStage<D> ks, vs;
+    __shared__ lat_u32x4 qs[kFewRows / 8][kG][kWave];
+    __shared__ float2 ml[4][kFewRows];
+    __shared__ int row_at[kFewRows];
+    const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const HeadLine line = head_line(p, [&](const LatentReq& r) { return head_units(p, r, kFewRows, kFewTokens); });
+    const int per = head_share(kHeadFew, line.total), group = head_group(kHeadFew, blockIdx.x);
+    const int share0 = (int)min((long long)group * per, (long long)line.total), share1 = min(share0 + per, line.total);
+
+    const int kp0 = (n >> 3) * (kG * kWave) + (n & 7) * 8 + (hf ^ lat_swz(n));
+    const int vrow = 4 * hf + ((lane & 15) >> 2);
+    int vpos[2][2];       // [column tile parity][eight of a 16-token step]
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            vpos[j][e] = 2 * (vrow * 8 + ((4 * j + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ lat_swz(8 * e + vrow))) + (lane & 1);
+    const uint32_t row_bytes = (uint32_t)p.c.row_stride * 2u;
+
+    for (int u = share0; u < share1;) {
+        const int b = head_line_find(p, line, u);
+        int at_u;
+        const LatentReq rq = head_line_req(p, line, b, &at_u);
+        const int rows = rq.add * p.ratio, tiles = (rows + kFewRows - 1) / kFewRows;
+        const int n_u = (rq.seq + kFewTokens - 1) / kFewTokens;
+        const int rel = u - at_u, tile = rel / n_u, first = rel - tile * n_u;
+        const int g = tile / tiles, rt = tile - g * tiles;
+        const int last = min(n_u, first + (share1 - u));
+        const bool whole = first == 0 && last == n_u, head = u == share0;
+        u += last - first;
+
+        const int row0 = rt * kFewRows, n_rows = min(kFewRows, rows - row0);
+        const int row = row0 + min(n, n_rows - 1), tok = row / p.ratio;
+        const int limit = head_sees(p, rq, tok);
+        // Tokens from lim_min on some row does not see.
+        const int lim_min = __builtin_amdgcn_readfirstlane(kTree ? min(max(rq.before, 0), rq.seq) : head_sees(p, rq, row0 / p.ratio));
+        const int end = min(last * kFewTokens, head_sees(p, rq, (row0 + n_rows - 1) / p.ratio));
+        const int tok0 = first * kFewTokens + kWaveTokens * wave;
+        const int steps = end > tok0 ? (end - tok0 + kFewTokens - 1) / kFewTokens : 0;
+        const uint32_t* mask = kTree ? p.tree + (size_t)(rq.t0 + tok) * p.words : nullptr;
+
+        auto eights = [&](int s, HeadEight (&e)[4]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = head_eight(p, b, rq.seq, tok0 + s * kFewTokens + 8 * i);
+        };
+        auto piece = [&](int i) __attribute__((always_inline)) { return 16u * ((lane & 7) ^ lat_swz(8 * (i & 1) + (lane >> 3))); };
+        // A buffer of size 0 where nothing is to be loaded: its loads cost no
+        // traffic, and their number does not depend on a branch.
+        auto fetch = [&](const uint16_t* cache, FewStage<D>& st, int s, const HeadEight (&e)[4], bool there) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __amdgpu_buffer_rsrc_t buf =
+                    __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)cache + head_offset(p, e[i].page, e[i].at, g)), 0,
+                                                      there && e[i].one ? kLatBufBytes : 0, kLatBufWord3);
+                const uint32_t at = (uint32_t)min(lane >> 3, e[i].span) * row_bytes + piece(i);
+#pragma unroll
+                for (int gg = 0; gg < kG; ++gg) {
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st.v[wave][i][gg][0], 16, at, 128 * gg, 0, kOnce ? 2 : 0);
+                }
+            }
+            if (there && !(e[0].one && e[1].one && e[2].one && e[3].one)) {
+                // Rows in several pages go one by one.
+                lat_wait_vm<0>();
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i) {
+                    const int p0 = tok0 + s * kFewTokens + 8 * i, r0 = min(p0, rq.seq - 1), r1 = min(p0 + 7, rq.seq - 1);
+                    if (r0 / p.c.block == r1 / p.c.block) continue;
+#pragma unroll 1
+                    for (int r = 0; r < 8; ++r) {
+                        const int pos = min(p0 + r, rq.seq - 1);
+                        const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)pos / (unsigned)p.c.block);
+                        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
+                            (void*)((const char*)cache + head_offset(p, head_entry(p, b, j), pos - (int)(j * (unsigned)p.c.block), g)), 0,
+                            kLatBufBytes, kLatBufWord3);
+                        if (lane >> 3 == r) {
+#pragma unroll
+                            for (int gg = 0; gg < kG; ++gg)
+                                __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st.v[wave][i][gg][0], 16, piece(i), 128 * gg, 0, 0);
+                        }
+                    }
+                }
+                lat_wait_vm<0>();
+            }
+        };
+
+        __syncthreads();       // the row tile before is done with LDS
+        {
+            const int r = 8 * wave + (lane >> 3), rr = row0 + min(r, n_rows - 1), i = rr / p.ratio;
+            const uint16_t* src = p.q + (size_t)(rq.t0 + i) * p.q_stride + (size_t)(g * p.ratio + rr - i * p.ratio) * D +
+                                  8 * ((lane & 7) ^ lat_swz(r));
+#pragma unroll
+            for (int gg = 0; gg < kG; ++gg)
+                __builtin_amdgcn_global_load_lds((lat_g_void*)(src + 64 * gg), (lat_lds_void*)&qs[wave][gg][0], 16, 0, 0);
+            if ((lane & 7) == 0) row_at[r] = (rq.t0 + i) * p.H + g * p.ratio + rr - i * p.ratio;
+        }
+        HeadEight now[4];
+        eights(0, now);
+        fetch(p.k, ks, 0, now, steps > 0);
+        fetch(p.v, vs, 0, now, steps > 0);
+        eights(1, now);
+        lat_wait_vm<2 * kLoads>();
+        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+        lat_barrier();
+        lat_u32x4 qf[kJ];
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) qf[j] = (&qs[0][0][0])[(kp0 ^ (2 * (j & 3))) + (j >> 2) * kWave];
+        lat_f32x16 o[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[c] = lat_f32x16{};
+        float m = kNoScore, l = 0.0f;
+        bool odd = false;      // an infinity or NaN was taken out of the values
+
+        for (int s = 0; s < steps; ++s) {
+            const int tb = tok0 + s * kFewTokens;
+            lat_wait_vm<kLoads>();             // the keys are there, the values may be on their way
+            asm volatile("" ::: "memory");
+            const lat_u32x4* keys = &ks.v[wave][0][0][0];
+            lat_f32x16 sc = {};
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < kJ; ++j) sc = lat_mma(keys[(kp0 ^ (2 * (j & 3))) + (j >> 2) * kWave], qf[j], sc);
+            __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(p.k, ks, s + 1, now, s + 1 < steps);
+            const bool masked = tb + kWaveTokens > lim_min;
+            if (masked) {
+                asm volatile("");       // a branch, not selects in every step
+                const uint32_t bits = kTree ? head_tree_bits(mask, p.words, tb - rq.before) : 0u;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int e = 8 * (i >> 2) + 4 * hf + (i & 3);
+                    if (tb + e >= limit || (kTree && !(bits >> e & 1))) sc[i] = -INFINITY;
+                }
+            }
+            // The weights by the running maximum; where one exceeds the slack the
+            // maximum moves and they are made again.
+            lat_u32x4 pf[2], pr[2];
+            float big = 0.0f, more = 0.0f;
+            auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float a = lat_weight(sc[8 * k + 2 * i], p.scale_log2, m);
+                        const float e = lat_weight(sc[8 * k + 2 * i + 1], p.scale_log2, m);
+                        big = fmaxf(fmaxf(big, a), e);
+                        pf[k][i] = lat_pack(a, e);
+                        const lat_f32x2 rest = lat_rest(pf[k][i], a, e);
+                        pr[k][i] = lat_pack(rest[0], rest[1]);
+                        more += a + e;
+                    }
+            };
+            if (s > 0) weights();
+            if (s == 0 || __any(big > kMaxWeight)) {
+                float mt = sc[0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) mt = fmaxf(mt, sc[i]);
+                mt = lat_max_pair(mt) * p.scale_log2;
+                const float mn = fmaxf(m, mt), f = __builtin_amdgcn_exp2f(m - mn);
+                l *= f;
+                m = mn;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) o[c] *= f;
+                more = 0.0f;
+                weights();
+            }
+            l += more;
+            lat_wait_vm<kLoads>();             // the values are there
+            asm volatile("" ::: "memory");
+            if (masked) {
+                // Tokens that some rows do not see may hold anything: infinities
+                // and NaNs must not meet their zero weights.
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (tb + 8 * i + (lane >> 3) >= lim_min) {
+#pragma unroll
+                        for (int gg = 0; gg < kG; ++gg) {
+                            const lat_u32x4 v = vs.v[wave][i][gg][lane];
+                            lat_u32x4 w;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                w[e] = lat_finite(v[e]);
+                                odd |= w[e] != v[e];
+                            }
+                            vs.v[wave][i][gg][lane] = w;
+                        }
+                    }
+                __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+                asm volatile("" ::: "memory");
+            }
+            const lat_u32x2* base = (const lat_u32x2*)&vs.v[wave][0][0][0];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    lat_u32x2 w[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const lat_u32x2* at = base + ((2 * k + e) * kG + (c >> 1)) * (2 * kWave) + vpos[c & 1][e];
+                        w[e] = __builtin_bit_cast(lat_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lat_lds_s16x4*)at));
+                    }
+                    const lat_u32x4 vf = {w[0][0], w[0][1], w[1][0], w[1][1]};
+                    o[c] = lat_mma(vf, pf[k], o[c]);
+                    o[c] = lat_mma(vf, pr[k], o[c]);
+                }
+            __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(p.v, vs, s + 1, now, s + 1 < steps);
+            eights(s + 2, now);
+        }
+        lat_wait_vm<0>();
+        l = lat_sum_pair(l);
+        if (__any(odd || head_odd(o, l)))
+            head_put_odd(p, b, g, tok0, kWaveTokens, kFewTokens, end, o, [&](int pos) {
+                return pos < limit && (!kTree || (head_tree_bits(mask, p.words, pos - rq.before) & 1));
+            });
+
+        // The waves' results through LDS, 16 rows in the wave's keys and 16 in its
+        // values, unit c (16 bytes) of a row at c ^ (row % units).
+        constexpr int kUnits = D / 4;
+        if (hf == 0) ml[wave][n] = make_float2(m, l);
+        auto place = [&](int w, int r, int c) __attribute__((always_inline)) {
+            return (float4*)(r < 16 ? &ks.v[w][0][0][0] : &vs.v[w][0][0][0]) + (r & 15) * kUnits + (c ^ (r & 15));
+        };
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *place(wave, n, 8 * c + 2 * i + hf) = make_float4(o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]);
+        __syncthreads();
+        const size_t slot0 = ((size_t)blockIdx.x * 2 + (head ? 0 : 1)) * kFewRows;
+        for (int x = threadIdx.x; x < n_rows * kUnits; x += kFewThreads) {
+            const int r = x / kUnits, c = x % kUnits;
+            float2 w[4];
+            float mx = kNoScore, lx = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = ml[i][r];
+                mx = fmaxf(mx, w[i].x);
+            }
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float f = __builtin_amdgcn_exp2f(w[i].x - mx);
+                const float4 t = *place(i, r, c);
+                lx += w[i].y * f;
+                if (f != 0.0f) v = make_float4(v.x + t.x * f, v.y + t.y * f, v.z + t.z * f, v.w + t.w * f);
+            }
+            if (!whole) {
+                *(float4*)(p.part + (slot0 + r) * D + 4 * c) = v;
+                if (c == 0) *(float2*)(p.part_ml + 2 * (slot0 + r)) = make_float2(mx, lx);
+                continue;
+            }
+            const float f = lat_inverse(lx);
+            const size_t at = (size_t)row_at[r];
+            if (p.y_bf16) *(lat_u32x2*)((uint16_t*)p.y + at * D + 4 * c) = lat_u32x2{lat_pack(v.x * f, v.y * f), lat_pack(v.z * f, v.w * f)};
+            else *(float4*)((float*)p.y + at * D + 4 * c) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+            if (p.lse && c == 0) p.lse[at] = lat_lse(mx, lx);
+        }
+    }
+#endif
+}
+
+// One wave per (token, head) row: rows whose tokens lie in one share are done;
+// the others are the sum of their shares' partial results; rows that see no
+// token are zero.
+template <int D>
+__global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, HeadSplit sp) {
+    constexpr int V = D / kWave;              // values of a lane
+    const int lane = threadIdx.x & 63;
+    const size_t at = (size_t)lat_workgroup() * (kFewThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int t = (int)(at / p.H), h = (int)(at - (size_t)t * p.H), kv = h / p.ratio;
+    if (t >= p.T) return;
+    const HeadLine line = head_line(p, [&](const LatentReq& r) { return head_units(p, r, sp.rows, sp.tokens); });
+    auto leave = [&](const float (&v)[V], float m, float l) {
+        const float inv = lat_inverse(l);
+        if (p.lse && lane == 0) p.lse[at] = lat_lse(m, l);
+        if constexpr (V == 2) {
+            if (p.y_bf16) ((uint32_t*)p.y)[at * (D / 2) + lane] = lat_pack(v[0] * inv, v[1] * inv);
+            else ((float2*)p.y)[at * (D / 2) + lane] = make_float2(v[0] * inv, v[1] * inv);
+        } else {
+            if (p.y_bf16) ((__bf16*)p.y)[at * D + lane] = (__bf16)(v[0] * inv);
+            else ((float*)p.y)[at * D + lane] = v[0] * inv;
+        }
+    };
+    float sum[V] = {};
+    const int end = p.B > 0 ? p.cu_new[p.B] : 0;
+    bool none = t >= end || t < p.cu_new[0];
+    int g0 = 0, g1 = 0, a = 0, rr = 0, per = 1;
+    if (!none) {
+        const int b = lat_find_wave(p.cu_new, p.B, t);
+        int at_u;
+        const LatentReq rq = head_line_req(p, line, b, &at_u);
+        const int n_u = (rq.seq + sp.tokens - 1) / sp.tokens, tiles = (rq.add * p.ratio + sp.rows - 1) / sp.rows;
+        rr = (t - rq.t0) * p.ratio + h - kv * p.ratio;
+        none = n_u == 0 || t - rq.t0 >= rq.add;
+        if (!none) {
+            per = head_share(sp, line.total);
+            a = at_u + (kv * tiles + rr / sp.rows) * n_u;
+            g0 = min(a / per, sp.groups - 1);
+            g1 = min((a + n_u - 1) / per, sp.groups - 1);
+        }
+    }
+    if (none) return leave(sum, kNoScore, 0.0f);
+    if (g0 == g1) return;
+    // Share g's slot: its second when the row tile's line begins inside it.
+    auto slot = [&](int g) {
+        return ((size_t)head_workgroup(sp, g) * 2 + (g == g0 && a > g0 * per ? 1 : 0)) * sp.rows + rr % sp.rows;
+    };
+    const float2* ml = (const float2*)p.part_ml;
+    float m = kNoScore, l = 0.0f;
+    for (int g = g0; g <= g1; g += kWave) {
+        const float2 v = g + lane <= g1 ? ml[slot(g + lane)] : make_float2(kNoScore, 0.0f);
+        float mn = fmaxf(m, v.x);
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) mn = fmaxf(mn, __shfl_xor(mn, d));
+        float s = v.y * __builtin_amdgcn_exp2f(v.x - mn);
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d);
+        l = l * __builtin_amdgcn_exp2f(m - mn) + s;
+        m = mn;
+    }
+    auto add = [&](int g, auto count) __attribute__((always_inline)) {
+        constexpr int U = decltype(count)::value;       // partial rows in flight
+        float w[U], x[U][V];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const size_t sl = slot(g + i);
+            w[i] = ml[sl].x;
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[i][v] = p.part[sl * D + V * lane + v];
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const float f = __builtin_amdgcn_exp2f(w[i] - m);
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[v] += f != 0.0f ? x[i][v] * f : 0.0f;
+        }
+    };
+    int g = g0;
+    for (; g + 7 <= g1; g += 8) add(g, LatInt<8>{});
+    for (; g <= g1; ++g) add(g, LatInt<1>{});
+    leave(sum, m, l);
+}
+
+}  // namespace
+
+hipError_t launch_head_few(const HeadParams& p, hipStream_t s) {
+    if (p.B > kWave) hipLaunchKernelGGL(k_head_meta, dim3(1), dim3(kFewThreads), 0, s, p, kHeadFew);
+    const dim3 grid(kHeadFew.groups), block(kFewThreads);
+    const bool once = (long long)p.max_new * p.ratio <= kFewRows;      // one row tile a request and group reads its tokens
+    auto run = [&](auto dim) {
+        constexpr int D = decltype(dim)::value;
+        auto few = [&](auto tree, auto reads) {
+            hipLaunchKernelGGL((k_head_few<D, decltype(tree)::value != 0, decltype(reads)::value != 0>), grid, block, 0, s, p);
+        };
+        if (p.tree) {
+            if (once) few(LatInt<1>{}, LatInt<1>{});
+            else few(LatInt<1>{}, LatInt<0>{});
+        } else {
+            if (once) few(LatInt<0>{}, LatInt<1>{});
+            else few(LatInt<0>{}, LatInt<0>{});
+        }
+        hipLaunchKernelGGL(k_head_join<D>, lat_grid((unsigned)(((long long)p.T * p.H + 3) / 4)), block, 0, s, p, kHeadFew);
+    };
+    if (p.dim == 128) run(LatInt<128>{});
+    else run(LatInt<64>{});
+    return hipGetLastError();
+}
+
+}  // namespace caee
