@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcaee.so")
 SOURCES = ["api.hip", "route.hip", "ffn.hip", "ffn_fp8.hip", "ffn_gemm.hip", "ffn_prefill8.hip", "ffn_prefill8_down.hip",
            "offload.hip", "paged.hip", "latent.hip", "latent_absorbed.hip", "latent_expanded.hip", "block_matmul.hip",
-           "heads.hip", "heads_store.hip", "heads_few.hip", "heads_attend.hip"]
+           "heads.hip", "heads_store.hip", "heads_few.hip", "heads_tile_64.hip", "heads_tile_128.hip"]
 
 # Packed-fp32 VALU ops are disabled on every HIP translation unit.
 HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

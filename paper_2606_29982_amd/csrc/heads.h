@@ -23,7 +23,18 @@ caee_status_t head_cache(int kv_heads, int dim, int block_size, int n_blocks, lo
 struct HeadSplit {
     int groups, rows, tokens;
 };
-constexpr HeadSplit kHeadFew = {512, 32, 128};     // up to 32 rows a request and group: two workgroups a CU
+constexpr HeadSplit kHeadFew = {512, 32, 128};     // few rows: two workgroups a CU
+constexpr HeadSplit kHeadMany = {256, 256, 64};    // many rows: one
+constexpr unsigned kHeadBlank = 64;                // workgroups that blank the rows of no request (whole form)
+// A quotient of uniform numbers, in a scalar register.
+__device__ inline int head_div(int a, int b) { return __builtin_amdgcn_readfirstlane(a / b); }
+__device__ inline int head_share(const HeadSplit& sp, int total) { return max((total + sp.groups - 1) / sp.groups, 1); }
+// Neighbouring shares, which have row tiles of the same tokens, run on one XCD.
+__device__ inline int head_group(const HeadSplit& sp, int wg) { return wg % kXcds * (sp.groups / kXcds) + wg / kXcds; }
+__device__ inline int head_workgroup(const HeadSplit& sp, int g) {
+    const int per = sp.groups / kXcds;
+    return g % per * kXcds + g / per;
+}
 
 struct HeadWs {
     size_t meta;           // [B + 1] unit or query tile prefix sums, of more than 64 requests
@@ -88,7 +99,7 @@ template <class Units>
 __device__ inline HeadLine head_line(const HeadParams& p, Units&& units) {
     HeadLine h = {};
     if (p.B > kWave) {
-        h.total = p.meta[p.B];
+        h.total = __builtin_amdgcn_readfirstlane(p.meta[p.B]);
         return h;
     }
     const int lane = threadIdx.x & (kWave - 1);
@@ -110,8 +121,10 @@ __device__ inline HeadLine head_line(const HeadParams& p, Units&& units) {
 // Request b of the line: its lengths and first unit.
 __device__ inline LatentReq head_line_req(const HeadParams& p, const HeadLine& h, int b, int* at) {
     if (p.B > kWave) {
-        *at = p.meta[b];
-        return head_req(p, b);
+        *at = __builtin_amdgcn_readfirstlane(p.meta[b]);
+        const LatentReq r = head_req(p, b);
+        return {__builtin_amdgcn_readfirstlane(r.t0), __builtin_amdgcn_readfirstlane(r.add),
+                __builtin_amdgcn_readfirstlane(r.seq), __builtin_amdgcn_readfirstlane(r.before)};
     }
     *at = __builtin_amdgcn_readlane(h.at, b);
     return {__builtin_amdgcn_readlane(h.mine.t0, b), __builtin_amdgcn_readlane(h.mine.add, b),
@@ -164,37 +177,41 @@ __device__ inline bool head_odd(const lat_f32x16 (&o)[NC], float l) {
         for (int i = 0; i < 16; ++i) t += fabsf(o[c][i]);
     return !(t < INFINITY) && l < INFINITY;
 }
-// Puts that right, for what it may cost: where values of tokens that the row
-// sees (spans of `width` tokens, `step` apart, from tok0 to end) are infinities or
-// NaNs, the sum is theirs.
-template <int NC, class Sees>
-__device__ inline void head_put_odd(const HeadParams& p, int b, int g, int tok0, int width, int step, int end,
-                                    lat_f32x16 (&o)[NC], Sees&& sees) {
-    const int hf = (threadIdx.x >> 5) & 1;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        float odd[16] = {};
+// Puts that right, for what it may cost, after the sums of row n (a lane of each
+// half) were written: where values of tokens that the row sees (spans of `width`
+// tokens, `step` apart, from tok0 to end) are infinities or NaNs, the sum is
+// theirs: put(d, sum).
+template <int D, class Sees, class Put>
+__device__ inline void head_put_odd(const HeadParams& p, int b, int g, int tok0, int width, int step, int end, Sees&& sees,
+                                    Put&& put) {
+#pragma unroll 1
+    for (int c = (threadIdx.x >> 5) & 1; c < D / 4; c += 2) {
+        float odd[4] = {};
 #pragma unroll 1
         for (int t0 = tok0; t0 < end; t0 += step)
 #pragma unroll 1
             for (int pos = t0; pos < min(t0 + width, end); ++pos) {
                 const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)pos / (unsigned)p.c.block);
-                const lat_u32x2* v = (const lat_u32x2*)((const char*)p.v + head_offset(p, head_entry(p, b, j), pos - (int)(j * (unsigned)p.c.block), g)) + 8 * c + hf;
+                const char* row = (const char*)p.v + head_offset(p, head_entry(p, b, j), pos - (int)(j * (unsigned)p.c.block), g);
+                const lat_u32x2 v = ((const lat_u32x2*)row)[c];
                 const bool seen = sees(pos);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const uint32_t w = v[2 * (i >> 2)][(i >> 1) & 1];
-                    const float x = __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
+                for (int i = 0; i < 4; ++i) {
+                    const float x = __uint_as_float(i & 1 ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16);
                     if (seen && !(fabsf(x) < INFINITY)) odd[i] += x;
                 }
             }
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (odd[i] != 0.0f) o[c][i] = odd[i];
+        for (int i = 0; i < 4; ++i)
+            if (odd[i] != 0.0f) put(4 * c + i, odd[i]);
     }
 }
 
+// Split form of few and of many rows; whole form.
 hipError_t launch_head_few(const HeadParams& p, hipStream_t s);
-hipError_t launch_head_attention(const HeadParams& p, hipStream_t s);
+hipError_t launch_head_many(const HeadParams& p, hipStream_t s);
+hipError_t launch_head_whole(const HeadParams& p, hipStream_t s);
+hipError_t launch_head_tile_64(const HeadParams& p, bool split, unsigned grid, int tiles, hipStream_t s);
+hipError_t launch_head_tile_128(const HeadParams& p, bool split, unsigned grid, int tiles, hipStream_t s);
 
 }  // namespace caee

@@ -2,6 +2,8 @@
 // launches of caee_head_attention.
 #include <math.h>
 
+#include <algorithm>
+
 #include "heads.h"
 
 namespace caee {
@@ -15,6 +17,16 @@ bool split_fits(const caee_head_desc_t& d, const HeadSplit& sp) {
     return (double)(d.max_kv / sp.tokens + d.B) * tiles <= kHeadMaxUnits;
 }
 
+// One of three: the split form of few rows, of many, the whole form.
+bool head_whole(const caee_head_desc_t& d) {
+    if (d.form != CAEE_HEAD_AUTO) return d.form == CAEE_HEAD_WHOLE;
+    if (d.tree_words > 0 || !split_fits(d, kHeadMany)) return d.tree_words == 0;
+    return d.T >= 64ll * (d.B > 0 ? d.B : 1) && d.max_kv <= 8ll * d.T;
+}
+bool head_few(const caee_head_desc_t& d) {
+    return (long long)d.max_new * (d.heads / d.kv_heads) <= 64 && split_fits(d, kHeadFew);
+}
+
 HeadWs head_ws(const caee_head_desc_t& d) {
     HeadWs L{};
     size_t at = 0;
@@ -24,7 +36,9 @@ HeadWs head_ws(const caee_head_desc_t& d) {
         return here;
     };
     L.meta = take((size_t)(d.B + 1) * 4);
-    const size_t part_rows = (size_t)2 * kHeadFew.groups * kHeadFew.rows;
+    // One size for whatever the split form takes, and for AUTO: smaller calls need no more.
+    const size_t part_rows =
+        d.form == CAEE_HEAD_WHOLE ? 0 : (size_t)2 * std::max(kHeadFew.groups * kHeadFew.rows, kHeadMany.groups * kHeadMany.rows);
     L.part = take(part_rows * d.dim * 4);
     L.part_ml = take(part_rows * 2 * 4);
     L.total = at;
@@ -62,7 +76,7 @@ caee_status_t check_heads(const caee_head_desc_t* d, HeadCache* c) {
         return fail(CAEE_ERR_UNSUPPORTED, "%lld tokens in all exceed 2^30", (long long)d->max_kv);
     if (d->tree_words > 0 && d->form == CAEE_HEAD_WHOLE)
         return fail(CAEE_ERR_UNSUPPORTED, "trees are taken by the split form only");
-    if (d->form == CAEE_HEAD_SPLIT && !split_fits(*d, kHeadFew))
+    if ((d->form == CAEE_HEAD_SPLIT || d->tree_words > 0) && !split_fits(*d, kHeadMany))
         return fail(CAEE_ERR_UNSUPPORTED, "max_new=%d new tokens over max_kv=%lld: too many pairs for the split form",
                     d->max_new, (long long)d->max_kv);
     return CAEE_OK;
@@ -137,7 +151,7 @@ caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, c
     p.part_ml = (float*)(w + L.part_ml);
     hipStream_t s = (hipStream_t)stream;
     return timed_launch(CAEE_KERNEL_ATTENTION, s, "head attention", [&] {
-        return d.form == CAEE_HEAD_WHOLE ? launch_head_attention(p, s) : launch_head_few(p, s);
+        return head_whole(d) ? launch_head_whole(p, s) : head_few(d) ? launch_head_few(p, s) : launch_head_many(p, s);
     });
 }
 

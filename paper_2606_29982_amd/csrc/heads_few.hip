@@ -4,6 +4,8 @@
 //   k_head_meta   unit prefix sums, where there are more than 64 requests
 //   k_head_few    a share of all requests' tokens a workgroup
 //   k_head_join   partial results of rows whose tokens several shares have
+#include <algorithm>
+
 #include "heads.h"
 
 namespace caee {
@@ -12,14 +14,18 @@ namespace {
 constexpr int kFewThreads = 256;
 constexpr int kFewRows = kHeadFew.rows, kFewTokens = kHeadFew.tokens, kWaveTokens = 32;
 
-// First unit of each request (meta[b]; meta[B] the total).
-__global__ __launch_bounds__(kFewThreads) void k_head_meta(HeadParams p, HeadSplit sp) {
+// First unit (whole form: row tile) of each request (meta[b]; meta[B] the total).
+__global__ __launch_bounds__(kFewThreads) void k_head_meta(HeadParams p, HeadSplit sp, int whole) {
     __shared__ int part[kFewThreads];
     const int tid = threadIdx.x;
     const int chunk = (p.B + kFewThreads - 1) / kFewThreads;
     const int b0 = min(tid * chunk, p.B), b1 = min(b0 + chunk, p.B);
+    auto units = [&](int b) {
+        const LatentReq r = head_req(p, b);
+        return whole ? (r.add * p.ratio + sp.rows - 1) / sp.rows : head_units(p, r, sp.rows, sp.tokens);
+    };
     int n = 0;
-    for (int b = b0; b < b1; ++b) n = head_add_units(n, head_units(p, head_req(p, b), sp.rows, sp.tokens));
+    for (int b = b0; b < b1; ++b) n = head_add_units(n, units(b));
     part[tid] = n;
     __syncthreads();
     for (int d = 1; d < kFewThreads; d <<= 1) {
@@ -31,17 +37,9 @@ __global__ __launch_bounds__(kFewThreads) void k_head_meta(HeadParams p, HeadSpl
     int at = tid > 0 ? part[tid - 1] : 0;
     for (int b = b0; b < b1; ++b) {
         p.meta[b] = at;
-        at = head_add_units(at, head_units(p, head_req(p, b), sp.rows, sp.tokens));
+        at = head_add_units(at, units(b));
     }
     if (tid == kFewThreads - 1) p.meta[p.B] = part[kFewThreads - 1];
-}
-
-__device__ inline int head_share(const HeadSplit& sp, int total) { return max((total + sp.groups - 1) / sp.groups, 1); }
-// Neighbouring shares, which have row tiles of the same tokens, run on one XCD.
-__device__ inline int head_group(const HeadSplit& sp, int wg) { return wg % kXcds * (sp.groups / kXcds) + wg / kXcds; }
-__device__ inline int head_workgroup(const HeadSplit& sp, int g) {
-    const int per = sp.groups / kXcds;
-    return g % per * kXcds + g / per;
 }
 
 // Keys or values of 32 tokens for each wave: blocks of 8 rows x 128 bytes,
@@ -88,8 +86,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         const LatentReq rq = head_line_req(p, line, b, &at_u);
         const int rows = rq.add * p.ratio, tiles = (rows + kFewRows - 1) / kFewRows;
         const int n_u = (rq.seq + kFewTokens - 1) / kFewTokens;
-        const int rel = u - at_u, tile = rel / n_u, first = rel - tile * n_u;
-        const int g = tile / tiles, rt = tile - g * tiles;
+        const int rel = u - at_u, tile = head_div(rel, n_u), first = rel - tile * n_u;
+        const int g = head_div(tile, tiles), rt = tile - g * tiles;
         const int last = min(n_u, first + (share1 - u));
         const bool whole = first == 0 && last == n_u, head = u == share0;
         u += last - first;
@@ -98,8 +96,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         const int row = row0 + min(n, n_rows - 1), tok = row / p.ratio;
         const int limit = head_sees(p, rq, tok);
         // Tokens from lim_min on some row does not see.
-        const int lim_min = __builtin_amdgcn_readfirstlane(kTree ? min(max(rq.before, 0), rq.seq) : head_sees(p, rq, row0 / p.ratio));
-        const int end = min(last * kFewTokens, head_sees(p, rq, (row0 + n_rows - 1) / p.ratio));
+        const int lim_min = kTree ? min(max(rq.before, 0), rq.seq) : head_sees(p, rq, head_div(row0, p.ratio));
+        const int end = min(last * kFewTokens, head_sees(p, rq, head_div(row0 + n_rows - 1, p.ratio)));
         const int tok0 = first * kFewTokens + kWaveTokens * wave;
         const int steps = end > tok0 ? (end - tok0 + kFewTokens - 1) / kFewTokens : 0;
         const uint32_t* mask = kTree ? p.tree + (size_t)(rq.t0 + tok) * p.words : nullptr;
@@ -190,11 +188,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
             const bool masked = tb + kWaveTokens > lim_min;
             if (masked) {
                 asm volatile("");       // a branch, not selects in every step
-                const uint32_t bits = kTree ? head_tree_bits(mask, p.words, tb - rq.before) : 0u;
+                const int left = limit - (tb + 4 * hf);
+                const uint32_t bits = kTree ? head_tree_bits(mask, p.words, tb - rq.before) >> (4 * hf) : 0u;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int e = 8 * (i >> 2) + 4 * hf + (i & 3);
-                    if (tb + e >= limit || (kTree && !(bits >> e & 1))) sc[i] = -INFINITY;
+                    constexpr auto at = [](int x) constexpr { return 8 * (x >> 2) + (x & 3); };
+                    if (at(i) >= left || (kTree && !(bits >> at(i) & 1))) sc[i] = -INFINITY;
                 }
             }
             // The weights by the running maximum; where one exceeds the slack the
@@ -275,14 +274,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         }
         lat_wait_vm<0>();
         l = lat_sum_pair(l);
-        if (__any(odd || head_odd(o, l)))
-            head_put_odd(p, b, g, tok0, kWaveTokens, kFewTokens, end, o, [&](int pos) {
-                return pos < limit && (!kTree || (head_tree_bits(mask, p.words, pos - rq.before) & 1));
-            });
-
+        odd |= head_odd(o, l);
         // The waves' results through LDS, 16 rows in the wave's keys and 16 in its
         // values, unit c (16 bytes) of a row at c ^ (row % units).
         constexpr int kUnits = D / 4;
+        int ln = lane;         // addresses made here: the registers that they would take through the loop are not there
+        asm volatile("" : "+v"(ln));
         if (hf == 0) ml[wave][n] = make_float2(m, l);
         auto place = [&](int w, int r, int c) __attribute__((always_inline)) {
             return (float4*)(r < 16 ? &ks.v[w][0][0][0] : &vs.v[w][0][0][0]) + (r & 15) * kUnits + (c ^ (r & 15));
@@ -291,7 +288,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                *place(wave, n, 8 * c + 2 * i + hf) = make_float4(o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]);
+                *place(wave, ln & 31, 8 * c + 2 * i + (ln >> 5)) = make_float4(o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]);
+        if (__any(odd)) {
+            auto sees = [&](int pos) { return pos < limit && (!kTree || (head_tree_bits(mask, p.words, pos - rq.before) & 1)); };
+            head_put_odd<D>(p, b, g, tok0, kWaveTokens, kFewTokens, end, sees,
+                            [&](int d, float v) { ((float*)place(wave, n, d >> 2))[d & 3] = v; });
+        }
         __syncthreads();
         const size_t slot0 = ((size_t)blockIdx.x * 2 + (head ? 0 : 1)) * kFewRows;
         for (int x = threadIdx.x; x < n_rows * kUnits; x += kFewThreads) {
@@ -387,17 +389,19 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, HeadSpl
     }
     auto add = [&](int g, auto count) __attribute__((always_inline)) {
         constexpr int U = decltype(count)::value;       // partial rows in flight
-        float w[U], x[U][V];
+        float2 w[U];
+        float x[U][V];
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const size_t sl = slot(g + i);
-            w[i] = ml[sl].x;
+            w[i] = ml[sl];
 #pragma unroll
             for (int v = 0; v < V; ++v) x[i][v] = p.part[sl * D + V * lane + v];
         }
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const float f = __builtin_amdgcn_exp2f(w[i] - m);
+            // shares that saw nothing for the row have written no sums
+            const float f = w[i].y != 0.0f ? __builtin_amdgcn_exp2f(w[i].x - m) : 0.0f;
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[v] += f != 0.0f ? x[i][v] * f : 0.0f;
         }
@@ -410,27 +414,61 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, HeadSpl
 
 }  // namespace
 
+namespace {
+
+void meta(const HeadParams& p, const HeadSplit& sp, int whole, hipStream_t s) {
+    if (p.B > kWave) hipLaunchKernelGGL(k_head_meta, dim3(1), dim3(kFewThreads), 0, s, p, sp, whole);
+}
+
+void join(const HeadParams& p, const HeadSplit& sp, hipStream_t s) {
+    const dim3 grid = lat_grid((unsigned)(((long long)p.T * p.H + 3) / 4));
+    if (p.dim == 128) hipLaunchKernelGGL(k_head_join<128>, grid, dim3(kFewThreads), 0, s, p, sp);
+    else hipLaunchKernelGGL(k_head_join<64>, grid, dim3(kFewThreads), 0, s, p, sp);
+}
+
+hipError_t tile(const HeadParams& p, bool split, unsigned grid, int tiles, hipStream_t s) {
+    return p.dim == 128 ? launch_head_tile_128(p, split, grid, tiles, s) : launch_head_tile_64(p, split, grid, tiles, s);
+}
+
+}  // namespace
+
 hipError_t launch_head_few(const HeadParams& p, hipStream_t s) {
-    if (p.B > kWave) hipLaunchKernelGGL(k_head_meta, dim3(1), dim3(kFewThreads), 0, s, p, kHeadFew);
-    const dim3 grid(kHeadFew.groups), block(kFewThreads);
+    meta(p, kHeadFew, 0, s);
     const bool once = (long long)p.max_new * p.ratio <= kFewRows;      // one row tile a request and group reads its tokens
-    auto run = [&](auto dim) {
-        constexpr int D = decltype(dim)::value;
-        auto few = [&](auto tree, auto reads) {
-            hipLaunchKernelGGL((k_head_few<D, decltype(tree)::value != 0, decltype(reads)::value != 0>), grid, block, 0, s, p);
-        };
-        if (p.tree) {
-            if (once) few(LatInt<1>{}, LatInt<1>{});
-            else few(LatInt<1>{}, LatInt<0>{});
-        } else {
-            if (once) few(LatInt<0>{}, LatInt<1>{});
-            else few(LatInt<0>{}, LatInt<0>{});
-        }
-        hipLaunchKernelGGL(k_head_join<D>, lat_grid((unsigned)(((long long)p.T * p.H + 3) / 4)), block, 0, s, p, kHeadFew);
+    auto few = [&](auto dim, auto tree, auto reads) {
+        hipLaunchKernelGGL((k_head_few<decltype(dim)::value, decltype(tree)::value != 0, decltype(reads)::value != 0>),
+                           dim3(kHeadFew.groups), dim3(kFewThreads), 0, s, p);
     };
-    if (p.dim == 128) run(LatInt<128>{});
-    else run(LatInt<64>{});
+    auto trees = [&](auto dim, auto reads) {
+        if (p.tree) few(dim, LatInt<1>{}, reads);
+        else few(dim, LatInt<0>{}, reads);
+    };
+    auto dims = [&](auto reads) {
+        if (p.dim == 128) trees(LatInt<128>{}, reads);
+        else trees(LatInt<64>{}, reads);
+    };
+    if (once) dims(LatInt<1>{});
+    else dims(LatInt<0>{});
+    join(p, kHeadFew, s);
     return hipGetLastError();
+}
+
+hipError_t launch_head_many(const HeadParams& p, hipStream_t s) {
+    meta(p, kHeadMany, 0, s);
+    const hipError_t err = tile(p, true, kHeadMany.groups, 0, s);
+    if (err != hipSuccess) return err;
+    join(p, kHeadMany, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_head_whole(const HeadParams& p, hipStream_t s) {
+    meta(p, kHeadMany, 1, s);
+    long long tiles = std::max(p.B, 1) * (((long long)p.max_new * p.ratio + kHeadMany.rows - 1) / kHeadMany.rows);
+    tiles = std::max(std::min(tiles, (long long)p.T * p.ratio / kHeadMany.rows + p.B), 1ll);
+    // Row tiles of all heads; where some XCDs share a head, as many for each of them; blanks.
+    long long grid = tiles * p.G;
+    if (p.G % kXcds && kXcds % p.G == 0) grid = (tiles + kXcds / p.G - 1) / (kXcds / p.G) * kXcds;
+    return tile(p, false, (unsigned)(grid + kHeadBlank), (int)tiles, s);
 }
 
 }  // namespace caee
