@@ -584,7 +584,7 @@ typedef struct caee_head_desc {
     int32_t max_blocks;   /* row length of block_table */
     int32_t max_new;      /* no request has more new tokens than this */
     int32_t causal;       /* 1: new token i of a request sees its first seq_len - new + i + 1 tokens; 0: all seq_len */
-    int32_t tree_words;   /* 0, or 32-bit words of a token's tree mask, 1..32 (causal is 1, form not CAEE_HEAD_WHOLE) */
+    int32_t tree_words;   /* 0, or 32-bit words of a token's tree mask, 1..32 (causal is 1) */
     int32_t form;         /* caee_head_form_t */
     int32_t y_dtype;      /* CAEE_BF16 or CAEE_F32 */
     int64_t max_kv;       /* sum of seq_len at most, <= 2^30 */

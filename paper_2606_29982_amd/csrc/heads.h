@@ -166,6 +166,18 @@ __device__ inline long long head_offset(const HeadParams& p, int page, int at, i
     return 2 * (min(max(page, 0), p.c.n_blocks - 1) * p.c.page_stride + at * p.c.row_stride + g * p.c.head_stride);
 }
 
+// Adds a partial result (sums x of weights by the maximum w.x, whose total is w.y)
+// to one.
+__device__ inline void head_merge(float4& v, float& m, float& l, const float4& x, const float2& w) {
+    const float mn = fmaxf(m, w.x), f = __builtin_amdgcn_exp2f(m - mn), e = __builtin_amdgcn_exp2f(w.x - mn);
+    // (an infinity among the sums stays where it is)
+    if (f == 0.0f || l == 0.0f) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    else v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+    if (e != 0.0f) v = make_float4(v.x + x.x * e, v.y + x.y * e, v.z + x.z * e, v.w + x.w * e);
+    l = l * f + w.y * e;
+    m = mn;
+}
+
 // Whether values that are no numbers may have met weights of zero, or weights'
 // remainders, in a lane's sums o of a row whose weights add up to l.
 template <int NC>

@@ -20,11 +20,12 @@ bool split_fits(const caee_head_desc_t& d, const HeadSplit& sp) {
 // One of three: the split form of few rows, of many, the whole form.
 bool head_whole(const caee_head_desc_t& d) {
     if (d.form != CAEE_HEAD_AUTO) return d.form == CAEE_HEAD_WHOLE;
-    if (d.tree_words > 0 || !split_fits(d, kHeadMany)) return d.tree_words == 0;
+    if (!split_fits(d, kHeadMany)) return true;
     return d.T >= 64ll * (d.B > 0 ? d.B : 1) && d.max_kv <= 8ll * d.T;
 }
+constexpr int kHeadFewRows = 64;
 bool head_few(const caee_head_desc_t& d) {
-    return (long long)d.max_new * (d.heads / d.kv_heads) <= 64 && split_fits(d, kHeadFew);
+    return (long long)d.max_new * (d.heads / d.kv_heads) <= kHeadFewRows && split_fits(d, kHeadFew);
 }
 
 HeadWs head_ws(const caee_head_desc_t& d) {
@@ -74,9 +75,7 @@ caee_status_t check_heads(const caee_head_desc_t* d, HeadCache* c) {
     CAEE_TRY(head_cache(d->kv_heads, d->dim, d->block_size, d->n_blocks, d->page_stride, d->row_stride, d->head_stride, c));
     if (d->max_kv > (1 << 30))
         return fail(CAEE_ERR_UNSUPPORTED, "%lld tokens in all exceed 2^30", (long long)d->max_kv);
-    if (d->tree_words > 0 && d->form == CAEE_HEAD_WHOLE)
-        return fail(CAEE_ERR_UNSUPPORTED, "trees are taken by the split form only");
-    if ((d->form == CAEE_HEAD_SPLIT || d->tree_words > 0) && !split_fits(*d, kHeadMany))
+    if (d->form == CAEE_HEAD_SPLIT && !split_fits(*d, kHeadMany))
         return fail(CAEE_ERR_UNSUPPORTED, "max_new=%d new tokens over max_kv=%lld: too many pairs for the split form",
                     d->max_new, (long long)d->max_kv);
     return CAEE_OK;

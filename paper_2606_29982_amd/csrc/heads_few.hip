@@ -328,88 +328,113 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
 #endif
 }
 
-// One wave per (token, head) row: rows whose tokens lie in one share are done;
-// the others are the sum of their shares' partial results; rows that see no
-// token are zero.
-template <int D>
+// Rows whose tokens lie in one share are done; the others are the sum of their
+// shares' partial results, D / 4 lanes a row and 16 bytes a lane; rows that see
+// no token are zero.  A workgroup has a token's heads: few rows, which have many
+// partial results, one pass of heads (64 / (D / 4)) whose shares go over the four
+// waves in turn, their sums added in order; many rows four passes a wave.
+constexpr int kJoinRows = 4096;        // (token, head) rows from which on they are many
+template <int D, bool kMany>
 __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, HeadSplit sp) {
-    constexpr int V = D / kWave;              // values of a lane
-    const int lane = threadIdx.x & 63;
-    const size_t at = (size_t)lat_workgroup() * (kFewThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int t = (int)(at / p.H), h = (int)(at - (size_t)t * p.H), kv = h / p.ratio;
+    constexpr int kLanes = D / 4, kHeads = kWave / kLanes, kPasses = kMany ? 4 : 1, kWaves = kFewThreads / kWave;
+    __shared__ float4 red_v[kMany ? 1 : kWaves - 1][kWave];
+    __shared__ float2 red_ml[kMany ? 1 : kWaves - 1][kWave];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int per_wg = kMany ? kHeads * kPasses * kWaves : kHeads, wgs = (p.H + per_wg - 1) / per_wg;
+    const int wg = (int)lat_workgroup(), t = head_div(wg, wgs);
     if (t >= p.T) return;
+    const int h0 = (wg - t * wgs) * per_wg + (kMany ? kHeads * kPasses * wave : 0) + lane / kLanes, c = lane % kLanes;
     const HeadLine line = head_line(p, [&](const LatentReq& r) { return head_units(p, r, sp.rows, sp.tokens); });
-    auto leave = [&](const float (&v)[V], float m, float l) {
+    auto leave = [&](int h, const float4& v, float m, float l) __attribute__((always_inline)) {
+        const size_t at = (size_t)t * p.H + h;
         const float inv = lat_inverse(l);
-        if (p.lse && lane == 0) p.lse[at] = lat_lse(m, l);
-        if constexpr (V == 2) {
-            if (p.y_bf16) ((uint32_t*)p.y)[at * (D / 2) + lane] = lat_pack(v[0] * inv, v[1] * inv);
-            else ((float2*)p.y)[at * (D / 2) + lane] = make_float2(v[0] * inv, v[1] * inv);
-        } else {
-            if (p.y_bf16) ((__bf16*)p.y)[at * D + lane] = (__bf16)(v[0] * inv);
-            else ((float*)p.y)[at * D + lane] = v[0] * inv;
-        }
+        if (p.lse && c == 0) p.lse[at] = lat_lse(m, l);
+        if (p.y_bf16) *(lat_u32x2*)((uint16_t*)p.y + at * D + 4 * c) = lat_u32x2{lat_pack(v.x * inv, v.y * inv), lat_pack(v.z * inv, v.w * inv)};
+        else *(float4*)((float*)p.y + at * D + 4 * c) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
     };
-    float sum[V] = {};
-    const int end = p.B > 0 ? p.cu_new[p.B] : 0;
-    bool none = t >= end || t < p.cu_new[0];
-    int g0 = 0, g1 = 0, a = 0, rr = 0, per = 1;
-    if (!none) {
-        const int b = lat_find_wave(p.cu_new, p.B, t);
-        int at_u;
-        const LatentReq rq = head_line_req(p, line, b, &at_u);
-        const int n_u = (rq.seq + sp.tokens - 1) / sp.tokens, tiles = (rq.add * p.ratio + sp.rows - 1) / sp.rows;
-        rr = (t - rq.t0) * p.ratio + h - kv * p.ratio;
-        none = n_u == 0 || t - rq.t0 >= rq.add;
-        if (!none) {
-            per = head_share(sp, line.total);
-            a = at_u + (kv * tiles + rr / sp.rows) * n_u;
-            g0 = min(a / per, sp.groups - 1);
-            g1 = min((a + n_u - 1) / per, sp.groups - 1);
+    const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    // Units of a row tile; 0 where the row sees nothing.
+    int b = 0, at_u = 0, n_u = 0;
+    LatentReq rq = {};
+    if (p.B > kWave) {
+        if (t < p.cu_new[p.B]) {
+            b = lat_find_wave(p.cu_new, p.B, t);
+            rq = head_line_req(p, line, b, &at_u);
+        }
+    } else {
+        // the last request whose tokens begin at or before t; rows past it have none
+        const unsigned long long before = __ballot(lane < p.B && line.mine.t0 <= t);
+        if (before) {
+            b = 63 - __clzll(before);
+            rq = head_line_req(p, line, b, &at_u);
         }
     }
-    if (none) return leave(sum, kNoScore, 0.0f);
-    if (g0 == g1) return;
-    // Share g's slot: its second when the row tile's line begins inside it.
-    auto slot = [&](int g) {
-        return ((size_t)head_workgroup(sp, g) * 2 + (g == g0 && a > g0 * per ? 1 : 0)) * sp.rows + rr % sp.rows;
-    };
-    const float2* ml = (const float2*)p.part_ml;
-    float m = kNoScore, l = 0.0f;
-    for (int g = g0; g <= g1; g += kWave) {
-        const float2 v = g + lane <= g1 ? ml[slot(g + lane)] : make_float2(kNoScore, 0.0f);
-        float mn = fmaxf(m, v.x);
+    if (t >= rq.t0 && t - rq.t0 < rq.add) n_u = (rq.seq + sp.tokens - 1) / sp.tokens;
+    if (n_u == 0) {
 #pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) mn = fmaxf(mn, __shfl_xor(mn, d));
-        float s = v.y * __builtin_amdgcn_exp2f(v.x - mn);
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d);
-        l = l * __builtin_amdgcn_exp2f(m - mn) + s;
-        m = mn;
+        for (int i = 0; i < kPasses; ++i)
+            if (h0 + kHeads * i < p.H && (kMany || wave == 0)) leave(h0 + kHeads * i, zero, kNoScore, 0.0f);
+        return;
     }
-    auto add = [&](int g, auto count) __attribute__((always_inline)) {
-        constexpr int U = decltype(count)::value;       // partial rows in flight
-        float2 w[U];
-        float x[U][V];
+    const int tiles = head_div(rq.add * p.ratio + sp.rows - 1, sp.rows), per = head_share(sp, line.total);
+    float4 sum[kPasses];
+    float m[kPasses], l[kPasses];
+    int g0[kPasses], g1[kPasses], a[kPasses], rr[kPasses], most = 0;
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const size_t sl = slot(g + i);
-            w[i] = ml[sl];
+    for (int i = 0; i < kPasses; ++i) {
+        const int h = min(h0 + kHeads * i, p.H - 1), kv = h / p.ratio, r = (t - rq.t0) * p.ratio + h - kv * p.ratio;
+        a[i] = at_u + (kv * tiles + r / sp.rows) * n_u;
+        rr[i] = r % sp.rows;
+        g0[i] = min((int)((unsigned)a[i] / (unsigned)per), sp.groups - 1);
+        g1[i] = min((int)((unsigned)(a[i] + n_u - 1) / (unsigned)per), sp.groups - 1);
+        if (g0[i] < g1[i] && h0 + kHeads * i < p.H) most = max(most, g1[i] - g0[i] + 1);
+        sum[i] = zero;
+        m[i] = kNoScore;
+        l[i] = 0.0f;
+    }
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[i][v] = p.part[sl * D + V * lane + v];
-        }
+    for (int d = 32; d >= 1; d >>= 1) most = max(most, __shfl_xor(most, d));
+    if (most == 0 && kMany) return;
+    // Share k of each pass's row: its second slot when the row tile's line begins inside the share.
+    auto add = [&](int k0, auto count) __attribute__((always_inline)) {
+        constexpr int U = decltype(count)::value;
+        float2 w[U][kPasses];
+        float4 x[U][kPasses];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            // shares that saw nothing for the row have written no sums
-            const float f = w[i].y != 0.0f ? __builtin_amdgcn_exp2f(w[i].x - m) : 0.0f;
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int v = 0; v < V; ++v) sum[v] += f != 0.0f ? x[i][v] * f : 0.0f;
-        }
+            for (int i = 0; i < kPasses; ++i) {
+                const int g = min(g0[i] + k0 + (kMany ? u : kWaves * u), g1[i]);
+                const size_t slot = ((size_t)head_workgroup(sp, g) * 2 + (g == g0[i] && a[i] > g0[i] * per ? 1 : 0)) * sp.rows + rr[i];
+                w[u][i] = ((const float2*)p.part_ml)[slot];
+                x[u][i] = *(const float4*)(p.part + slot * D + 4 * c);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i) {
+                // shares that saw nothing for the row have written no sums
+                if (g0[i] + k0 + (kMany ? u : kWaves * u) > g1[i] || w[u][i].y == 0.0f) continue;
+                head_merge(sum[i], m[i], l[i], x[u][i], w[u][i]);
+            }
     };
-    int g = g0;
-    for (; g + 7 <= g1; g += 8) add(g, LatInt<8>{});
-    for (; g <= g1; ++g) add(g, LatInt<1>{});
-    leave(sum, m, l);
+    if constexpr (kMany) {
+        for (int k = 0; k < most; k += 2) add(k, LatInt<2>{});
+    } else {
+        for (int k = wave; k < most; k += 8 * kWaves) add(k, LatInt<8>{});
+        if (wave > 0) {
+            red_v[wave - 1][lane] = sum[0];
+            red_ml[wave - 1][lane] = make_float2(m[0], l[0]);
+        }
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int w = 0; w < kWaves - 1; ++w)
+            if (red_ml[w][lane].y != 0.0f) head_merge(sum[0], m[0], l[0], red_v[w][lane], red_ml[w][lane]);
+    }
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i)
+        if (h0 + kHeads * i < p.H && g0[i] < g1[i]) leave(h0 + kHeads * i, sum[i], m[i], l[i]);
 }
 
 }  // namespace
@@ -421,9 +446,17 @@ void meta(const HeadParams& p, const HeadSplit& sp, int whole, hipStream_t s) {
 }
 
 void join(const HeadParams& p, const HeadSplit& sp, hipStream_t s) {
-    const dim3 grid = lat_grid((unsigned)(((long long)p.T * p.H + 3) / 4));
-    if (p.dim == 128) hipLaunchKernelGGL(k_head_join<128>, grid, dim3(kFewThreads), 0, s, p, sp);
-    else hipLaunchKernelGGL(k_head_join<64>, grid, dim3(kFewThreads), 0, s, p, sp);
+    auto run = [&](auto dim, auto many) {
+        constexpr int D = decltype(dim)::value, kPer = kWave / (D / 4) * (decltype(many)::value ? 16 : 1);
+        hipLaunchKernelGGL((k_head_join<D, decltype(many)::value != 0>), lat_grid((unsigned)(p.T * ((p.H + kPer - 1) / kPer))),
+                           dim3(kFewThreads), 0, s, p, sp);
+    };
+    auto dims = [&](auto many) {
+        if (p.dim == 128) run(LatInt<128>{}, many);
+        else run(LatInt<64>{}, many);
+    };
+    if ((long long)p.T * p.H >= kJoinRows) dims(LatInt<1>{});
+    else dims(LatInt<0>{});
 }
 
 hipError_t tile(const HeadParams& p, bool split, unsigned grid, int tiles, hipStream_t s) {

@@ -4,8 +4,8 @@
 namespace caee {
 
 hipError_t launch_head_tile_128(const HeadParams& p, bool split, unsigned grid, int tiles, hipStream_t s) {
-    if (!split) return head_tile<128, false, false>(p, grid, tiles, s);
-    return p.tree ? head_tile<128, true, true>(p, grid, tiles, s) : head_tile<128, true, false>(p, grid, tiles, s);
+    if (p.tree) return split ? head_tile<128, true, true>(p, grid, tiles, s) : head_tile<128, false, true>(p, grid, tiles, s);
+    return split ? head_tile<128, true, false>(p, grid, tiles, s) : head_tile<128, false, false>(p, grid, tiles, s);
 }
 
 }  // namespace caee

@@ -133,18 +133,18 @@ def test_unseen_tokens_may_hold_anything(bad, which, form):
         assert np.all(np.isnan(got[0][4]))
 
 
-@pytest.mark.parametrize("form", FORMS + ["tree"])
+@pytest.mark.parametrize("form", FORMS + ["split tree", "whole tree"])
 @pytest.mark.parametrize("at", [3, 64, 66])
 def test_values_without_a_number_reach_who_sees_them(at, form):
     """Infinities and NaNs in single places of a seen value (before the new tokens or among them) are in those places
     of the results that see it, and in no others."""
     new = 6
-    tree = chain_tree([new], 1) if form == "tree" else None
+    tree = chain_tree([new], 1) if "tree" in form else None
     c = HeadCase(seq=[70], new=[new], seed=16, tree=tree)
     v = c.v[0][at].clone()
     v[:, 5], v[:, 17], v[:, 100] = float("inf"), float("nan"), -float("inf")
     c.put(0, at, v=v)
-    got = c.run(DEV, "split" if form == "tree" else form)
+    got = c.run(DEV, form.split()[0])
     clean = c.v[0][at].clone()
     clean[:, [5, 17, 100]] = 0.0
     c.put(0, at, v=clean)
@@ -173,10 +173,11 @@ def test_long_prompt(form):
 @pytest.mark.parametrize("H,G,new,ctx,words", [
     (8, 2, [1], [40], 1), (8, 2, [5, 0, 13], [100, 7, 0], 1), (32, 4, [33, 64, 2], [500, 31, 1000], 2),
     (16, 2, [61, 61], [2000, 0], 3), (64, 1, [9, 30], [33, 64], 1), (4, 4, [130], [90], 5), (4, 1, [32, 31], [64, 1], 1)])
-def test_trees(H, G, new, ctx, words, D, y_dtype):
+@pytest.mark.parametrize("form", FORMS)
+def test_trees(form, H, G, new, ctx, words, D, y_dtype):
     rng = np.random.default_rng(sum(new) + H)
     seq = np.array(ctx) + np.array(new)
-    _check("split", y_dtype=y_dtype, seq=seq, new=new, H=H, G=G, D=D, pad=3, seed=18, tree=random_tree(new, words, rng))
+    _check(form, y_dtype=y_dtype, seq=seq, new=new, H=H, G=G, D=D, pad=3, seed=18, tree=random_tree(new, words, rng))
 
 
 def test_tree_with_more_tokens_than_bits():
@@ -185,27 +186,30 @@ def test_tree_with_more_tokens_than_bits():
     _check("auto", seq=[100, 41], new=[40, 41], H=4, G=2, seed=19, tree=random_tree([40, 41], 2, rng)[:, :1].copy())
 
 
-def test_tree_with_empty_masks_and_an_empty_cache():
-    _check("split", seq=[5, 3], new=[5, 3], seed=20, tree=np.zeros((8, 1), np.uint32))
+@pytest.mark.parametrize("form", FORMS)
+def test_tree_with_empty_masks_and_an_empty_cache(form):
+    _check(form, seq=[5, 3], new=[5, 3], seed=20, tree=np.zeros((8, 1), np.uint32))
 
 
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("new", [[7, 20], [61, 3]])
-def test_a_chain_is_the_causal_order(new):
+def test_a_chain_is_the_causal_order(new, form):
     seq = [300, 90]
     c, t = HeadCase(seq=seq, new=new, seed=21), HeadCase(seq=seq, new=new, seed=21, tree=chain_tree(new, 2))
-    a, b = c.run(DEV, "split"), t.run(DEV, "split")
+    a, b = c.run(DEV, form), t.run(DEV, form)
     assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), 3.3e38])
-def test_tree_tokens_off_the_path_may_hold_anything(bad):
+def test_tree_tokens_off_the_path_may_hold_anything(bad, form):
     """Token 2 of five is on nobody's path."""
     tree = chain_tree([5], 1)
     tree[2] = 0
     tree &= np.uint32(~(1 << 2) & 0xFFFFFFFF)
     c = HeadCase(seq=[75], new=[5], seed=22, tree=tree)
     c.put(0, 72, k=torch.full((c.G, c.D), bad, dtype=BF), v=torch.full((c.G, c.D), bad, dtype=BF))
-    check_heads(c.run(DEV), c.ref())
+    check_heads(c.run(DEV, form), c.ref())
 
 
 def test_auto_takes_every_call():

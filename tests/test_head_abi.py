@@ -78,7 +78,7 @@ def _ws(d):
     (dict(kv_heads=32), BAD), (dict(dim=80), LIMIT), (dict(dim=0), LIMIT), (dict(block_size=0), BAD), (dict(n_blocks=0), BAD),
     (dict(max_blocks=0), BAD), (dict(max_new=-1), BAD), (dict(max_kv=-1), BAD), (dict(causal=2), BAD),
     (dict(tree_words=-1), BAD), (dict(tree_words=1, causal=0), BAD), (dict(tree_words=33), LIMIT),
-    (dict(tree_words=1, form=2), LIMIT), (dict(form=3), BAD), (dict(y_dtype=2), BAD), (dict(scale=0.0), BAD),
+    (dict(tree_words=1, form=2), OK), (dict(form=3), BAD), (dict(y_dtype=2), BAD), (dict(scale=0.0), BAD),
     (dict(scale=float("inf")), BAD), (dict(q_stride=2040), BAD), (dict(q_stride=2052), BAD), (dict(q_stride=1 << 41), LIMIT),
     (dict(heads=1026, q_stride=1026 * 128), LIMIT), (dict(B=65537), LIMIT), (dict(T=(1 << 20) + 1), LIMIT),
     (dict(max_kv=(1 << 30) + 1), LIMIT), (dict(row_stride=128), BAD), (dict(page_stride=256), BAD),
