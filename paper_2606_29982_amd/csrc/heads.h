@@ -161,10 +161,28 @@ __device__ inline HeadEight head_eight(const HeadParams& p, int b, int seq, int 
     const int at = r0 - (int)(j * (unsigned)p.c.block);
     return {head_entry(p, b, j), at, r1 - r0, at + (r1 - r0) < p.c.block};
 }
-// Byte offset of row `at` of a page's head g.
-__device__ inline long long head_offset(const HeadParams& p, int page, int at, int g) {
-    return 2 * (min(max(page, 0), p.c.n_blocks - 1) * p.c.page_stride + at * p.c.row_stride + g * p.c.head_stride);
+// Byte offset of row `at` of a page from the first one's (of the same head).
+__device__ inline long long head_offset(const HeadParams& p, int page, int at) {
+    return 2 * (min(max(page, 0), p.c.n_blocks - 1) * p.c.page_stride + at * p.c.row_stride);
 }
+// The same for row `pos` of request b.
+__device__ inline long long head_row(const HeadParams& p, int b, int pos) {
+    const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)pos / (unsigned)p.c.block);
+    return head_offset(p, head_entry(p, b, j), pos - (int)(j * (unsigned)p.c.block));
+}
+__device__ inline const char* head_base(const HeadParams& p, const uint16_t* cache, int g) {
+    return (const char*)(cache + g * p.c.head_stride);
+}
+
+// Softmax weight of score s where the running maximum is m, by one multiply-add:
+// what m's product with scale_log2 lost to rounding is a factor that all weights
+// of the row have in common, next to 1 while m is of a size up to kFusedMax (the
+// largest scores take lat_weight).
+constexpr float kFusedMax = 0x1p20f;
+__device__ inline float head_weight(float s, float scale_log2, float m) { return __builtin_amdgcn_exp2f(fmaf(s, scale_log2, -m)); }
+// While the weights of a lane's tile add up to no more than kMaxWeight none of
+// them exceeds it, and the maximum need not move.
+__device__ inline bool head_moves(float more, float m) { return more > kMaxWeight || !(fabsf(m) <= kFusedMax); }
 
 // Adds a partial result (sums x of weights by the maximum w.x, whose total is w.y)
 // to one.
@@ -203,9 +221,7 @@ __device__ inline void head_put_odd(const HeadParams& p, int b, int g, int tok0,
         for (int t0 = tok0; t0 < end; t0 += step)
 #pragma unroll 1
             for (int pos = t0; pos < min(t0 + width, end); ++pos) {
-                const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)pos / (unsigned)p.c.block);
-                const char* row = (const char*)p.v + head_offset(p, head_entry(p, b, j), pos - (int)(j * (unsigned)p.c.block), g);
-                const lat_u32x2 v = ((const lat_u32x2*)row)[c];
+                const lat_u32x2 v = ((const lat_u32x2*)(head_base(p, p.v, g) + head_row(p, b, pos)))[c];
                 const bool seen = sees(pos);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {

@@ -56,7 +56,7 @@ struct FewStage {
 // weights are, in that order, a fragment of the second product; values are read
 // transposed.  The next keys are fetched as soon as the scores are made, the
 // next values after the sums; another workgroup of the CU fills the gaps.
-template <int D, bool kTree, bool kOnce>
+template <int D, bool kTree, bool kOnce, bool kLast>
 __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
     constexpr int kG = D / 64, kJ = D / 16, NC = D / 32, kLoads = kWaveTokens / 8 * kG;
@@ -109,11 +109,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         auto piece = [&](int i) __attribute__((always_inline)) { return 16u * ((lane & 7) ^ lat_swz(8 * (i & 1) + (lane >> 3))); };
         // A buffer of size 0 where nothing is to be loaded: its loads cost no
         // traffic, and their number does not depend on a branch.
-        auto fetch = [&](const uint16_t* cache, FewStage<D>& st, int s, const HeadEight (&e)[4], bool there) __attribute__((always_inline)) {
+        const char *const k_base = head_base(p, p.k, g), *const v_base = head_base(p, p.v, g);
+        auto fetch = [&](const char* cache, FewStage<D>& st, int s, const HeadEight (&e)[4], bool there) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const __amdgpu_buffer_rsrc_t buf =
-                    __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)cache + head_offset(p, e[i].page, e[i].at, g)), 0,
+                    __builtin_amdgcn_make_buffer_rsrc((void*)(cache + head_offset(p, e[i].page, e[i].at)), 0,
                                                       there && e[i].one ? kLatBufBytes : 0, kLatBufWord3);
                 const uint32_t at = (uint32_t)min(lane >> 3, e[i].span) * row_bytes + piece(i);
 #pragma unroll
@@ -130,11 +131,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
                     if (r0 / p.c.block == r1 / p.c.block) continue;
 #pragma unroll 1
                     for (int r = 0; r < 8; ++r) {
-                        const int pos = min(p0 + r, rq.seq - 1);
-                        const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)pos / (unsigned)p.c.block);
                         const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
-                            (void*)((const char*)cache + head_offset(p, head_entry(p, b, j), pos - (int)(j * (unsigned)p.c.block), g)), 0,
-                            kLatBufBytes, kLatBufWord3);
+                            (void*)(cache + head_row(p, b, min(p0 + r, rq.seq - 1))), 0, kLatBufBytes, kLatBufWord3);
                         if (lane >> 3 == r) {
 #pragma unroll
                             for (int gg = 0; gg < kG; ++gg)
@@ -158,8 +156,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         }
         HeadEight now[4];
         eights(0, now);
-        fetch(p.k, ks, 0, now, steps > 0);
-        fetch(p.v, vs, 0, now, steps > 0);
+        fetch(k_base, ks, 0, now, steps > 0);
+        fetch(v_base, vs, 0, now, steps > 0);
         eights(1, now);
         lat_wait_vm<2 * kLoads>();
         __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
@@ -184,7 +182,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
             for (int j = 0; j < kJ; ++j) sc = lat_mma(keys[(kp0 ^ (2 * (j & 3))) + (j >> 2) * kWave], qf[j], sc);
             __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
             __builtin_amdgcn_sched_barrier(0);
-            fetch(p.k, ks, s + 1, now, s + 1 < steps);
+            fetch(k_base, ks, s + 1, now, s + 1 < steps);
             const bool masked = tb + kWaveTokens > lim_min;
             if (masked) {
                 asm volatile("");       // a branch, not selects in every step
@@ -196,26 +194,28 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
                     if (at(i) >= left || (kTree && !(bits >> at(i) & 1))) sc[i] = -INFINITY;
                 }
             }
-            // The weights by the running maximum; where one exceeds the slack the
-            // maximum moves and they are made again.
-            lat_u32x4 pf[2], pr[2];
-            float big = 0.0f, more = 0.0f;
-            auto weights = [&]() __attribute__((always_inline)) {
+            // The weights by the running maximum; where it has to move they are made again.
+            lat_u32x4 pf[2], pr[2], pl[2];
+            float more = 0.0f;
+            auto weights = [&](auto&& weight) __attribute__((always_inline)) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float a = lat_weight(sc[8 * k + 2 * i], p.scale_log2, m);
-                        const float e = lat_weight(sc[8 * k + 2 * i + 1], p.scale_log2, m);
-                        big = fmaxf(fmaxf(big, a), e);
+                        const float a = weight(sc[8 * k + 2 * i], p.scale_log2, m);
+                        const float e = weight(sc[8 * k + 2 * i + 1], p.scale_log2, m);
                         pf[k][i] = lat_pack(a, e);
                         const lat_f32x2 rest = lat_rest(pf[k][i], a, e);
                         pr[k][i] = lat_pack(rest[0], rest[1]);
+                        if constexpr (kLast) {
+                            const lat_f32x2 last = lat_rest(pr[k][i], rest[0], rest[1]);
+                            pl[k][i] = lat_pack(last[0], last[1]);
+                        }
                         more += a + e;
                     }
             };
-            if (s > 0) weights();
-            if (s == 0 || __any(big > kMaxWeight)) {
+            if (s > 0) weights(head_weight);
+            if (s == 0 || __any(head_moves(more, m))) {
                 float mt = sc[0];
 #pragma unroll
                 for (int i = 1; i < 16; ++i) mt = fmaxf(mt, sc[i]);
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
 #pragma unroll
                 for (int c = 0; c < NC; ++c) o[c] *= f;
                 more = 0.0f;
-                weights();
+                weights(lat_weight);
             }
             l += more;
             lat_wait_vm<kLoads>();             // the values are there
@@ -266,10 +266,11 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
                     const lat_u32x4 vf = {w[0][0], w[0][1], w[1][0], w[1][1]};
                     o[c] = lat_mma(vf, pf[k], o[c]);
                     o[c] = lat_mma(vf, pr[k], o[c]);
+                    if constexpr (kLast) o[c] = lat_mma(vf, pl[k], o[c]);
                 }
             __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
             __builtin_amdgcn_sched_barrier(0);
-            fetch(p.v, vs, s + 1, now, s + 1 < steps);
+            fetch(v_base, vs, s + 1, now, s + 1 < steps);
             eights(s + 2, now);
         }
         lat_wait_vm<0>();
@@ -469,8 +470,10 @@ hipError_t launch_head_few(const HeadParams& p, hipStream_t s) {
     meta(p, kHeadFew, 0, s);
     const bool once = (long long)p.max_new * p.ratio <= kFewRows;      // one row tile a request and group reads its tokens
     auto few = [&](auto dim, auto tree, auto reads) {
-        hipLaunchKernelGGL((k_head_few<decltype(dim)::value, decltype(tree)::value != 0, decltype(reads)::value != 0>),
-                           dim3(kHeadFew.groups), dim3(kFewThreads), 0, s, p);
+        constexpr int D = decltype(dim)::value;
+        constexpr bool kTree = decltype(tree)::value != 0, kOnce = decltype(reads)::value != 0;
+        if (p.y_bf16) hipLaunchKernelGGL((k_head_few<D, kTree, kOnce, false>), dim3(kHeadFew.groups), dim3(kFewThreads), 0, s, p);
+        else hipLaunchKernelGGL((k_head_few<D, kTree, kOnce, true>), dim3(kHeadFew.groups), dim3(kFewThreads), 0, s, p);
     };
     auto trees = [&](auto dim, auto reads) {
         if (p.tree) few(dim, LatInt<1>{}, reads);

@@ -141,9 +141,10 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
         // A wave fetches 8 tokens of a tile; the pages of tiles are looked up a
         // step before their keys are.
         auto eight = [&](int s) __attribute__((always_inline)) { return head_eight(p, b, rq.seq, tok0 + min(s, steps - 1) * kTileTokens + 8 * wave); };
-        auto load = [&](const uint16_t* cache, const HeadEight& e, int s, Stage& st) __attribute__((always_inline)) {
+        const char *const k_base = head_base(p, p.k, g), *const v_base = head_base(p, p.v, g);
+        auto load = [&](const char* cache, const HeadEight& e, int s, Stage& st) __attribute__((always_inline)) {
             const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
-                (void*)((const char*)cache + head_offset(p, e.page, e.at, g)), 0, e.one ? kLatBufBytes : 0, kLatBufWord3);
+                (void*)(cache + head_offset(p, e.page, e.at)), 0, e.one ? kLatBufBytes : 0, kLatBufWord3);
             const uint32_t at = (uint32_t)min(lane >> 3, e.span) * row_bytes + swz;
 #pragma unroll
             for (int gg = 0; gg < kG; ++gg)
@@ -153,11 +154,8 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
                 const int p0 = tok0 + min(s, steps - 1) * kTileTokens + 8 * wave;
 #pragma unroll 1
                 for (int r = 0; r < 8; ++r) {
-                    const int pos = min(p0 + r, rq.seq - 1);
-                    const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)pos / (unsigned)p.c.block);
                     const __amdgpu_buffer_rsrc_t far = __builtin_amdgcn_make_buffer_rsrc(
-                        (void*)((const char*)cache + head_offset(p, head_entry(p, b, j), pos - (int)(j * (unsigned)p.c.block), g)), 0,
-                        kLatBufBytes, kLatBufWord3);
+                        (void*)(cache + head_row(p, b, min(p0 + r, rq.seq - 1))), 0, kLatBufBytes, kLatBufWord3);
                     if (lane >> 3 == r) {
 #pragma unroll
                         for (int gg = 0; gg < kG; ++gg)
@@ -206,7 +204,7 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
             asm volatile("" ::: "memory");
             clear(s, values);
         };
-        lat_u32x4 pf[4] = {}, pr[kRest ? 4 : 1] = {};          // weights of the tile before, their remainders
+        lat_u32x4 pf[4] = {}, pr[kRest ? 4 : 1] = {}, pl[kRest ? 4 : 1] = {};       // weights of the tile before, their remainders
         lat_f32x16 sc[2];
         // X's MFMAs, 2 kJ of the scores and 4 NC of the sums, evenly mixed (two
         // chains of sums alone would wait for each other), their fragments read
@@ -226,7 +224,10 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
         };
         auto sum = [&](const lat_u32x4& v, int i) __attribute__((always_inline)) {
             o[i % NC] = lat_mma(v, pf[i / NC], o[i % NC]);
-            if constexpr (kRest) o[i % NC] = lat_mma(v, pr[i / NC], o[i % NC]);
+            if constexpr (kRest) {
+                o[i % NC] = lat_mma(v, pr[i / NC], o[i % NC]);
+                o[i % NC] = lat_mma(v, pl[i / NC], o[i % NC]);
+            }
         };
         HeadEight e_k = {}, e_v = {}, e_next = {};      // of the keys and values that Y loads, and of the next keys
         const int more_k = second ? 3 : 2;
@@ -265,11 +266,11 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
             e_v = e_k;
             e_k = e_next;
             if (second) {
-                load(p.k, e_k, s + more_k, k);
-                load(p.v, e_v, s + more_k - 1, v0);
+                load(k_base, e_k, s + more_k, k);
+                load(v_base, e_v, s + more_k - 1, v0);
             } else {
-                load(p.k, e_k, s + more_k, k2);
-                load(p.v, e_v, s + more_k - 1, v2);
+                load(k_base, e_k, s + more_k, k2);
+                load(v_base, e_v, s + more_k - 1, v2);
             }
             e_next = eight(s + more_k + 1);
             if (tb + kTileTokens > lim_min) {
@@ -285,29 +286,29 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
                     }
                 }
             }
-            // The weights by the running maximum; where one exceeds the slack the
-            // maximum moves and they are made again.
-            float big = 0.0f, more = 0.0f;
-            auto weights = [&]() __attribute__((always_inline)) {
+            // The weights by the running maximum; where it has to move they are made again.
+            float more = 0.0f;
+            auto weights = [&](auto&& weight) __attribute__((always_inline)) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float a = lat_weight(sc[k >> 1][8 * (k & 1) + 2 * i], p.scale_log2, m);
-                        const float e = lat_weight(sc[k >> 1][8 * (k & 1) + 2 * i + 1], p.scale_log2, m);
-                        big = fmaxf(fmaxf(big, a), e);
+                        const float a = weight(sc[k >> 1][8 * (k & 1) + 2 * i], p.scale_log2, m);
+                        const float e = weight(sc[k >> 1][8 * (k & 1) + 2 * i + 1], p.scale_log2, m);
                         pf[k][i] = lat_pack(a, e);
                         if constexpr (kRest) {
                             const lat_f32x2 rest = lat_rest(pf[k][i], a, e);
                             pr[k][i] = lat_pack(rest[0], rest[1]);
+                            const lat_f32x2 last = lat_rest(pr[k][i], rest[0], rest[1]);
+                            pl[k][i] = lat_pack(last[0], last[1]);
                             more += a + e;
                         } else {
                             more = lat_sum2(pf[k][i], more);
                         }
                     }
             };
-            weights();
-            if (__any(big > kMaxWeight)) {
+            weights(head_weight);
+            if (__any(head_moves(more, m))) {
                 float mt = fmaxf(sc[0][0], sc[1][0]);
 #pragma unroll
                 for (int i = 1; i < 16; ++i) mt = fmaxf(mt, fmaxf(sc[0][i], sc[1][i]));
@@ -318,7 +319,7 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
 #pragma unroll
                 for (int c = 0; c < NC; ++c) o[c] *= f;
                 more = 0.0f;
-                weights();
+                weights(lat_weight);
             }
             l += more;
             if (!second) odd_end(s, v1);
@@ -328,8 +329,8 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
             // Tile 0, the keys of tile 1 (and what the second waves' Y(-1) would
             // have loaded); the values of "tile -1" are zeros.
             const HeadEight e0 = eight(0), e1 = eight(1), e2 = eight(2);
-            load(p.k, e0, 0, kt0);
-            load(p.v, e0, 0, vt0);
+            load(k_base, e0, 0, kt0);
+            load(v_base, e0, 0, vt0);
             lat_wait_vm<kLoads>();
             asm volatile("" ::: "memory");
 #pragma unroll
@@ -337,10 +338,10 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
                 qf[j] = own[(kp0 ^ (2 * (j & 3))) + (j >> 2) * kWave];
             __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
             lat_barrier();             // the stages the queries came through are free
-            load(p.k, e1, 1, kt1);
+            load(k_base, e1, 1, kt1);
             if (second) {
-                load(p.k, e2, 2, kt2);
-                load(p.v, e1, 1, vt1);
+                load(k_base, e2, 2, kt2);
+                load(v_base, e1, 1, vt1);
                 e_k = e2;
                 e_next = eight(3);
             } else {
