@@ -15,30 +15,30 @@ struct HeadCache {
 caee_status_t head_cache(int kv_heads, int dim, int block_size, int n_blocks, long long page_stride,
                          long long row_stride, long long head_stride, HeadCache* c);
 
-// Split form: the work of all requests is one line of units, kTokens tokens of
-// one row tile (kRows rows of a request, its new tokens' heads of one group) each,
-// by request, group, row tile and token.  It is cut into equal shares, one a
-// workgroup; a share begins and ends inside a row tile's line, so a workgroup
-// leaves at most two partial results.
-struct HeadSplit {
-    int groups, rows, tokens;
-};
-constexpr HeadSplit kHeadFew = {512, 32, 128};     // few rows: two workgroups a CU
-constexpr HeadSplit kHeadMany = {256, 256, 64};    // many rows: one
+// Two kernels attend.  Few rows (k_head_few): the work of all requests is one line
+// of units, kFewTokens tokens of one row tile (kFewRows rows of a request, its new
+// tokens' heads of one group) each, by request, group, row tile and token.  It is
+// cut into equal shares, one a workgroup; a share begins and ends inside a row
+// tile's line, so a workgroup leaves at most two partial results.
+constexpr int kFewRows = 32, kFewTokens = 128;
+constexpr int kFewGroups = 512;                    // two workgroups a CU
+// Many rows (k_head_tile): row tiles of kTileRows rows, a workgroup each, or,
+// where that leaves CUs idle, one for each of equal pieces of the row tile's
+// tokens, which leave partial results: at most kTilePieces pieces then.
+constexpr int kTileRows = 256, kTileTokens = 64;
+constexpr int kTilePieces = 512;
+constexpr int kHeadCus = 256;
 constexpr unsigned kHeadBlank = 64;                // workgroups that blank the rows of no request (whole form)
 // A quotient of uniform numbers, in a scalar register.
 __device__ inline int head_div(int a, int b) { return __builtin_amdgcn_readfirstlane(a / b); }
-__device__ inline int head_share(const HeadSplit& sp, int total) { return max((total + sp.groups - 1) / sp.groups, 1); }
+__device__ inline int head_share(int total) { return max((total + kFewGroups - 1) / kFewGroups, 1); }
 // Neighbouring shares, which have row tiles of the same tokens, run on one XCD.
-__device__ inline int head_group(const HeadSplit& sp, int wg) { return wg % kXcds * (sp.groups / kXcds) + wg / kXcds; }
-__device__ inline int head_workgroup(const HeadSplit& sp, int g) {
-    const int per = sp.groups / kXcds;
-    return g % per * kXcds + g / per;
-}
+__device__ inline int head_group(int wg) { return wg % kXcds * (kFewGroups / kXcds) + wg / kXcds; }
+__device__ inline int head_workgroup(int g) { return g % (kFewGroups / kXcds) * kXcds + g / (kFewGroups / kXcds); }
 
 struct HeadWs {
-    size_t meta;           // [B + 1] unit or query tile prefix sums, of more than 64 requests
-    size_t part, part_ml;  // split: [2 groups][rows][dim] partial sums and [..][rows][2] (maximum, sum)
+    size_t meta;           // [B + 1] unit or piece prefix sums, of more than 64 requests; [1] tokens of a piece
+    size_t part, part_ml;  // split: [2 shares or pieces][rows][dim] partial sums and [..][rows][2] (maximum, sum)
     size_t total;
 };
 
@@ -57,7 +57,7 @@ struct HeadParams {
     void* y;
     float* lse;
     int32_t* meta;
-    float* part;
+    float* part;          // NULL: whole form
     float* part_ml;
 };
 
@@ -80,45 +80,45 @@ __device__ inline int head_sees(const HeadParams& p, const LatentReq& r, int i) 
 }
 
 
-// Units of the split form are counted up to this; no request has more (a limit
-// of the host's, as is that of all requests while their lengths add up to
-// max_kv at most).
+// Units and pieces are counted up to this; no request has more (a limit of the
+// host's, as is that of all requests while their lengths add up to max_kv at
+// most).
 constexpr int kHeadMaxUnits = INT32_MAX / 2;
 __device__ inline int head_add_units(int a, int b) { return min(a + b, kHeadMaxUnits); }
-__device__ inline int head_units(const HeadParams& p, const LatentReq& r, int rows, int tokens) {
-    return p.G * ((r.add * p.ratio + rows - 1) / rows) * ((r.seq + tokens - 1) / tokens);
+__device__ inline int head_few_units(const HeadParams& p, const LatentReq& r) {
+    return p.G * ((r.add * p.ratio + kFewRows - 1) / kFewRows) * ((r.seq + kFewTokens - 1) / kFewTokens);
 }
+__device__ inline int head_tiles(const HeadParams& p, const LatentReq& r) { return (r.add * p.ratio + kTileRows - 1) / kTileRows; }
+__device__ inline int head_steps(const LatentReq& r) { return (r.seq + kTileTokens - 1) / kTileTokens; }
+// Pieces of a row tile of n steps.
+__device__ inline int head_cut(int n, int per) { return max((n + per - 1) / per, 1); }
 
-// Request of a unit.  Up to 64 requests every wave sums their units up by
-// itself, a lane each; of more, p.meta has the sums.
+// Prefix sums over the requests of a number each has.  Up to 64 requests every
+// wave makes them by itself, a lane each; of more, p.meta has them.
 struct HeadLine {
     LatentReq mine;      // lane b: request b
-    int at, total;       // its first unit; all units
+    int n, at, total;    // its number and the sum of those before; all requests'
 };
-template <class Units>
-__device__ inline HeadLine head_line(const HeadParams& p, Units&& units) {
+__device__ inline HeadLine head_line(const HeadParams& p) {
     HeadLine h = {};
-    if (p.B > kWave) {
-        h.total = __builtin_amdgcn_readfirstlane(p.meta[p.B]);
-        return h;
-    }
+    if (p.B > kWave) h.total = __builtin_amdgcn_readfirstlane(p.meta[p.B]);
+    else if ((int)(threadIdx.x & (kWave - 1)) < p.B) h.mine = head_req(p, threadIdx.x & (kWave - 1));
+    return h;
+}
+__device__ inline void head_line_sum(const HeadParams& p, HeadLine* h, int n) {
+    if (p.B > kWave) return;
     const int lane = threadIdx.x & (kWave - 1);
-    int n = 0;
-    if (lane < p.B) {
-        h.mine = head_req(p, lane);
-        n = units(h.mine);
-    }
-    int sum = n;
+    h->n = lane < p.B ? n : 0;
+    int sum = h->n;
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) {
         const int u = __shfl_up(sum, d);
         if (lane >= d) sum = head_add_units(sum, u);
     }
-    h.at = sum - n;
-    h.total = __builtin_amdgcn_readlane(sum, kWave - 1);
-    return h;
+    h->at = sum - h->n;
+    h->total = __builtin_amdgcn_readlane(sum, kWave - 1);
 }
-// Request b of the line: its lengths and first unit.
+// Request b of the line: its lengths and what is before it.
 __device__ inline LatentReq head_line_req(const HeadParams& p, const HeadLine& h, int b, int* at) {
     if (p.B > kWave) {
         *at = __builtin_amdgcn_readfirstlane(p.meta[b]);
@@ -130,7 +130,7 @@ __device__ inline LatentReq head_line_req(const HeadParams& p, const HeadLine& h
     return {__builtin_amdgcn_readlane(h.mine.t0, b), __builtin_amdgcn_readlane(h.mine.add, b),
             __builtin_amdgcn_readlane(h.mine.seq, b), __builtin_amdgcn_readlane(h.mine.before, b)};
 }
-// Request that unit u is of (u below the total).
+// Request that number u of the line is of (u below the total).
 __device__ inline int head_line_find(const HeadParams& p, const HeadLine& h, int u) {
     if (p.B > kWave) return lat_find_wave(p.meta, p.B, u);
     return 63 - __clzll(__ballot((int)(threadIdx.x & (kWave - 1)) < p.B && h.at <= u) | 1ull);
@@ -235,11 +235,10 @@ __device__ inline void head_put_odd(const HeadParams& p, int b, int g, int tok0,
     }
 }
 
-// Split form of few and of many rows; whole form.
+// Split form of few rows; of many, or whole form.
 hipError_t launch_head_few(const HeadParams& p, hipStream_t s);
 hipError_t launch_head_many(const HeadParams& p, hipStream_t s);
-hipError_t launch_head_whole(const HeadParams& p, hipStream_t s);
-hipError_t launch_head_tile_64(const HeadParams& p, bool split, unsigned grid, int tiles, hipStream_t s);
-hipError_t launch_head_tile_128(const HeadParams& p, bool split, unsigned grid, int tiles, hipStream_t s);
+hipError_t launch_head_tile_64(const HeadParams& p, unsigned grid, int pieces, hipStream_t s);
+hipError_t launch_head_tile_128(const HeadParams& p, unsigned grid, int pieces, hipStream_t s);
 
 }  // namespace caee

@@ -11,21 +11,23 @@ namespace {
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Units of the split form are counted in 32 bits.
-bool split_fits(const caee_head_desc_t& d, const HeadSplit& sp) {
-    const double tiles = (double)d.kv_heads * (((long long)d.max_new * (d.heads / d.kv_heads) + sp.rows - 1) / sp.rows);
-    return (double)(d.max_kv / sp.tokens + d.B) * tiles <= kHeadMaxUnits;
+// Units and pieces are counted in 32 bits.
+bool few_fits(const caee_head_desc_t& d) {
+    const double tiles = (double)d.kv_heads * (((long long)d.max_new * (d.heads / d.kv_heads) + kFewRows - 1) / kFewRows);
+    return (double)(d.max_kv / kFewTokens + d.B) * tiles <= kHeadMaxUnits;
 }
 
-// One of three: the split form of few rows, of many, the whole form.
-bool head_whole(const caee_head_desc_t& d) {
-    if (d.form != CAEE_HEAD_AUTO) return d.form == CAEE_HEAD_WHOLE;
-    if (!split_fits(d, kHeadMany)) return true;
-    return d.T >= 64ll * (d.B > 0 ? d.B : 1) && d.max_kv <= 8ll * d.T;
-}
+// Which kernel: that of few rows or of many.
 constexpr int kHeadFewRows = 64;
 bool head_few(const caee_head_desc_t& d) {
-    return (long long)d.max_new * (d.heads / d.kv_heads) <= kHeadFewRows && split_fits(d, kHeadFew);
+    return d.form != CAEE_HEAD_WHOLE && (long long)d.max_new * (d.heads / d.kv_heads) <= kHeadFewRows && few_fits(d);
+}
+// Whether row tiles stay whole.
+bool head_whole(const caee_head_desc_t& d) {
+    if (d.form != CAEE_HEAD_AUTO) return d.form == CAEE_HEAD_WHOLE;
+    if (head_few(d)) return false;
+    const long long before = d.max_kv > d.T ? d.max_kv - d.T : 0;
+    return (long long)d.T * d.heads >= kTilePieces * kTileRows || before + d.max_new <= 24 * kTileTokens;
 }
 
 HeadWs head_ws(const caee_head_desc_t& d) {
@@ -36,10 +38,9 @@ HeadWs head_ws(const caee_head_desc_t& d) {
         at += up256(bytes);
         return here;
     };
-    L.meta = take((size_t)(d.B + 1) * 4);
+    L.meta = take((size_t)(d.B + 2) * 4);
     // One size for whatever the split form takes, and for AUTO: smaller calls need no more.
-    const size_t part_rows =
-        d.form == CAEE_HEAD_WHOLE ? 0 : (size_t)2 * std::max(kHeadFew.groups * kHeadFew.rows, kHeadMany.groups * kHeadMany.rows);
+    const size_t part_rows = d.form == CAEE_HEAD_WHOLE ? 0 : (size_t)std::max(2 * kFewGroups * kFewRows, kTilePieces * kTileRows);
     L.part = take(part_rows * d.dim * 4);
     L.part_ml = take(part_rows * 2 * 4);
     L.total = at;
@@ -75,9 +76,6 @@ caee_status_t check_heads(const caee_head_desc_t* d, HeadCache* c) {
     CAEE_TRY(head_cache(d->kv_heads, d->dim, d->block_size, d->n_blocks, d->page_stride, d->row_stride, d->head_stride, c));
     if (d->max_kv > (1 << 30))
         return fail(CAEE_ERR_UNSUPPORTED, "%lld tokens in all exceed 2^30", (long long)d->max_kv);
-    if (d->form == CAEE_HEAD_SPLIT && !split_fits(*d, kHeadMany))
-        return fail(CAEE_ERR_UNSUPPORTED, "max_new=%d new tokens over max_kv=%lld: too many pairs for the split form",
-                    d->max_new, (long long)d->max_kv);
     return CAEE_OK;
 }
 
@@ -146,11 +144,11 @@ caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, c
     p.y = y;
     p.lse = lse;
     p.meta = (int32_t*)(w + L.meta);
-    p.part = (float*)(w + L.part);
+    p.part = head_whole(d) ? nullptr : (float*)(w + L.part);
     p.part_ml = (float*)(w + L.part_ml);
     hipStream_t s = (hipStream_t)stream;
     return timed_launch(CAEE_KERNEL_ATTENTION, s, "head attention", [&] {
-        return head_whole(d) ? launch_head_whole(p, s) : head_few(d) ? launch_head_few(p, s) : launch_head_many(p, s);
+        return head_few(d) ? launch_head_few(p, s) : launch_head_many(p, s);
     });
 }
 

@@ -1,7 +1,7 @@
 // Attention with grouped heads, split form of few rows: decode steps and small
 // trees, up to 32 query rows a tile.
 //
-//   k_head_meta   unit prefix sums, where there are more than 64 requests
+//   k_head_meta   prefix sums, where there are more than 64 requests
 //   k_head_few    a share of all requests' tokens a workgroup
 //   k_head_join   partial results of rows whose tokens several shares have
 #include <algorithm>
@@ -12,20 +12,47 @@ namespace caee {
 namespace {
 
 constexpr int kFewThreads = 256;
-constexpr int kFewRows = kHeadFew.rows, kFewTokens = kHeadFew.tokens, kWaveTokens = 32;
+constexpr int kWaveTokens = 32;
 
-// First unit (whole form: row tile) of each request (meta[b]; meta[B] the total).
-__global__ __launch_bounds__(kFewThreads) void k_head_meta(HeadParams p, HeadSplit sp, int whole) {
+// First unit of each request (meta[b]; meta[B] the total); or first piece, of one
+// group, and the steps of a piece (meta[B + 1]): row tiles are cut where all of
+// them would leave CUs idle.
+__global__ __launch_bounds__(kFewThreads) void k_head_meta(HeadParams p, int few) {
     __shared__ int part[kFewThreads];
+    __shared__ float work[kFewThreads];
     const int tid = threadIdx.x;
     const int chunk = (p.B + kFewThreads - 1) / kFewThreads;
     const int b0 = min(tid * chunk, p.B), b1 = min(b0 + chunk, p.B);
-    auto units = [&](int b) {
+    int per = INT32_MAX / 2;
+    if (!few && p.part) {
+        int tiles = 0;
+        float steps = 0.0f;
+        for (int b = b0; b < b1; ++b) {
+            const LatentReq r = head_req(p, b);
+            const int t = head_tiles(p, r);
+            tiles = head_add_units(tiles, t);
+            steps += (float)t * (float)head_steps(r);
+        }
+        part[tid] = tiles;
+        work[tid] = steps;
+        __syncthreads();
+        for (int d = kFewThreads / 2; d >= 1; d >>= 1) {
+            if (tid < d) {
+                part[tid] = head_add_units(part[tid], part[tid + d]);
+                work[tid] += work[tid + d];
+            }
+            __syncthreads();
+        }
+        // (a row tile has fewer than steps / per + 1 pieces; what is rounded in `work` has room)
+        if ((long long)part[0] * p.G < kHeadCus) per = max((int)ceilf(work[0] * (1.001f / kHeadCus) * (float)p.G), 1);
+        __syncthreads();
+    }
+    auto number = [&](int b) {
         const LatentReq r = head_req(p, b);
-        return whole ? (r.add * p.ratio + sp.rows - 1) / sp.rows : head_units(p, r, sp.rows, sp.tokens);
+        return few ? head_few_units(p, r) : head_tiles(p, r) * head_cut(head_steps(r), per);
     };
     int n = 0;
-    for (int b = b0; b < b1; ++b) n = head_add_units(n, units(b));
+    for (int b = b0; b < b1; ++b) n = head_add_units(n, number(b));
     part[tid] = n;
     __syncthreads();
     for (int d = 1; d < kFewThreads; d <<= 1) {
@@ -37,9 +64,12 @@ __global__ __launch_bounds__(kFewThreads) void k_head_meta(HeadParams p, HeadSpl
     int at = tid > 0 ? part[tid - 1] : 0;
     for (int b = b0; b < b1; ++b) {
         p.meta[b] = at;
-        at = head_add_units(at, units(b));
+        at = head_add_units(at, number(b));
     }
-    if (tid == kFewThreads - 1) p.meta[p.B] = part[kFewThreads - 1];
+    if (tid == kFewThreads - 1) {
+        p.meta[p.B] = part[kFewThreads - 1];
+        p.meta[p.B + 1] = per;
+    }
 }
 
 // Keys or values of 32 tokens for each wave: blocks of 8 rows x 128 bytes,
@@ -66,8 +96,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
     __shared__ int row_at[kFewRows];
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const HeadLine line = head_line(p, [&](const LatentReq& r) { return head_units(p, r, kFewRows, kFewTokens); });
-    const int per = head_share(kHeadFew, line.total), group = head_group(kHeadFew, blockIdx.x);
+    HeadLine line = head_line(p);
+    head_line_sum(p, &line, head_few_units(p, line.mine));
+    const int per = head_share(line.total), group = head_group(blockIdx.x);
     const int share0 = (int)min((long long)group * per, (long long)line.total), share1 = min(share0 + per, line.total);
 
     const int kp0 = (n >> 3) * (kG * kWave) + (n & 7) * 8 + (hf ^ lat_swz(n));
@@ -329,14 +360,14 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
 #endif
 }
 
-// Rows whose tokens lie in one share are done; the others are the sum of their
-// shares' partial results, D / 4 lanes a row and 16 bytes a lane; rows that see
+// Rows whose tokens lie in one share (piece) are done; the others are the sum of
+// their shares' partial results, D / 4 lanes a row and 16 bytes a lane; rows that see
 // no token are zero.  A workgroup has a token's heads: few rows, which have many
 // partial results, one pass of heads (64 / (D / 4)) whose shares go over the four
 // waves in turn, their sums added in order; many rows four passes a wave.
 constexpr int kJoinRows = 4096;        // (token, head) rows from which on they are many
 template <int D, bool kMany>
-__global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, HeadSplit sp) {
+__global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few) {
     constexpr int kLanes = D / 4, kHeads = kWave / kLanes, kPasses = kMany ? 4 : 1, kWaves = kFewThreads / kWave;
     __shared__ float4 red_v[kMany ? 1 : kWaves - 1][kWave];
     __shared__ float2 red_ml[kMany ? 1 : kWaves - 1][kWave];
@@ -345,7 +376,9 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, HeadSpl
     const int wg = (int)lat_workgroup(), t = head_div(wg, wgs);
     if (t >= p.T) return;
     const int h0 = (wg - t * wgs) * per_wg + (kMany ? kHeads * kPasses * wave : 0) + lane / kLanes, c = lane % kLanes;
-    const HeadLine line = head_line(p, [&](const LatentReq& r) { return head_units(p, r, sp.rows, sp.tokens); });
+    HeadLine line = head_line(p);
+    const int piece = few ? 1 : __builtin_amdgcn_readfirstlane(p.meta[p.B + 1]);
+    head_line_sum(p, &line, few ? head_few_units(p, line.mine) : head_tiles(p, line.mine) * head_cut(head_steps(line.mine), piece));
     auto leave = [&](int h, const float4& v, float m, float l) __attribute__((always_inline)) {
         const size_t at = (size_t)t * p.H + h;
         const float inv = lat_inverse(l);
@@ -370,24 +403,33 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, HeadSpl
             rq = head_line_req(p, line, b, &at_u);
         }
     }
-    if (t >= rq.t0 && t - rq.t0 < rq.add) n_u = (rq.seq + sp.tokens - 1) / sp.tokens;
+    if (t >= rq.t0 && t - rq.t0 < rq.add) n_u = few ? (rq.seq + kFewTokens - 1) / kFewTokens : head_steps(rq);
     if (n_u == 0) {
 #pragma unroll
         for (int i = 0; i < kPasses; ++i)
             if (h0 + kHeads * i < p.H && (kMany || wave == 0)) leave(h0 + kHeads * i, zero, kNoScore, 0.0f);
         return;
     }
-    const int tiles = head_div(rq.add * p.ratio + sp.rows - 1, sp.rows), per = head_share(sp, line.total);
+    const int tile_rows = few ? kFewRows : kTileRows;
+    const int tiles = (rq.add * p.ratio + tile_rows - 1) / tile_rows;
+    const int per = few ? head_share(line.total) : 1, cut = few ? 1 : __builtin_amdgcn_readfirstlane(head_cut(n_u, piece));
+    if (!few && cut == 1) return;
     float4 sum[kPasses];
     float m[kPasses], l[kPasses];
     int g0[kPasses], g1[kPasses], a[kPasses], rr[kPasses], most = 0;
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
         const int h = min(h0 + kHeads * i, p.H - 1), kv = h / p.ratio, r = (t - rq.t0) * p.ratio + h - kv * p.ratio;
-        a[i] = at_u + (kv * tiles + r / sp.rows) * n_u;
-        rr[i] = r % sp.rows;
-        g0[i] = min((int)((unsigned)a[i] / (unsigned)per), sp.groups - 1);
-        g1[i] = min((int)((unsigned)(a[i] + n_u - 1) / (unsigned)per), sp.groups - 1);
+        rr[i] = r % tile_rows;
+        if (few) {         // shares
+            a[i] = at_u + (kv * tiles + r / kFewRows) * n_u;
+            g0[i] = min((int)((unsigned)a[i] / (unsigned)per), kFewGroups - 1);
+            g1[i] = min((int)((unsigned)(a[i] + n_u - 1) / (unsigned)per), kFewGroups - 1);
+        } else {           // pieces
+            g0[i] = kv * line.total + at_u + r / kTileRows * cut;
+            g1[i] = g0[i] + cut - 1;
+            a[i] = 0;
+        }
         if (g0[i] < g1[i] && h0 + kHeads * i < p.H) most = max(most, g1[i] - g0[i] + 1);
         sum[i] = zero;
         m[i] = kNoScore;
@@ -406,7 +448,8 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, HeadSpl
 #pragma unroll
             for (int i = 0; i < kPasses; ++i) {
                 const int g = min(g0[i] + k0 + (kMany ? u : kWaves * u), g1[i]);
-                const size_t slot = ((size_t)head_workgroup(sp, g) * 2 + (g == g0[i] && a[i] > g0[i] * per ? 1 : 0)) * sp.rows + rr[i];
+                const size_t at = few ? (size_t)head_workgroup(g) * 2 + (g == g0[i] && a[i] > g0[i] * per ? 1 : 0) : (size_t)g;
+                const size_t slot = at * tile_rows + rr[i];
                 w[u][i] = ((const float2*)p.part_ml)[slot];
                 x[u][i] = *(const float4*)(p.part + slot * D + 4 * c);
             }
@@ -442,15 +485,15 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, HeadSpl
 
 namespace {
 
-void meta(const HeadParams& p, const HeadSplit& sp, int whole, hipStream_t s) {
-    if (p.B > kWave) hipLaunchKernelGGL(k_head_meta, dim3(1), dim3(kFewThreads), 0, s, p, sp, whole);
+void meta(const HeadParams& p, int few, hipStream_t s) {
+    if (p.B > kWave) hipLaunchKernelGGL(k_head_meta, dim3(1), dim3(kFewThreads), 0, s, p, few);
 }
 
-void join(const HeadParams& p, const HeadSplit& sp, hipStream_t s) {
+void join(const HeadParams& p, int few, hipStream_t s) {
     auto run = [&](auto dim, auto many) {
         constexpr int D = decltype(dim)::value, kPer = kWave / (D / 4) * (decltype(many)::value ? 16 : 1);
         hipLaunchKernelGGL((k_head_join<D, decltype(many)::value != 0>), lat_grid((unsigned)(p.T * ((p.H + kPer - 1) / kPer))),
-                           dim3(kFewThreads), 0, s, p, sp);
+                           dim3(kFewThreads), 0, s, p, few);
     };
     auto dims = [&](auto many) {
         if (p.dim == 128) run(LatInt<128>{}, many);
@@ -460,20 +503,16 @@ void join(const HeadParams& p, const HeadSplit& sp, hipStream_t s) {
     else dims(LatInt<0>{});
 }
 
-hipError_t tile(const HeadParams& p, bool split, unsigned grid, int tiles, hipStream_t s) {
-    return p.dim == 128 ? launch_head_tile_128(p, split, grid, tiles, s) : launch_head_tile_64(p, split, grid, tiles, s);
-}
-
 }  // namespace
 
 hipError_t launch_head_few(const HeadParams& p, hipStream_t s) {
-    meta(p, kHeadFew, 0, s);
+    meta(p, 1, s);
     const bool once = (long long)p.max_new * p.ratio <= kFewRows;      // one row tile a request and group reads its tokens
     auto few = [&](auto dim, auto tree, auto reads) {
         constexpr int D = decltype(dim)::value;
         constexpr bool kTree = decltype(tree)::value != 0, kOnce = decltype(reads)::value != 0;
-        if (p.y_bf16) hipLaunchKernelGGL((k_head_few<D, kTree, kOnce, false>), dim3(kHeadFew.groups), dim3(kFewThreads), 0, s, p);
-        else hipLaunchKernelGGL((k_head_few<D, kTree, kOnce, true>), dim3(kHeadFew.groups), dim3(kFewThreads), 0, s, p);
+        if (p.y_bf16) hipLaunchKernelGGL((k_head_few<D, kTree, kOnce, false>), dim3(kFewGroups), dim3(kFewThreads), 0, s, p);
+        else hipLaunchKernelGGL((k_head_few<D, kTree, kOnce, true>), dim3(kFewGroups), dim3(kFewThreads), 0, s, p);
     };
     auto trees = [&](auto dim, auto reads) {
         if (p.tree) few(dim, LatInt<1>{}, reads);
@@ -485,26 +524,24 @@ hipError_t launch_head_few(const HeadParams& p, hipStream_t s) {
     };
     if (once) dims(LatInt<1>{});
     else dims(LatInt<0>{});
-    join(p, kHeadFew, s);
+    join(p, 1, s);
     return hipGetLastError();
 }
 
 hipError_t launch_head_many(const HeadParams& p, hipStream_t s) {
-    meta(p, kHeadMany, 0, s);
-    const hipError_t err = tile(p, true, kHeadMany.groups, 0, s);
-    if (err != hipSuccess) return err;
-    join(p, kHeadMany, s);
-    return hipGetLastError();
-}
-
-hipError_t launch_head_whole(const HeadParams& p, hipStream_t s) {
-    meta(p, kHeadMany, 1, s);
-    long long tiles = std::max(p.B, 1) * (((long long)p.max_new * p.ratio + kHeadMany.rows - 1) / kHeadMany.rows);
-    tiles = std::max(std::min(tiles, (long long)p.T * p.ratio / kHeadMany.rows + p.B), 1ll);
-    // Row tiles of all heads; where some XCDs share a head, as many for each of them; blanks.
+    meta(p, 0, s);
+    // Row tiles of a group at most; pieces, where they are cut.
+    long long tiles = std::max(p.B, 1) * (((long long)p.max_new * p.ratio + kTileRows - 1) / kTileRows);
+    tiles = std::max(std::min(tiles, (long long)p.T * p.ratio / kTileRows + p.B), 1ll);
+    if (p.part) tiles = std::max(tiles, (long long)(kTilePieces / p.G));
+    // As many for each of the XCDs that share a group; blanks.
     long long grid = tiles * p.G;
     if (p.G % kXcds && kXcds % p.G == 0) grid = (tiles + kXcds / p.G - 1) / (kXcds / p.G) * kXcds;
-    return tile(p, false, (unsigned)(grid + kHeadBlank), (int)tiles, s);
+    if (!p.part) grid += kHeadBlank;
+    const hipError_t err = p.dim == 128 ? launch_head_tile_128(p, (unsigned)grid, (int)tiles, s)
+                                        : launch_head_tile_64(p, (unsigned)grid, (int)tiles, s);
+    if (err == hipSuccess && p.part) join(p, 0, s);
+    return err == hipSuccess ? hipGetLastError() : err;
 }
 
 }  // namespace caee

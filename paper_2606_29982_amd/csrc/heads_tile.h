@@ -1,7 +1,6 @@
 // Attention with grouped heads, many rows: 256 query rows of a request and
-// group (its new tokens' heads, head fastest) a workgroup.
-//   whole   a workgroup takes all tokens its rows see
-//   split   a workgroup takes a share of all row tiles' tokens (see HeadSplit)
+// group (its new tokens' heads, head fastest) a workgroup, over all tokens that
+// the rows see or a piece of them.
 #pragma once
 
 #include "heads.h"
@@ -10,7 +9,93 @@ namespace caee {
 namespace {
 
 constexpr int kTileThreads = 512;
-constexpr int kTileRows = kHeadMany.rows, kTileTokens = kHeadMany.tokens;
+
+// Steps of a piece at most.  A lane tries cutting the longest request's row tiles
+// into lane + 1 pieces, others' as far as theirs are longer; what decides is
+// the time that the CUs take for all pieces, with kStart steps for a piece's start
+// and end and kJoin for the partial results.
+__device__ inline int head_piece(const HeadParams& p, const HeadLine& line) {
+    constexpr float kStart = 5.0f, kJoin = 8.0f;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int tiles = lane < p.B ? head_tiles(p, line.mine) : 0, n = tiles > 0 ? head_steps(line.mine) : 0;
+    int most = n, least = tiles > 0 ? n : INT32_MAX, all = tiles;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+        most = max(most, __shfl_xor(most, d));
+        least = min(least, __shfl_xor(least, d));
+        all = head_add_units(all, __shfl_xor(all, d));
+    }
+    most = max(__builtin_amdgcn_readfirstlane(most), 1);
+    all = __builtin_amdgcn_readfirstlane(all);
+    if (!p.part || (long long)all * p.G > kTilePieces) return most;
+    const int per = (most + lane) / (lane + 1);
+    const float inverse = 1.0f / (float)per;
+    int pieces = 0;
+    float units = 0.0f;
+    for (int b = 0; b < p.B; ++b) {
+        const int t = __builtin_amdgcn_readlane(tiles, b), m = __builtin_amdgcn_readlane(n, b);
+        int c = (int)((float)m * inverse);      // ceil(m / per), in two corrections
+        c += c * per < m;
+        c -= (c - 1) * per >= m;
+        pieces += t * max(c, 1);
+        units += (float)t * (float)m;
+    }
+    pieces *= p.G;
+    const int rounds = (pieces + kHeadCus - 1) / kHeadCus;
+    const float each = (float)per + kStart;
+    const float mean = (units * (float)p.G + (float)pieces * kStart) * (1.0f / kHeadCus);
+    // Pieces of one size run in rounds; others fill each other's gaps.
+    float cost = __builtin_amdgcn_readfirstlane(least) == most ? (float)rounds * each : fmaxf(each, mean + 0.5f * (float)per);
+    if (lane > 0) cost = pieces <= kTilePieces ? cost + kJoin : INFINITY;
+    float best = cost;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) best = fminf(best, __shfl_xor(best, d));
+    return __builtin_amdgcn_readlane(per, __ffsll((unsigned long long)__ballot(cost == best)) - 1);
+}
+
+// Row tile q of all requests' by where it begins in its request, the last first:
+// those see the most tokens, and what starts last should be short.  (Up to
+// kOrdered requests; a lane tries a place, all 64 at a time.)
+constexpr int kOrdered = 16;
+struct HeadAt {
+    int b, rt;
+};
+__device__ inline HeadAt head_order(const HeadParams& p, const HeadLine& line, int q) {
+    const int lane = threadIdx.x & (kWave - 1);
+    // Row tiles of a request that begin at token x or later.
+    auto from = [&](int tiles, int before, int add, int x) {
+        return tiles - min(tiles, (min(max(x - before, 0), add) * p.ratio + kTileRows - 1) / kTileRows);
+    };
+    const int tiles = line.n;
+    int lo = 0, hi = 1;
+    for (int b = 0; b < p.B; ++b) {
+        const int before = __builtin_amdgcn_readlane(line.mine.before, b);
+        lo = min(lo, before);
+        hi = max(hi, before + __builtin_amdgcn_readlane(line.mine.add, b));
+    }
+    auto count = [&](int x) {
+        int n = 0;
+        for (int b = 0; b < p.B; ++b)
+            n += from(__builtin_amdgcn_readlane(tiles, b), __builtin_amdgcn_readlane(line.mine.before, b),
+                      __builtin_amdgcn_readlane(line.mine.add, b), x);
+        return n;
+    };
+    while (hi - lo > 1) {          // count(lo) > q >= count(hi)
+        const int step = (hi - lo + kWave - 1) / kWave, x = lo + (lane + 1) * step;
+        const int n = count(x), k = __popcll(__ballot(x < hi && n > q));
+        hi = min(hi, lo + (k + 1) * step);
+        lo += k * step;
+    }
+    int left = q - __builtin_amdgcn_readfirstlane(count(lo + 1));
+    const int here = from(tiles, line.mine.before, line.mine.add, lo), later = from(tiles, line.mine.before, line.mine.add, lo + 1);
+    HeadAt at = {0, 0};
+    for (int b = 0; b < p.B; ++b) {
+        const int h = __builtin_amdgcn_readlane(here, b), n = h - __builtin_amdgcn_readlane(later, b);
+        if (left >= 0 && left < n) at = {b, __builtin_amdgcn_readlane(tiles, b) - h + left};
+        left -= n;
+    }
+    return at;
+}
 
 // Keys or values of 64 tokens, or the queries of two waves, 32 each: blocks of 8
 // rows x 128 bytes, swizzled.
@@ -19,7 +104,7 @@ struct HeadTile {
     lat_u32x4 v[kTileTokens / 8][G][kWave];
 };
 
-template <int D, bool kSplit, bool kTree, bool kRest>
+template <int D, bool kTree, bool kRest>
 __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
     constexpr int kG = D / 64, kJ = D / 16, NC = D / 32;
@@ -33,77 +118,66 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool second = wave >= 4;
-    const HeadLine line = head_line(p, [&](const LatentReq& r) {
-        return kSplit ? head_units(p, r, kTileRows, kTileTokens) : (r.add * p.ratio + kTileRows - 1) / kTileRows;
-    });
-
     const int kp0 = (n >> 3) * (kG * kWave) + (n & 7) * 8 + (hf ^ lat_swz(n));
     const int vrow = 4 * hf + ((lane & 15) >> 2);
     const int vp0 = 2 * (vrow * 8 + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ lat_swz(vrow))) + (lane & 1);
     const uint32_t row_bytes = (uint32_t)p.c.row_stride * 2u;
     const uint32_t swz = 16u * ((lane & 7) ^ lat_swz(8 * wave + (lane >> 3)));
 
-    int u = 0, share1 = 1, per = 1, share0 = 0, g = 0;
-    if constexpr (kSplit) {
-        per = head_share(kHeadMany, line.total);
-        share0 = (int)min((long long)head_group(kHeadMany, blockIdx.x) * per, (long long)line.total);
-        share1 = min(share0 + per, line.total);
-        u = share0;
+    // Workgroups go to the XCDs round robin.  The last ones blank the rows of no request.
+    const unsigned wg = lat_workgroup();
+    int g, q;
+    if (p.G % kXcds == 0) {            // all row tiles of a group on one XCD, whose L2 holds its keys and values
+        const int k = wg / kXcds;
+        g = wg % kXcds + kXcds * (k / tiles);
+        q = k % tiles;
+    } else if (kXcds % p.G == 0) {     // or on some of them
+        const int x = wg % kXcds, subs = kXcds / p.G;
+        g = x % p.G;
+        q = (int)(wg / kXcds) * subs + x / p.G;
+        if (q >= (tiles + subs - 1) / subs * subs) g = p.G;
     } else {
-        // The workgroups of the last line blank the rows of no request.
-        const unsigned wg = lat_workgroup();
-        int q;
-        if (p.G % kXcds == 0) {            // all tiles of a head on one XCD, whose L2 holds its keys and values
-            const int k = wg / kXcds;
-            g = wg % kXcds + kXcds * (k / tiles);
-            q = k % tiles;
-        } else if (kXcds % p.G == 0) {     // or on some of them
-            const int x = wg % kXcds, subs = kXcds / p.G;
-            g = x % p.G;
-            q = (int)(wg / kXcds) * subs + x / p.G;
-            if (q >= (tiles + subs - 1) / subs * subs) g = p.G;
-        } else {
-            g = wg / tiles;
-            q = wg % tiles;
-        }
-        if (g >= p.G) {
-            const long long words = (long long)p.H * D * (p.y_bf16 ? 2 : 4) / 16;
-            const int from = p.B > 0 ? min(max(p.cu_new[p.B], 0), p.T) : 0;
-            const long long n_w = (p.T - from) * words, n_r = (long long)(p.T - from) * p.H;
-            const long long first = ((long long)gridDim.x * gridDim.y - 1 - wg) * kTileThreads + threadIdx.x;
-            constexpr long long kBy = (long long)kHeadBlank * kTileThreads;
-            if (first >= kBy) return;
-            for (long long i = first; i < n_w; i += kBy) ((lat_u32x4*)p.y)[from * words + i] = lat_u32x4{0, 0, 0, 0};
-            if (p.lse)
-                for (long long i = first; i < n_r; i += kBy) p.lse[(long long)from * p.H + i] = -INFINITY;
-            return;
-        }
-        u = line.total - 1 - q;            // the last tiles, which see the most tokens, first
-        if (u < 0) return;
-        share1 = u + 1;
+        g = wg / tiles;
+        q = wg % tiles;
     }
-
-    while (u < share1) {
-        const int b = head_line_find(p, line, u);
+    if (g >= p.G) {
+        const long long words = (long long)p.H * D * (p.y_bf16 ? 2 : 4) / 16;
+        const int from = p.B > 0 ? min(max(p.cu_new[p.B], 0), p.T) : 0;
+        const long long n_w = (p.T - from) * words, n_r = (long long)(p.T - from) * p.H;
+        const long long first = ((long long)gridDim.x * gridDim.y - 1 - wg) * kTileThreads + threadIdx.x;
+        constexpr long long kBy = (long long)kHeadBlank * kTileThreads;
+        if (first >= kBy) return;
+        for (long long i = first; i < n_w; i += kBy) ((lat_u32x4*)p.y)[from * words + i] = lat_u32x4{0, 0, 0, 0};
+        if (p.lse)
+            for (long long i = first; i < n_r; i += kBy) p.lse[(long long)from * p.H + i] = -INFINITY;
+        return;
+    }
+    HeadLine line = head_line(p);
+    const int per = p.B > kWave ? __builtin_amdgcn_readfirstlane(p.meta[p.B + 1]) : head_piece(p, line);
+    if (p.B <= kWave && wg == 0 && threadIdx.x == 0) p.meta[p.B + 1] = per;       // for the join
+    head_line_sum(p, &line, head_tiles(p, line.mine) * head_cut(head_steps(line.mine), per));
+    if (q >= line.total) return;
+    int b, rt, part = 0, parts = 1;
+    const bool cut = p.B <= kWave && __any(line.n > head_tiles(p, line.mine));
+    if (p.B > 1 && p.B <= kOrdered && !cut && line.total * p.G > kHeadCus) {
+        const HeadAt at = head_order(p, line, q);
+        b = at.b;
+        rt = at.rt;
+    } else {
+        const int u = line.total - 1 - q;
         int at_u;
-        const LatentReq rq = head_line_req(p, line, b, &at_u);
-        const int rows = rq.add * p.ratio;
-        int rt, first = 0, last = (rq.seq + kTileTokens - 1) / kTileTokens;
-        bool whole = true, head = true;
-        if constexpr (kSplit) {
-            const int n_t = (rows + kTileRows - 1) / kTileRows, n_u = last;
-            const int rel = u - at_u, tile = head_div(rel, n_u);
-            g = head_div(tile, n_t);
-            rt = tile - g * n_t;
-            first = rel - tile * n_u;
-            last = min(n_u, first + (share1 - u));
-            whole = first == 0 && last == n_u;
-            head = u == share0;
-            u += last - first;
-        } else {
-            rt = u - at_u;
-            u = share1;
-        }
+        b = head_line_find(p, line, u);
+        const LatentReq r = head_line_req(p, line, b, &at_u);
+        parts = __builtin_amdgcn_readfirstlane(head_cut(head_steps(r), per));
+        rt = head_div(u - at_u, parts);
+        part = u - at_u - rt * parts;
+    }
+    int at_b;
+    const LatentReq rq = head_line_req(p, line, b, &at_b);
+    {
+        const int rows = rq.add * p.ratio, steps_all = head_steps(rq);
+        const int first = head_div(steps_all * part, parts), last = head_div(steps_all * (part + 1), parts);
+        const bool whole = parts == 1;
         const int row0 = rt * kTileRows, my0 = row0 + 32 * wave;
         auto sees = [&](int r) { return head_sees(p, rq, head_div(min(r, rows - 1), p.ratio)); };
         const int row = min(my0 + n, rows - 1), tok = row / p.ratio;
@@ -117,7 +191,6 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
         const int at_row = (rq.t0 + tok) * p.H + g * p.ratio + row - tok * p.ratio;      // of y and lse
         const uint32_t* mask = kTree ? p.tree + (size_t)(rq.t0 + tok) * p.words : nullptr;
 
-        if constexpr (kSplit) __syncthreads();       // the row tile before is done with LDS
         if (threadIdx.x == 0) odd_values = 0;
         // A wave's queries, as its results at the end, go through a part of LDS of
         // its own, eight lanes a 128-byte line.  The stages of tile 0, fetched
@@ -379,7 +452,7 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
         lat_barrier();             // nobody's loads are on their way into the stages any more
         l = lat_sum_pair(l);
         const bool odd = __builtin_amdgcn_readfirstlane(odd_values) || __any(head_odd(o, l));
-        const size_t slot0 = ((size_t)blockIdx.x * 2 + (head ? 0 : 1)) * kTileRows;
+        const size_t slot0 = ((size_t)g * line.total + at_b + rt * parts + part) * kTileRows;
         const float f = whole ? lat_inverse(l) : 1.0f;
         if (hf == 0 && my0 + n < rows) {
             if (!whole) *(float2*)(p.part_ml + 2 * (slot0 + 32 * wave + n)) = make_float2(m, l);
@@ -441,11 +514,19 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
 #endif
 }
 
-template <int D, bool kSplit, bool kTree>
-hipError_t head_tile(const HeadParams& p, unsigned grid, int tiles, hipStream_t s) {
+template <int D>
+hipError_t head_tile(const HeadParams& p, unsigned grid, int pieces, hipStream_t s) {
+    auto run = [&](auto tree, auto rest) {
+        hipLaunchKernelGGL((k_head_tile<D, decltype(tree)::value != 0, decltype(rest)::value != 0>), lat_grid(grid),
+                           dim3(kTileThreads), 0, s, p, pieces);
+    };
+    auto trees = [&](auto rest) {
+        if (p.tree) run(LatInt<1>{}, rest);
+        else run(LatInt<0>{}, rest);
+    };
     // Weights' remainders for 32-bit results only.
-    if (p.y_bf16) hipLaunchKernelGGL((k_head_tile<D, kSplit, kTree, false>), lat_grid(grid), dim3(kTileThreads), 0, s, p, tiles);
-    else hipLaunchKernelGGL((k_head_tile<D, kSplit, kTree, true>), lat_grid(grid), dim3(kTileThreads), 0, s, p, tiles);
+    if (p.y_bf16) trees(LatInt<0>{});
+    else trees(LatInt<1>{});
     return hipGetLastError();
 }
 
