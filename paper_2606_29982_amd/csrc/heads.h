@@ -25,9 +25,9 @@ constexpr int kFewGroups = 512;                    // two workgroups a CU
 // Many rows (k_head_tile): row tiles of kTileRows rows, a workgroup each, or,
 // where that leaves CUs idle, one for each of equal pieces of the row tile's
 // tokens, which leave partial results: at most kTilePieces pieces then.
-constexpr int kTileRows = 256, kTileTokens = 64;
-constexpr int kTilePieces = 512;
-constexpr int kHeadCus = 256;
+constexpr int kTileRows = 128, kTileTokens = 64;
+constexpr int kTileSlots = 512;                    // workgroups that run at a time, two a CU
+constexpr int kTilePieces = 2 * kTileSlots;
 constexpr unsigned kHeadBlank = 64;                // workgroups that blank the rows of no request (whole form)
 // A quotient of uniform numbers, in a scalar register.
 __device__ inline int head_div(int a, int b) { return __builtin_amdgcn_readfirstlane(a / b); }

@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kFewThreads) void k_head_meta(HeadParams p, int few
             __syncthreads();
         }
         // (a row tile has fewer than steps / per + 1 pieces; what is rounded in `work` has room)
-        if ((long long)part[0] * p.G < kHeadCus) per = max((int)ceilf(work[0] * (1.001f / kHeadCus) * (float)p.G), 1);
+        if ((long long)part[0] * p.G < kTileSlots) per = max((int)ceilf(work[0] * (1.001f / kTileSlots) * (float)p.G), 1);
         __syncthreads();
     }
     auto number = [&](int b) {

@@ -1,4 +1,4 @@
-// Attention with grouped heads, many rows: 256 query rows of a request and
+// Attention with grouped heads, many rows: 128 query rows of a request and
 // group (its new tokens' heads, head fastest) a workgroup, over all tokens that
 // the rows see or a piece of them.
 #pragma once
@@ -8,7 +8,7 @@
 namespace caee {
 namespace {
 
-constexpr int kTileThreads = 512;
+constexpr int kTileThreads = 256;
 
 // Steps of a piece at most.  A lane tries cutting the longest request's row tiles
 // into lane + 1 pieces, others' as far as theirs are longer; what decides is
@@ -41,9 +41,9 @@ __device__ inline int head_piece(const HeadParams& p, const HeadLine& line) {
         units += (float)t * (float)m;
     }
     pieces *= p.G;
-    const int rounds = (pieces + kHeadCus - 1) / kHeadCus;
+    const int rounds = (pieces + kTileSlots - 1) / kTileSlots;
     const float each = (float)per + kStart;
-    const float mean = (units * (float)p.G + (float)pieces * kStart) * (1.0f / kHeadCus);
+    const float mean = (units * (float)p.G + (float)pieces * kStart) * (1.0f / kTileSlots);
     // Pieces of one size run in rounds; others fill each other's gaps.
     float cost = __builtin_amdgcn_readfirstlane(least) == most ? (float)rounds * each : fmaxf(each, mean + 0.5f * (float)per);
     if (lane > 0) cost = pieces <= kTilePieces ? cost + kJoin : INFINITY;
@@ -105,24 +105,22 @@ struct HeadTile {
 };
 
 template <int D, bool kTree, bool kRest>
-__global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int tiles) {
+__global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
     constexpr int kG = D / 64, kJ = D / 16, NC = D / 32;
     constexpr int kAhead = 5;                  // fragments read from LDS ahead of their MFMAs
-    constexpr int kLoads = 2 * kG;             // loads of a wave per tile: one block of 8 tokens
+    constexpr int kEights = 2, kLoads = kEights * kG;      // blocks of 8 tokens that a wave fetches of a tile; loads
     using Stage = HeadTile<kG>;
     // An object per stage: the compiler can tell the reads of one from the
-    // loads that fill another.
-    __shared__ Stage kt0, kt1, kt2, vt0, vt1, vt2;
+    // loads that fill the other.
+    __shared__ Stage kt0, kt1, vt0, vt1;
     __shared__ int odd_values;                 // an infinity or NaN was taken out of the values
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bool second = wave >= 4;
     const int kp0 = (n >> 3) * (kG * kWave) + (n & 7) * 8 + (hf ^ lat_swz(n));
     const int vrow = 4 * hf + ((lane & 15) >> 2);
     const int vp0 = 2 * (vrow * 8 + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ lat_swz(vrow))) + (lane & 1);
     const uint32_t row_bytes = (uint32_t)p.c.row_stride * 2u;
-    const uint32_t swz = 16u * ((lane & 7) ^ lat_swz(8 * wave + (lane >> 3)));
 
     // Workgroups go to the XCDs round robin.  The last ones blank the rows of no request.
     const unsigned wg = lat_workgroup();
@@ -159,7 +157,7 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
     if (q >= line.total) return;
     int b, rt, part = 0, parts = 1;
     const bool cut = p.B <= kWave && __any(line.n > head_tiles(p, line.mine));
-    if (p.B > 1 && p.B <= kOrdered && !cut && line.total * p.G > kHeadCus) {
+    if (p.B > 1 && p.B <= kOrdered && !cut && line.total * p.G > kTileSlots) {
         const HeadAt at = head_order(p, line, q);
         b = at.b;
         rt = at.rt;
@@ -193,9 +191,9 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
 
         if (threadIdx.x == 0) odd_values = 0;
         // A wave's queries, as its results at the end, go through a part of LDS of
-        // its own, eight lanes a 128-byte line.  The stages of tile 0, fetched
-        // meanwhile, are left out.
-        lat_u32x4* const own = &(wave < 2 ? kt1 : wave < 4 ? kt2 : wave < 6 ? vt1 : vt2).v[4 * (wave & 1)][0][0];
+        // its own, eight lanes a 128-byte line: the other stages than tile 0's,
+        // fetched meanwhile.
+        lat_u32x4* const own = &(wave < 2 ? kt1 : vt1).v[4 * (wave & 1)][0][0];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = 8 * i + (lane >> 3), rr = min(my0 + r, rows - 1), t = rr / p.ratio;
@@ -211,79 +209,77 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
         for (int c = 0; c < NC; ++c) o[c] = lat_f32x16{};
         float m = kNoScore, l = 0.0f;
 
-        // A wave fetches 8 tokens of a tile; the pages of tiles are looked up a
-        // step before their keys are.
-        auto eight = [&](int s) __attribute__((always_inline)) { return head_eight(p, b, rq.seq, tok0 + min(s, steps - 1) * kTileTokens + 8 * wave); };
+        // A wave fetches 16 tokens of a tile; their pages are looked up a step before.
+        struct Eights {
+            HeadEight e[kEights];
+        };
+        auto place = [&](int s, int i) __attribute__((always_inline)) { return tok0 + s * kTileTokens + 8 * (kEights * wave + i); };
+        auto eights = [&](int s) __attribute__((always_inline)) {
+            Eights x;
+#pragma unroll
+            for (int i = 0; i < kEights; ++i) x.e[i] = head_eight(p, b, rq.seq, place(s, i));
+            return x;
+        };
+        auto piece = [&](int i) __attribute__((always_inline)) { return 16u * ((lane & 7) ^ lat_swz(8 * i + (lane >> 3))); };
         const char *const k_base = head_base(p, p.k, g), *const v_base = head_base(p, p.v, g);
-        auto load = [&](const char* cache, const HeadEight& e, int s, Stage& st) __attribute__((always_inline)) {
-            const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
-                (void*)(cache + head_offset(p, e.page, e.at)), 0, e.one ? kLatBufBytes : 0, kLatBufWord3);
-            const uint32_t at = (uint32_t)min(lane >> 3, e.span) * row_bytes + swz;
+        auto load = [&](const char* cache, const Eights& x, int s, Stage& st) __attribute__((always_inline)) {
 #pragma unroll
-            for (int gg = 0; gg < kG; ++gg)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st.v[wave][gg][0], 16, at, 128 * gg, 0, 0);
-            if (!e.one) {      // rows in several pages go one by one, after the loads above, which touch nothing
+            for (int i = 0; i < kEights; ++i) {
+                const HeadEight& e = x.e[i];
+                const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc((void*)(cache + head_offset(p, e.page, e.at)), 0,
+                                                                                    e.one ? kLatBufBytes : 0, kLatBufWord3);
+                const uint32_t at = (uint32_t)min(lane >> 3, e.span) * row_bytes + piece(i);
+#pragma unroll
+                for (int gg = 0; gg < kG; ++gg)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st.v[kEights * wave + i][gg][0], 16, at, 128 * gg, 0, 0);
+            }
+            if (!(x.e[0].one && x.e[1].one)) {
+                // Rows in several pages go one by one, after the loads above, which touch nothing there.
                 lat_wait_vm<0>();
-                const int p0 = tok0 + min(s, steps - 1) * kTileTokens + 8 * wave;
 #pragma unroll 1
-                for (int r = 0; r < 8; ++r) {
-                    const __amdgpu_buffer_rsrc_t far = __builtin_amdgcn_make_buffer_rsrc(
-                        (void*)(cache + head_row(p, b, min(p0 + r, rq.seq - 1))), 0, kLatBufBytes, kLatBufWord3);
-                    if (lane >> 3 == r) {
+                for (int i = 0; i < kEights; ++i) {
+                    const int p0 = place(s, i), r0 = min(p0, rq.seq - 1), r1 = min(p0 + 7, rq.seq - 1);
+                    if (r0 / p.c.block == r1 / p.c.block) continue;
+#pragma unroll 1
+                    for (int r = 0; r < 8; ++r) {
+                        const __amdgpu_buffer_rsrc_t far = __builtin_amdgcn_make_buffer_rsrc(
+                            (void*)(cache + head_row(p, b, min(p0 + r, rq.seq - 1))), 0, kLatBufBytes, kLatBufWord3);
+                        if (lane >> 3 == r) {
 #pragma unroll
-                        for (int gg = 0; gg < kG; ++gg)
-                            __builtin_amdgcn_raw_ptr_buffer_load_lds(far, (lat_lds_void*)&st.v[wave][gg][0], 16, swz, 128 * gg, 0, 0);
+                            for (int gg = 0; gg < kG; ++gg)
+                                __builtin_amdgcn_raw_ptr_buffer_load_lds(far, (lat_lds_void*)&st.v[kEights * wave + i][gg][0], 16, piece(i),
+                                                                         128 * gg, 0, 0);
+                        }
                     }
                 }
                 lat_wait_vm<0>();
             }
         };
-        // Step s has two phases: X multiplies the keys of tile s and sums the
-        // values of tile s - 1, Y makes the weights of tile s (exponentials) and
-        // starts loads.  The two waves of a SIMD take turns: waves 4 .. 7 run one
-        // barrier behind waves 0 .. 3, so that one is in X while the other is in Y.
-        // Keys of tile s are read in phases 2 s (waves 0 .. 3) and 2 s + 1 (4 .. 7),
-        // values in 2 s + 2 and 2 s + 3; so in Y(s) the first waves, in phase 2 s + 1,
-        // may load the keys of tile s + 2 and the values of tile s + 1 into rings of
-        // three, the others, in phase 2 s + 2, those of one tile more.  At the end of
-        // the odd phases (Y of the first waves, X of the others) a wave waits for
-        // all but its latest step's loads: what the next phase reads is then there.
-        // Past the last tile the loads read it again, for nobody.
-        auto clear = [&](int s, Stage& d) __attribute__((always_inline)) {
+        auto clear = [&](int tb, Stage& d) __attribute__((always_inline)) {
             // Tokens that some rows do not see may hold anything: infinities and NaNs
             // must not meet their zero weights, so a wave clears them from the
             // values that it loaded, before the barrier that publishes them.
-            const int tb = tok0 + s * kTileTokens;
-            if (s >= steps || tb + kTileTokens <= lim_wg) return;
-            if (tb + 8 * wave + (lane >> 3) >= lim_wg) {
-                bool odd = false;
 #pragma unroll
-                for (int gg = 0; gg < kG; ++gg) {
-                    const lat_u32x4 v = d.v[wave][gg][lane];
-                    lat_u32x4 w;
+            for (int i = 0; i < kEights; ++i)
+                if (tb + 8 * (kEights * wave + i) + (lane >> 3) >= lim_wg) {
+                    bool odd = false;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        w[e] = lat_finite(v[e]);
-                        odd |= w[e] != v[e];
+                    for (int gg = 0; gg < kG; ++gg) {
+                        const lat_u32x4 v = d.v[kEights * wave + i][gg][lane];
+                        lat_u32x4 w;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            w[e] = lat_finite(v[e]);
+                            odd |= w[e] != v[e];
+                        }
+                        d.v[kEights * wave + i][gg][lane] = w;
                     }
-                    d.v[wave][gg][lane] = w;
+                    if (odd) odd_values = 1;
                 }
-                if (odd) odd_values = 1;
-            }
             __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
         };
-        auto odd_end = [&](int s, Stage& values) __attribute__((always_inline)) {
-            lat_wait_vm<kLoads>();
-            asm volatile("" ::: "memory");
-            clear(s, values);
-        };
-        lat_u32x4 pf[4] = {}, pr[kRest ? 4 : 1] = {}, pl[kRest ? 4 : 1] = {};       // weights of the tile before, their remainders
+        lat_u32x4 pf[4], pr[kRest ? 4 : 1], pl[kRest ? 4 : 1];       // weights, their remainders
         lat_f32x16 sc[2];
-        // X's MFMAs, 2 kJ of the scores and 4 NC of the sums, evenly mixed (two
-        // chains of sums alone would wait for each other), their fragments read
-        // kAhead before they are used.
-        constexpr int kOps = 2 * kJ + 4 * NC;
-        auto sums_before = [](int i) constexpr { return i * (4 * NC) / kOps; };
         auto value = [&](const Stage& d, int i, int vp) __attribute__((always_inline)) {
             const lat_u32x2* base = (const lat_u32x2*)&d.v[0][0][0];
             const int ks = i / NC, c = i % NC;
@@ -295,57 +291,40 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
             }
             return lat_u32x4{w[0][0], w[0][1], w[1][0], w[1][1]};
         };
-        auto sum = [&](const lat_u32x4& v, int i) __attribute__((always_inline)) {
-            o[i % NC] = lat_mma(v, pf[i / NC], o[i % NC]);
-            if constexpr (kRest) {
-                o[i % NC] = lat_mma(v, pr[i / NC], o[i % NC]);
-                o[i % NC] = lat_mma(v, pl[i / NC], o[i % NC]);
-            }
-        };
-        HeadEight e_k = {}, e_v = {}, e_next = {};      // of the keys and values that Y loads, and of the next keys
-        const int more_k = second ? 3 : 2;
-        // k, k2: the keys of tile s (their stage then takes those of tile s + 3)
-        // and the stage for those of tile s + 2; v0, v1, v2: the values of tiles
-        // s - 1 (their stage then takes those of tile s + 2) and s and the stage
-        // for those of tile s + 1.
-        auto step = [&](int s, Stage& k, Stage& k2, Stage& v0, Stage& v1, Stage& v2) __attribute__((always_inline)) {
+        Eights next;
+        // Tile s in k and v; the next one into k2 and v2.
+        auto step = [&](int s, Stage& k, Stage& v, Stage& k2, Stage& v2) __attribute__((always_inline)) {
             const int tb = tok0 + s * kTileTokens;
-            const lat_u32x4* keys = &k.v[0][0][0];
+            lat_wait_vm<0>();              // this wave's part of the tile is there; after the barrier all of it is,
+            asm volatile("" ::: "memory"); // and nobody reads the other stage
+            if (tb + kTileTokens > lim_wg) clear(tb, v);
+            lat_barrier();
+            if (s + 1 < steps) {
+                load(k_base, next, s + 1, k2);
+                load(v_base, next, s + 1, v2);
+                next = eights(s + 2);
+            }
             // made here: the registers that a stage's addresses would take through the loop are not there
             int kp = kp0, vp = vp0;
             asm volatile("" : "+v"(kp), "+v"(vp));
-            auto fetch = [&](auto ic) __attribute__((always_inline)) {
-                constexpr int i = decltype(ic)::value, v = sums_before(i);
-                if constexpr (sums_before(i + 1) > v) {
-                    return value(v0, v, vp);
-                } else {
-                    constexpr int j = (i - v) >> 1, e = (i - v) & 1;
-                    return keys[(kp ^ (2 * (j % 4))) + (4 * e * kG + j / 4) * kWave];
-                }
+            const lat_u32x4* keys = &k.v[0][0][0];
+            auto key = [&](int i) __attribute__((always_inline)) {
+                const int j = i >> 1, e = i & 1;
+                return keys[(kp ^ (2 * (j % 4))) + (4 * e * kG + j / 4) * kWave];
             };
             __builtin_amdgcn_sched_barrier(0);
             lat_u32x4 fr[kAhead];
             sc[0] = sc[1] = lat_f32x16{};
-            lat_for<0, kAhead>([&](auto ic) __attribute__((always_inline)) { fr[decltype(ic)::value] = fetch(ic); });
-            lat_for<0, kOps>([&](auto ic) __attribute__((always_inline)) {
-                constexpr int i = decltype(ic)::value, v = sums_before(i), j = i - v;
-                if constexpr (sums_before(i + 1) > v) sum(fr[i % kAhead], v);
-                else sc[j & 1] = lat_mma(fr[i % kAhead], qf[j >> 1], sc[j & 1]);
-                if constexpr (i + kAhead < kOps) fr[i % kAhead] = fetch(LatInt<i + kAhead>{});
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) fr[i] = key(i);
+            lat_for<0, 2 * kJ>([&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value;
+                sc[i & 1] = lat_mma(fr[i % kAhead], qf[i >> 1], sc[i & 1]);
+                if constexpr (i + kAhead < 2 * kJ) fr[i % kAhead] = key(i + kAhead);
                 __builtin_amdgcn_sched_barrier(0);
             });
-            if (second) odd_end(s, v1);
-            lat_barrier();
-            e_v = e_k;
-            e_k = e_next;
-            if (second) {
-                load(k_base, e_k, s + more_k, k);
-                load(v_base, e_v, s + more_k - 1, v0);
-            } else {
-                load(k_base, e_k, s + more_k, k2);
-                load(v_base, e_v, s + more_k - 1, v2);
-            }
-            e_next = eight(s + more_k + 1);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) fr[i] = value(v, i, vp);
             if (tb + kTileTokens > lim_min) {
                 asm volatile("");       // a branch, not 32 selects in every step
 #pragma unroll
@@ -395,61 +374,38 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
                 weights(lat_weight);
             }
             l += more;
-            if (!second) odd_end(s, v1);
-            lat_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            lat_for<0, 4 * NC>([&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value;
+                const lat_u32x4 f = fr[i % kAhead];
+                o[i % NC] = lat_mma(f, pf[i / NC], o[i % NC]);
+                if constexpr (kRest) {
+                    o[i % NC] = lat_mma(f, pr[i / NC], o[i % NC]);
+                    o[i % NC] = lat_mma(f, pl[i / NC], o[i % NC]);
+                }
+                if constexpr (i + kAhead < 4 * NC) fr[i % kAhead] = value(v, i + kAhead, vp);
+                __builtin_amdgcn_sched_barrier(0);
+            });
         };
         if (steps > 0) {
-            // Tile 0, the keys of tile 1 (and what the second waves' Y(-1) would
-            // have loaded); the values of "tile -1" are zeros.
-            const HeadEight e0 = eight(0), e1 = eight(1), e2 = eight(2);
+            const Eights e0 = eights(0);
             load(k_base, e0, 0, kt0);
             load(v_base, e0, 0, vt0);
-            lat_wait_vm<kLoads>();
+            next = eights(1);
+            lat_wait_vm<2 * kLoads>();
             asm volatile("" ::: "memory");
 #pragma unroll
-            for (int j = 0; j < kJ; ++j)
-                qf[j] = own[(kp0 ^ (2 * (j & 3))) + (j >> 2) * kWave];
+            for (int j = 0; j < kJ; ++j) qf[j] = own[(kp0 ^ (2 * (j & 3))) + (j >> 2) * kWave];
             __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
-            lat_barrier();             // the stages the queries came through are free
-            load(k_base, e1, 1, kt1);
-            if (second) {
-                load(k_base, e2, 2, kt2);
-                load(v_base, e1, 1, vt1);
-                e_k = e2;
-                e_next = eight(3);
-            } else {
-                e_k = e1;
-                e_next = e2;
+            lat_barrier();                 // odd_values is set
+            for (int s = 0; s < steps; s += 2) {
+                step(s, kt0, vt0, kt1, vt1);
+                if (s + 1 < steps) step(s + 1, kt1, vt1, kt0, vt0);
             }
-#pragma unroll
-            for (int gg = 0; gg < kG; ++gg) vt2.v[wave][gg][lane] = lat_u32x4{0, 0, 0, 0};
-            // Tile 0 is there; the keys of tile 1 are waited for at the end of phase 1.
-            if (second) lat_wait_vm<kG + kLoads>();
-            else lat_wait_vm<kG>();
-            asm volatile("" ::: "memory");
-            clear(0, vt0);
-            __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
-            lat_barrier();
-            if (second) lat_barrier();
-            for (int s = 0; s < steps; s += 3) {
-                step(s, kt0, kt2, vt2, vt0, vt1);
-                if (s + 1 < steps) step(s + 1, kt1, kt0, vt0, vt1, vt2);
-                if (s + 2 < steps) step(s + 2, kt2, kt1, vt1, vt2, vt0);
-            }
-            if (!second) lat_barrier();
-            lat_wait_vm<0>();          // the last tile's second readings have landed
-            auto finish = [&](const Stage& d) __attribute__((always_inline)) {
-#pragma unroll
-                for (int i = 0; i < 4 * NC; ++i) sum(value(d, i, vp0), i);
-            };
-            const int at = (steps - 1) % 3;
-            if (at == 0) finish(vt0);
-            else if (at == 1) finish(vt1);
-            else finish(vt2);
         }
 
         lat_wait_vm<0>();
-        lat_barrier();             // nobody's loads are on their way into the stages any more
+        __syncthreads();           // nobody reads the stages any more
         l = lat_sum_pair(l);
         const bool odd = __builtin_amdgcn_readfirstlane(odd_values) || __any(head_odd(o, l));
         const size_t slot0 = ((size_t)g * line.total + at_b + rt * parts + part) * kTileRows;
@@ -460,7 +416,7 @@ __global__ __launch_bounds__(kTileThreads) void k_head_tile(HeadParams p, int ti
         }
         // 8 (dim 64: 4) KiB a wave: as much of a row at a time as a bf16 row has, unit
         // u (16 bytes) of it at u ^ (row % units).
-        lat_u32x4* const out = &(wave < 2 ? kt0 : wave < 4 ? kt1 : wave < 6 ? kt2 : vt0).v[4 * (wave & 1)][0][0];
+        lat_u32x4* const out = &(wave < 2 ? kt0 : vt0).v[4 * (wave & 1)][0][0];
         constexpr int kUnits = D / 8;
         // (made here, as above)
         int ln = lane;
