@@ -93,6 +93,23 @@ __device__ inline int head_steps(const LatentReq& r) { return (r.seq + kTileToke
 // Pieces of a row tile of n steps.
 __device__ inline int head_cut(int n, int per) { return max((n + per - 1) / per, 1); }
 
+// Inclusive scan over the lanes, in registers (a shuffle through LDS takes ten
+// times as long, and a workgroup begins with a chain of these), and its last.
+template <int C, int ROWS, class Op>
+__device__ inline int head_scan_step(int v, int none, Op&& op) {
+    return op(v, __builtin_amdgcn_update_dpp(none, v, C, ROWS, 0xF, false));
+}
+template <class Op>
+__device__ inline int head_scan(int v, int none, Op&& op) {
+    v = head_scan_step<0x111, 0xF>(v, none, op);       // 1, 2, 4 and 8 lanes down a row of 16
+    v = head_scan_step<0x112, 0xF>(v, none, op);
+    v = head_scan_step<0x114, 0xF>(v, none, op);
+    v = head_scan_step<0x118, 0xF>(v, none, op);
+    v = head_scan_step<0x142, 0xA>(v, none, op);       // the rows' last lanes to the next row, the second's to both after it
+    return head_scan_step<0x143, 0xC>(v, none, op);
+}
+__device__ inline int head_last(int v) { return __builtin_amdgcn_readlane(v, kWave - 1); }
+
 // Prefix sums over the requests of a number each has.  Up to 64 requests every
 // wave makes them by itself, a lane each; of more, p.meta has them.
 struct HeadLine {
@@ -109,14 +126,9 @@ __device__ inline void head_line_sum(const HeadParams& p, HeadLine* h, int n) {
     if (p.B > kWave) return;
     const int lane = threadIdx.x & (kWave - 1);
     h->n = lane < p.B ? n : 0;
-    int sum = h->n;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int u = __shfl_up(sum, d);
-        if (lane >= d) sum = head_add_units(sum, u);
-    }
+    const int sum = head_scan(h->n, 0, head_add_units);
     h->at = sum - h->n;
-    h->total = __builtin_amdgcn_readlane(sum, kWave - 1);
+    h->total = head_last(sum);
 }
 // Request b of the line: its lengths and what is before it.
 __device__ inline LatentReq head_line_req(const HeadParams& p, const HeadLine& h, int b, int* at) {
@@ -145,30 +157,42 @@ __device__ inline uint32_t head_tree_bits(const uint32_t* mask, int words, int b
     return sh ? (a >> sh) | (b << (32 - sh)) : a;
 }
 
-// Eight tokens from `pos` on (the last of a request again for those past it),
-// whose rows are fetched by one load where they lie in one page.
-struct HeadEight {
-    int page, at, span;       // of the first row; the others follow up to at + span
-    bool one;
+// Where the tokens that a wave fetches lie: eights of them, whose rows one load
+// gets where they lie in one page, E of a tile.  A lane looks up one eight, so
+// that a look covers kHeadWindow / E tiles and a step reads lanes (in scalar
+// instructions, a tile's addresses take as long as its products).
+constexpr int kHeadWindow = kWave;
+struct HeadWindow {
+    uint32_t lo, hi;      // byte offset of the eight's first row from the cache's (of the group)
+    int span;             // the others follow up to this row after it; -1: they lie in several pages
 };
-__device__ inline int head_entry(const HeadParams& p, int b, unsigned j) {
-    const size_t i = (size_t)b * p.max_blocks + min(j, (unsigned)p.max_blocks - 1u);
-    return ((const __attribute__((address_space(4))) int32_t*)p.table)[i];
+// The eight that begins at token `pos` (tokens past the request's are its last
+// one), in two parts: what the first asks for may be on its way for a while.
+struct HeadLook {
+    int entry, at, span;
+};
+__device__ inline HeadLook head_look(const HeadParams& p, int b, int seq, int pos) {
+    const int r0 = min(pos, seq - 1), span = min(pos + 7, seq - 1) - r0;
+    const unsigned j = (unsigned)r0 / (unsigned)p.c.block;
+    return {p.table[(size_t)b * p.max_blocks + min(j, (unsigned)p.max_blocks - 1u)], r0 - (int)(j * (unsigned)p.c.block), span};
 }
-__device__ inline HeadEight head_eight(const HeadParams& p, int b, int seq, int pos) {
-    const int r0 = min(pos, seq - 1), r1 = min(pos + 7, seq - 1);
-    const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)r0 / (unsigned)p.c.block);
-    const int at = r0 - (int)(j * (unsigned)p.c.block);
-    return {head_entry(p, b, j), at, r1 - r0, at + (r1 - r0) < p.c.block};
+__device__ inline HeadWindow head_window(const HeadParams& p, const HeadLook& l) {
+    const unsigned long long off =
+        2ull * (unsigned long long)(min(max(l.entry, 0), p.c.n_blocks - 1) * p.c.page_stride + l.at * p.c.row_stride);
+    return {(uint32_t)off, (uint32_t)(off >> 32), l.at + l.span < p.c.block ? l.span : -1};
 }
-// Byte offset of row `at` of a page from the first one's (of the same head).
-__device__ inline long long head_offset(const HeadParams& p, int page, int at) {
-    return 2 * (min(max(page, 0), p.c.n_blocks - 1) * p.c.page_stride + at * p.c.row_stride);
-}
-// The same for row `pos` of request b.
+// Byte offset of row `pos` of request b.
 __device__ inline long long head_row(const HeadParams& p, int b, int pos) {
-    const unsigned j = __builtin_amdgcn_readfirstlane((unsigned)pos / (unsigned)p.c.block);
-    return head_offset(p, head_entry(p, b, j), pos - (int)(j * (unsigned)p.c.block));
+    const HeadWindow w = head_window(p, head_look(p, b, pos + 1, pos));
+    return (long long)((unsigned long long)w.hi << 32 | w.lo);
+}
+struct HeadEight {
+    unsigned long long off;
+    int span;
+};
+__device__ inline HeadEight head_eight(const HeadWindow& w, int i) {
+    return {(unsigned long long)(uint32_t)__builtin_amdgcn_readlane(w.hi, i) << 32 | (uint32_t)__builtin_amdgcn_readlane(w.lo, i),
+            __builtin_amdgcn_readlane(w.span, i)};
 }
 __device__ inline const char* head_base(const HeadParams& p, const uint16_t* cache, int g) {
     return (const char*)(cache + g * p.c.head_stride);
@@ -176,13 +200,13 @@ __device__ inline const char* head_base(const HeadParams& p, const uint16_t* cac
 
 // Softmax weight of score s where the running maximum is m, by one multiply-add:
 // what m's product with scale_log2 lost to rounding is a factor that all weights
-// of the row have in common, next to 1 while m is of a size up to kFusedMax (the
-// largest scores take lat_weight).
-constexpr float kFusedMax = 0x1p20f;
+// of the row have in common.  Up to kFusedMax it is at most 2^64 (half a step of
+// m), and neither it nor the sums leave the range of 32 bits.
+constexpr float kFusedMax = 0x1p30f;
 __device__ inline float head_weight(float s, float scale_log2, float m) { return __builtin_amdgcn_exp2f(fmaf(s, scale_log2, -m)); }
 // While the weights of a lane's tile add up to no more than kMaxWeight none of
 // them exceeds it, and the maximum need not move.
-__device__ inline bool head_moves(float more, float m) { return more > kMaxWeight || !(fabsf(m) <= kFusedMax); }
+__device__ inline bool head_moves(float more, float m) { return more > kMaxWeight || !(fabsf(m) <= 0x1p20f); }
 
 // Adds a partial result (sums x of weights by the maximum w.x, whose total is w.y)
 // to one.

@@ -133,43 +133,39 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         const int steps = end > tok0 ? (end - tok0 + kFewTokens - 1) / kFewTokens : 0;
         const uint32_t* mask = kTree ? p.tree + (size_t)(rq.t0 + tok) * p.words : nullptr;
 
-        auto eights = [&](int s, HeadEight (&e)[4]) __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = head_eight(p, b, rq.seq, tok0 + s * kFewTokens + 8 * i);
+        constexpr int kEights = kWaveTokens / 8, kLook = kHeadWindow / kEights;
+        auto look = [&](int s) __attribute__((always_inline)) {
+            return head_look(p, b, rq.seq, tok0 + (s + lane / kEights) * kFewTokens + 8 * (lane % kEights));
         };
         auto piece = [&](int i) __attribute__((always_inline)) { return 16u * ((lane & 7) ^ lat_swz(8 * (i & 1) + (lane >> 3))); };
-        // A buffer of size 0 where nothing is to be loaded: its loads cost no
-        // traffic, and their number does not depend on a branch.
         const char *const k_base = head_base(p, p.k, g), *const v_base = head_base(p, p.v, g);
-        auto fetch = [&](const char* cache, FewStage<D>& st, int s, const HeadEight (&e)[4], bool there) __attribute__((always_inline)) {
+        // A buffer of size 0 past the last tile: its loads cost no traffic, and their
+        // number does not depend on a branch.
+        auto fetch = [&](const char* cache, FewStage<D>& st, int s, const HeadWindow& w) __attribute__((always_inline)) {
+            const bool there = s < steps;
+            bool far = false;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < kEights; ++i) {
+                const HeadEight e = head_eight(w, s % kLook * kEights + i);
                 const __amdgpu_buffer_rsrc_t buf =
-                    __builtin_amdgcn_make_buffer_rsrc((void*)(cache + head_offset(p, e[i].page, e[i].at)), 0,
-                                                      there && e[i].one ? kLatBufBytes : 0, kLatBufWord3);
-                const uint32_t at = (uint32_t)min(lane >> 3, e[i].span) * row_bytes + piece(i);
+                    __builtin_amdgcn_make_buffer_rsrc((void*)(cache + e.off), 0, there && e.span >= 0 ? kLatBufBytes : 0, kLatBufWord3);
+                const uint32_t at = (uint32_t)min(lane >> 3, e.span) * row_bytes + piece(i);
 #pragma unroll
-                for (int gg = 0; gg < kG; ++gg) {
+                for (int gg = 0; gg < kG; ++gg)
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st.v[wave][i][gg][0], 16, at, 128 * gg, 0, kOnce ? 2 : 0);
-                }
+                far |= e.span < 0;
             }
-            if (there && !(e[0].one && e[1].one && e[2].one && e[3].one)) {
-                // Rows in several pages go one by one.
+            if (there && far) {
+                // Rows in several pages, each by an address of its own, after the loads above, which touch nothing there.
                 lat_wait_vm<0>();
 #pragma unroll 1
-                for (int i = 0; i < 4; ++i) {
-                    const int p0 = tok0 + s * kFewTokens + 8 * i, r0 = min(p0, rq.seq - 1), r1 = min(p0 + 7, rq.seq - 1);
-                    if (r0 / p.c.block == r1 / p.c.block) continue;
-#pragma unroll 1
-                    for (int r = 0; r < 8; ++r) {
-                        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
-                            (void*)(cache + head_row(p, b, min(p0 + r, rq.seq - 1))), 0, kLatBufBytes, kLatBufWord3);
-                        if (lane >> 3 == r) {
+                for (int i = 0; i < kEights; ++i) {
+                    if (__builtin_amdgcn_readlane(w.span, s % kLook * kEights + i) >= 0) continue;
+                    const int pos = min(tok0 + s * kFewTokens + 8 * i + (lane >> 3), rq.seq - 1);
+                    const char* row = cache + head_row(p, b, pos) + piece(i);
 #pragma unroll
-                            for (int gg = 0; gg < kG; ++gg)
-                                __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st.v[wave][i][gg][0], 16, piece(i), 128 * gg, 0, 0);
-                        }
-                    }
+                    for (int gg = 0; gg < kG; ++gg)
+                        __builtin_amdgcn_global_load_lds((lat_g_void*)(row + 128 * gg), (lat_lds_void*)&st.v[wave][i][gg][0], 16, 0, 0);
                 }
                 lat_wait_vm<0>();
             }
@@ -185,11 +181,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
                 __builtin_amdgcn_global_load_lds((lat_g_void*)(src + 64 * gg), (lat_lds_void*)&qs[wave][gg][0], 16, 0, 0);
             if ((lane & 7) == 0) row_at[r] = (rq.t0 + i) * p.H + g * p.ratio + rr - i * p.ratio;
         }
-        HeadEight now[4];
-        eights(0, now);
-        fetch(k_base, ks, 0, now, steps > 0);
-        fetch(v_base, vs, 0, now, steps > 0);
-        eights(1, now);
+        HeadWindow win = head_window(p, look(0));      // of kLook tiles
+        HeadLook soon = {};                            // of the next ones
+        fetch(k_base, ks, 0, win);
+        fetch(v_base, vs, 0, win);
         lat_wait_vm<2 * kLoads>();
         __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
         lat_barrier();
@@ -213,7 +208,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
             for (int j = 0; j < kJ; ++j) sc = lat_mma(keys[(kp0 ^ (2 * (j & 3))) + (j >> 2) * kWave], qf[j], sc);
             __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
             __builtin_amdgcn_sched_barrier(0);
-            fetch(k_base, ks, s + 1, now, s + 1 < steps);
+            // the window of tile s + 1 on, asked for half a window before
+            if ((s + 1) % kLook == kLook / 2) soon = look((s + 1) / kLook * kLook + kLook);
+            if ((s + 1) % kLook == 0) win = head_window(p, soon);
+            fetch(k_base, ks, s + 1, win);
             const bool masked = tb + kWaveTokens > lim_min;
             if (masked) {
                 asm volatile("");       // a branch, not selects in every step
@@ -301,8 +299,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
                 }
             __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
             __builtin_amdgcn_sched_barrier(0);
-            fetch(v_base, vs, s + 1, now, s + 1 < steps);
-            eights(s + 2, now);
+            fetch(v_base, vs, s + 1, win);
         }
         lat_wait_vm<0>();
         l = lat_sum_pair(l);

@@ -16,18 +16,13 @@ constexpr int kTileThreads = 256;
 // and end and kJoin for the partial results.
 __device__ inline int head_piece(const HeadParams& p, const HeadLine& line) {
     constexpr float kStart = 5.0f, kJoin = 8.0f;
+    if (!p.part) return INT32_MAX / 2;
     const int lane = threadIdx.x & (kWave - 1);
     const int tiles = lane < p.B ? head_tiles(p, line.mine) : 0, n = tiles > 0 ? head_steps(line.mine) : 0;
-    int most = n, least = tiles > 0 ? n : INT32_MAX, all = tiles;
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) {
-        most = max(most, __shfl_xor(most, d));
-        least = min(least, __shfl_xor(least, d));
-        all = head_add_units(all, __shfl_xor(all, d));
-    }
-    most = max(__builtin_amdgcn_readfirstlane(most), 1);
-    all = __builtin_amdgcn_readfirstlane(all);
-    if (!p.part || (long long)all * p.G > kTilePieces) return most;
+    const int most = max(head_last(head_scan(n, 0, [](int a, int b) { return max(a, b); })), 1);
+    const int least = head_last(head_scan(tiles > 0 ? n : INT32_MAX, INT32_MAX, [](int a, int b) { return min(a, b); }));
+    const int all = head_last(head_scan(tiles, 0, head_add_units));
+    if ((long long)all * p.G > kTilePieces) return most;
     const int per = (most + lane) / (lane + 1);
     const float inverse = 1.0f / (float)per;
     int pieces = 0;
@@ -45,12 +40,11 @@ __device__ inline int head_piece(const HeadParams& p, const HeadLine& line) {
     const float each = (float)per + kStart;
     const float mean = (units * (float)p.G + (float)pieces * kStart) * (1.0f / kTileSlots);
     // Pieces of one size run in rounds; others fill each other's gaps.
-    float cost = __builtin_amdgcn_readfirstlane(least) == most ? (float)rounds * each : fmaxf(each, mean + 0.5f * (float)per);
+    float cost = least == most ? (float)rounds * each : fmaxf(each, mean + 0.5f * (float)per);
     if (lane > 0) cost = pieces <= kTilePieces ? cost + kJoin : INFINITY;
-    float best = cost;
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) best = fminf(best, __shfl_xor(best, d));
-    return __builtin_amdgcn_readlane(per, __ffsll((unsigned long long)__ballot(cost == best)) - 1);
+    // (costs are positive: their order is that of their bits)
+    const int best = head_last(head_scan(__float_as_int(cost), INT32_MAX, [](int a, int b) { return min(a, b); }));
+    return __builtin_amdgcn_readlane(per, __ffsll((unsigned long long)__ballot(__float_as_int(cost) == best)) - 1);
 }
 
 // Row tile q of all requests' by where it begins in its request, the last first:
@@ -209,50 +203,47 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
         for (int c = 0; c < NC; ++c) o[c] = lat_f32x16{};
         float m = kNoScore, l = 0.0f;
 
-        // A wave fetches 16 tokens of a tile; their pages are looked up a step before.
+        // A wave fetches 16 tokens of a tile.
+        auto place = [&](int s, int i) __attribute__((always_inline)) { return tok0 + s * kTileTokens + 8 * (kEights * wave + i); };
+        constexpr int kLook = kHeadWindow / kEights;
+        HeadWindow win = {};           // of kLook tiles
+        HeadLook soon = {};            // of the next ones
+        auto look = [&](int s) __attribute__((always_inline)) { return head_look(p, b, rq.seq, place(s + lane / kEights, lane % kEights)); };
+        auto piece = [&](int i) __attribute__((always_inline)) { return 16u * ((lane & 7) ^ lat_swz(8 * i + (lane >> 3))); };
+        const char *const k_base = head_base(p, p.k, g), *const v_base = head_base(p, p.v, g);
+        // Load n of a wave's part of tile s, the keys' and then the values' eights.  (A
+        // buffer of size 0 past the last tile: its loads cost no traffic, and their
+        // number does not depend on a branch.)
         struct Eights {
             HeadEight e[kEights];
         };
-        auto place = [&](int s, int i) __attribute__((always_inline)) { return tok0 + s * kTileTokens + 8 * (kEights * wave + i); };
         auto eights = [&](int s) __attribute__((always_inline)) {
             Eights x;
 #pragma unroll
-            for (int i = 0; i < kEights; ++i) x.e[i] = head_eight(p, b, rq.seq, place(s, i));
+            for (int i = 0; i < kEights; ++i) x.e[i] = head_eight(win, s % kLook * kEights + i);
             return x;
         };
-        auto piece = [&](int i) __attribute__((always_inline)) { return 16u * ((lane & 7) ^ lat_swz(8 * i + (lane >> 3))); };
-        const char *const k_base = head_base(p, p.k, g), *const v_base = head_base(p, p.v, g);
-        auto load = [&](const char* cache, const Eights& x, int s, Stage& st) __attribute__((always_inline)) {
+        auto load = [&](int n, const Eights& x, int s, Stage& k, Stage& v) __attribute__((always_inline)) {
+            const int i = n % kLoads / kG, gg = n % kG;
+            const HeadEight& e = x.e[i];
+            const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc((void*)((n < kLoads ? k_base : v_base) + e.off), 0,
+                                                                                s < steps && e.span >= 0 ? kLatBufBytes : 0, kLatBufWord3);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&(n < kLoads ? k : v).v[kEights * wave + i][gg][0], 16,
+                                                     (uint32_t)min(lane >> 3, e.span) * row_bytes + piece(i), 128 * gg, 0, 0);
+        };
+        // Rows in several pages, each by an address of its own, after the loads above, which touch nothing there.
+        auto load_far = [&](const Eights& x, int s, Stage& k, Stage& v) __attribute__((always_inline)) {
+            if (s >= steps || (x.e[0].span >= 0 && x.e[1].span >= 0)) return;
+            lat_wait_vm<0>();
 #pragma unroll
             for (int i = 0; i < kEights; ++i) {
-                const HeadEight& e = x.e[i];
-                const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc((void*)(cache + head_offset(p, e.page, e.at)), 0,
-                                                                                    e.one ? kLatBufBytes : 0, kLatBufWord3);
-                const uint32_t at = (uint32_t)min(lane >> 3, e.span) * row_bytes + piece(i);
+                if (x.e[i].span >= 0) continue;
+                const long long row = head_row(p, b, min(place(s, i) + (lane >> 3), rq.seq - 1)) + piece(i);
 #pragma unroll
-                for (int gg = 0; gg < kG; ++gg)
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lat_lds_void*)&st.v[kEights * wave + i][gg][0], 16, at, 128 * gg, 0, 0);
-            }
-            if (!(x.e[0].one && x.e[1].one)) {
-                // Rows in several pages go one by one, after the loads above, which touch nothing there.
-                lat_wait_vm<0>();
-#pragma unroll 1
-                for (int i = 0; i < kEights; ++i) {
-                    const int p0 = place(s, i), r0 = min(p0, rq.seq - 1), r1 = min(p0 + 7, rq.seq - 1);
-                    if (r0 / p.c.block == r1 / p.c.block) continue;
-#pragma unroll 1
-                    for (int r = 0; r < 8; ++r) {
-                        const __amdgpu_buffer_rsrc_t far = __builtin_amdgcn_make_buffer_rsrc(
-                            (void*)(cache + head_row(p, b, min(p0 + r, rq.seq - 1))), 0, kLatBufBytes, kLatBufWord3);
-                        if (lane >> 3 == r) {
-#pragma unroll
-                            for (int gg = 0; gg < kG; ++gg)
-                                __builtin_amdgcn_raw_ptr_buffer_load_lds(far, (lat_lds_void*)&st.v[kEights * wave + i][gg][0], 16, piece(i),
-                                                                         128 * gg, 0, 0);
-                        }
-                    }
+                for (int gg = 0; gg < kG; ++gg) {
+                    __builtin_amdgcn_global_load_lds((lat_g_void*)(k_base + row + 128 * gg), (lat_lds_void*)&k.v[kEights * wave + i][gg][0], 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((lat_g_void*)(v_base + row + 128 * gg), (lat_lds_void*)&v.v[kEights * wave + i][gg][0], 16, 0, 0);
                 }
-                lat_wait_vm<0>();
             }
         };
         auto clear = [&](int tb, Stage& d) __attribute__((always_inline)) {
@@ -291,7 +282,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
             }
             return lat_u32x4{w[0][0], w[0][1], w[1][0], w[1][1]};
         };
-        Eights next;
         // Tile s in k and v; the next one into k2 and v2.
         auto step = [&](int s, Stage& k, Stage& v, Stage& k2, Stage& v2) __attribute__((always_inline)) {
             const int tb = tok0 + s * kTileTokens;
@@ -299,11 +289,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
             asm volatile("" ::: "memory"); // and nobody reads the other stage
             if (tb + kTileTokens > lim_wg) clear(tb, v);
             lat_barrier();
-            if (s + 1 < steps) {
-                load(k_base, next, s + 1, k2);
-                load(v_base, next, s + 1, v2);
-                next = eights(s + 2);
-            }
+            // the window of tile s + 1 on, asked for half a window before
+            if ((s + 1) % kLook == kLook / 2) soon = look((s + 1) / kLook * kLook + kLook);
+            if ((s + 1) % kLook == 0) win = head_window(p, soon);
+            const Eights x = eights(s + 1);
             // made here: the registers that a stage's addresses would take through the loop are not there
             int kp = kp0, vp = vp0;
             asm volatile("" : "+v"(kp), "+v"(vp));
@@ -321,8 +310,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
                 constexpr int i = decltype(ic)::value;
                 sc[i & 1] = lat_mma(fr[i % kAhead], qf[i >> 1], sc[i & 1]);
                 if constexpr (i + kAhead < 2 * kJ) fr[i % kAhead] = key(i + kAhead);
+                if constexpr (i % 2 == 1 && i / 2 < 2 * kLoads) load(i / 2, x, s + 1, k2, v2);
                 __builtin_amdgcn_sched_barrier(0);
             });
+            static_assert(kJ >= 2 * kLoads, "a load between two products");
+            load_far(x, s + 1, k2, v2);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) fr[i] = value(v, i, vp);
             if (tb + kTileTokens > lim_min) {
@@ -338,66 +330,78 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
                     }
                 }
             }
-            // The weights by the running maximum; where it has to move they are made again.
-            float more = 0.0f;
-            auto weights = [&](auto&& weight) __attribute__((always_inline)) {
+            // The running maximum moves only when a score exceeds it by more than kMaxSlack.
+            float mt = fmaxf(sc[0][0], sc[1][0]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float a = weight(sc[k >> 1][8 * (k & 1) + 2 * i], p.scale_log2, m);
-                        const float e = weight(sc[k >> 1][8 * (k & 1) + 2 * i + 1], p.scale_log2, m);
-                        pf[k][i] = lat_pack(a, e);
-                        if constexpr (kRest) {
-                            const lat_f32x2 rest = lat_rest(pf[k][i], a, e);
-                            pr[k][i] = lat_pack(rest[0], rest[1]);
-                            const lat_f32x2 last = lat_rest(pr[k][i], rest[0], rest[1]);
-                            pl[k][i] = lat_pack(last[0], last[1]);
-                            more += a + e;
-                        } else {
-                            more = lat_sum2(pf[k][i], more);
-                        }
-                    }
-            };
-            weights(head_weight);
-            if (__any(head_moves(more, m))) {
-                float mt = fmaxf(sc[0][0], sc[1][0]);
-#pragma unroll
-                for (int i = 1; i < 16; ++i) mt = fmaxf(mt, fmaxf(sc[0][i], sc[1][i]));
+            for (int i = 1; i < 16; ++i) mt = fmaxf(mt, fmaxf(sc[0][i], sc[1][i]));
+            if (__any(mt * p.scale_log2 > m + kMaxSlack)) {
                 mt = lat_max_pair(mt) * p.scale_log2;
                 const float mn = fmaxf(m, mt), f = __builtin_amdgcn_exp2f(m - mn);
                 l *= f;
                 m = mn;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) o[c] *= f;
-                more = 0.0f;
-                weights(lat_weight);
             }
-            l += more;
-            __builtin_amdgcn_sched_barrier(0);
-            lat_for<0, 4 * NC>([&](auto ic) __attribute__((always_inline)) {
-                constexpr int i = decltype(ic)::value;
-                const lat_u32x4 f = fr[i % kAhead];
-                o[i % NC] = lat_mma(f, pf[i / NC], o[i % NC]);
+            // Weights are powers of two of sc factor - base: the products go into the
+            // multiply-add unrounded, which scales all weights of a row by what m lost to
+            // rounding; from kFusedMax on, where that might be too much, they are rounded.
+            float factor = p.scale_log2, base = m;
+            if (__any(fabsf(m) > kFusedMax && m > kNoScore)) {
+#pragma clang fp contract(off)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    sc[0][i] = sc[0][i] * factor - m;
+                    sc[1][i] = sc[1][i] * factor - m;
+                }
+                factor = 1.0f;
+                base = 0.0f;
+            }
+            auto weights = [&](auto kc, auto ic) __attribute__((always_inline)) {
+                constexpr int k = decltype(kc)::value, i = decltype(ic)::value;
+                const float a = head_weight(sc[k >> 1][8 * (k & 1) + 2 * i], factor, base);
+                const float e = head_weight(sc[k >> 1][8 * (k & 1) + 2 * i + 1], factor, base);
+                pf[k][i] = lat_pack(a, e);
                 if constexpr (kRest) {
-                    o[i % NC] = lat_mma(f, pr[i / NC], o[i % NC]);
-                    o[i % NC] = lat_mma(f, pl[i / NC], o[i % NC]);
+                    const lat_f32x2 rest = lat_rest(pf[k][i], a, e);
+                    pr[k][i] = lat_pack(rest[0], rest[1]);
+                    const lat_f32x2 last = lat_rest(pr[k][i], rest[0], rest[1]);
+                    pl[k][i] = lat_pack(last[0], last[1]);
+                    l += a + e;
+                } else {
+                    l = lat_sum2(pf[k][i], l);
+                }
+            };
+            lat_for<0, 4>([&](auto ic) __attribute__((always_inline)) { weights(LatInt<0>{}, ic); });
+            __builtin_amdgcn_sched_barrier(0);
+            // The sums, and the next 16 tokens' weights between them.
+            lat_for<0, 4 * NC>([&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value, k = i / NC, kPairs = 4 / NC;
+                const lat_u32x4 f = fr[i % kAhead];
+                o[i % NC] = lat_mma(f, pf[k], o[i % NC]);
+                if constexpr (kRest) {
+                    o[i % NC] = lat_mma(f, pr[k], o[i % NC]);
+                    o[i % NC] = lat_mma(f, pl[k], o[i % NC]);
                 }
                 if constexpr (i + kAhead < 4 * NC) fr[i % kAhead] = value(v, i + kAhead, vp);
+                if constexpr (k < 3)
+                    lat_for<0, kPairs>([&](auto jc) __attribute__((always_inline)) {
+                        weights(LatInt<(k < 3 ? k + 1 : 3)>{}, LatInt<i % NC * kPairs + decltype(jc)::value>{});
+                    });
                 __builtin_amdgcn_sched_barrier(0);
             });
         };
         if (steps > 0) {
-            const Eights e0 = eights(0);
-            load(k_base, e0, 0, kt0);
-            load(v_base, e0, 0, vt0);
-            next = eights(1);
+            win = head_window(p, look(0));
+            const Eights x = eights(0);
+#pragma unroll
+            for (int n2 = 0; n2 < 2 * kLoads; ++n2) load(n2, x, 0, kt0, vt0);
+            load_far(x, 0, kt0, vt0);
             lat_wait_vm<2 * kLoads>();
             asm volatile("" ::: "memory");
 #pragma unroll
             for (int j = 0; j < kJ; ++j) qf[j] = own[(kp0 ^ (2 * (j & 3))) + (j >> 2) * kWave];
             __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
-            lat_barrier();                 // odd_values is set
+            lat_barrier();                 // the stages the queries came through are free
             for (int s = 0; s < steps; s += 2) {
                 step(s, kt0, vt0, kt1, vt1);
                 if (s + 1 < steps) step(s + 1, kt1, vt1, kt0, vt0);
