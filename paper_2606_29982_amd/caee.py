@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -102,6 +103,10 @@ class HeadDesc(ctypes.Structure):
         ("scale", ctypes.c_float)]
 
 
+# The same two, packed: a structure of twenty fields takes four times as long to make (2 us of a call's 10).
+_HEAD_STORE, _HEAD = struct.Struct("9if7q"), struct.Struct("13i5qf4x")
+
+
 class BlockMatmulDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("M", "N", "K", "x_dtype", "y_dtype", "layout")] + [
         ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64)]
@@ -143,9 +148,10 @@ def _load(path: str = LIB_PATH):
         "caee_latent_workspace_size": (st, [ctypes.POINTER(LatentDesc), ctypes.POINTER(ctypes.c_size_t)]),
         "caee_latent_attention": (st, [ctypes.POINTER(LatentDesc), P, ctypes.POINTER(LatentWeights), P, P, P, P, P, P,
                                        P, P, ctypes.c_size_t, P]),
-        "caee_head_store": (st, [ctypes.POINTER(HeadStoreDesc)] + [P] * 12),
+        # (descriptors that are packed by the caller, see _HEAD_STORE, or a structure's reference)
+        "caee_head_store": (st, [P] * 13),
         "caee_head_workspace_size": (st, [ctypes.POINTER(HeadDesc), ctypes.POINTER(ctypes.c_size_t)]),
-        "caee_head_attention": (st, [ctypes.POINTER(HeadDesc)] + [P] * 10 + [ctypes.c_size_t, P]),
+        "caee_head_attention": (st, [P] * 11 + [ctypes.c_size_t, P]),
         "caee_block_matmul_workspace_size": (st, [ctypes.POINTER(BlockMatmulDesc), ctypes.POINTER(ctypes.c_size_t)]),
         "caee_block_matmul": (st, [ctypes.POINTER(BlockMatmulDesc), P, P, P, P, P, P, ctypes.c_size_t, P]),
         "caee_status_str": (ctypes.c_char_p, [st]),
@@ -581,13 +587,13 @@ def _head_caches(k_cache, v_cache, kv_heads: int, dim: int) -> tuple:
 def _heads(t, name: str, dim: int):
     """Tokens, heads and token stride of [T][heads][dim] whose heads are dense (tokens may be strided)."""
     shape, stride = t.shape, t.stride()
+    if t.is_cuda and len(shape) == 3 and shape[2] == dim and stride[2] == 1 and (stride[1] == dim or shape[1] == 1):
+        return shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1] * dim
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if len(shape) != 3 or shape[2] != dim:
         raise ValueError(f"{name} must be [T][heads][{dim}]")
-    if stride[2] != 1 or (shape[1] > 1 and stride[1] != dim):
-        raise ValueError(f"{name} must have dense heads")
-    return shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1] * dim
+    raise ValueError(f"{name} must have dense heads")
 
 
 def head_store(q, k, v, slots, q_out, k_cache, v_cache, q_norm=None, k_norm=None, eps: float = 1e-6, position=None,
@@ -612,8 +618,8 @@ def head_store(q, k, v, slots, q_out, k_cache, v_cache, q_norm=None, k_norm=None
     rope = 0 if freq is None else 2 * freq.shape[0]
     if rope and position is None:
         raise ValueError("a rotation needs position")
-    d = HeadStoreDesc(T, H, G, dim, rope, 1 if adjacent else 0, _code(q), block, pages, eps, qs, ks, vs, os, ps, rs, hs)
-    _check(lib.caee_head_store(ctypes.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    d = _HEAD_STORE.pack(T, H, G, dim, rope, 1 if adjacent else 0, _code(q), block, pages, eps, qs, ks, vs, os, ps, rs, hs)
+    _check(lib.caee_head_store(d, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                None if q_norm is None else _at(q_norm, "q_norm", f32, one),
                                None if k_norm is None else _at(k_norm, "k_norm", f32, one),
                                None if freq is None else _at(freq, "freq", torch.float64, (rope // 2,)),
@@ -685,8 +691,9 @@ def head_attention(att: Heads, q, k_cache, v_cache, block_table, plan: dict, y, 
         tree_at = _at(tree, "tree", i32, (T, words))
     y_at = _at(y, "y", y.dtype, (T, H, D))
     lse_at = None if lse is None else _at(lse, "lse", torch.float32, (T, H))
-    d = att.desc(T, B, max_new, max_kv, block, pages, width, words, qs, (ps, rs, hs), _code(y))
-    _check(lib.caee_head_attention(ctypes.byref(d), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table_at, cu_at,
+    d = _HEAD.pack(T, B, H, att.kv_heads, D, block, pages, width, max_new, 1 if att.causal else 0, words,
+                   HEAD_FORM_CODE[att.form], _code(y), max_kv, qs, ps, rs, hs, att.scale)
+    _check(lib.caee_head_attention(d, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table_at, cu_at,
                                    seq_at, tree_at, y_at, lse_at, ws_at, ws_bytes, _stream(y)))
     return y
 

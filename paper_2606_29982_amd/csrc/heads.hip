@@ -11,23 +11,46 @@ namespace {
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Units and pieces are counted in 32 bits.
-bool few_fits(const caee_head_desc_t& d) {
-    const double tiles = (double)d.kv_heads * (((long long)d.max_new * (d.heads / d.kv_heads) + kFewRows - 1) / kFewRows);
-    return (double)(d.max_kv / kFewTokens + d.B) * tiles <= kHeadMaxUnits;
+// Bounds of what the device will find: the longest request's tokens, the row tiles
+// of a request and the units of all requests of the kernel of few rows.
+struct HeadBounds {
+    long long longest, few_tiles;
+    double few_units;
+};
+HeadBounds head_bounds(const caee_head_desc_t& d) {
+    HeadBounds b;
+    const long long kv = d.max_kv, before = std::max(kv - d.T, 0ll);
+    b.longest = std::min(std::min(kv, (long long)d.max_blocks * d.block_size), before + d.max_new);
+    b.few_tiles = ((long long)d.max_new * (d.heads / d.kv_heads) + kFewRows - 1) / kFewRows;
+    const long long per = (b.longest + kFewTokens - 1) / kFewTokens;
+    b.few_units = (double)std::min(d.B * per, kv / kFewTokens + d.B) * (double)b.few_tiles * d.kv_heads;
+    return b;
 }
 
-// Which kernel: that of few rows or of many.
-constexpr int kHeadFewRows = 64;
-bool head_few(const caee_head_desc_t& d) {
-    return d.form != CAEE_HEAD_WHOLE && (long long)d.max_new * (d.heads / d.kv_heads) <= kHeadFewRows && few_fits(d);
-}
-// Whether row tiles stay whole.
-bool head_whole(const caee_head_desc_t& d) {
-    if (d.form != CAEE_HEAD_AUTO) return d.form == CAEE_HEAD_WHOLE;
-    if (head_few(d)) return false;
-    const long long before = d.max_kv > d.T ? d.max_kv - d.T : 0;
-    return (long long)d.T * d.heads >= kTilePieces * kTileRows || before + d.max_new <= 24 * kTileTokens;
+// Which kernel: of few rows, of many, of many whose row tiles stay whole.  The
+// kernel of few rows reads its tokens once for each 32 rows, that of many once
+// for 128 and with more to do before and after.  us, few and many: 1 request of
+// 4000 tokens, 8 groups of 8 heads, with 1 new token (256 units) 14.7 and 16.9,
+// 13 (1024) 21.5 and 26.0, 32 (2048) 27.9 and 29.4, 61 (4096) 39.6 and 33.7; of
+// 30000 with 8 (3760) 54.6 and 34.9; 16 requests of 4000, 1 group, with 32 (4096)
+// 37.4 and 38.8, 61 (8192) 53.0 and 41.2.  One row tile a request and group, in
+// which neither reads a token twice: 16 requests of 4000, 8 groups 54.0 and 53.3.
+// Up to kHeadShort tokens cutting row tiles gains nothing, and joining costs 6 us
+// and more: 61 requests of 200, 1 group, with 1 new token few 13.8, whole 11.4, with
+// 61 few 39.5, many 29.4, whole 17.0; 16 of 500, 8 groups, with 4 (512 units) 23.2,
+// 20.7, 17.6; only a handful of units is faster by the kernel of few rows: 1 of 500, 8
+// groups, with 1 (32 units) 12.5 and 16.0, 16 of 500, 1 group, with 1 (64) 14.5 and
+// 16.2.  Where there are kTilePieces row tiles or more none is cut.
+constexpr long long kHeadShort = 24 * kTileTokens;
+constexpr double kHeadShortUnits = 64, kHeadFewUnits = 2048;
+enum class HeadWay { few, many, whole };
+HeadWay head_way(const caee_head_desc_t& d) {
+    if (d.form == CAEE_HEAD_WHOLE) return HeadWay::whole;
+    const HeadBounds b = head_bounds(d);
+    if (d.form == CAEE_HEAD_AUTO && b.longest <= kHeadShort) return b.few_units <= kHeadShortUnits ? HeadWay::few : HeadWay::whole;
+    // (units are counted in 32 bits)
+    if (b.few_units <= kHeadFewUnits || (b.few_tiles <= 1 && b.few_units <= kHeadMaxUnits)) return HeadWay::few;
+    return d.form == CAEE_HEAD_AUTO && (long long)d.T * d.heads >= kTilePieces * kTileRows ? HeadWay::whole : HeadWay::many;
 }
 
 HeadWs head_ws(const caee_head_desc_t& d) {
@@ -144,11 +167,12 @@ caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, c
     p.y = y;
     p.lse = lse;
     p.meta = (int32_t*)(w + L.meta);
-    p.part = head_whole(d) ? nullptr : (float*)(w + L.part);
+    const HeadWay way = head_way(d);
+    p.part = way == HeadWay::whole ? nullptr : (float*)(w + L.part);
     p.part_ml = (float*)(w + L.part_ml);
     hipStream_t s = (hipStream_t)stream;
     return timed_launch(CAEE_KERNEL_ATTENTION, s, "head attention", [&] {
-        return head_few(d) ? launch_head_few(p, s) : launch_head_many(p, s);
+        return way == HeadWay::few ? launch_head_few(p, s) : launch_head_many(p, s);
     });
 }
 
