@@ -1,4 +1,4 @@
-"""A decoder layer that serves a batch from a paged latent cache.
+"""A decoder layer that serves a batch from a paged cache.
 
 One step, for requests with any number of new tokens each (a prompt, or the
 one token of a decode step):
@@ -9,11 +9,19 @@ one token of a decode step):
     attention over the cached rows, output projection            caee.latent_attention, caee.block_matmul
     experts   router, cost-aware selection and the expert FFN    caee.moe_layer
 
-Norms, rotary embedding and the router's scores are torch operations.  The
+With --attention heads the layer keeps keys and values of grouped heads in its
+pages instead of latent rows:
+
+    queries, keys, values   x -> heads, 8-bit weights            caee.block_matmul
+    cache     norms, rotation, keys and values into their slots  caee.head_store
+    attention over the cached heads, output projection           caee.head_attention, caee.block_matmul
+
+Other norms, the latent rows' rotary embedding and the router's scores are torch operations.  The
 plan, the cache's pages and all sums of lengths stay on the device; the host
 knows only bounds.  Weights are random; a step's output is the next input.
 
     python examples/decoder_layer.py                             # small shape
+    python examples/decoder_layer.py --attention heads
     python examples/decoder_layer.py --shape deepseek-r1-fp8     # 128 heads, 256 experts
 """
 import argparse
@@ -93,18 +101,22 @@ class DecoderLayer:
         gen = torch.Generator(device=device).manual_seed(seed)
         d = shape.d
         self.shape, self.heads, self.device = shape, heads, device
-        self.q_down, self.q_up = Linear8(q_rank, d, gen), Linear8(heads * (NOPE + ROPE), q_rank, gen)
-        self.kv_down, self.out = Linear8(LATENT + ROPE, d, gen), Linear8(d, heads * V, gen)
-        rand = lambda *s: (torch.randn(s, generator=gen, device=device) * LATENT ** -0.5).bfloat16()  # noqa: E731
-        self.heads_kv = caee.pack_latent_weights(rand(heads, NOPE, LATENT), rand(heads, V, LATENT))
-        self.att = caee.Latent(heads=heads, nope=NOPE, rope=ROPE, latent=LATENT, v=V, scale=(NOPE + ROPE) ** -0.5)
-        self.cache = torch.zeros((n_pages, block, LATENT + ROPE), dtype=torch.bfloat16, device=device)
+        self.make_attention(heads, q_rank, n_pages, block, gen)
         self.router = torch.randn((shape.E, d), generator=gen, device=device) * d ** -0.5
         inp = make_routing_inputs(shape, seed=seed)
         to = lambda a: None if a is None else torch.from_numpy(a).to(device)  # noqa: E731
         self.bias, self.cost, self.bins = to(inp.bias), to(inp.cost), to(inp.bins)
         self.experts = make_expert_weights_torch(shape, seed, device)
         self.over = {} if tau is None else {"tau": tau}
+
+    def make_attention(self, heads, q_rank, n_pages, block, gen):
+        d, device = self.shape.d, self.device
+        self.q_down, self.q_up = Linear8(q_rank, d, gen), Linear8(heads * (NOPE + ROPE), q_rank, gen)
+        self.kv_down, self.out = Linear8(LATENT + ROPE, d, gen), Linear8(d, heads * V, gen)
+        rand = lambda *s: (torch.randn(s, generator=gen, device=device) * LATENT ** -0.5).bfloat16()  # noqa: E731
+        self.heads_kv = caee.pack_latent_weights(rand(heads, NOPE, LATENT), rand(heads, V, LATENT))
+        self.att = caee.Latent(heads=heads, nope=NOPE, rope=ROPE, latent=LATENT, v=V, scale=(NOPE + ROPE) ** -0.5)
+        self.cache = torch.zeros((n_pages, block, LATENT + ROPE), dtype=torch.bfloat16, device=device)
 
     def attention(self, x, plan, table, max_new, max_kv):
         """x + attention(norm(x)); the new tokens' rows go into the cache on the way."""
@@ -130,9 +142,33 @@ class DecoderLayer:
         return self.ffn(self.attention(x, plan, table, max_new, max_kv))
 
 
+class HeadsLayer(DecoderLayer):
+    """The same with grouped heads: four query heads share a head's keys and values."""
+
+    def make_attention(self, heads, q_rank, n_pages, block, gen):
+        d, device, kv = self.shape.d, self.device, max(heads // 4, 1)
+        self.split = [heads, kv, kv]
+        self.qkv, self.out = Linear8(sum(self.split) * V, d, gen), Linear8(d, heads * V, gen)
+        self.q_norm, self.k_norm = 1 + 0.1 * torch.randn((2, V), generator=gen, device=device)
+        self.freq = 10000.0 ** (-torch.arange(0, V, 2, device=device, dtype=torch.float64) / V)
+        self.att = caee.Heads(heads=heads, kv_heads=kv, dim=V, scale=V ** -0.5)
+        self.k_cache, self.v_cache = torch.zeros((2, n_pages, block, kv, V), dtype=torch.bfloat16, device=device)
+
+    def attention(self, x, plan, table, max_new, max_kv):
+        T = x.shape[0]
+        q, k, v = self.qkv(rms_norm(x).bfloat16()).view(T, sum(self.split), V).split(self.split, 1)
+        caee.head_store(q, k, v, plan["slots"], q, self.k_cache, self.v_cache, q_norm=self.q_norm, k_norm=self.k_norm,
+                        position=plan["position"], freq=self.freq)
+        y = torch.empty((T, self.heads, V), dtype=torch.bfloat16, device=x.device)
+        ws = caee.alloc_head_workspace(self.att, T, table.shape[0], max_new, max_kv, x.device)
+        caee.head_attention(self.att, q, self.k_cache, self.v_cache, table, plan, y, ws, max_new, max_kv)
+        return x + self.out(y.view(T, self.heads * V))
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--shape", choices=SHAPES, default="tiny")
+    ap.add_argument("--attention", choices=("latent", "heads"), default="latent")
     ap.add_argument("--prompts", type=int, nargs="+", default=[300, 17, 1, 129])
     ap.add_argument("--steps", type=int, default=16)
     ap.add_argument("--block", type=int, default=64)
@@ -141,7 +177,7 @@ def main():
     shape, heads, q_rank = SHAPES[args.shape]
     B, longest = len(args.prompts), max(args.prompts) + args.steps
     n_pages = sum(-(-(n + args.steps) // args.block) for n in args.prompts)
-    layer = DecoderLayer(shape, heads, q_rank, n_pages, args.block, device)
+    layer = (HeadsLayer if args.attention == "heads" else DecoderLayer)(shape, heads, q_rank, n_pages, args.block, device)
     pages = Pages(B, n_pages, args.block, longest, device)
     x = torch.randn((sum(args.prompts), shape.d), device=device).bfloat16()
     new, cached = torch.tensor(args.prompts, dtype=torch.int32, device=device), 0

@@ -562,12 +562,15 @@ caee_status_t caee_head_store(const caee_head_store_desc_t* desc, const void* q,
                               const float* q_norm, const float* k_norm, const double* freq, const int32_t* position,
                               const int64_t* slots, void* q_out, void* k_cache, void* v_cache, void* stream);
 
-/* How the work is dealt to the GPU.  Both give the same function. */
+/* How the work is dealt to the GPU.  All give the same function. */
 typedef enum caee_head_form {
+    /* Whole where no request can have more than 1536 tokens (by max_kv,
+     * max_blocks * block_size, and max_kv - T + max_new) or T * heads >= 131072;
+     * else split. */
     CAEE_HEAD_AUTO = 0,
-    /* Every request's tokens are cut into equal shares for all CUs, partial
-     * results joined: few new tokens (decode steps, trees, the next part of a
-     * long prompt). */
+    /* The requests' tokens are cut so that all CUs have a share, partial results
+     * are joined: few new tokens (decode steps, trees, the next part of a long
+     * prompt). */
     CAEE_HEAD_SPLIT = 1,
     /* A workgroup takes all tokens that its query rows see: prompts. */
     CAEE_HEAD_WHOLE = 2
@@ -593,7 +596,8 @@ typedef struct caee_head_desc {
     float scale;          /* factor on the scores, finite and > 0 */
 } caee_head_desc_t;
 
-/* Bytes of workspace caee_head_attention needs.  Host-only. */
+/* Bytes of workspace caee_head_attention needs: 4 (B + 2), and, but for
+ * CAEE_HEAD_WHOLE, 131072 (4 dim + 8), whatever the call's sizes.  Host-only. */
 caee_status_t caee_head_workspace_size(const caee_head_desc_t* desc, size_t* bytes);
 
 /* Softmax attention of the new tokens over the paged cache, which holds their
@@ -615,9 +619,11 @@ caee_status_t caee_head_workspace_size(const caee_head_desc_t* desc, size_t* byt
  * have rows, whose results are as if all had.  Cache rows at or past a request's
  * seq_len are never read; rows that a query does not see do not change its
  * result, whatever they hold.
+ * An infinity or NaN in a value that a row sees is in that place of its result;
+ * in a key it makes the row NaN.
  * Scores, softmax statistics and sums are fp32; the softmax weights are rounded
- * to bf16 before their products, for an fp32 y with a second bf16 part that
- * holds what the first leaves.
+ * to bf16 before their products (with few rows to two bf16 parts, the second
+ * what the first leaves), for an fp32 y to three parts, which lose nothing.
  * Preconditions on device contents (violations: unspecified results,
  * memory-safe): page numbers in [0, n_blocks) for the pages seq_len covers, at
  * most max_new new tokens per request and max_kv tokens in all. */

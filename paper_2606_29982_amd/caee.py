@@ -658,7 +658,8 @@ def head_workspace_size(att: Heads, T: int, B: int, max_new: int, max_kv: int, t
 
 
 def alloc_head_workspace(att: Heads, T: int, B: int, max_new: int, max_kv: int, device, tree: bool = False):
-    """Workspace of ``head_attention`` calls of this size; ``tree``: of calls with a tree."""
+    """Workspace of ``head_attention`` calls of up to ``B`` requests (the other sizes are checked, and with or without a
+    ``tree`` it is the same)."""
     import torch
     return torch.empty(max(head_workspace_size(att, T, B, max_new, max_kv, tree), 256), dtype=torch.uint8, device=device)
 

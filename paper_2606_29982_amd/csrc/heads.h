@@ -231,31 +231,51 @@ __device__ inline bool head_odd(const lat_f32x16 (&o)[NC], float l) {
         for (int i = 0; i < 16; ++i) t += fabsf(o[c][i]);
     return !(t < INFINITY) && l < INFINITY;
 }
-// Puts that right, for what it may cost, after the sums of row n (a lane of each
-// half) were written: where values of tokens that the row sees (spans of `width`
-// tokens, `step` apart, from tok0 to end) are infinities or NaNs, the sum is
-// theirs: put(d, sum).
+// Puts that right after the sums of row n (a lane of each half) were written: where
+// values of tokens that the row sees (spans of `width` tokens, `step` apart, from
+// tok0 to end) are infinities or NaNs, the sum is theirs: put(d, value, false), then
+// put(d, value, true) for what adds to it.  Each lane looks through a token's values.
 template <int D, class Sees, class Put>
 __device__ inline void head_put_odd(const HeadParams& p, int b, int g, int tok0, int width, int step, int end, Sees&& sees,
                                     Put&& put) {
+    const int lane = threadIdx.x & (kWave - 1), hf = lane >> 5;
+    const char* base = head_base(p, p.v, g);
+    unsigned long long touched = 0;
+    const int per = kWave / width;       // spans at a time
 #pragma unroll 1
-    for (int c = (threadIdx.x >> 5) & 1; c < D / 4; c += 2) {
-        float odd[4] = {};
-#pragma unroll 1
-        for (int t0 = tok0; t0 < end; t0 += step)
-#pragma unroll 1
-            for (int pos = t0; pos < min(t0 + width, end); ++pos) {
-                const lat_u32x2 v = ((const lat_u32x2*)(head_base(p, p.v, g) + head_row(p, b, pos)))[c];
-                const bool seen = sees(pos);
+    for (int t0 = tok0; t0 < end; t0 += per * step) {
+        const int mine = t0 + lane / width * step + lane % width;
+        bool odd = false;
+        if (mine < end) {
+            const lat_u32x4* row = (const lat_u32x4*)(base + head_row(p, b, mine));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float x = __uint_as_float(i & 1 ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16);
-                    if (seen && !(fabsf(x) < INFINITY)) odd[i] += x;
+            for (int c = 0; c < D / 8; ++c) {
+                const lat_u32x4 v = row[c];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) odd |= lat_finite(v[e]) != v[e];
+            }
+        }
+        unsigned long long found = __ballot(odd);
+#pragma unroll 1
+        while (found) {
+            const int i = __ffsll(found) - 1, pos = t0 + i / width * step + i % width;
+            found &= found - 1;
+            const lat_u32x2* row = (const lat_u32x2*)(base + head_row(p, b, pos));
+            if (!sees(pos)) continue;
+#pragma unroll 1
+            for (int c = hf; c < D / 4; c += 2) {
+                const lat_u32x2 v = row[c];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = __uint_as_float(e & 1 ? v[e >> 1] & 0xFFFF0000u : v[e >> 1] << 16);
+                    const unsigned long long bit = 1ull << (4 * (c >> 1) + e);
+                    if (!(fabsf(x) < INFINITY)) {
+                        put(4 * c + e, x, (touched & bit) != 0);
+                        touched |= bit;
+                    }
                 }
             }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (odd[i] != 0.0f) put(4 * c + i, odd[i]);
+        }
     }
 }
 

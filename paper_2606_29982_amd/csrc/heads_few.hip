@@ -321,7 +321,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         if (__any(odd)) {
             auto sees = [&](int pos) { return pos < limit && (!kTree || (head_tree_bits(mask, p.words, pos - rq.before) & 1)); };
             head_put_odd<D>(p, b, g, tok0, kWaveTokens, kFewTokens, end, sees,
-                            [&](int d, float v) { ((float*)place(wave, n, d >> 2))[d & 3] = v; });
+                            [&](int d, float v, bool again) {
+                                float& at = ((float*)place(wave, n, d >> 2))[d & 3];
+                                at = again ? at + v : v;
+                            });
         }
         __syncthreads();
         const size_t slot0 = ((size_t)blockIdx.x * 2 + (head ? 0 : 1)) * kFewRows;

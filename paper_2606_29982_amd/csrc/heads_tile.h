@@ -463,11 +463,18 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
         if (odd) {
             lat_wait_vm<0>();
             auto sees = [&](int pos) { return pos < limit && (!kTree || (head_tree_bits(mask, p.words, pos - rq.before) & 1)); };
-            head_put_odd<D>(p, b, g, tok0, kTileTokens, kTileTokens, end, sees, [&](int d, float v) {
+            head_put_odd<D>(p, b, g, tok0, kTileTokens, kTileTokens, end, sees, [&](int d, float v, bool again) {
                 if (my0 + n >= rows || !(l < INFINITY)) return;
-                if (!whole) p.part[(slot0 + 32 * wave + n) * D + d] = v;
-                else if (p.y_bf16) ((__bf16*)p.y)[(size_t)at_row * D + d] = (__bf16)v;
-                else ((float*)p.y)[(size_t)at_row * D + d] = v;
+                if (!whole) {
+                    float* at = p.part + (slot0 + 32 * wave + n) * D + d;
+                    *at = again ? *at + v : v;
+                } else if (p.y_bf16) {
+                    __bf16* at = (__bf16*)p.y + (size_t)at_row * D + d;
+                    *at = (__bf16)(again ? (float)*at + v : v);
+                } else {
+                    float* at = (float*)p.y + (size_t)at_row * D + d;
+                    *at = again ? *at + v : v;
+                }
             });
         }
     }

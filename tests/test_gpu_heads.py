@@ -158,6 +158,47 @@ def test_values_without_a_number_reach_who_sees_them(at, form):
     check_heads((y[:, :, keep], got[1]), (ref[0][:, :, keep], ref[1], ref[2][:, :, keep], ref[3]))
 
 
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("y_dtype", [BF, F32])
+def test_several_values_without_a_number_in_one_place(y_dtype, D, form):
+    """Infinities of one sign add up to one, of both signs to NaN, over tiles and pieces."""
+    c = HeadCase(seq=[3000], new=[9], H=16, G=2, D=D, seed=16)
+    for at, signs in ((3, (1, 1)), (70, (0, -1)), (2995, (1, 0))):
+        v = c.v[0][at].clone()
+        for d, sign in zip((2, D - 1), signs):
+            if sign:
+                v[:, d] = sign * float("inf")
+        c.put(0, at, v=v)
+    y, _ = c.run(DEV, form, y_dtype=y_dtype)
+    assert np.all(y[:, :, 2] == np.inf) and np.all(np.isnan(y[:, :, D - 1]))
+    keep = [d for d in range(D) if d not in (2, D - 1)]
+    for at in (3, 70, 2995):
+        v = c.v[0][at].clone()
+        v[:, [2, D - 1]] = 0.0
+        c.put(0, at, v=v)
+    got, ref = c.run(DEV, form, y_dtype=y_dtype), c.ref()
+    check_heads(got, ref, y_dtype)
+    # (weights of 2^-9 and less of the values' own make no difference to the other places)
+    assert np.array_equal(got[0][:, :, keep], y[:, :, keep])
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("H,G", [(64, 8), (32, 2), (48, 3)])
+def test_many_row_tiles_of_several_requests(H, G, form):
+    """More row tiles than run at a time: the latest in their requests go first."""
+    c = HeadCase(seq=[300, 17, 700, 130, 64], new=[280, 17, 200, 130, 1], H=H, G=G, D=64, pad=2, seed=17)
+    check_heads(c.run(DEV, form), c.ref())
+
+
+@pytest.mark.parametrize("G", [1, 2])
+def test_many_requests_whose_row_tiles_are_cut(G):
+    rng = np.random.default_rng(5)
+    seq, new = rng.integers(1, 80, 70), np.ones(70, np.int64)
+    seq[33], new[33], seq[50], new[50] = 9000, 40, 5000, 3
+    _check("split", seq=seq, new=new, H=4 * G, G=G, D=64, seed=18, block=64)
+
+
 @pytest.mark.parametrize("H,G,new,D", [(64, 8, 1, 128), (16, 2, 3, 64), (32, 1, 4, 128), (8, 8, 1, 128), (16, 1, 20, 64)])
 def test_long_context_is_split_and_joined(H, G, new, D):
     _check("split", seq=[20000, 3], new=[new, 1], H=H, G=G, D=D, block=64, seed=16)
