@@ -564,9 +564,9 @@ caee_status_t caee_head_store(const caee_head_store_desc_t* desc, const void* q,
 
 /* How the work is dealt to the GPU.  All give the same function. */
 typedef enum caee_head_form {
-    /* Whole where no request can have more than 1536 tokens (by max_kv,
-     * max_blocks * block_size, and max_kv - T + max_new) or T * heads >= 131072;
-     * else split. */
+    /* Whole where requests have 1536 tokens at most, as far as max_kv,
+     * max_blocks * block_size and max_kv - T + max_new tell, but for a handful of
+     * rows, and where T * heads >= 131072; else split. */
     CAEE_HEAD_AUTO = 0,
     /* The requests' tokens are cut so that all CUs have a share, partial results
      * are joined: few new tokens (decode steps, trees, the next part of a long
@@ -626,7 +626,8 @@ caee_status_t caee_head_workspace_size(const caee_head_desc_t* desc, size_t* byt
  * what the first leaves), for an fp32 y to three parts, which lose nothing.
  * Preconditions on device contents (violations: unspecified results,
  * memory-safe): page numbers in [0, n_blocks) for the pages seq_len covers, at
- * most max_new new tokens per request and max_kv tokens in all. */
+ * most max_new new tokens per request and max_kv tokens in all.  Calls that run
+ * at the same time take a workspace each. */
 caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, const void* k_cache, const void* v_cache,
                                   const int32_t* block_table, const int32_t* cu_new, const int32_t* seq_len,
                                   const uint32_t* tree, void* y, float* lse, void* ws, size_t ws_bytes, void* stream);

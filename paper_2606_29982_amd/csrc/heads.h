@@ -45,7 +45,8 @@ struct HeadWs {
 struct HeadParams {
     int T, B, H, G, ratio, dim, max_blocks, max_new, causal, y_bf16, words;
     HeadCache c;
-    long long max_kv, q_stride;
+    long long max_kv;     // no request is longer (what max_kv and the table's rows allow)
+    long long q_stride;
     float scale_log2;     // scale * log2(e): softmax in powers of two
     const uint16_t* q;
     const uint16_t* k;
@@ -80,13 +81,13 @@ __device__ inline int head_sees(const HeadParams& p, const LatentReq& r, int i) 
 }
 
 
-// Units and pieces are counted up to this; no request has more (a limit of the
-// host's, as is that of all requests while their lengths add up to max_kv at
-// most).
+// Units and pieces are counted up to this; requests within the host's bounds have
+// no more, one by one and together.
 constexpr int kHeadMaxUnits = INT32_MAX / 2;
 __device__ inline int head_add_units(int a, int b) { return min(a + b, kHeadMaxUnits); }
 __device__ inline int head_few_units(const HeadParams& p, const LatentReq& r) {
-    return p.G * ((r.add * p.ratio + kFewRows - 1) / kFewRows) * ((r.seq + kFewTokens - 1) / kFewTokens);
+    const long long n = (long long)(p.G * ((r.add * p.ratio + kFewRows - 1) / kFewRows)) * ((r.seq + kFewTokens - 1) / kFewTokens);
+    return (int)min(n, (long long)kHeadMaxUnits);
 }
 __device__ inline int head_tiles(const HeadParams& p, const LatentReq& r) { return (r.add * p.ratio + kTileRows - 1) / kTileRows; }
 __device__ inline int head_steps(const LatentReq& r) { return (r.seq + kTileTokens - 1) / kTileTokens; }

@@ -11,8 +11,9 @@ namespace {
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Bounds of what the device will find: the longest request's tokens, the row tiles
-// of a request and the units of all requests of the kernel of few rows.
+// What the device will find by the host's bounds: the longest request's tokens
+// (padded rows count as new ones), the row tiles of a request and the units of
+// all requests of the kernel of few rows.
 struct HeadBounds {
     long long longest, few_tiles;
     double few_units;
@@ -154,7 +155,7 @@ caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, c
     p.y_bf16 = d.y_dtype == CAEE_BF16;
     p.words = d.tree_words;
     p.c = c;
-    p.max_kv = d.max_kv;
+    p.max_kv = std::min((long long)d.max_kv, (long long)d.max_blocks * d.block_size);
     p.q_stride = d.q_stride;
     p.scale_log2 = d.scale * 1.4426950408889634f;
     p.q = (const uint16_t*)q;

@@ -332,3 +332,45 @@ def test_lengths_past_the_bounds_are_left_out(form):
     assert torch.all(y[0] == 7.0) and torch.all(y[c.T + 1] == 7.0)
     got = y[1:c.T + 1].float().cpu().numpy().astype(np.float64), lse.cpu().numpy()
     check_heads(got, c.ref(), rows=[9, 10, 11])
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_lengths_past_the_table_are_cut(form):
+    c = HeadCase(seq=[200, 90], new=[2, 3], seed=29)
+    a = c.arguments(DEV, form)
+    a["plan"]["seq_len"][0] = 5000
+    a["max_kv"] = 1 << 20
+    y = torch.full((c.T + 2, c.H, c.D), 7.0, dtype=BF, device=DEV)
+    lse = torch.empty(4, c.H * c.T // 4, device=DEV).view(-1)[:c.T * c.H].view(c.T, c.H)
+    caee.head_attention(y=y[1:c.T + 1], lse=lse, **a)
+    torch.cuda.synchronize()
+    assert torch.all(y[0] == 7.0) and torch.all(y[c.T + 1] == 7.0)
+    got = y[1:c.T + 1].float().cpu().numpy().astype(np.float64), lse.cpu().numpy()
+    check_heads(got, c.ref(), rows=[2, 3, 4])
+
+
+@pytest.mark.parametrize("form", FORMS + ["auto"])
+def test_no_requests(form):
+    i32 = dict(dtype=torch.int32, device=DEV)
+    att = caee.Heads(heads=4, kv_heads=2, dim=64, scale=0.1, form=form)
+    k, v = (torch.zeros(2, 16, 2, 64, dtype=BF, device=DEV) for _ in range(2))
+    y, lse = torch.full((5, 4, 64), 7.0, device=DEV), torch.full((5, 4), 7.0, device=DEV)
+    caee.head_attention(att, torch.zeros(5, 4, 64, dtype=BF, device=DEV), k, v, torch.zeros(0, 3, **i32),
+                        dict(cu_new=torch.zeros(1, **i32), seq_len=torch.zeros(0, **i32)), y,
+                        caee.alloc_head_workspace(att, 5, 0, 0, 0, DEV), 0, 0, lse=lse)
+    torch.cuda.synchronize()
+    assert torch.all(y == 0) and torch.all(torch.isneginf(lse))
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_queries_without_a_number_stay_in_their_rows(form):
+    c = HeadCase(seq=[300, 90], new=[4, 30], seed=30)
+    c.q[1, 3, 7] = float("nan")
+    c.q[20, 0, 0] = float("inf")
+    y, lse = c.run(DEV, form)
+    assert np.all(np.isnan(y[1, 3])) and np.all(np.isnan(y[20, 0]))
+    c.q[1, 3], c.q[20, 0] = 0.0, 0.0
+    ry, rl, ya, sa = c.ref()
+    for t, h in ((1, 3), (20, 0)):
+        y[t, h], lse[t, h] = ry[t, h], rl[t, h]
+    check_heads((y, lse), (ry, rl, ya, sa))
