@@ -48,6 +48,7 @@ caee_status_t head_cache(int kv_heads, int dim, int block_size, int n_blocks, lo
 namespace {
 
 constexpr int kStoreThreads = 256;
+constexpr int kStoreSpread = 2048;     // workgroups up to which a token's passes are spread
 
 struct HeadStoreParams {
     int T, H, G, rope, steps;          // steps: passes of a workgroup over its token's heads
@@ -247,7 +248,9 @@ extern "C" caee_status_t caee_head_store(const caee_head_store_desc_t* desc, con
                       (int64_t)d.n_blocks * d.block_size, c, d.eps, q, k, v, q_norm, k_norm, freq, position, slots,
                       (uint16_t*)q_out, (uint16_t*)k_cache, (uint16_t*)v_cache};
     const int per = kStoreThreads / (d.dim / 8), passes = (d.heads + 2 * d.kv_heads + per - 1) / per;
-    p.steps = passes;
+    // Passes one after the other make the angles once; of a few tokens each has a
+    // workgroup of its own.
+    p.steps = (long long)d.T * passes <= kStoreSpread ? 1 : passes;
     const dim3 grid(d.T, (passes + p.steps - 1) / p.steps);
     hipStream_t s = (hipStream_t)stream;
     return timed_launch(CAEE_KERNEL_PLAN, s, "head store", [&] {
