@@ -549,7 +549,7 @@ typedef struct caee_head_store_desc {
  *   q_out[t][h] = rotate(norm(q[t][h], q_norm)),
  *   key   g of slots[t] = rotate(norm(k[t][g], k_norm)),
  *   value g of slots[t] = v[t][g],
- * rounded to bf16 (nearest, ties to even).  norm(x, w) = x / sqrt(mean(x^2) +
+ * rounded to bf16 (nearest, ties to even), all before it in fp32.  norm(x, w) = x / sqrt(mean(x^2) +
  * eps) * w over a head's dim values (w [dim] fp32; NULL: x itself); rotate turns
  * pair i by the angle position[t] * freq[i] (freq [rope/2] in double, radians;
  * the angle is reduced in double, so far positions keep their precision).
@@ -593,7 +593,7 @@ typedef struct caee_head_desc {
     int64_t max_kv;       /* sum of seq_len at most, <= 2^30 */
     int64_t q_stride;     /* elements from one token of q to the next, a multiple of 8, >= heads * dim */
     int64_t page_stride, row_stride, head_stride;
-    float scale;          /* factor on the scores, finite and > 0 */
+    float scale;          /* factor on the scores, finite (times log2(e), too) and > 0 */
 } caee_head_desc_t;
 
 /* Bytes of workspace caee_head_attention needs: 4 (B + 2), and, but for
@@ -620,7 +620,8 @@ caee_status_t caee_head_workspace_size(const caee_head_desc_t* desc, size_t* byt
  * seq_len are never read; rows that a query does not see do not change its
  * result, whatever they hold.
  * An infinity or NaN in a value that a row sees is in that place of its result;
- * in a key it makes the row NaN.
+ * of a key, or of the query, what it makes of the score counts: NaN or +inf
+ * makes the row NaN, -inf the token's weight 0 (a row of none but those is zero).
  * Scores, softmax statistics and sums are fp32; the softmax weights are rounded
  * to bf16 before their products (with few rows to two bf16 parts, the second
  * what the first leaves), for an fp32 y to three parts, which lose nothing.

@@ -424,6 +424,18 @@ def _at(t, name: str, dtype, shape) -> int:
     return _need(t, name, dtype, shape).data_ptr()
 
 
+def _stream_here(*tensors) -> int:
+    """Stream of the one device that all tensors are on, which has to be the current one: kernels are launched there."""
+    import torch
+    at = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"tensors must be on one device, got {tensors[0].device} and {t.device}")
+    if at != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors are on {tensors[0].device}, which is not the current device")
+    return torch._C._cuda_getCurrentRawStream(at)
+
+
 def _workspace(ws) -> tuple:
     """Address and bytes of a workspace."""
     if ws is None:
@@ -625,7 +637,8 @@ def head_store(q, k, v, slots, q_out, k_cache, v_cache, q_norm=None, k_norm=None
                                None if freq is None else _at(freq, "freq", torch.float64, (rope // 2,)),
                                None if position is None else _at(position, "position", torch.int32, (T,)),
                                _at(slots, "slots", torch.int64, (T,)), q_out.data_ptr(), k_cache.data_ptr(),
-                               v_cache.data_ptr(), _stream(k_cache)))
+                               v_cache.data_ptr(),
+                               _stream_here(k_cache, v_cache, q, k, v, q_out, slots, position, freq, q_norm, k_norm)))
     return q_out
 
 
@@ -695,7 +708,9 @@ def head_attention(att: Heads, q, k_cache, v_cache, block_table, plan: dict, y, 
     d = _HEAD.pack(T, B, H, att.kv_heads, D, block, pages, width, max_new, 1 if att.causal else 0, words,
                    HEAD_FORM_CODE[att.form], _code(y), max_kv, qs, ps, rs, hs, att.scale)
     _check(lib.caee_head_attention(d, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table_at, cu_at,
-                                   seq_at, tree_at, y_at, lse_at, ws_at, ws_bytes, _stream(y)))
+                                   seq_at, tree_at, y_at, lse_at, ws_at, ws_bytes,
+                                   _stream_here(y, q, k_cache, v_cache, block_table, plan["cu_new"], plan["seq_len"], tree,
+                                                lse, ws)))
     return y
 
 

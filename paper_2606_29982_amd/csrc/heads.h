@@ -64,15 +64,16 @@ struct HeadParams {
 
 // New tokens and length of request b as the kernels use them: 0 <= new <=
 // max_new, rows within [0, T), 0 <= seq <= max_kv, and the tokens before its
-// new ones, by the lengths as they are.
+// new ones, by the lengths as they are (within bounds whose sums and differences
+// 32 bits hold, whatever the arrays do).
 __device__ inline LatentReq head_req(const HeadParams& p, int b) {
     LatentReq r;
-    const int a = p.cu_new[b], e = p.cu_new[b + 1];
-    r.t0 = min(max(a, 0), p.T);
+    const int a = max(p.cu_new[b], 0), e = max(p.cu_new[b + 1], 0);
+    r.t0 = min(a, p.T);
     r.add = min(max(min(e, p.T) - r.t0, 0), p.max_new);
-    const int len = max(p.seq_len[b], 0);
+    const int len = min(max(p.seq_len[b], 0), 1 << 30);
     r.seq = min(len, (int)p.max_kv);
-    r.before = len - (e - a);
+    r.before = max(len - max(e - a, 0), -(1 << 29));
     return r;
 }
 // Tokens up to which new token i of the request may see some; with a tree not all of them.

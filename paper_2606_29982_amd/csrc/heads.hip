@@ -9,6 +9,8 @@
 namespace caee {
 namespace {
 
+constexpr float kLog2E = 1.4426950408889634f;
+
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // What the device will find by the host's bounds: the longest request's tokens
@@ -16,7 +18,7 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 // all requests of the kernel of few rows.
 struct HeadBounds {
     long long longest, few_tiles;
-    double few_units;
+    double few_units, few_limit;       // as the device will find; no more than these, whatever rows are padded
 };
 HeadBounds head_bounds(const caee_head_desc_t& d) {
     HeadBounds b;
@@ -25,6 +27,7 @@ HeadBounds head_bounds(const caee_head_desc_t& d) {
     b.few_tiles = ((long long)d.max_new * (d.heads / d.kv_heads) + kFewRows - 1) / kFewRows;
     const long long per = (b.longest + kFewTokens - 1) / kFewTokens;
     b.few_units = (double)std::min(d.B * per, kv / kFewTokens + d.B) * (double)b.few_tiles * d.kv_heads;
+    b.few_limit = (double)(kv / kFewTokens + d.B) * (double)b.few_tiles * d.kv_heads;
     return b;
 }
 
@@ -50,7 +53,7 @@ HeadWay head_way(const caee_head_desc_t& d) {
     const HeadBounds b = head_bounds(d);
     if (d.form == CAEE_HEAD_AUTO && b.longest <= kHeadShort) return b.few_units <= kHeadShortUnits ? HeadWay::few : HeadWay::whole;
     // (units are counted in 32 bits)
-    if (b.few_units <= kHeadFewUnits || (b.few_tiles <= 1 && b.few_units <= kHeadMaxUnits)) return HeadWay::few;
+    if (b.few_units <= kHeadFewUnits || (b.few_tiles <= 1 && b.few_limit <= kHeadMaxUnits)) return HeadWay::few;
     return d.form == CAEE_HEAD_AUTO && (long long)d.T * d.heads >= kTilePieces * kTileRows ? HeadWay::whole : HeadWay::many;
 }
 
@@ -86,7 +89,8 @@ caee_status_t check_heads(const caee_head_desc_t* d, HeadCache* c) {
         return fail(CAEE_ERR_INVALID_ARG, "unknown form=%d", d->form);
     if (d->y_dtype != CAEE_F32 && d->y_dtype != CAEE_BF16)
         return fail(CAEE_ERR_INVALID_ARG, "y_dtype=%d must be CAEE_F32 or CAEE_BF16", d->y_dtype);
-    if (!(isfinite(d->scale) && d->scale > 0.0f)) return fail(CAEE_ERR_INVALID_ARG, "scale must be finite and > 0");
+    if (!(isfinite(d->scale * kLog2E) && d->scale > 0.0f))
+        return fail(CAEE_ERR_INVALID_ARG, "scale must be > 0 and finite, times log2(e) too");
     // Limits of this build.
     if (d->dim != 64 && d->dim != 128) return fail(CAEE_ERR_UNSUPPORTED, "dim=%d must be 64 or 128", d->dim);
     if (d->q_stride % 8 || d->q_stride < (int64_t)d->heads * d->dim)
@@ -157,7 +161,7 @@ caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, c
     p.c = c;
     p.max_kv = std::min((long long)d.max_kv, (long long)d.max_blocks * d.block_size);
     p.q_stride = d.q_stride;
-    p.scale_log2 = d.scale * 1.4426950408889634f;
+    p.scale_log2 = d.scale * kLog2E;
     p.q = (const uint16_t*)q;
     p.k = (const uint16_t*)k_cache;
     p.v = (const uint16_t*)v_cache;

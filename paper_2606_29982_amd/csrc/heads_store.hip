@@ -220,7 +220,9 @@ extern "C" caee_status_t caee_head_store(const caee_head_store_desc_t* desc, con
     CAEE_TRY(check_ptr(k_cache, "k_cache", any));
     CAEE_TRY(check_ptr(v_cache, "v_cache", any));
     if (!any) return CAEE_OK;
-    if (k_cache == v_cache) return fail(CAEE_ERR_INVALID_ARG, "k_cache and v_cache are one array");
+    const uintptr_t k_at = (uintptr_t)k_cache, v_at = (uintptr_t)v_cache;
+    if ((k_at < v_at ? v_at - k_at : k_at - v_at) < (uintptr_t)(2 * d.dim))
+        return fail(CAEE_ERR_INVALID_ARG, "heads of k_cache and v_cache overlap");
     // Queries may be written over themselves; other tokens' rows that a
     // workgroup may still have to read may not be.
     if (q_out == q ? d.x_dtype != CAEE_BF16 || (d.T > 1 && d.q_out_stride != d.q_stride) : false)

@@ -335,6 +335,58 @@ def test_lengths_past_the_bounds_are_left_out(form):
 
 
 @pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("B", [3, 70])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("junk", [(2 ** 31 - 1, 2 ** 31 - 1), (-2 ** 31, 2 ** 31 - 1), (2 ** 31 - 1, -2 ** 31), (-7, -9)])
+def test_lengths_that_are_none(junk, D, B, form):
+    """A request whose length and count of new tokens are junk: nothing outside the outputs is written; the lists before
+    it, whose new tokens are right, have theirs."""
+    new = [520] * (B - 2) + [1, 1] if B < 64 else [20] * (B - 2) + [1, 1]
+    c = HeadCase(seq=[n + 30 for n in new], new=new, H=128, G=8, D=D, seed=28)
+    a = c.arguments(DEV, form)
+    a["plan"]["seq_len"][B - 1], a["plan"]["cu_new"][B] = junk
+    y = torch.full((c.T + 2, c.H, c.D), 7.0, dtype=BF, device=DEV)
+    lse = torch.empty(c.T, c.H, device=DEV)
+    caee.head_attention(y=y[1:c.T + 1], lse=lse, **a)
+    torch.cuda.synchronize()
+    assert torch.all(y[0] == 7.0) and torch.all(y[c.T + 1] == 7.0)
+    got = y[1:c.T + 1].float().cpu().numpy().astype(np.float64), lse.cpu().numpy()
+    if junk[1] > 0:
+        check_heads(got, c.ref(), rows=range(c.T - 1))
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("new", [2, 60])
+def test_infinite_keys_count_by_their_scores(new, form):
+    """One infinity in a key of one group: +inf where the query is positive there, which is NaN, -inf where it is
+    negative, which leaves the token out."""
+    c = HeadCase(seq=[150], new=[new], H=4, G=2, seed=31)
+    k = c.k[0][40].clone()
+    k[1, 9] = float("inf")
+    c.put(0, 40, k=k)
+    y, lse = c.run(DEV, form)
+    up = (c.q[:, :, 9] > 0).numpy() & (np.arange(4) // 2 == 1)
+    assert np.all(np.isnan(y[up])) and np.all(np.isnan(lse[up]))
+    k[1, 9] = 0.0
+    c.put(0, 40, k=k)
+    ry, rl, ya, sa = c.ref()
+    # the token left out of the others of the group
+    q64, k64, v64 = c.q.double().numpy(), c.k[0].double().numpy(), c.v[0].double().numpy()
+    for t in range(new):
+        for h in range(2, 4):
+            if up[t, h]:
+                y[t, h], lse[t, h] = ry[t, h], rl[t, h]
+                continue
+            seen = [j for j in range(150 - new + t + 1) if j != 40]
+            s = c.scale * k64[seen, 1] @ q64[t, h]
+            w = np.exp(s - s.max())
+            rl[t, h] = s.max() + np.log(w.sum())
+            w /= w.sum()
+            ry[t, h], ya[t, h] = w @ v64[seen, 1], w @ np.abs(v64[seen, 1])
+    check_heads((y, lse), (ry, rl, ya, sa))
+
+
+@pytest.mark.parametrize("form", FORMS)
 def test_lengths_past_the_table_are_cut(form):
     c = HeadCase(seq=[200, 90], new=[2, 3], seed=29)
     a = c.arguments(DEV, form)

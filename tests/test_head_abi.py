@@ -47,7 +47,8 @@ def test_store_descriptor(kw, status):
 
 @pytest.mark.parametrize("kw", [
     dict(q=None), dict(k=FAKE + MB + 2), dict(v=None), dict(qn=FAKE + 8), dict(kn=FAKE + 4), dict(freq=None), dict(pos=None),
-    dict(slots=None), dict(out=None), dict(kc=None), dict(vc=FAKE + 8), dict(kc=FAKE + 5 * MB),
+    dict(slots=None), dict(out=None), dict(kc=None), dict(vc=FAKE + 8), dict(kc=FAKE + 5 * MB), dict(vc=FAKE + 4 * MB + 240),
+    dict(vc=FAKE + 4 * MB - 16),
     dict(out=FAKE, x_dtype=caee.CAEE_F32),                                 # over itself only in bf16,
     dict(out=FAKE, q_out_stride=1032),                                     # and of the same stride
     dict(out=FAKE + 16), dict(out=FAKE + 2048), dict(out=FAKE + MB), dict(out=FAKE + 2 * MB - 512),
@@ -79,7 +80,7 @@ def _ws(d):
     (dict(max_blocks=0), BAD), (dict(max_new=-1), BAD), (dict(max_kv=-1), BAD), (dict(causal=2), BAD),
     (dict(tree_words=-1), BAD), (dict(tree_words=1, causal=0), BAD), (dict(tree_words=33), LIMIT),
     (dict(tree_words=1, form=2), OK), (dict(form=3), BAD), (dict(y_dtype=2), BAD), (dict(scale=0.0), BAD),
-    (dict(scale=float("inf")), BAD), (dict(q_stride=2040), BAD), (dict(q_stride=2052), BAD), (dict(q_stride=1 << 41), LIMIT),
+    (dict(scale=float("inf")), BAD), (dict(scale=3e38), BAD), (dict(q_stride=2040), BAD), (dict(q_stride=2052), BAD), (dict(q_stride=1 << 41), LIMIT),
     (dict(heads=1026, q_stride=1026 * 128), LIMIT), (dict(B=65537), LIMIT), (dict(T=(1 << 20) + 1), LIMIT),
     (dict(max_kv=(1 << 30) + 1), LIMIT), (dict(row_stride=128), BAD), (dict(page_stride=256), BAD),
     (dict(n_blocks=1 << 28), LIMIT),
@@ -125,3 +126,23 @@ def test_host_tensors_are_refused_before_the_library_sees_them():
     z = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="device"):
         caee.head_store(z, z, z, torch.zeros(2, dtype=torch.int64), z, z, z)
+
+
+class _At:
+    """What the device check reads of a tensor."""
+
+    def __init__(self, index):
+        self.index, self.device = index, torch.device("cuda", index)
+
+    def get_device(self):
+        return self.index
+
+
+def test_tensors_of_other_devices_are_refused(monkeypatch):
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 100 + i, raising=False)
+    assert caee._stream_here(_At(1), None, _At(1)) == 101
+    with pytest.raises(ValueError, match="one device"):
+        caee._stream_here(_At(1), _At(1), None, _At(0))
+    with pytest.raises(ValueError, match="current device"):
+        caee._stream_here(_At(0), _At(0))
