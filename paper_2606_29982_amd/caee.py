@@ -424,16 +424,22 @@ def _at(t, name: str, dtype, shape) -> int:
     return _need(t, name, dtype, shape).data_ptr()
 
 
-def _stream_here(*tensors) -> int:
-    """Stream of the one device that all tensors are on, which has to be the current one: kernels are launched there."""
+def _on(t, device: int, name: str, dtype, shape) -> int:
+    """``_at`` for a tensor that has to be on the same device as the call's others."""
+    if t.get_device() == device and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    at = _need(t, name, dtype, shape).data_ptr()
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the other tensors' device, got {t.device}")
+    return at
+
+
+def _stream_on(device: int) -> int:
+    """Stream of a device, which has to be the current one: kernels are launched there."""
     import torch
-    at = tensors[0].get_device()
-    for t in tensors:
-        if t is not None and t.get_device() != at:
-            raise ValueError(f"tensors must be on one device, got {tensors[0].device} and {t.device}")
-    if at != torch._C._cuda_getDevice():
-        raise ValueError(f"tensors are on {tensors[0].device}, which is not the current device")
-    return torch._C._cuda_getCurrentRawStream(at)
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors are on cuda:{device}, which is not the current device")
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _workspace(ws) -> tuple:
@@ -578,13 +584,13 @@ def latent_attention(att: Latent, q, weights: dict, cache, block_table, plan: di
     return y
 
 
-def _head_caches(k_cache, v_cache, kv_heads: int, dim: int) -> tuple:
+def _head_caches(k_cache, v_cache, device: int, kv_heads: int, dim: int) -> tuple:
     """Shape and strides of the two caches, [n_blocks][block_size][kv_heads][dim] bf16 views of the same strides whose
     last dimension is dense (pages that hold a head's tokens next to each other: their transposed view)."""
     import torch
     shape, strides = k_cache.shape, k_cache.stride()
-    if not (k_cache.is_cuda and v_cache.is_cuda):
-        raise ValueError("k_cache and v_cache must be device tensors")
+    if k_cache.get_device() != device or v_cache.get_device() != device:
+        raise ValueError("k_cache and v_cache must be device tensors, on the others' device")
     if k_cache.dtype is not torch.bfloat16 or v_cache.dtype is not torch.bfloat16:
         raise TypeError("k_cache and v_cache must be torch.bfloat16")
     if len(shape) != 4 or shape[2] != kv_heads or shape[3] != dim or v_cache.shape != shape:
@@ -596,13 +602,13 @@ def _head_caches(k_cache, v_cache, kv_heads: int, dim: int) -> tuple:
     return shape, strides
 
 
-def _heads(t, name: str, dim: int):
+def _heads(t, name: str, device: int, dim: int):
     """Tokens, heads and token stride of [T][heads][dim] whose heads are dense (tokens may be strided)."""
     shape, stride = t.shape, t.stride()
-    if t.is_cuda and len(shape) == 3 and shape[2] == dim and stride[2] == 1 and (stride[1] == dim or shape[1] == 1):
+    if t.get_device() == device >= 0 and len(shape) == 3 and shape[2] == dim and stride[2] == 1 and (stride[1] == dim or shape[1] == 1):
         return shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1] * dim
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
+    if not t.is_cuda or t.get_device() != device:
+        raise ValueError(f"{name} must be a device tensor, on the others' device")
     if len(shape) != 3 or shape[2] != dim:
         raise ValueError(f"{name} must be [T][heads][{dim}]")
     raise ValueError(f"{name} must have dense heads")
@@ -618,27 +624,26 @@ def head_store(q, k, v, slots, q_out, k_cache, v_cache, q_norm=None, k_norm=None
     or None (no norm).  ``freq`` [rope/2] float64: the angles, per position, of the pairs that are rotated, the first
     ``rope`` values by halves or (``adjacent``) neighbours; ``position`` [T] int32; without ``freq`` no rotation."""
     import torch
-    dim = q.shape[-1]
-    (T, H, qs), (Tk, G, ks), (Tv, Gv, vs) = _heads(q, "q", dim), _heads(k, "k", dim), _heads(v, "v", dim)
-    To, Ho, os = _heads(q_out, "q_out", dim)
+    dim, at = q.shape[-1], q.get_device()
+    (T, H, qs), (Tk, G, ks), (Tv, Gv, vs) = _heads(q, "q", at, dim), _heads(k, "k", at, dim), _heads(v, "v", at, dim)
+    To, Ho, os = _heads(q_out, "q_out", at, dim)
     if k.dtype != q.dtype or v.dtype != q.dtype or Tk != T or Tv != T or Gv != G or To != T or Ho != H:
         raise ValueError("q, k, v and q_out do not fit together")
     if q_out.dtype is not torch.bfloat16:
         raise TypeError("q_out must be torch.bfloat16")
-    (pages, block, _, _), (ps, rs, hs, _) = _head_caches(k_cache, v_cache, G, dim)
+    (pages, block, _, _), (ps, rs, hs, _) = _head_caches(k_cache, v_cache, at, G, dim)
     f32, one = torch.float32, (dim,)
     rope = 0 if freq is None else 2 * freq.shape[0]
     if rope and position is None:
         raise ValueError("a rotation needs position")
     d = _HEAD_STORE.pack(T, H, G, dim, rope, 1 if adjacent else 0, _code(q), block, pages, eps, qs, ks, vs, os, ps, rs, hs)
     _check(lib.caee_head_store(d, q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                               None if q_norm is None else _at(q_norm, "q_norm", f32, one),
-                               None if k_norm is None else _at(k_norm, "k_norm", f32, one),
-                               None if freq is None else _at(freq, "freq", torch.float64, (rope // 2,)),
-                               None if position is None else _at(position, "position", torch.int32, (T,)),
-                               _at(slots, "slots", torch.int64, (T,)), q_out.data_ptr(), k_cache.data_ptr(),
-                               v_cache.data_ptr(),
-                               _stream_here(k_cache, v_cache, q, k, v, q_out, slots, position, freq, q_norm, k_norm)))
+                               None if q_norm is None else _on(q_norm, at, "q_norm", f32, one),
+                               None if k_norm is None else _on(k_norm, at, "k_norm", f32, one),
+                               None if freq is None else _on(freq, at, "freq", torch.float64, (rope // 2,)),
+                               None if position is None else _on(position, at, "position", torch.int32, (T,)),
+                               _on(slots, at, "slots", torch.int64, (T,)), q_out.data_ptr(), k_cache.data_ptr(),
+                               v_cache.data_ptr(), _stream_on(at)))
     return q_out
 
 
@@ -686,31 +691,32 @@ def head_attention(att: Heads, q, k_cache, v_cache, block_table, plan: dict, y, 
     sum of ``seq_len``; ``y`` [T][heads][dim] bf16 or f32; ``tree`` [T][words] int32: bit j of a token's words is set
     where it sees new token j of its request (None: causal, or all by ``att``); ``lse`` [T][heads] f32."""
     import torch
-    i32, H, D = torch.int32, att.heads, att.dim
+    i32, H, D, at = torch.int32, att.heads, att.dim, q.get_device()
     ws_at, ws_bytes = _workspace(ws)
-    T, heads, qs = _heads(q, "q", D)
+    T, heads, qs = _heads(q, "q", at, D)
+    if ws is not None and ws.get_device() != at:
+        raise ValueError("ws must be on the other tensors' device")
     if heads != H or q.dtype is not torch.bfloat16:
         raise ValueError(f"q must be [T][{H}][{D}] torch.bfloat16")
-    (pages, block, _, _), (ps, rs, hs, _) = _head_caches(k_cache, v_cache, att.kv_heads, D)
+    (pages, block, _, _), (ps, rs, hs, _) = _head_caches(k_cache, v_cache, at, att.kv_heads, D)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [B][max_blocks]")
     B, width = block_table.shape
-    table_at = _at(block_table, "block_table", i32, (B, width))
-    cu_at, seq_at = _at(plan["cu_new"], "cu_new", i32, (B + 1,)), _at(plan["seq_len"], "seq_len", i32, (B,))
+    table_at = _on(block_table, at, "block_table", i32, (B, width))
+    cu_at, seq_at = _on(plan["cu_new"], at, "cu_new", i32, (B + 1,)), _on(plan["seq_len"], at, "seq_len", i32, (B,))
     tree_at, words = None, 0
     if tree is not None:
         if tree.dim() != 2 or tree.shape[1] < 1:
             raise ValueError(f"tree must be [{T}][words]")
         words = tree.shape[1]
-        tree_at = _at(tree, "tree", i32, (T, words))
-    y_at = _at(y, "y", y.dtype, (T, H, D))
-    lse_at = None if lse is None else _at(lse, "lse", torch.float32, (T, H))
+        tree_at = _on(tree, at, "tree", i32, (T, words))
+    y_at = _on(y, at, "y", y.dtype, (T, H, D))
+    lse_at = None if lse is None else _on(lse, at, "lse", torch.float32, (T, H))
     d = _HEAD.pack(T, B, H, att.kv_heads, D, block, pages, width, max_new, 1 if att.causal else 0, words,
                    HEAD_FORM_CODE[att.form], _code(y), max_kv, qs, ps, rs, hs, att.scale)
     _check(lib.caee_head_attention(d, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table_at, cu_at,
                                    seq_at, tree_at, y_at, lse_at, ws_at, ws_bytes,
-                                   _stream_here(y, q, k_cache, v_cache, block_table, plan["cu_new"], plan["seq_len"], tree,
-                                                lse, ws)))
+                                   _stream_on(at)))
     return y
 
 

@@ -128,21 +128,31 @@ def test_host_tensors_are_refused_before_the_library_sees_them():
         caee.head_store(z, z, z, torch.zeros(2, dtype=torch.int64), z, z, z)
 
 
-class _At:
-    """What the device check reads of a tensor."""
-
-    def __init__(self, index):
-        self.index, self.device = index, torch.device("cuda", index)
+class _At(torch.Tensor):
+    """A host tensor that says it is on a device."""
 
     def get_device(self):
         return self.index
 
 
+def _said_on(index, *shape, dtype=torch.bfloat16):
+    t = torch.zeros(*shape, dtype=dtype).as_subclass(_At)
+    t.index = index
+    return t
+
+
 def test_tensors_of_other_devices_are_refused(monkeypatch):
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 100 + i, raising=False)
-    assert caee._stream_here(_At(1), None, _At(1)) == 101
-    with pytest.raises(ValueError, match="one device"):
-        caee._stream_here(_At(1), _At(1), None, _At(0))
+    assert caee._stream_on(1) == 101
     with pytest.raises(ValueError, match="current device"):
-        caee._stream_here(_At(0), _At(0))
+        caee._stream_on(0)
+    assert caee._on(_said_on(1, 4), 1, "slots", torch.bfloat16, (4,)) > 0
+    assert caee._heads(_said_on(1, 2, 4, 64), "q", 1, 64) == (2, 4, 256)
+    monkeypatch.setattr(caee, "_need", lambda t, *a: t)
+    with pytest.raises(ValueError, match="slots must be on the other"):
+        caee._on(_said_on(0, 4), 1, "slots", torch.bfloat16, (4,))
+    with pytest.raises(ValueError, match="device"):
+        caee._heads(_said_on(0, 2, 4, 64), "q", 1, 64)
+    with pytest.raises(ValueError, match="device"):
+        caee._head_caches(_said_on(1, 3, 16, 2, 64), _said_on(0, 3, 16, 2, 64), 1, 2, 64)
