@@ -47,48 +47,38 @@ __device__ inline int head_piece(const HeadParams& p, const HeadLine& line) {
     return __builtin_amdgcn_readlane(per, __ffsll((unsigned long long)__ballot(__float_as_int(cost) == best)) - 1);
 }
 
-// Row tile q of all requests' by where it begins in its request, the last first:
-// those see the most tokens, and what starts last should be short.  (Up to
-// kOrdered requests; a lane tries a place, all 64 at a time.)
+// Row tile q of all requests', by where it ends, the last first: those see the
+// most tokens, and what starts last should be short.  Request b's tiles lie in
+// places first .. first + n - 1, a place for each kTileRows rows before the end
+// that is the last of all.  (Up to kOrdered requests; a lane tries a place, all 64
+// at a time.)
 constexpr int kOrdered = 16;
 struct HeadAt {
     int b, rt;
 };
 __device__ inline HeadAt head_order(const HeadParams& p, const HeadLine& line, int q) {
     const int lane = threadIdx.x & (kWave - 1);
-    // Row tiles of a request that begin at token x or later.
-    auto from = [&](int tiles, int before, int add, int x) {
-        return tiles - min(tiles, (min(max(x - before, 0), add) * p.ratio + kTileRows - 1) / kTileRows);
-    };
-    const int tiles = line.n;
-    int lo = 0, hi = 1;
-    for (int b = 0; b < p.B; ++b) {
-        const int before = __builtin_amdgcn_readlane(line.mine.before, b);
-        lo = min(lo, before);
-        hi = max(hi, before + __builtin_amdgcn_readlane(line.mine.add, b));
-    }
-    auto count = [&](int x) {
-        int n = 0;
-        for (int b = 0; b < p.B; ++b)
-            n += from(__builtin_amdgcn_readlane(tiles, b), __builtin_amdgcn_readlane(line.mine.before, b),
-                      __builtin_amdgcn_readlane(line.mine.add, b), x);
-        return n;
-    };
-    while (hi - lo > 1) {          // count(lo) > q >= count(hi)
+    const int n = line.n, end = n > 0 ? line.mine.before + line.mine.add : INT32_MIN;
+    const auto larger = [](int a, int b) { return max(a, b); };
+    const int latest = head_last(head_scan(end, INT32_MIN, larger));
+    const int first = n > 0 ? min(latest - end, 1 << 20) * p.ratio / kTileRows : 0;
+    int lo = 0, hi = head_last(head_scan(first + n, 0, larger)), before = 0;
+    while (hi - lo > 1) {          // before: the tiles in places before lo; at most q, and in those before hi more
         const int step = (hi - lo + kWave - 1) / kWave, x = lo + (lane + 1) * step;
-        const int n = count(x), k = __popcll(__ballot(x < hi && n > q));
+        int tiles = 0;
+        for (int b = 0; b < p.B; ++b)
+            tiles += min(max(x - __builtin_amdgcn_readlane(first, b), 0), __builtin_amdgcn_readlane(n, b));
+        const int k = __popcll(__ballot(x < hi && tiles <= q));
+        if (k > 0) before = __builtin_amdgcn_readlane(tiles, k - 1);
         hi = min(hi, lo + (k + 1) * step);
         lo += k * step;
     }
-    int left = q - __builtin_amdgcn_readfirstlane(count(lo + 1));
-    const int here = from(tiles, line.mine.before, line.mine.add, lo), later = from(tiles, line.mine.before, line.mine.add, lo + 1);
-    HeadAt at = {0, 0};
-    for (int b = 0; b < p.B; ++b) {
-        const int h = __builtin_amdgcn_readlane(here, b), n = h - __builtin_amdgcn_readlane(later, b);
-        if (left >= 0 && left < n) at = {b, __builtin_amdgcn_readlane(tiles, b) - h + left};
-        left -= n;
-    }
-    return at;
+    // The requests that have a tile in place lo, by number.
+    const bool here = lo >= first && lo - first < n;
+    const unsigned long long all = __ballot(here);
+    const int at = __popcll(all & ((1ull << lane) - 1));
+    const int b = __ffsll((unsigned long long)__ballot(here && at == q - before)) - 1;
+    return {b, __builtin_amdgcn_readlane(n - 1 - (lo - first), b)};
 }
 
 // Keys or values of 64 tokens, or the queries of two waves, 32 each: blocks of 8
