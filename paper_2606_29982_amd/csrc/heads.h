@@ -42,9 +42,24 @@ struct HeadWs {
     size_t total;
 };
 
+// Division of 0 <= n < 2^31 by d: n m / 2^(31 + shift), rounded down, with m =
+// 2^(31 + shift) / d, rounded up, and 2^shift >= d > 2^(shift - 1): m is off by less
+// than 2^shift / d of n's step, so the quotient is right.
+struct HeadBy {
+    uint32_t m;
+    int shift;
+};
+inline HeadBy head_by(int d) {
+    int shift = 0;
+    while (1 << shift < d) ++shift;
+    return {(uint32_t)(((1ull << (31 + shift)) + (unsigned)d - 1) / (unsigned)d), shift};
+}
+__device__ inline int head_over(int n, const HeadBy& d) { return (int)(__umulhi(2u * (unsigned)n, d.m) >> d.shift); }
+
 struct HeadParams {
     int T, B, H, G, ratio, dim, max_blocks, max_new, causal, y_bf16, words;
     HeadCache c;
+    HeadBy by_ratio, by_block;
     long long max_kv;     // no request is longer (what max_kv and the table's rows allow)
     long long q_stride;
     float scale_log2;     // scale * log2(e): softmax in powers of two
@@ -175,7 +190,7 @@ struct HeadLook {
 };
 __device__ inline HeadLook head_look(const HeadParams& p, int b, int seq, int pos) {
     const int r0 = min(pos, seq - 1), span = min(pos + 7, seq - 1) - r0;
-    const unsigned j = (unsigned)r0 / (unsigned)p.c.block;
+    const unsigned j = (unsigned)head_over(r0, p.by_block);
     return {p.table[(size_t)b * p.max_blocks + min(j, (unsigned)p.max_blocks - 1u)], r0 - (int)(j * (unsigned)p.c.block), span};
 }
 __device__ inline HeadWindow head_window(const HeadParams& p, const HeadLook& l) {

@@ -159,6 +159,8 @@ caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, c
     p.y_bf16 = d.y_dtype == CAEE_BF16;
     p.words = d.tree_words;
     p.c = c;
+    p.by_ratio = head_by(p.ratio);
+    p.by_block = head_by(c.block);
     p.max_kv = std::min((long long)d.max_kv, (long long)d.max_blocks * d.block_size);
     p.q_stride = d.q_stride;
     p.scale_log2 = d.scale * kLog2E;

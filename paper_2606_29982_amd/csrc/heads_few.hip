@@ -124,11 +124,11 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         u += last - first;
 
         const int row0 = rt * kFewRows, n_rows = min(kFewRows, rows - row0);
-        const int row = row0 + min(n, n_rows - 1), tok = row / p.ratio;
+        const int row = row0 + min(n, n_rows - 1), tok = head_over(row, p.by_ratio);
         const int limit = head_sees(p, rq, tok);
         // Tokens from lim_min on some row does not see.
-        const int lim_min = kTree ? min(max(rq.before, 0), rq.seq) : head_sees(p, rq, head_div(row0, p.ratio));
-        const int end = min(last * kFewTokens, head_sees(p, rq, head_div(row0 + n_rows - 1, p.ratio)));
+        const int lim_min = kTree ? min(max(rq.before, 0), rq.seq) : head_sees(p, rq, head_over(row0, p.by_ratio));
+        const int end = min(last * kFewTokens, head_sees(p, rq, head_over(row0 + n_rows - 1, p.by_ratio)));
         const int tok0 = first * kFewTokens + kWaveTokens * wave;
         const int steps = end > tok0 ? (end - tok0 + kFewTokens - 1) / kFewTokens : 0;
         const uint32_t* mask = kTree ? p.tree + (size_t)(rq.t0 + tok) * p.words : nullptr;
@@ -172,8 +172,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         };
 
         __syncthreads();       // the row tile before is done with LDS
+        HeadLook soon = look(0);                       // of kLook tiles, the first ones and then the next
         {
-            const int r = 8 * wave + (lane >> 3), rr = row0 + min(r, n_rows - 1), i = rr / p.ratio;
+            const int r = 8 * wave + (lane >> 3), rr = row0 + min(r, n_rows - 1), i = head_over(rr, p.by_ratio);
             const uint16_t* src = p.q + (size_t)(rq.t0 + i) * p.q_stride + (size_t)(g * p.ratio + rr - i * p.ratio) * D +
                                   8 * ((lane & 7) ^ lat_swz(r));
 #pragma unroll
@@ -181,8 +182,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
                 __builtin_amdgcn_global_load_lds((lat_g_void*)(src + 64 * gg), (lat_lds_void*)&qs[wave][gg][0], 16, 0, 0);
             if ((lane & 7) == 0) row_at[r] = (rq.t0 + i) * p.H + g * p.ratio + rr - i * p.ratio;
         }
-        HeadWindow win = head_window(p, look(0));      // of kLook tiles
-        HeadLook soon = {};                            // of the next ones
+        HeadWindow win = head_window(p, soon);         // of kLook tiles
         fetch(k_base, ks, 0, win);
         fetch(v_base, vs, 0, win);
         lat_wait_vm<2 * kLoads>();
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
     int g0[kPasses], g1[kPasses], a[kPasses], rr[kPasses], most = 0;
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
-        const int h = min(h0 + kHeads * i, p.H - 1), kv = h / p.ratio, r = (t - rq.t0) * p.ratio + h - kv * p.ratio;
+        const int h = min(h0 + kHeads * i, p.H - 1), kv = head_over(h, p.by_ratio), r = (t - rq.t0) * p.ratio + h - kv * p.ratio;
         rr[i] = r % tile_rows;
         if (few) {         // shares
             a[i] = at_u + (kv * tiles + r / kFewRows) * n_u;

@@ -158,11 +158,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
     const LatentReq rq = head_line_req(p, line, b, &at_b);
     {
         const int rows = rq.add * p.ratio, steps_all = head_steps(rq);
-        const int first = head_div(steps_all * part, parts), last = head_div(steps_all * (part + 1), parts);
         const bool whole = parts == 1;
+        const int first = whole ? 0 : head_div(steps_all * part, parts), last = whole ? steps_all : head_div(steps_all * (part + 1), parts);
         const int row0 = rt * kTileRows, my0 = row0 + 32 * wave;
-        auto sees = [&](int r) { return head_sees(p, rq, head_div(min(r, rows - 1), p.ratio)); };
-        const int row = min(my0 + n, rows - 1), tok = row / p.ratio;
+        auto sees = [&](int r) { return head_sees(p, rq, head_over(min(r, rows - 1), p.by_ratio)); };
+        const int row = min(my0 + n, rows - 1), tok = head_over(row, p.by_ratio);
         const int limit = head_sees(p, rq, tok);
         // Tokens from lim_min (lim_wg) on some row of the wave (the workgroup) does not see.
         const int lim_tree = min(max(rq.before, 0), rq.seq);
@@ -173,6 +173,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
         const int at_row = (rq.t0 + tok) * p.H + g * p.ratio + row - tok * p.ratio;      // of y and lse
         const uint32_t* mask = kTree ? p.tree + (size_t)(rq.t0 + tok) * p.words : nullptr;
 
+        // A wave fetches 16 tokens of a tile.
+        auto place = [&](int s, int i) __attribute__((always_inline)) { return tok0 + s * kTileTokens + 8 * (kEights * wave + i); };
+        constexpr int kLook = kHeadWindow / kEights;
+        HeadWindow win = {};           // of kLook tiles
+        auto look = [&](int s) __attribute__((always_inline)) { return head_look(p, b, rq.seq, place(s + lane / kEights, lane % kEights)); };
+        HeadLook soon = {};            // of the next ones
+        if (steps > 0) soon = look(0);
+
         if (threadIdx.x == 0) odd_values = 0;
         // A wave's queries, as its results at the end, go through a part of LDS of
         // its own, eight lanes a 128-byte line: the other stages than tile 0's,
@@ -180,7 +188,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
         lat_u32x4* const own = &(wave < 2 ? kt1 : vt1).v[4 * (wave & 1)][0][0];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = 8 * i + (lane >> 3), rr = min(my0 + r, rows - 1), t = rr / p.ratio;
+            const int r = 8 * i + (lane >> 3), rr = min(my0 + r, rows - 1), t = head_over(rr, p.by_ratio);
             const uint16_t* src = p.q + (size_t)(rq.t0 + t) * p.q_stride + (size_t)(g * p.ratio + rr - t * p.ratio) * D +
                                   8 * ((lane & 7) ^ lat_swz(r));
 #pragma unroll
@@ -193,12 +201,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
         for (int c = 0; c < NC; ++c) o[c] = lat_f32x16{};
         float m = kNoScore, l = 0.0f;
 
-        // A wave fetches 16 tokens of a tile.
-        auto place = [&](int s, int i) __attribute__((always_inline)) { return tok0 + s * kTileTokens + 8 * (kEights * wave + i); };
-        constexpr int kLook = kHeadWindow / kEights;
-        HeadWindow win = {};           // of kLook tiles
-        HeadLook soon = {};            // of the next ones
-        auto look = [&](int s) __attribute__((always_inline)) { return head_look(p, b, rq.seq, place(s + lane / kEights, lane % kEights)); };
         auto piece = [&](int i) __attribute__((always_inline)) { return 16u * ((lane & 7) ^ lat_swz(8 * i + (lane >> 3))); };
         const char *const k_base = head_base(p, p.k, g), *const v_base = head_base(p, p.v, g);
         // Load n of a wave's part of tile s, the keys' and then the values' eights.  (A
@@ -381,7 +383,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
             });
         };
         if (steps > 0) {
-            win = head_window(p, look(0));
+            win = head_window(p, soon);
             const Eights x = eights(0);
 #pragma unroll
             for (int n2 = 0; n2 < 2 * kLoads; ++n2) load(n2, x, 0, kt0, vt0);
