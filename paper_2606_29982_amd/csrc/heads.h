@@ -15,7 +15,13 @@ struct HeadCache {
 caee_status_t head_cache(int kv_heads, int dim, int block_size, int n_blocks, long long page_stride,
                          long long row_stride, long long head_stride, HeadCache* c);
 
-// Two kernels attend.  Few rows (k_head_few): the work of all requests is one line
+// Both kernels of attention go over the tokens once.  With m the largest score so
+// far (in powers of two: c = scale log2 e), l = sum 2^(c s_j - m) and o = sum
+// 2^(c s_j - m) v_j, a tile of tokens adds to l and o, and where its scores exceed m
+// by much, m moves to m' and l and o are multiplied by 2^(m - m') first.  Results
+// over parts of the tokens are joined by the same rule; y = o / l at the end.
+//
+// Few rows (k_head_few): the work of all requests is one line
 // of units, kFewTokens tokens of one row tile (kFewRows rows of a request, its new
 // tokens' heads of one group) each, by request, group, row tile and token.  It is
 // cut into equal shares, one a workgroup; a share begins and ends inside a row
@@ -37,8 +43,8 @@ __device__ inline int head_group(int wg) { return wg % kXcds * (kFewGroups / kXc
 __device__ inline int head_workgroup(int g) { return g % (kFewGroups / kXcds) * kXcds + g / (kFewGroups / kXcds); }
 
 struct HeadWs {
-    size_t meta;           // [B + 1] unit or piece prefix sums, of more than 64 requests; [1] tokens of a piece
-    size_t part, part_ml;  // split: [2 shares or pieces][rows][dim] partial sums and [..][rows][2] (maximum, sum)
+    size_t meta;           // [B + 1] unit or piece prefix sums, of more than 64 requests; [1] steps of a piece
+    size_t part, part_ml;  // split: [two a share, or a piece][rows][dim] partial sums and [..][rows][2] (maximum, sum)
     size_t total;
 };
 
@@ -95,7 +101,6 @@ __device__ inline LatentReq head_req(const HeadParams& p, int b) {
 __device__ inline int head_sees(const HeadParams& p, const LatentReq& r, int i) {
     return p.causal && !p.tree ? min(max(r.before + i + 1, 0), r.seq) : r.seq;
 }
-
 
 // Units and pieces are counted up to this; requests within the host's bounds have
 // no more, one by one and together.
@@ -222,7 +227,8 @@ __device__ inline const char* head_base(const HeadParams& p, const uint16_t* cac
 constexpr float kFusedMax = 0x1p30f;
 __device__ inline float head_weight(float s, float scale_log2, float m) { return __builtin_amdgcn_exp2f(fmaf(s, scale_log2, -m)); }
 // While the weights of a lane's tile add up to no more than kMaxWeight none of
-// them exceeds it, and the maximum need not move.
+// them exceeds it, and the maximum need not move; past 2^20 it moves with every
+// tile, so that the weights are made by lat_weight, whose products are rounded.
 __device__ inline bool head_moves(float more, float m) { return more > kMaxWeight || !(fabsf(m) <= 0x1p20f); }
 
 // Adds a partial result (sums x of weights by the maximum w.x, whose total is w.y)
@@ -296,7 +302,8 @@ __device__ inline void head_put_odd(const HeadParams& p, int b, int g, int tok0,
     }
 }
 
-// Split form of few rows; of many, or whole form.
+// The kernel of few rows and its join; that of many, with a join where p.part is
+// there, and without (whole).
 hipError_t launch_head_few(const HeadParams& p, hipStream_t s);
 hipError_t launch_head_many(const HeadParams& p, hipStream_t s);
 hipError_t launch_head_tile_64(const HeadParams& p, unsigned grid, int pieces, hipStream_t s);

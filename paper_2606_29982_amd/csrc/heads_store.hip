@@ -84,10 +84,14 @@ __device__ inline float head_sum(float v) {
 
 // A workgroup has one token and kStoreThreads / (D / 8) heads in a pass (of its
 // queries, keys and values, in that order), D / 8 lanes a head, 16 bytes of
-// bf16 a lane.  Memory bounds it.  The token's angles are made once for all
-// heads: position * freq in 64 bits, whose whole turns are taken off before the
-// sine and cosine of 32 bits.  The norm is in 32 bits; q, k and v are rounded
-// once, at the end, to the type the attention reads.
+// bf16 a lane.  The token's angles are made once for all heads: position * freq in
+// 64 bits, whose whole turns are taken off before the sine and cosine of 32 bits.
+// The norm is in 32 bits; q, k and v are rounded once, at the end, to the type the
+// attention reads.
+// Memory bounds it: 16381 tokens of 32 + 2 x 8 heads of 128, 403 MB read and
+// written in 87 us (4.6 TB/s; a large copy 5.0).  The next head's load issued before
+// this one's work gained nothing (99 to 107 us), as six to eight workgroups a CU hide it.
+// 32 tokens take 3.9 us, a launch and a chain of three loads.
 template <bool kF32, int D, bool kAdjacent>
 __global__ __launch_bounds__(kStoreThreads) void k_head_store(HeadStoreParams p) {
     constexpr int kLanes = D / 8, kHeads = kStoreThreads / kLanes;
@@ -251,7 +255,7 @@ extern "C" caee_status_t caee_head_store(const caee_head_store_desc_t* desc, con
                       (uint16_t*)q_out, (uint16_t*)k_cache, (uint16_t*)v_cache};
     const int per = kStoreThreads / (d.dim / 8), passes = (d.heads + 2 * d.kv_heads + per - 1) / per;
     // Passes one after the other make the angles once; of a few tokens each has a
-    // workgroup of its own.
+    // workgroup of its own (32 tokens, 5 passes: 5.8 and 4.3 us on the GPU).
     p.steps = (long long)d.T * passes <= kStoreSpread ? 1 : passes;
     const dim3 grid(d.T, (passes + p.steps - 1) / p.steps);
     hipStream_t s = (hipStream_t)stream;

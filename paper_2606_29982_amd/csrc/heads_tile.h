@@ -13,7 +13,9 @@ constexpr int kTileThreads = 256;
 // Steps of a piece at most.  A lane tries cutting the longest request's row tiles
 // into lane + 1 pieces, others' as far as theirs are longer; what decides is
 // the time that the CUs take for all pieces, with kStart steps for a piece's start
-// and end and kJoin for the partial results.
+// and end and kJoin for the partial results.  (The next 259 tokens of
+// 2 prompts behind 30000, 144 row tiles: 1008 pieces of 68 steps, 315 us; values of kStart and
+// kJoin between half and twice these made no difference.)
 __device__ inline int head_piece(const HeadParams& p, const HeadLine& line) {
     constexpr float kStart = 5.0f, kJoin = 8.0f;
     if (!p.part) return INT32_MAX / 2;
@@ -50,12 +52,21 @@ __device__ inline int head_piece(const HeadParams& p, const HeadLine& line) {
 // Row tile q of all requests', by where it ends, the last first: those see the
 // most tokens, and what starts last should be short.  Request b's tiles lie in
 // places first .. first + n - 1, a place for each kTileRows rows before the end
-// that is the last of all.  (Up to kOrdered requests; a lane tries a place, all 64
-// at a time.)
-constexpr int kOrdered = 16;
+// that is the last of all; a lane tries a place, all 64 at a time.
 struct HeadAt {
     int b, rt;
 };
+// Whether that pays: while the CUs take the row tiles in a few rounds.  After more
+// rounds they end together anyway, and neighbours of one request share its keys in
+// the L2.  us, by place and by request, 32 heads, 8 groups, lengths at random up to:
+// 8 prompts of 700 (2 rounds) 25.4 and 27.0, 24 (4) 78 and 81, 40 (7) 121 and 118; 61 of
+// 400 (6) 104 and 85, of 1500 (22) 620 and 565; 16 of 1400 (5) 146 and 154.  Behind up to
+// 4000 cached tokens 16 of 200 107 and 136, behind 2000 61 of 100 102 and 123, 3 of 2000 156
+// and 151.
+__device__ inline bool head_ordered(const HeadParams& p, int tiles) {
+    return p.B > 1 && p.B <= kWave && (long long)tiles * p.G > kTileSlots &&
+           (long long)tiles * p.G <= (p.B <= 16 ? 6 : 4) * kTileSlots;
+}
 __device__ inline HeadAt head_order(const HeadParams& p, const HeadLine& line, int q) {
     const int lane = threadIdx.x & (kWave - 1);
     const int n = line.n, end = n > 0 ? line.mine.before + line.mine.add : INT32_MIN;
@@ -66,8 +77,10 @@ __device__ inline HeadAt head_order(const HeadParams& p, const HeadLine& line, i
     while (hi - lo > 1) {          // before: the tiles in places before lo; at most q, and in those before hi more
         const int step = (hi - lo + kWave - 1) / kWave, x = lo + (lane + 1) * step;
         int tiles = 0;
-        for (int b = 0; b < p.B; ++b)
-            tiles += min(max(x - __builtin_amdgcn_readlane(first, b), 0), __builtin_amdgcn_readlane(n, b));
+        for (int b0 = 0; b0 < p.B; b0 += 4)          // (lanes without a request have no tiles)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                tiles += min(max(x - __builtin_amdgcn_readlane(first, b0 + i), 0), __builtin_amdgcn_readlane(n, b0 + i));
         const int k = __popcll(__ballot(x < hi && tiles <= q));
         if (k > 0) before = __builtin_amdgcn_readlane(tiles, k - 1);
         hi = min(hi, lo + (k + 1) * step);
@@ -88,6 +101,25 @@ struct HeadTile {
     lat_u32x4 v[kTileTokens / 8][G][kWave];
 };
 
+// A row tile, or a piece of it: a wave has 32 rows, whose sums, statistics and
+// queries stay in registers, the workgroup 64 tokens at a time in LDS, two tiles in
+// turn.  As in k_head_few keys are the M side of the scores and the weights a
+// fragment of the second product as they are.  The next tile's loads go out between
+// the products with the keys, the next 16 tokens' weights are made between the
+// products with the values: a wave's vector instructions run beside its own MFMAs
+// (an MFMA of 32x32x16 takes 13.6 ns, with four vector instructions and an exponential
+// beside it 15.5).  Weights are rounded to bf16, and l sums the rounded ones; for a
+// 32-bit result they have three parts.
+// Two workgroups a CU fill each other's gaps; one of 256 rows, which reads the keys
+// and values half as often, has none to fill them (tree-shaped calls of 16 users
+// 159 us, 97 with two; 8 ragged prompts 42 and 38, one of 7161 tokens 508 and 527).
+// What bounds it: the matrix units at the clock that power leaves.  7161 tokens
+// behind 1030, 32 heads: 535 us (1010 TFLOP/s; a large library product reaches 1217 on that
+// card), MFMAs 50 % of the cycles at 1.9 GHz; without the loads it takes 516, without
+// the products with the values 452, with the keys 433.  Filling one stage in two parts at
+// two barriers a step was slower (540 beside 527).  Short calls are bound by a tile's start
+// and end (7 to 8 us: lengths 1.8, pages and queries 1.7, fetch 0.8, out 2) beside
+// 1.6 us a step.
 template <int D, bool kTree, bool kRest>
 __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
@@ -141,7 +173,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
     if (q >= line.total) return;
     int b, rt, part = 0, parts = 1;
     const bool cut = p.B <= kWave && __any(line.n > head_tiles(p, line.mine));
-    if (p.B > 1 && p.B <= kOrdered && !cut && line.total * p.G > kTileSlots) {
+    if (!cut && head_ordered(p, line.total)) {
         const HeadAt at = head_order(p, line, q);
         b = at.b;
         rt = at.rt;
@@ -439,7 +471,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
                 for (int i = 0; i < kUnits / 2; ++i) {
                     const int r = (64 * i + ln) / kUnits, un = (64 * i + ln) % kUnits;
                     const lat_u32x4 v = out[r * kUnits + (un ^ (r & (kUnits - 1)))];
-                    if (my0 + r < rows) *(lat_u32x4*)((char*)row_of(r) + 16 * kUnits * pass + 16 * un) = v;
+                    char* const to = (char*)row_of(r) + 16 * kUnits * pass + 16 * un;      // (by a shuffle: all lanes take part)
+                    if (my0 + r < rows) *(lat_u32x4*)to = v;
                 }
                 __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
                 asm volatile("" ::: "memory");

@@ -84,6 +84,36 @@ def test_many_requests(B, form):
 
 
 @pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("y_dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_number_of_rows(D, y_dtype, form):
+    """Requests of 1 to 128 rows, so that the last row tile of one has each of its numbers of rows."""
+    new = list(range(1, 129))
+    _check(form, y_dtype=y_dtype, seq=[n + 3 for n in new], new=new, H=1, G=1, D=D, seed=11)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_length(D, form):
+    """Requests of 0 to 263 tokens, the last 0 to 4 of them new."""
+    seq = list(range(264))
+    _check(form, seq=seq, new=[min(n, n % 5) for n in seq], H=4, G=2, D=D, seed=11)
+
+
+@pytest.mark.parametrize("ratio", [3, 8])
+@pytest.mark.parametrize("B", [2, 7, 40, 64])
+def test_row_tiles_of_several_requests_by_place(B, ratio):
+    """More row tiles than run at a time, few enough to be taken by place: some requests without new tokens, prefixes of
+    any length, one far behind the others."""
+    rng = np.random.default_rng(B)
+    new = rng.integers(0, 2 * (9600 // (ratio * B)), B)
+    seq = new + rng.integers(0, 150, B)
+    new[B // 2], seq[B // 2] = (0, 5) if B > 2 else (new[1], seq[1])
+    seq[0] += 900
+    _check("whole", seq=seq, new=new, H=8 * ratio, G=8, D=64, seed=11)
+
+
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("D", [64, 128])
 def test_float32_output_and_strided_queries(D, form):
     _check(form, y_dtype=F32, seq=[50, 130, 700], new=[2, 9, 1], D=D, wide=40, seed=12)
