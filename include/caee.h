@@ -679,7 +679,7 @@ typedef enum caee_kernel_kind {
     CAEE_KERNEL_COMBINE = 3,  /* weighted combine into y */
     CAEE_KERNEL_QUANT = 4,    /* fp8 activation quantisation (x and the SwiGLU rows) */
     CAEE_KERNEL_PLAN = 5,     /* paging plan and cache stores */
-    CAEE_KERNEL_ATTENTION = 6,/* latent attention, its products with W_uk and W_uv included */
+    CAEE_KERNEL_ATTENTION = 6,/* attention (latent: its products with W_uk and W_uv included) */
     CAEE_KERNEL_MATMUL = 7,   /* block-scaled 8-bit products (their quantisation counts as QUANT) */
     CAEE_KERNEL_KINDS = 8
 } caee_kernel_kind_t;
