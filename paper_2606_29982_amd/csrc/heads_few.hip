@@ -74,6 +74,34 @@ __global__ __launch_bounds__(kFewThreads) void k_head_meta(HeadParams p, int few
     }
 }
 
+// A list of units of one row tile, and where in it a share goes on.
+struct FewList {
+    int b, at;            // request, its first unit
+    LatentReq rq;
+    int n, tile, first;   // units of each of the request's lists; which list; the first unit of it
+};
+__device__ inline int few_tiles(const HeadParams& p, const FewList& x) { return (x.rq.add * p.ratio + kFewRows - 1) / kFewRows; }
+__device__ inline FewList few_request(const HeadParams& p, const HeadLine& line, int b) {
+    FewList x = {};
+    x.b = b;
+    x.rq = head_line_req(p, line, b, &x.at);
+    x.n = (x.rq.seq + kFewTokens - 1) / kFewTokens;
+    return x;
+}
+// The list that unit u is of.
+__device__ inline FewList few_list(const HeadParams& p, const HeadLine& line, int u) {
+    FewList x = few_request(p, line, head_line_find(p, line, u));
+    x.tile = head_div(u - x.at, x.n);
+    x.first = u - x.at - x.tile * x.n;
+    return x;
+}
+// The list after x, which begins with unit u: mostly of the same request, or of the next one.
+__device__ inline FewList few_after(const HeadParams& p, const HeadLine& line, const FewList& x, int u) {
+    if (x.tile + 1 < p.G * few_tiles(p, x)) return {x.b, x.at, x.rq, x.n, x.tile + 1, 0};
+    if (p.B > kWave && x.b + 1 < p.B && __builtin_amdgcn_readfirstlane(p.meta[x.b + 2]) > u) return few_request(p, line, x.b + 1);
+    return few_request(p, line, head_line_find(p, line, u));
+}
+
 // Keys or values of 32 tokens for each wave: blocks of 8 rows x 128 bytes,
 // swizzled, so that one direct-to-LDS load fills a block.
 template <int D>
@@ -106,7 +134,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
     __shared__ FewStage<D> ks, vs;
     __shared__ lat_u32x4 qs[kFewRows / 8][kG][kWave];
     __shared__ float2 ml[4][kFewRows];
-    __shared__ int row_at[kFewRows];
+    __shared__ int row_at[2][kFewRows];    // of this list and the next
     const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     HeadLine line = head_line(p);
@@ -124,14 +152,31 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
             vpos[j][e] = 2 * (vrow * 8 + ((4 * j + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ lat_swz(8 * e + vrow))) + (lane & 1);
     const uint32_t row_bytes = (uint32_t)p.c.row_stride * 2u;
 
-    for (int u = share0; u < share1;) {
-        const int b = head_line_find(p, line, u);
-        int at_u;
-        const LatentReq rq = head_line_req(p, line, b, &at_u);
-        const int rows = rq.add * p.ratio, tiles = (rows + kFewRows - 1) / kFewRows;
-        const int n_u = (rq.seq + kFewTokens - 1) / kFewTokens;
-        const int rel = u - at_u, tile = head_div(rel, n_u), first = rel - tile * n_u;
-        const int g = head_div(tile, tiles), rt = tile - g * tiles;
+    constexpr int kEights = kWaveTokens / 8, kLook = kHeadWindow / kEights;
+    auto look_at = [&](const FewList& x, int s) __attribute__((always_inline)) {
+        return head_look(p, x.b, x.rq.seq, (x.first + s + lane / kEights) * kFewTokens + kWaveTokens * wave + 8 * (lane % kEights));
+    };
+    // Asks for a list's queries and its first pages.
+    auto open = [&](const FewList& x, int parity) __attribute__((always_inline)) {
+        const int tiles = few_tiles(p, x), g = head_div(x.tile, tiles), row0 = (x.tile - g * tiles) * kFewRows;
+        const HeadLook soon = look_at(x, 0);
+        const int r = 8 * wave + (lane >> 3), rr = min(row0 + r, x.rq.add * p.ratio - 1), i = head_over(rr, p.by_ratio);
+        const uint16_t* src = p.q + (size_t)(x.rq.t0 + i) * p.q_stride + (size_t)(g * p.ratio + rr - i * p.ratio) * D +
+                              8 * ((lane & 7) ^ lat_swz(r));
+#pragma unroll
+        for (int gg = 0; gg < kG; ++gg)
+            __builtin_amdgcn_global_load_lds((lat_g_void*)(src + 64 * gg), (lat_lds_void*)&qs[wave][gg][0], 16, 0, 0);
+        if ((lane & 7) == 0) row_at[parity][r] = (x.rq.t0 + i) * p.H + g * p.ratio + rr - i * p.ratio;
+        return soon;
+    };
+    if (share0 >= share1) return;
+    FewList list = few_list(p, line, share0);
+    HeadLook soon = open(list, 0);     // of kLook tiles: the first ones, and then the next
+    for (int u = share0, parity = 0;; parity ^= 1) {
+        const int b = list.b, n_u = list.n, first = list.first;
+        const LatentReq rq = list.rq;
+        const int rows = rq.add * p.ratio, tiles = few_tiles(p, list);
+        const int g = head_div(list.tile, tiles), rt = list.tile - g * tiles;
         const int last = min(n_u, first + (share1 - u));
         const bool whole = first == 0 && last == n_u, head = u == share0;
         u += last - first;
@@ -146,10 +191,6 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         const int steps = end > tok0 ? (end - tok0 + kFewTokens - 1) / kFewTokens : 0;
         const uint32_t* mask = kTree ? p.tree + (size_t)(rq.t0 + tok) * p.words : nullptr;
 
-        constexpr int kEights = kWaveTokens / 8, kLook = kHeadWindow / kEights;
-        auto look = [&](int s) __attribute__((always_inline)) {
-            return head_look(p, b, rq.seq, tok0 + (s + lane / kEights) * kFewTokens + 8 * (lane % kEights));
-        };
         auto piece = [&](int i) __attribute__((always_inline)) { return 16u * ((lane & 7) ^ lat_swz(8 * (i & 1) + (lane >> 3))); };
         const char *const k_base = head_base(p, p.k, g), *const v_base = head_base(p, p.v, g);
         // A buffer of size 0 past the last tile: its loads cost no traffic, and their
@@ -184,23 +225,11 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
             }
         };
 
-        __syncthreads();       // the row tile before is done with LDS
-        HeadLook soon = look(0);                       // of kLook tiles, the first ones and then the next
-        {
-            const int r = 8 * wave + (lane >> 3), rr = row0 + min(r, n_rows - 1), i = head_over(rr, p.by_ratio);
-            const uint16_t* src = p.q + (size_t)(rq.t0 + i) * p.q_stride + (size_t)(g * p.ratio + rr - i * p.ratio) * D +
-                                  8 * ((lane & 7) ^ lat_swz(r));
-#pragma unroll
-            for (int gg = 0; gg < kG; ++gg)
-                __builtin_amdgcn_global_load_lds((lat_g_void*)(src + 64 * gg), (lat_lds_void*)&qs[wave][gg][0], 16, 0, 0);
-            if ((lane & 7) == 0) row_at[r] = (rq.t0 + i) * p.H + g * p.ratio + rr - i * p.ratio;
-        }
         HeadWindow win = head_window(p, soon);         // of kLook tiles
+        lat_wait_vm<0>();
+        __syncthreads();       // the queries are there, the list before is done with LDS
         fetch(k_base, ks, 0, win);
         fetch(v_base, vs, 0, win);
-        lat_wait_vm<2 * kLoads>();
-        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
-        lat_barrier();
         lat_u32x4 qf[kJ];
 #pragma unroll
         for (int j = 0; j < kJ; ++j) qf[j] = (&qs[0][0][0])[(kp0 ^ (2 * (j & 3))) + (j >> 2) * kWave];
@@ -222,7 +251,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
             __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
             __builtin_amdgcn_sched_barrier(0);
             // the window of tile s + 1 on, asked for half a window before
-            if ((s + 1) % kLook == kLook / 2) soon = look((s + 1) / kLook * kLook + kLook);
+            if ((s + 1) % kLook == kLook / 2) soon = look_at(list, (s + 1) / kLook * kLook + kLook);
             if ((s + 1) % kLook == 0) win = head_window(p, soon);
             fetch(k_base, ks, s + 1, win);
             const bool masked = tb + kWaveTokens > lim_min;
@@ -340,6 +369,11 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
                             });
         }
         __syncthreads();
+        const bool more = u < share1;
+        if (more) {            // the next list's queries and pages are on their way while this one's results leave
+            list = few_after(p, line, list, u);
+            soon = open(list, parity ^ 1);
+        }
         const size_t slot0 = ((size_t)blockIdx.x * 2 + (head ? 0 : 1)) * kFewRows;
         for (int x = threadIdx.x; x < n_rows * kUnits; x += kFewThreads) {
             const int r = x / kUnits, c = x % kUnits;
@@ -364,11 +398,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
                 continue;
             }
             const float f = lat_inverse(lx);
-            const size_t at = (size_t)row_at[r];
+            const size_t at = (size_t)row_at[parity][r];
             if (p.y_bf16) *(lat_u32x2*)((uint16_t*)p.y + at * D + 4 * c) = lat_u32x2{lat_pack(v.x * f, v.y * f), lat_pack(v.z * f, v.w * f)};
             else *(float4*)((float*)p.y + at * D + 4 * c) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
             if (p.lse && c == 0) p.lse[at] = lat_lse(mx, lx);
         }
+        if (!more) return;
     }
 #endif
 }
