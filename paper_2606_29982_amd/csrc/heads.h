@@ -25,7 +25,9 @@ caee_status_t head_cache(int kv_heads, int dim, int block_size, int n_blocks, lo
 // of units, kFewTokens tokens of one row tile (kFewRows rows of a request, its new
 // tokens' heads of one group) each, by request, group, row tile and token.  It is
 // cut into equal shares, one a workgroup; a share begins and ends inside a row
-// tile's line, so a workgroup leaves at most two partial results.
+// tile's line, so a workgroup leaves at most two partial results.  A row tile's
+// start and end take as long as some tokens and count as units before them
+// (few_start).
 constexpr int kFewRows = 32, kFewTokens = 128;
 constexpr int kFewGroups = 512;                    // two workgroups a CU
 // Many rows (k_head_tile): row tiles of kTileRows rows, a workgroup each, or,
@@ -63,7 +65,7 @@ inline HeadBy head_by(int d) {
 __device__ inline int head_over(int n, const HeadBy& d) { return (int)(__umulhi(2u * (unsigned)n, d.m) >> d.shift); }
 
 struct HeadParams {
-    int T, B, H, G, ratio, dim, max_blocks, max_new, causal, y_bf16, words;
+    int T, B, H, G, ratio, dim, max_blocks, max_new, causal, y_bf16, words, few_start;
     HeadCache c;
     HeadBy by_ratio, by_block;
     long long max_kv;     // no request is longer (what max_kv and the table's rows allow)
@@ -106,8 +108,12 @@ __device__ inline int head_sees(const HeadParams& p, const LatentReq& r, int i) 
 // no more, one by one and together.
 constexpr int kHeadMaxUnits = INT32_MAX / 2;
 __device__ inline int head_add_units(int a, int b) { return min(a + b, kHeadMaxUnits); }
+// Units of a list: those of a row tile's tokens, and few_start.
+__device__ inline int head_few_list(const HeadParams& p, const LatentReq& r) {
+    return r.seq > 0 ? (r.seq + kFewTokens - 1) / kFewTokens + p.few_start : 0;
+}
 __device__ inline int head_few_units(const HeadParams& p, const LatentReq& r) {
-    const long long n = (long long)(p.G * ((r.add * p.ratio + kFewRows - 1) / kFewRows)) * ((r.seq + kFewTokens - 1) / kFewTokens);
+    const long long n = (long long)(p.G * ((r.add * p.ratio + kFewRows - 1) / kFewRows)) * head_few_list(p, r);
     return (int)min(n, (long long)kHeadMaxUnits);
 }
 __device__ inline int head_tiles(const HeadParams& p, const LatentReq& r) { return (r.add * p.ratio + kTileRows - 1) / kTileRows; }

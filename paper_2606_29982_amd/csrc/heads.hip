@@ -13,6 +13,14 @@ constexpr float kLog2E = 1.4426950408889634f;
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// Units that a list's start and end count as, by the rows' size, where there are
+// more units than shares.  us for 0, 1, 2 and 3 of them: decode of 64 users, 64
+// heads, 8 groups, lengths at random up to 4100, heads of 128 127, 107, 107 and 106, of
+// 64 89, 66, 64 and 63; 256 users up to 2000, 32 heads 234, 199, 197 and 200, up to 500 87,
+// 73, 70 and 71; of one length nothing changes (64 of 2048 100).  With fewer units than
+// shares they are only more partial results (13 drafts behind 2000 16.6 and 17.1).
+constexpr int kFewStarts = 128;
+
 // What the device will find by the host's bounds: the longest request's tokens
 // (padded rows count as new ones), the row tiles of a request and the units of
 // all requests of the kernel of few rows.
@@ -27,7 +35,7 @@ HeadBounds head_bounds(const caee_head_desc_t& d) {
     b.few_tiles = ((long long)d.max_new * (d.heads / d.kv_heads) + kFewRows - 1) / kFewRows;
     const long long per = (b.longest + kFewTokens - 1) / kFewTokens;
     b.few_units = (double)std::min(d.B * per, kv / kFewTokens + d.B) * (double)b.few_tiles * d.kv_heads;
-    b.few_limit = (double)(kv / kFewTokens + d.B) * (double)b.few_tiles * d.kv_heads;
+    b.few_limit = (double)(kv / kFewTokens + (1 + kFewStarts / d.dim) * (long long)d.B) * (double)b.few_tiles * d.kv_heads;
     return b;
 }
 
@@ -175,6 +183,7 @@ caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, c
     p.lse = lse;
     p.meta = (int32_t*)(w + L.meta);
     const HeadWay way = head_way(d);
+    p.few_start = head_bounds(d).few_units > kFewGroups ? kFewStarts / d.dim : 0;
     p.part = way == HeadWay::whole ? nullptr : (float*)(w + L.part);
     p.part_ml = (float*)(w + L.part_ml);
     hipStream_t s = (hipStream_t)stream;

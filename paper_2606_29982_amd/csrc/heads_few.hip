@@ -80,12 +80,14 @@ struct FewList {
     LatentReq rq;
     int n, tile, first;   // units of each of the request's lists; which list; the first unit of it
 };
+// Units of tokens before unit i of a list.
+__device__ inline int few_before(const HeadParams& p, int i) { return max(i - p.few_start, 0); }
 __device__ inline int few_tiles(const HeadParams& p, const FewList& x) { return (x.rq.add * p.ratio + kFewRows - 1) / kFewRows; }
 __device__ inline FewList few_request(const HeadParams& p, const HeadLine& line, int b) {
     FewList x = {};
     x.b = b;
     x.rq = head_line_req(p, line, b, &x.at);
-    x.n = (x.rq.seq + kFewTokens - 1) / kFewTokens;
+    x.n = head_few_list(p, x.rq);
     return x;
 }
 // The list that unit u is of.
@@ -154,7 +156,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
 
     constexpr int kEights = kWaveTokens / 8, kLook = kHeadWindow / kEights;
     auto look_at = [&](const FewList& x, int s) __attribute__((always_inline)) {
-        return head_look(p, x.b, x.rq.seq, (x.first + s + lane / kEights) * kFewTokens + kWaveTokens * wave + 8 * (lane % kEights));
+        return head_look(p, x.b, x.rq.seq, (few_before(p, x.first) + s + lane / kEights) * kFewTokens + kWaveTokens * wave + 8 * (lane % kEights));
     };
     // Asks for a list's queries and its first pages.
     auto open = [&](const FewList& x, int parity) __attribute__((always_inline)) {
@@ -186,8 +188,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
         const int limit = head_sees(p, rq, tok);
         // Tokens from lim_min on some row does not see.
         const int lim_min = kTree ? min(max(rq.before, 0), rq.seq) : head_sees(p, rq, head_over(row0, p.by_ratio));
-        const int end = min(last * kFewTokens, head_sees(p, rq, head_over(row0 + n_rows - 1, p.by_ratio)));
-        const int tok0 = first * kFewTokens + kWaveTokens * wave;
+        const int end = min(few_before(p, last) * kFewTokens, head_sees(p, rq, head_over(row0 + n_rows - 1, p.by_ratio)));
+        const int tok0 = few_before(p, first) * kFewTokens + kWaveTokens * wave;
         const int steps = end > tok0 ? (end - tok0 + kFewTokens - 1) / kFewTokens : 0;
         const uint32_t* mask = kTree ? p.tree + (size_t)(rq.t0 + tok) * p.words : nullptr;
 
@@ -454,7 +456,7 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
             rq = head_line_req(p, line, b, &at_u);
         }
     }
-    if (t >= rq.t0 && t - rq.t0 < rq.add) n_u = few ? (rq.seq + kFewTokens - 1) / kFewTokens : head_steps(rq);
+    if (t >= rq.t0 && t - rq.t0 < rq.add) n_u = few ? head_few_list(p, rq) : head_steps(rq);
     if (n_u == 0) {
 #pragma unroll
         for (int i = 0; i < kPasses; ++i)
