@@ -123,10 +123,12 @@ struct FewStage {
 // second part is free; a result of 32 bits has three).
 // Memory bounds it: 5 users of 120000 tokens, 8 groups 367 us for 2.34 GB (6.4
 // TB/s, of the 6.95 that a large copy reads); 64 users of 2050 tokens on average
-// 93 us for 503 MB (5.4), as the 512 shares, equal in tokens, end 61 to 93 us after
-// the start: finer ones dealt out in turn gained nothing (2 and 4 times as many: 354 and
-// 360 us beside 351 for long lists, 104 and 109 beside 100 for short ones).  A
-// user of 902 tokens takes 7.7, a chain of launch, lengths, pages, fetch, one step
+// 93 us for 503 MB (5.4), as a share begins and ends two lists, which the other
+// workgroup of the CU hides in part; the next list's queries and pages are asked for
+// while the last one's results leave (256 users of 1000 tokens 224 and 235).  Finer shares
+// dealt out in turn gained nothing (2 and 4 times as many: 354 and 360 us beside 351
+// for long lists, 104 and 109 beside 100 for short ones).  A user of 902 tokens
+// takes 7.9, a chain of launch, lengths, pages, fetch, one step
 // and the result's way out.  Pages by head are 6 % faster than by token (92 and 98 us
 // for 64 users), as a wave's eight rows are one line after the other.
 template <int D, bool kTree, bool kOnce, bool kLast>
