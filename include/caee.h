@@ -565,8 +565,8 @@ caee_status_t caee_head_store(const caee_head_store_desc_t* desc, const void* q,
 /* How the work is dealt to the GPU.  All give the same function. */
 typedef enum caee_head_form {
     /* Whole where requests have 1536 tokens at most, as far as max_kv,
-     * max_blocks * block_size and max_kv - T + max_new tell, but for a handful of
-     * rows, and where T * heads >= 131072; else split. */
+     * max_blocks * block_size and max_kv - T + max_new tell, unless there are few
+     * rows for that length, and where T * heads >= 131072; else split. */
     CAEE_HEAD_AUTO = 0,
     /* The requests' tokens are cut so that all CUs have a share, partial results
      * are joined: few new tokens (decode steps, trees, the next part of a long

@@ -47,21 +47,28 @@ HeadBounds head_bounds(const caee_head_desc_t& d) {
 // 30000 with 8 (3760) 54.6 and 34.9; 16 requests of 4000, 1 group, with 32 (4096)
 // 37.4 and 38.8, 61 (8192) 53.0 and 41.2.  One row tile a request and group, in
 // which neither reads a token twice: 16 requests of 4000, 8 groups 54.0 and 53.3.
-// Up to kHeadShort tokens cutting row tiles gains nothing, and joining costs 6 us
-// and more: 61 requests of 200, 1 group, with 1 new token few 13.8, whole 11.4, with
-// 61 few 39.5, many 29.4, whole 17.0; 16 of 500, 8 groups, with 4 (512 units) 23.2,
-// 20.7, 17.6; only a handful of units is faster by the kernel of few rows: 1 of 500, 8
-// groups, with 1 (32 units) 12.5 and 16.0, 16 of 500, 1 group, with 1 (64) 14.5 and
-// 16.2.  Where there are kTilePieces row tiles or more none is cut.
-constexpr long long kHeadShort = 24 * kTileTokens;
-constexpr double kHeadShortUnits = 64, kHeadFewUnits = 2048;
+// Up to kHeadShort tokens cutting row tiles gains nothing over leaving them whole
+// (61 requests of 200, 1 group, with 61 new tokens: few 39.5, many 29.4, whole 17.0),
+// which takes 7 us and 1.2 a step, however many requests there are, up to a
+// round of workgroups.  Few rows take 12 and more with their units.  Few and whole, 8
+// groups of 4 heads: 1 request with 13 new tokens of 213 (32 units) 14.1 and 11.4, of
+// 463 (64) 16.2 and 16.2, of 813 (112) 16.8 and 21.8, of 1413 (192) 17.1 and 34.0; 4 of
+// 463 (256) 18.6 and 16.4, of 813 (448) 20.1 and 22.1, of 1413 (768) 22.1 and 34.4; 4 with
+// 30 of 830 (896) 25.9 and 22.2, of 1430 (1536) 32.0 and 34.3; 16 with 30 of 1430 (6144)
+// 38.6 and 36.2.  One row tile: 16 requests up to 200 14.7 and 11.4, up to 500 15.1 and
+// 16.3, 1000 18.3 and 26.3, 1400 18.6 and 33.2; 64 23.0 and 14.6, 26.4 and 23.0, 33.7 and
+// 35.3, 45.3 and 44.5; 256 up to 1000 108 and 133.
+// Where there are kTilePieces row tiles or more none is cut.
+constexpr long long kHeadShort = 24 * kTileTokens, kHeadShorter = 8 * kTileTokens;
+constexpr double kHeadFewUnits = 2048;
 enum class HeadWay { few, many, whole };
 HeadWay head_way(const caee_head_desc_t& d) {
     if (d.form == CAEE_HEAD_WHOLE) return HeadWay::whole;
     const HeadBounds b = head_bounds(d);
-    if (d.form == CAEE_HEAD_AUTO && b.longest <= kHeadShort) return b.few_units <= kHeadShortUnits ? HeadWay::few : HeadWay::whole;
-    // (units are counted in 32 bits)
-    if (b.few_units <= kHeadFewUnits || (b.few_tiles <= 1 && b.few_limit <= kHeadMaxUnits)) return HeadWay::few;
+    const bool once = b.few_tiles <= 1 && b.few_limit <= kHeadMaxUnits;        // (units are counted in 32 bits)
+    if (d.form == CAEE_HEAD_AUTO && b.longest <= kHeadShort)
+        return b.few_units <= (double)b.longest - 400.0 || (once && b.longest > kHeadShorter) ? HeadWay::few : HeadWay::whole;
+    if (b.few_units <= kHeadFewUnits || once) return HeadWay::few;
     return d.form == CAEE_HEAD_AUTO && (long long)d.T * d.heads >= kTilePieces * kTileRows ? HeadWay::whole : HeadWay::many;
 }
 

@@ -289,6 +289,11 @@ def test_auto_takes_every_call():
         _check("auto", seed=23, **kw)
 
 
+@pytest.mark.parametrize("B,new,S", [(1, 13, 213), (1, 13, 1413), (4, 30, 463), (4, 30, 830), (16, 1, 300), (16, 1, 900), (3, 60, 1600)])
+def test_auto_by_rows_and_length(B, new, S):
+    _check("auto", seq=[S - 7 * b for b in range(B)], new=[new] * B, H=8, G=2, seed=23)
+
+
 @pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("new", [[2, 1, 30], [200, 40, 300]])
 def test_results_repeat_bit_for_bit(new, form):
