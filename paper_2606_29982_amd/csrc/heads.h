@@ -120,6 +120,12 @@ __device__ inline int head_tiles(const HeadParams& p, const LatentReq& r) { retu
 __device__ inline int head_steps(const LatentReq& r) { return (r.seq + kTileTokens - 1) / kTileTokens; }
 // Pieces of a row tile of n steps.
 __device__ inline int head_cut(int n, int per) { return max((n + per - 1) / per, 1); }
+// Step that piece `part` of `parts` of n steps begins with (part == parts: n), n part / parts:
+// that product passes 32 bits for 2^28 tokens in 512 pieces, these do not.
+__host__ __device__ inline int head_piece_at(int n, int part, int parts) {
+    const int each = n / parts;
+    return each * part + (n - each * parts) * part / parts;
+}
 
 // Inclusive scan over the lanes, in registers (a shuffle through LDS takes ten
 // times as long, and a workgroup begins with a chain of these), and its last.

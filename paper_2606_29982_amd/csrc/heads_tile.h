@@ -191,7 +191,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
     {
         const int rows = rq.add * p.ratio, steps_all = head_steps(rq);
         const bool whole = parts == 1;
-        const int first = whole ? 0 : head_div(steps_all * part, parts), last = whole ? steps_all : head_div(steps_all * (part + 1), parts);
+        const int first = whole ? 0 : __builtin_amdgcn_readfirstlane(head_piece_at(steps_all, part, parts));
+        const int last = whole ? steps_all : __builtin_amdgcn_readfirstlane(head_piece_at(steps_all, part + 1, parts));
         const int row0 = rt * kTileRows, my0 = row0 + 32 * wave;
         auto sees = [&](int r) { return head_sees(p, rq, head_over(min(r, rows - 1), p.by_ratio)); };
         const int row = min(my0 + n, rows - 1), tok = head_over(row, p.by_ratio);
