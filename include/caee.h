@@ -619,9 +619,10 @@ caee_status_t caee_head_workspace_size(const caee_head_desc_t* desc, size_t* byt
  * have rows, whose results are as if all had.  Cache rows at or past a request's
  * seq_len are never read; rows that a query does not see do not change its
  * result, whatever they hold.
- * An infinity or NaN in a value that a row sees is in that place of its result;
- * of a key, or of the query, what it makes of the score counts: NaN or +inf
- * makes the row NaN, -inf the token's weight 0 (a row of none but those is zero).
+ * An infinity or NaN in a value that a row sees is in that place of its result,
+ * whatever its weight; of a key, or of the query, what it makes of the score
+ * counts: NaN or +inf makes the row NaN, -inf the token's weight 0 (a row of none
+ * but those is zero where its values are finite).
  * Scores, softmax statistics and sums are fp32; the softmax weights are rounded
  * to bf16 before their products (with few rows to two bf16 parts, the second
  * what the first leaves), for an fp32 y to three parts, which lose nothing.

@@ -243,17 +243,26 @@ __device__ inline float head_weight(float s, float scale_log2, float m) { return
 // tile, so that the weights are made by lat_weight, whose products are rounded.
 __device__ inline bool head_moves(float more, float m) { return more > kMaxWeight || !(fabsf(m) <= 0x1p20f); }
 
+// a f + x e.  An infinity or NaN among the sums, of a value that the row sees, stays
+// however little its part of the tokens weighs: a factor of zero leaves it alone.
+__device__ inline float head_join(float a, float f, float x, float e) {
+    const float r = fmaf(x, e, a * f);
+    if (fabsf(r) < INFINITY) return r;
+    return (fabsf(a) < INFINITY ? a * f : a) + (fabsf(x) < INFINITY ? x * e : x);
+}
 // Adds a partial result (sums x of weights by the maximum w.x, whose total is w.y)
 // to one.
 __device__ inline void head_merge(float4& v, float& m, float& l, const float4& x, const float2& w) {
     const float mn = fmaxf(m, w.x), f = __builtin_amdgcn_exp2f(m - mn), e = __builtin_amdgcn_exp2f(w.x - mn);
-    // (an infinity among the sums stays where it is)
-    if (f == 0.0f || l == 0.0f) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    else v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-    if (e != 0.0f) v = make_float4(v.x + x.x * e, v.y + x.y * e, v.z + x.z * e, v.w + x.w * e);
+    v = make_float4(head_join(v.x, f, x.x, e), head_join(v.y, f, x.y, e), head_join(v.z, f, x.z, e), head_join(v.w, f, x.w, e));
     l = l * f + w.y * e;
     m = mn;
 }
+// Maximum of a partial result without sums: none of its tokens is one that the row may see.
+constexpr float kNoPart = -INFINITY;
+// Factor of a row's sums: 1 / l.  Where no weight is left they are zero, but for infinities
+// and NaNs, which stay.
+__device__ inline float head_inverse(float l) { return l == 0.0f ? 1.0f : 1.0f / l; }
 
 // Whether values that are no numbers may have met weights of zero, or weights'
 // remainders, in a lane's sums o of a row whose weights add up to l.

@@ -394,14 +394,14 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
                 const float f = __builtin_amdgcn_exp2f(w[i].x - mx);
                 const float4 t = *place(i, r, c);
                 lx += w[i].y * f;
-                if (f != 0.0f) v = make_float4(v.x + t.x * f, v.y + t.y * f, v.z + t.z * f, v.w + t.w * f);
+                v = make_float4(head_join(v.x, 1.0f, t.x, f), head_join(v.y, 1.0f, t.y, f), head_join(v.z, 1.0f, t.z, f), head_join(v.w, 1.0f, t.w, f));
             }
             if (!whole) {
                 *(float4*)(p.part + (slot0 + r) * D + 4 * c) = v;
                 if (c == 0) *(float2*)(p.part_ml + 2 * (slot0 + r)) = make_float2(mx, lx);
                 continue;
             }
-            const float f = lat_inverse(lx);
+            const float f = head_inverse(lx);
             const size_t at = (size_t)row_at[parity][r];
             if (p.y_bf16) *(lat_u32x2*)((uint16_t*)p.y + at * D + 4 * c) = lat_u32x2{lat_pack(v.x * f, v.y * f), lat_pack(v.z * f, v.w * f)};
             else *(float4*)((float*)p.y + at * D + 4 * c) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
@@ -436,7 +436,7 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
     head_line_sum(p, &line, few ? head_few_units(p, line.mine) : head_tiles(p, line.mine) * head_cut(head_steps(line.mine), piece));
     auto leave = [&](int h, const float4& v, float m, float l) __attribute__((always_inline)) {
         const size_t at = (size_t)t * p.H + h;
-        const float inv = lat_inverse(l);
+        const float inv = head_inverse(l);
         if (p.lse && c == 0) p.lse[at] = lat_lse(m, l);
         if (p.y_bf16) *(lat_u32x2*)((uint16_t*)p.y + at * D + 4 * c) = lat_u32x2{lat_pack(v.x * inv, v.y * inv), lat_pack(v.z * inv, v.w * inv)};
         else *(float4*)((float*)p.y + at * D + 4 * c) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
@@ -512,8 +512,7 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < kPasses; ++i) {
-                // shares that saw nothing for the row have written no sums
-                if (g0[i] + k0 + (kMany ? u : kWaves * u) > g1[i] || w[u][i].y == 0.0f) continue;
+                if (g0[i] + k0 + (kMany ? u : kWaves * u) > g1[i] || w[u][i].x == kNoPart) continue;
                 head_merge(sum[i], m[i], l[i], x[u][i], w[u][i]);
             }
     };
@@ -529,7 +528,7 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
         if (wave > 0) return;
 #pragma unroll
         for (int w = 0; w < kWaves - 1; ++w)
-            if (red_ml[w][lane].y != 0.0f) head_merge(sum[0], m[0], l[0], red_v[w][lane], red_ml[w][lane]);
+            head_merge(sum[0], m[0], l[0], red_v[w][lane], red_ml[w][lane]);
     }
 #pragma unroll
     for (int i = 0; i < kPasses; ++i)

@@ -438,9 +438,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
         l = lat_sum_pair(l);
         const bool odd = __builtin_amdgcn_readfirstlane(odd_values) || __any(head_odd(o, l));
         const size_t slot0 = ((size_t)g * line.total + at_b + rt * parts + part) * kTileRows;
-        const float f = whole ? lat_inverse(l) : 1.0f;
+        const float f = whole ? head_inverse(l) : 1.0f;
         if (hf == 0 && my0 + n < rows) {
-            if (!whole) *(float2*)(p.part_ml + 2 * (slot0 + 32 * wave + n)) = make_float2(m, l);
+            if (!whole) *(float2*)(p.part_ml + 2 * (slot0 + 32 * wave + n)) = make_float2(steps > 0 ? m : kNoPart, l);
             else if (p.lse) p.lse[at_row] = lat_lse(m, l);
         }
         // 8 (dim 64: 4) KiB a wave: as much of a row at a time as a bf16 row has, unit
