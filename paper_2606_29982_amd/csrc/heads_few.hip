@@ -389,12 +389,21 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
                 mx = fmaxf(mx, w[i].x);
             }
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            auto sum = [&](auto odd) __attribute__((always_inline)) {
+                constexpr bool kOdd = decltype(odd)::value != 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float f = __builtin_amdgcn_exp2f(w[i].x - mx);
-                const float4 t = *place(i, r, c);
-                lx += w[i].y * f;
-                v = make_float4(head_join(v.x, 1.0f, t.x, f), head_join(v.y, 1.0f, t.y, f), head_join(v.z, 1.0f, t.z, f), head_join(v.w, 1.0f, t.w, f));
+                for (int i = 0; i < 4; ++i) {
+                    const float f = __builtin_amdgcn_exp2f(w[i].x - mx);
+                    const float4 t = *place(i, r, c);
+                    if (!kOdd) lx += w[i].y * f;
+                    v = make_float4(head_join<kOdd>(v.x, 1.0f, t.x, f), head_join<kOdd>(v.y, 1.0f, t.y, f), head_join<kOdd>(v.z, 1.0f, t.z, f),
+                                    head_join<kOdd>(v.w, 1.0f, t.w, f));
+                }
+            };
+            sum(LatInt<0>{});
+            if (!head_finite(v)) {
+                v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                sum(LatInt<1>{});
             }
             if (!whole) {
                 *(float4*)(p.part + (slot0 + r) * D + 4 * c) = v;
@@ -486,15 +495,12 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
             a[i] = 0;
         }
         if (g0[i] < g1[i] && h0 + kHeads * i < p.H) most = max(most, g1[i] - g0[i] + 1);
-        sum[i] = zero;
-        m[i] = kNoScore;
-        l[i] = 0.0f;
     }
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) most = max(most, __shfl_xor(most, d));
     if (most == 0 && kMany) return;
     // Share k of each pass's row: its second slot when the row tile's line begins inside the share.
-    auto add = [&](int k0, auto count) __attribute__((always_inline)) {
+    auto add = [&](int k0, auto count, auto odd) __attribute__((always_inline)) {
         constexpr int U = decltype(count)::value;
         float2 w[U][kPasses];
         float4 x[U][kPasses];
@@ -513,22 +519,44 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
 #pragma unroll
             for (int i = 0; i < kPasses; ++i) {
                 if (g0[i] + k0 + (kMany ? u : kWaves * u) > g1[i] || w[u][i].x == kNoPart) continue;
-                head_merge(sum[i], m[i], l[i], x[u][i], w[u][i]);
+                head_merge<decltype(odd)::value != 0>(sum[i], m[i], l[i], x[u][i], w[u][i]);
             }
     };
-    if constexpr (kMany) {
-        for (int k = 0; k < most; k += 2) add(k, LatInt<2>{});
-    } else {
-        for (int k = wave; k < most; k += 8 * kWaves) add(k, LatInt<8>{});
+    // The shares of this wave, and those with sums that are no numbers once more.
+    auto join = [&](auto count, auto odd) __attribute__((always_inline)) {
+        constexpr int kStep = kMany ? 1 : kWaves, U = decltype(count)::value;
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            sum[i] = zero;
+            m[i] = kNoScore;
+            l[i] = 0.0f;
+        }
+        for (int k = kMany ? 0 : wave; k < most; k += U * kStep) add(k, count, odd);
+    };
+    join(LatInt<kMany ? 2 : 8>{}, LatInt<0>{});
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) odd |= g0[i] < g1[i] && !head_finite(sum[i]);
+    if (odd) join(LatInt<1>{}, LatInt<1>{});
+    if constexpr (!kMany) {
         if (wave > 0) {
             red_v[wave - 1][lane] = sum[0];
             red_ml[wave - 1][lane] = make_float2(m[0], l[0]);
         }
         __syncthreads();
         if (wave > 0) return;
+        const float4 sum0 = sum[0];
+        const float m0 = m[0], l0 = l[0];
+        auto waves = [&](auto odd) __attribute__((always_inline)) {
 #pragma unroll
-        for (int w = 0; w < kWaves - 1; ++w)
-            head_merge(sum[0], m[0], l[0], red_v[w][lane], red_ml[w][lane]);
+            for (int w = 0; w < kWaves - 1; ++w)
+                head_merge<decltype(odd)::value != 0>(sum[0], m[0], l[0], red_v[w][lane], red_ml[w][lane]);
+        };
+        waves(LatInt<0>{});
+        if (g0[0] < g1[0] && !head_finite(sum[0])) {
+            sum[0] = sum0, m[0] = m0, l[0] = l0;
+            waves(LatInt<1>{});
+        }
     }
 #pragma unroll
     for (int i = 0; i < kPasses; ++i)
