@@ -249,8 +249,9 @@ __device__ inline bool head_moves(float more, float m) { return more > kMaxWeigh
 // (looked for at every sum, 31.4 us of a call became 40.0).
 template <bool kOdd>
 __device__ inline float head_join(float a, float f, float x, float e) {
-    if constexpr (!kOdd) return fmaf(x, e, a * f);
-    else return (fabsf(a) < INFINITY ? a * f : a) + (fabsf(x) < INFINITY ? x * e : x);
+    const float r = fmaf(x, e, a * f);
+    if (!kOdd || fabsf(r) < INFINITY) return r;        // (a row's numbers do not change by an infinity beside them)
+    return (fabsf(a) < INFINITY ? a * f : a) + (fabsf(x) < INFINITY ? x * e : x);
 }
 template <bool kOdd>
 __device__ inline void head_merge(float4& v, float& m, float& l, const float4& x, const float2& w) {
