@@ -597,7 +597,7 @@ typedef struct caee_head_desc {
 } caee_head_desc_t;
 
 /* Bytes of workspace caee_head_attention needs: 4 (B + 2), and, but for
- * CAEE_HEAD_WHOLE, 131072 (4 dim + 8), whatever the call's sizes.  Host-only. */
+ * CAEE_HEAD_WHOLE, 131072 (4 dim + 12), whatever the call's sizes.  Host-only. */
 caee_status_t caee_head_workspace_size(const caee_head_desc_t* desc, size_t* bytes);
 
 /* Softmax attention of the new tokens over the paged cache, which holds their
@@ -625,7 +625,8 @@ caee_status_t caee_head_workspace_size(const caee_head_desc_t* desc, size_t* byt
  * but those is zero where its values are finite).
  * Scores, softmax statistics and sums are fp32; the softmax weights are rounded
  * to bf16 before their products (with few rows to two bf16 parts, the second
- * what the first leaves), for an fp32 y to three parts, which lose nothing.
+ * what the first leaves), for an fp32 y to three parts, which lose nothing; lse
+ * is of the weights before that, and does not change y.
  * Preconditions on device contents (violations: unspecified results,
  * memory-safe): page numbers in [0, n_blocks) for the pages seq_len covers, at
  * most max_new new tokens per request and max_kv tokens in all.  Calls that run

@@ -47,6 +47,7 @@ __device__ inline int head_workgroup(int g) { return g % (kFewGroups / kXcds) * 
 struct HeadWs {
     size_t meta;           // [B + 1] unit or piece prefix sums, of more than 64 requests; [1] steps of a piece
     size_t part, part_ml;  // split: [two a share, or a piece][rows][dim] partial sums and [..][rows][2] (maximum, sum)
+    size_t part_sum;       // [piece][rows] sums of the weights before their rounding
     size_t total;
 };
 
@@ -83,6 +84,7 @@ struct HeadParams {
     int32_t* meta;
     float* part;          // NULL: whole form
     float* part_ml;
+    float* part_sum;      // NULL: those of part_ml are of weights that are not rounded, or there is no lse
 };
 
 // New tokens and length of request b as the kernels use them: 0 <= new <=
@@ -243,7 +245,8 @@ __device__ inline float head_weight(float s, float scale_log2, float m) { return
 // tile, so that the weights are made by lat_weight, whose products are rounded.
 __device__ inline bool head_moves(float more, float m) { return more > kMaxWeight || !(fabsf(m) <= 0x1p20f); }
 
-// Adds a partial result (sums x of weights by the maximum w.x, whose total is w.y) to one.  An infinity or NaN among the sums, of a
+// Adds a partial result (sums x of weights by the maximum w.x, whose total is w.y, and
+// `all` before the weights were rounded) to one.  An infinity or NaN among the sums, of a
 // value that the row sees, stays however little its part of the tokens weighs (kOdd); without,
 // it is no number afterwards, whatever its factor, and that is looked for once, at the end
 // (looked for at every sum, 31.4 us of a call became 40.0).
@@ -254,11 +257,12 @@ __device__ inline float head_join(float a, float f, float x, float e) {
     return (fabsf(a) < INFINITY ? a * f : a) + (fabsf(x) < INFINITY ? x * e : x);
 }
 template <bool kOdd>
-__device__ inline void head_merge(float4& v, float& m, float& l, const float4& x, const float2& w) {
+__device__ inline void head_merge(float4& v, float& m, float& l, float& sum, const float4& x, const float2& w, float all) {
     const float mn = fmaxf(m, w.x), f = __builtin_amdgcn_exp2f(m - mn), e = __builtin_amdgcn_exp2f(w.x - mn);
     v = make_float4(head_join<kOdd>(v.x, f, x.x, e), head_join<kOdd>(v.y, f, x.y, e), head_join<kOdd>(v.z, f, x.z, e),
                     head_join<kOdd>(v.w, f, x.w, e));
     l = fmaf(w.y, e, l * f);           // (in every kernel the same rounding)
+    sum = fmaf(all, e, sum * f);
     m = mn;
 }
 __device__ inline bool head_finite(const float4& v) { return fabsf(v.x) + fabsf(v.y) + fabsf(v.z) + fabsf(v.w) < INFINITY; }

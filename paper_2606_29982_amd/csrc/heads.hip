@@ -85,6 +85,7 @@ HeadWs head_ws(const caee_head_desc_t& d) {
     const size_t part_rows = d.form == CAEE_HEAD_WHOLE ? 0 : (size_t)std::max(2 * kFewGroups * kFewRows, kTilePieces * kTileRows);
     L.part = take(part_rows * d.dim * 4);
     L.part_ml = take(part_rows * 2 * 4);
+    L.part_sum = take(part_rows * 4);
     L.total = at;
     return L;
 }
@@ -193,6 +194,7 @@ caee_status_t caee_head_attention(const caee_head_desc_t* desc, const void* q, c
     p.few_start = head_bounds(d).few_units > kFewGroups ? kFewStarts / d.dim : 0;
     p.part = way == HeadWay::whole ? nullptr : (float*)(w + L.part);
     p.part_ml = (float*)(w + L.part_ml);
+    p.part_sum = way == HeadWay::many && p.y_bf16 && lse ? (float*)(w + L.part_sum) : nullptr;
     hipStream_t s = (hipStream_t)stream;
     return timed_launch(CAEE_KERNEL_ATTENTION, s, "head attention", [&] {
         return way == HeadWay::few ? launch_head_few(p, s) : launch_head_many(p, s);

@@ -430,11 +430,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_head_few(HeadParams p) {
 // 64 heads, 3.5 for 8 rows of a launch's latency; of many rows 50 MB in 13 us for 16
 // trees of 61 tokens, 60 in 17 for 259 tokens of 2 prompts behind 30000.
 constexpr int kJoinRows = 4096;        // (token, head) rows from which on they are many
-template <int D, bool kMany>
+template <int D, bool kMany, bool kSum>
 __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few) {
     constexpr int kLanes = D / 4, kHeads = kWave / kLanes, kPasses = kMany ? 4 : 1, kWaves = kFewThreads / kWave;
     __shared__ float4 red_v[kMany ? 1 : kWaves - 1][kWave];
     __shared__ float2 red_ml[kMany ? 1 : kWaves - 1][kWave];
+    __shared__ float red_all[kMany || !kSum ? 1 : kWaves - 1][kWave];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per_wg = kMany ? kHeads * kPasses * kWaves : kHeads, wgs = (p.H + per_wg - 1) / per_wg;
     const int wg = (int)lat_workgroup(), t = head_div(wg, wgs);
@@ -443,10 +444,10 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
     HeadLine line = head_line(p);
     const int piece = few ? 1 : __builtin_amdgcn_readfirstlane(p.meta[p.B + 1]);
     head_line_sum(p, &line, few ? head_few_units(p, line.mine) : head_tiles(p, line.mine) * head_cut(head_steps(line.mine), piece));
-    auto leave = [&](int h, const float4& v, float m, float l) __attribute__((always_inline)) {
+    auto leave = [&](int h, const float4& v, float m, float l, float all) __attribute__((always_inline)) {
         const size_t at = (size_t)t * p.H + h;
         const float inv = head_inverse(l);
-        if (p.lse && c == 0) p.lse[at] = lat_lse(m, l);
+        if (p.lse && c == 0) p.lse[at] = lat_lse(m, all);
         if (p.y_bf16) *(lat_u32x2*)((uint16_t*)p.y + at * D + 4 * c) = lat_u32x2{lat_pack(v.x * inv, v.y * inv), lat_pack(v.z * inv, v.w * inv)};
         else *(float4*)((float*)p.y + at * D + 4 * c) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
     };
@@ -471,7 +472,7 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
     if (n_u == 0) {
 #pragma unroll
         for (int i = 0; i < kPasses; ++i)
-            if (h0 + kHeads * i < p.H && (kMany || wave == 0)) leave(h0 + kHeads * i, zero, kNoScore, 0.0f);
+            if (h0 + kHeads * i < p.H && (kMany || wave == 0)) leave(h0 + kHeads * i, zero, kNoScore, 0.0f, 0.0f);
         return;
     }
     const int tile_rows = few ? kFewRows : kTileRows;
@@ -479,7 +480,7 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
     const int per = few ? head_share(line.total) : 1, cut = few ? 1 : __builtin_amdgcn_readfirstlane(head_cut(n_u, piece));
     if (!few && cut == 1) return;
     float4 sum[kPasses];
-    float m[kPasses], l[kPasses];
+    float m[kPasses], l[kPasses], all[kPasses];      // all: the sum before the weights were rounded
     int g0[kPasses], g1[kPasses], a[kPasses], rr[kPasses], most = 0;
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
@@ -504,6 +505,7 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
         constexpr int U = decltype(count)::value;
         float2 w[U][kPasses];
         float4 x[U][kPasses];
+        float wa[U][kPasses];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -513,13 +515,15 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
                 const size_t slot = at * tile_rows + rr[i];
                 w[u][i] = ((const float2*)p.part_ml)[slot];
                 x[u][i] = *(const float4*)(p.part + slot * D + 4 * c);
+                if constexpr (kSum) wa[u][i] = p.part_sum[slot];
+                else wa[u][i] = w[u][i].y;
             }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < kPasses; ++i) {
                 if (g0[i] + k0 + (kMany ? u : kWaves * u) > g1[i] || w[u][i].x == kNoPart) continue;
-                head_merge<decltype(odd)::value != 0>(sum[i], m[i], l[i], x[u][i], w[u][i]);
+                head_merge<decltype(odd)::value != 0>(sum[i], m[i], l[i], all[i], x[u][i], w[u][i], wa[u][i]);
             }
     };
     // The shares of this wave, and those with sums that are no numbers once more.
@@ -529,7 +533,7 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
         for (int i = 0; i < kPasses; ++i) {
             sum[i] = zero;
             m[i] = kNoScore;
-            l[i] = 0.0f;
+            l[i] = all[i] = 0.0f;
         }
         for (int k = kMany ? 0 : wave; k < most; k += U * kStep) add(k, count, odd);
     };
@@ -542,25 +546,28 @@ __global__ __launch_bounds__(kFewThreads) void k_head_join(HeadParams p, int few
         if (wave > 0) {
             red_v[wave - 1][lane] = sum[0];
             red_ml[wave - 1][lane] = make_float2(m[0], l[0]);
+            if constexpr (kSum) red_all[wave - 1][lane] = all[0];
         }
         __syncthreads();
         if (wave > 0) return;
         const float4 sum0 = sum[0];
-        const float m0 = m[0], l0 = l[0];
+        const float m0 = m[0], l0 = l[0], all0 = all[0];
         auto waves = [&](auto odd) __attribute__((always_inline)) {
 #pragma unroll
-            for (int w = 0; w < kWaves - 1; ++w)
-                head_merge<decltype(odd)::value != 0>(sum[0], m[0], l[0], red_v[w][lane], red_ml[w][lane]);
+            for (int w = 0; w < kWaves - 1; ++w) {
+                const float2 ml = red_ml[w][lane];
+                head_merge<decltype(odd)::value != 0>(sum[0], m[0], l[0], all[0], red_v[w][lane], ml, kSum ? red_all[w][lane] : ml.y);
+            }
         };
         waves(LatInt<0>{});
         if (g0[0] < g1[0] && !head_finite(sum[0])) {
-            sum[0] = sum0, m[0] = m0, l[0] = l0;
+            sum[0] = sum0, m[0] = m0, l[0] = l0, all[0] = all0;
             waves(LatInt<1>{});
         }
     }
 #pragma unroll
     for (int i = 0; i < kPasses; ++i)
-        if (h0 + kHeads * i < p.H && g0[i] < g1[i]) leave(h0 + kHeads * i, sum[i], m[i], l[i]);
+        if (h0 + kHeads * i < p.H && g0[i] < g1[i]) leave(h0 + kHeads * i, sum[i], m[i], l[i], all[i]);
 }
 
 }  // namespace
@@ -572,14 +579,18 @@ void meta(const HeadParams& p, int few, hipStream_t s) {
 }
 
 void join(const HeadParams& p, int few, hipStream_t s) {
-    auto run = [&](auto dim, auto many) {
+    auto run = [&](auto dim, auto many, auto sum) {
         constexpr int D = decltype(dim)::value, kPer = kWave / (D / 4) * (decltype(many)::value ? 16 : 1);
-        hipLaunchKernelGGL((k_head_join<D, decltype(many)::value != 0>), lat_grid((unsigned)(p.T * ((p.H + kPer - 1) / kPer))),
-                           dim3(kFewThreads), 0, s, p, few);
+        hipLaunchKernelGGL((k_head_join<D, decltype(many)::value != 0, decltype(sum)::value != 0>),
+                           lat_grid((unsigned)(p.T * ((p.H + kPer - 1) / kPer))), dim3(kFewThreads), 0, s, p, few);
+    };
+    auto sums = [&](auto dim, auto many) {
+        if (p.part_sum) run(dim, many, LatInt<1>{});
+        else run(dim, many, LatInt<0>{});
     };
     auto dims = [&](auto many) {
-        if (p.dim == 128) run(LatInt<128>{}, many);
-        else run(LatInt<64>{}, many);
+        if (p.dim == 128) sums(LatInt<128>{}, many);
+        else sums(LatInt<64>{}, many);
     };
     if ((long long)p.T * p.H >= kJoinRows) dims(LatInt<1>{});
     else dims(LatInt<0>{});

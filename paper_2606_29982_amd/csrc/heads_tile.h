@@ -108,8 +108,10 @@ struct HeadTile {
 // the products with the keys, the next 16 tokens' weights are made between the
 // products with the values: a wave's vector instructions run beside its own MFMAs
 // (an MFMA of 32x32x16 takes 13.6 ns, with four vector instructions and an exponential
-// beside it 15.5).  Weights are rounded to bf16, and l sums the rounded ones; for a
-// 32-bit result they have three parts.
+// beside it 15.5).  Weights are rounded to bf16, and l sums the rounded ones, so that
+// their roundings cancel where one token dominates; for a 32-bit result they have three
+// parts.  The log-sum-exp is of the weights themselves, whose sum is kept beside l where
+// it is asked for (kSum: the long prompt below 520 and 537 us).
 // Two workgroups a CU fill each other's gaps; one of 256 rows, which reads the keys
 // and values half as often, has none to fill them (tree-shaped calls of 16 users
 // 159 us, 97 with two; 8 ragged prompts 42 and 38, one of 7161 tokens 508 and 527).
@@ -120,7 +122,7 @@ struct HeadTile {
 // two barriers a step was slower (540 beside 527).  Short calls are bound by a tile's start
 // and end (7 to 8 us: lengths 1.8, pages and queries 1.7, fetch 0.8, out 2) beside
 // 1.6 us a step.
-template <int D, bool kTree, bool kRest>
+template <int D, bool kTree, bool kRest, bool kSum>
 __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-descriptor type exists for the GPU target only
     constexpr int kG = D / 64, kJ = D / 16, NC = D / 32;
@@ -232,7 +234,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
         lat_f32x16 o[NC];
 #pragma unroll
         for (int c = 0; c < NC; ++c) o[c] = lat_f32x16{};
-        float m = kNoScore, l = 0.0f;
+        float m = kNoScore, l = 0.0f, all = 0.0f;
 
         auto piece = [&](int i) __attribute__((always_inline)) { return 16u * ((lane & 7) ^ lat_swz(8 * i + (lane >> 3))); };
         const char *const k_base = head_base(p, p.k, g), *const v_base = head_base(p, p.v, g);
@@ -363,6 +365,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
                 mt = lat_max_pair(mt) * p.scale_log2;
                 const float mn = fmaxf(m, mt), f = __builtin_amdgcn_exp2f(m - mn);
                 l *= f;
+                if constexpr (kSum) all *= f;
                 m = mn;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) o[c] *= f;
@@ -394,6 +397,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
                     l += a + e;
                 } else {
                     l = lat_sum2(pf[k][i], l);
+                    if constexpr (kSum) all += a + e;
                 }
             };
             lat_for<0, 4>([&](auto ic) __attribute__((always_inline)) { weights(LatInt<0>{}, ic); });
@@ -436,12 +440,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
         lat_wait_vm<0>();
         __syncthreads();           // nobody reads the stages any more
         l = lat_sum_pair(l);
+        all = kSum ? lat_sum_pair(all) : l;
         const bool odd = __builtin_amdgcn_readfirstlane(odd_values) || __any(head_odd(o, l));
         const size_t slot0 = ((size_t)g * line.total + at_b + rt * parts + part) * kTileRows;
         const float f = whole ? head_inverse(l) : 1.0f;
         if (hf == 0 && my0 + n < rows) {
-            if (!whole) *(float2*)(p.part_ml + 2 * (slot0 + 32 * wave + n)) = make_float2(steps > 0 ? m : kNoPart, l);
-            else if (p.lse) p.lse[at_row] = lat_lse(m, l);
+            if (!whole) {
+                *(float2*)(p.part_ml + 2 * (slot0 + 32 * wave + n)) = make_float2(steps > 0 ? m : kNoPart, l);
+                if constexpr (kSum) p.part_sum[slot0 + 32 * wave + n] = all;
+            } else if (p.lse) {
+                p.lse[at_row] = lat_lse(m, all);
+            }
         }
         // 8 (dim 64: 4) KiB a wave: as much of a row at a time as a bf16 row has, unit
         // u (16 bytes) of it at u ^ (row % units).
@@ -509,17 +518,18 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_head_tile(HeadParams p, int
 
 template <int D>
 hipError_t head_tile(const HeadParams& p, unsigned grid, int pieces, hipStream_t s) {
-    auto run = [&](auto tree, auto rest) {
-        hipLaunchKernelGGL((k_head_tile<D, decltype(tree)::value != 0, decltype(rest)::value != 0>), lat_grid(grid),
-                           dim3(kTileThreads), 0, s, p, pieces);
+    auto run = [&](auto tree, auto rest, auto sum) {
+        hipLaunchKernelGGL((k_head_tile<D, decltype(tree)::value != 0, decltype(rest)::value != 0, decltype(sum)::value != 0>),
+                           lat_grid(grid), dim3(kTileThreads), 0, s, p, pieces);
     };
-    auto trees = [&](auto rest) {
-        if (p.tree) run(LatInt<1>{}, rest);
-        else run(LatInt<0>{}, rest);
+    auto trees = [&](auto rest, auto sum) {
+        if (p.tree) run(LatInt<1>{}, rest, sum);
+        else run(LatInt<0>{}, rest, sum);
     };
-    // Weights' remainders for 32-bit results only.
-    if (p.y_bf16) trees(LatInt<0>{});
-    else trees(LatInt<1>{});
+    // Weights' remainders for 32-bit results only, whose l is of the weights themselves.
+    if (!p.y_bf16) trees(LatInt<1>{}, LatInt<0>{});
+    else if (p.lse) trees(LatInt<0>{}, LatInt<1>{});
+    else trees(LatInt<0>{}, LatInt<0>{});
     return hipGetLastError();
 }
 
