@@ -1,0 +1,147 @@
+"""Row tiles cut into pieces of their tokens, and joined: every mask and type,
+up to 64 requests (whose workgroups sum by themselves) and more (whose sums a
+kernel makes first).  Each test sees that they were cut."""
+import numpy as np
+import pytest
+import torch
+
+from head_cases import HeadCase, check_heads, random_tree
+from head_ways import run_way
+from paper_2606_29982_amd import caee
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _many(B, seed):
+    """B requests, two of them long, some without new tokens, one without any."""
+    rng = np.random.default_rng(seed)
+    seq = rng.integers(1, 90, B)
+    new = np.where(rng.random(B) < 50 / B, np.minimum(seq, rng.integers(0, 3, B)), 0)
+    seq[7], new[7] = 0, 0
+    seq[33], new[33], seq[B - 1], new[B - 1] = 6000, 130, 2500, 61
+    return seq, new
+
+
+@pytest.mark.parametrize("mask", ["causal", "all", "tree"])
+@pytest.mark.parametrize("y_dtype", [BF, F32])
+@pytest.mark.parametrize("H,G,D", [(8, 1, 64), (24, 3, 128), (32, 4, 64), (8, 1, 128)])
+@pytest.mark.parametrize("B", [1, 3, 64, 65, 300])
+def test_cut(B, H, G, D, y_dtype, mask):
+    if B < 64:
+        seq, new = ([3000], [370]) if B == 1 else ([3000, 40, 1600], [250, 40, 129])
+    else:
+        seq, new = _many(B, B)
+    rng = np.random.default_rng(B)
+    tree = random_tree(new, -(-max(new) // 32), rng) if mask == "tree" else None
+    c = HeadCase(seq=seq, new=new, H=H, G=G, D=D, block=16 if B < 64 else 5, layout="head" if D == 64 else "token", pad=3, seed=B,
+                 tree=tree)
+    got, way = run_way(c, DEV, "split", mask != "all", y_dtype)
+    assert way == "cut"
+    check_heads(got, c.ref(mask != "all"), y_dtype)
+
+
+@pytest.mark.parametrize("B", [3, 70])
+@pytest.mark.parametrize("y_dtype", [BF, F32])
+def test_cut_rows_that_see_nothing(y_dtype, B):
+    """More new tokens than cached ones, and empty masks: rows without a token in any piece, or in some."""
+    seq, new = ([3000, 100, 1700], [200, 130, 150]) if B == 3 else _many(B, 1)
+    if B > 3:
+        seq[40], new[40] = 3, 9
+    tree = random_tree(new, -(-max(new) // 32), np.random.default_rng(2), empty=0.3)
+    for t in (None, tree):
+        c = HeadCase(seq=seq, new=new, H=16, G=2, D=64, block=16, pad=5, seed=6, tree=t)
+        got, way = run_way(c, DEV, "split", y_dtype=y_dtype)
+        assert way == "cut"
+        check_heads(got, c.ref(), y_dtype)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), 3.3e38])
+@pytest.mark.parametrize("B", [3, 70])
+def test_cut_unseen_tokens_may_hold_anything(B, bad):
+    seq, new = ([3000, 40, 1600], [180, 40, 129]) if B == 3 else _many(B, 3)
+    b = int(np.argmax(seq))
+    c = HeadCase(seq=seq, new=new, H=16, G=2, seed=7)
+    row = torch.full((c.G, c.D), bad, dtype=BF)
+    c.put(b, int(seq[b]) - 1, k=row, v=row)
+    got, way = run_way(c, DEV, "split")
+    assert way == "cut"
+    last = int(c.cu_new[b + 1]) - 1
+    check_heads(got, c.ref(), rows=[t for t in range(c.T) if t != last])
+
+
+@pytest.mark.parametrize("B", [3, 70])
+def test_cut_values_without_a_number(B):
+    """An infinity and a NaN in one value of a long request reach the rows that see it, in their places only."""
+    seq, new = ([3000, 40, 1600], [180, 40, 129]) if B == 3 else _many(B, 4)
+    b = int(np.argmax(seq))
+    c = HeadCase(seq=seq, new=new, H=16, G=2, seed=8)
+    at = int(seq[b]) - 20
+    v = c.v[b][at].clone()
+    v[:, 3], v[:, 90] = float("inf"), float("nan")
+    c.put(b, at, v=v)
+    (y, lse), way = run_way(c, DEV, "split")
+    assert way == "cut"
+    v[:, [3, 90]] = 0.0
+    c.put(b, at, v=v)
+    ry, rl, ya, sa = c.ref()
+    sees = np.zeros(c.T, bool)
+    sees[int(c.cu_new[b + 1]) - 20:int(c.cu_new[b + 1])] = True
+    assert np.array_equal(np.all(np.isposinf(y[:, :, 3]), axis=1), sees) and np.array_equal(np.all(np.isnan(y[:, :, 90]), axis=1), sees)
+    y[sees, :, 3], y[sees, :, 90] = ry[sees, :, 3], ry[sees, :, 90]
+    check_heads((y, lse), (ry, rl, ya, sa))
+
+
+@pytest.mark.parametrize("B", [3, 70])
+def test_cut_captured_with_other_calls_between(B):
+    """Two captured calls that share a workspace, one cut, replayed in turn with eager work between."""
+    seq, new = ([3000, 40, 1600], [180, 40, 129]) if B == 3 else _many(B, 9)
+    cases = [HeadCase(seq=seq, new=new, H=16, G=2, seed=9), HeadCase(seq=seq, new=np.minimum(new, 1), H=16, G=2, seed=10)]
+    calls = [c.arguments(DEV, "split") for c in cases]
+    calls[1]["ws"] = calls[0]["ws"]
+    want, ys, graphs = [], [], []
+    for c, a in zip(cases, calls):
+        y = torch.empty(c.T, c.H, c.D, dtype=BF, device=DEV)
+        caee.head_attention(y=y, **a)
+        want.append(y)
+        ys.append(torch.zeros_like(y))
+    torch.cuda.synchronize()
+    check_heads((want[0].float().cpu().numpy().astype(np.float64), cases[0].ref()[1]), cases[0].ref())
+    for y, a in zip(ys, calls):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            caee.head_attention(y=y, **a)
+        graphs.append(graph)
+    for _ in range(3):
+        for i in (0, 1):
+            ys[i].zero_()
+            graphs[i].replay()
+            caee.head_attention(y=torch.empty_like(want[1 - i]), **calls[1 - i])
+            torch.cuda.synchronize()
+            assert torch.equal(ys[i], want[i])
+
+
+@pytest.mark.parametrize("y_dtype", [BF, F32])
+def test_auto_leaves_row_tiles_whole_from_131072_rows_on(y_dtype):
+    """Prompts and users behind long contexts in one step."""
+    c = HeadCase(seq=[1100, 2500, 1900], new=[1021, 1, 3], H=128, G=8, D=64, block=64, seed=11)
+    assert c.T * c.H >= 131072
+    got, way = run_way(c, DEV, "auto", y_dtype=y_dtype)
+    assert way == "whole"
+    check_heads(got, c.ref(), y_dtype)
+    c = HeadCase(seq=[1100, 2500, 1900], new=[1010, 1, 3], H=128, G=8, D=64, block=64, seed=11)
+    assert c.T * c.H < 131072
+    got, way = run_way(c, DEV, "auto", y_dtype=y_dtype)
+    assert way != "few"
+    check_heads(got, c.ref(), y_dtype)
+
+
+def test_auto_gives_one_row_tile_a_request_to_few_rows():
+    """However many rows there are in all."""
+    c = HeadCase(seq=[1700] * 64, new=[16] * 64, H=128, G=64, D=64, block=64, seed=12)
+    assert c.T * c.H >= 131072
+    got, way = run_way(c, DEV, "auto")
+    split, also = run_way(c, DEV, "split")
+    assert way == also == "few"
+    assert np.array_equal(got[0], split[0]) and np.array_equal(got[1], split[1])

@@ -4,8 +4,8 @@ import numpy as np
 import pytest
 import torch
 
-from head_cases import HALF_BF16, HALF_F32, HeadCase, random_tree
-from head_ways import run_way
+from head_cases import HeadCase, random_tree
+from head_ways import precise, run_way
 
 pytestmark = pytest.mark.gpu
 DEV = torch.device("cuda:0")
@@ -55,3 +55,15 @@ def test_lse_does_not_change_the_result(D, call):
     (with_lse, _), _ = run_way(c, DEV, form)
     (without, _), _ = run_way(c, DEV, form, lse=False)
     assert np.array_equal(with_lse, without)
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("y_dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_results_have_the_parts_of_their_weights(D, y_dtype, tree, call):
+    """Three bf16 parts for 32-bit results; for bf16 results two in the kernel of few rows, one in that of many."""
+    c, form = _case(call, D, tree, 42)
+    (y, _), way = run_way(c, DEV, form, y_dtype=y_dtype)
+    assert way == call.split("-")[0]
+    assert precise(y, c.ref()[0], y_dtype, 3 if y_dtype == F32 else 2 if way == "few" else 1)
