@@ -557,7 +557,7 @@ typedef struct caee_head_store_desc {
  * is written.  Slots are distinct (see caee_latent_store).  freq and position
  * may be NULL where rope is 0.  q_out may be q itself (bf16, same stride) or
  * lie beside q, k and v in rows of the same stride; else it may not overlap them
- * (refused).  The caches overlap nothing else, nor each other. */
+ * (refused), as the caches may not each other.  They overlap nothing else. */
 caee_status_t caee_head_store(const caee_head_store_desc_t* desc, const void* q, const void* k, const void* v,
                               const float* q_norm, const float* k_norm, const double* freq, const int32_t* position,
                               const int64_t* slots, void* q_out, void* k_cache, void* v_cache, void* stream);

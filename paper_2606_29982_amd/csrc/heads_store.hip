@@ -2,6 +2,8 @@
 // head, rotation by position, rounding to bf16 (caee_head_store).
 #include <math.h>
 
+#include <utility>
+
 #include "heads.h"
 
 namespace caee {
@@ -46,6 +48,25 @@ caee_status_t head_cache(int kv_heads, int dim, int block_size, int n_blocks, lo
 }
 
 namespace {
+
+// Whether heads of two caches of the same strides, `apart` elements from one another, share a
+// place: some pages, rows and heads on, the other's head begins within one.  What lies inside
+// a page (row, head) takes no more than the stride, so two numbers of each come into question.
+bool caches_meet(const HeadCache& c, int kv_heads, int dim, long long apart) {
+    struct Level {
+        long long n, stride;
+    } levels[3] = {{c.n_blocks, c.page_stride}, {c.block, c.row_stride}, {kv_heads, c.head_stride}};
+    if (c.head_stride > c.row_stride && c.block > 1) std::swap(levels[1], levels[2]);
+    auto meet = [&](auto&& self, int i, long long left) -> bool {
+        if (i == 3) return left < dim && left > -dim;
+        if (levels[i].n == 1) return self(self, i + 1, left);
+        const long long n = levels[i].n, k = left / levels[i].stride - (left < 0);
+        for (long long at : {k, k + 1})
+            if (at < n && at > -n && self(self, i + 1, left - at * levels[i].stride)) return true;
+        return false;
+    };
+    return meet(meet, 0, apart);
+}
 
 constexpr int kStoreThreads = 256;
 constexpr int kStoreSpread = 2048;     // workgroups up to which a token's passes are spread
@@ -224,9 +245,8 @@ extern "C" caee_status_t caee_head_store(const caee_head_store_desc_t* desc, con
     CAEE_TRY(check_ptr(k_cache, "k_cache", any));
     CAEE_TRY(check_ptr(v_cache, "v_cache", any));
     if (!any) return CAEE_OK;
-    const uintptr_t k_at = (uintptr_t)k_cache, v_at = (uintptr_t)v_cache;
-    if ((k_at < v_at ? v_at - k_at : k_at - v_at) < (uintptr_t)(2 * d.dim))
-        return fail(CAEE_ERR_INVALID_ARG, "heads of k_cache and v_cache overlap");
+    if (caches_meet(c, d.kv_heads, d.dim, ((intptr_t)v_cache - (intptr_t)k_cache) / 2))
+        return fail(CAEE_ERR_INVALID_ARG, "k_cache and v_cache overlap");
     // Queries may be written over themselves; other tokens' rows that a
     // workgroup may still have to read may not be.
     if (q_out == q ? d.x_dtype != CAEE_BF16 || (d.T > 1 && d.q_out_stride != d.q_stride) : false)
