@@ -145,3 +145,14 @@ def test_auto_gives_one_row_tile_a_request_to_few_rows():
     split, also = run_way(c, DEV, "split")
     assert way == also == "few"
     assert np.array_equal(got[0], split[0]) and np.array_equal(got[1], split[1])
+
+
+@pytest.mark.parametrize("B", [3, 70])
+@pytest.mark.parametrize("causal", [True, False])
+def test_cut_rows_end_inside_a_request(causal, B):
+    """Fewer rows than new tokens: they see what they see among all of them."""
+    seq, new = ([3000, 40, 1600], [250, 40, 129]) if B == 3 else _many(B, 5)
+    c = HeadCase(seq=seq, new=new, H=16, G=2, D=64, seed=13, cut=33)
+    got, way = run_way(c, DEV, "split", causal)
+    assert way == "cut"
+    check_heads(got, c.ref(causal))
