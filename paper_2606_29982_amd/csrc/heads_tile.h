@@ -117,8 +117,9 @@ struct HeadTile {
 // 159 us, 97 with two; 8 ragged prompts 42 and 38, one of 7161 tokens 508 and 527).
 // What bounds it: the matrix units at the clock that power leaves.  7161 tokens
 // behind 1030, 32 heads: 535 us (1010 TFLOP/s; a large library product reaches 1217 on that
-// card), MFMAs 50 % of the cycles at 1.9 GHz; without the loads it takes 516, without
-// the products with the values 452, with the keys 433.  Filling one stage in two parts at
+// card), MFMAs 50 % of the cycles at 1.9 GHz; of 567 that copies for timing began with,
+// they took 516 without the loads, 452 without the products with the values, 433 without
+// those with the keys.  Filling one stage in two parts at
 // two barriers a step was slower (540 beside 527).  Short calls are bound by a tile's start
 // and end (7 to 8 us: lengths 1.8, pages and queries 1.7, fetch 0.8, out 2) beside
 // 1.6 us a step.
